@@ -20,6 +20,10 @@
  *                         and the per-row gradient coefficients.
  *   vsd_weighted_loss_bwd Gradient of that loss with respect to the draft
  *                         logits (derivative of Eq. advance).
+ *   vsd_cross_entropy,    The base losses that a trainer adds to it, with their
+ *   vsd_distill_loss      gradients: softmax cross entropy, and distillation
+ *                         from a teacher's top logits, which
+ *   vsd_top_logits        picks from the teacher's rows.
  *
  * Every call takes the logits either materialised ([R, ld] arrays) or, in
  * the fused LM-head variant (dims->hidden_dim > 0), as hidden states and an
@@ -195,6 +199,48 @@
  *   tokens at depths < i, so the draws go depth by depth, each with the
  *   Philox counters of the slot's global row (equal rows at every depth give
  *   exactly the tokens of vsd_sample_paths).
+ *
+ * Base losses and the teacher's top logits (vsd_cross_entropy, vsd_distill_loss,
+ * vsd_top_logits)
+ * ----------------------------------------------------------------------------
+ *   The recipe adds a base training loss to the VSD term.  These calls work on
+ *   any R rows of v logits (vsd_rows), with the row r's logits x_v at
+ *   temperature T = temp_draft, q_v = softmax(x / T)_v over all v columns:
+ *     cross entropy  l_r = -log q_y,  y = labels[r];
+ *     distillation   l_r = sum_k p_k (log p_k - log q_{i_k}) over the row's
+ *                    members: i_k = teacher_idx[r][k], teacher logit t_k =
+ *                    teacher_logits[r][k], p_k = exp(t_k / T_p - Z_r) with
+ *                    T_p = temp_target and Z_r = teacher_lse[r] (the teacher's
+ *                    log-sum-exp at T_p over its vocabulary), or, with
+ *                    teacher_lse NULL, the log-sum-exp of the row's members
+ *                    (renormalised).  An index of -1 is no member, a value of
+ *                    -inf a member of probability 0; a column named twice
+ *                    counts twice.
+ *   loss_row[r] = l_r, lse[r] = log sum_v exp(x_v / T),
+ *   loss_total = loss_scale sum_r w_r l_r (w = row_weight; NULL: 1), and the
+ *   gradient is that of loss_total:
+ *     g[r][v] = loss_scale w_r / T (P_r q_v - sum_{k: i_k = v} p_k),
+ *   P_r = sum_k p_k (cross entropy: the one member y with p = 1).
+ *   A row takes part unless its label is -1 (distillation: unless its members'
+ *   probabilities are all 0) or its weight is 0: other rows have loss, lse and
+ *   gradient 0 and whatever their logits or hidden states hold is not used.
+ *   -inf logits have probability 0 (a label there: loss +inf); a row without a
+ *   logit above -inf has loss 0, lse -inf and gradient 0.  A NaN or +inf logit
+ *   of a row that takes part makes that row's results NaN.
+ *   Logits: grad_logits has the logits' dtype and a stride of its own, and may
+ *   be the logits' own buffer; its padding columns are not touched.  Fused LM
+ *   head (rows->hidden_dim > 0): the logits are formed tile by tile, and again,
+ *   a piece of the vocabulary at a time, for the gradient; neither they nor
+ *   their gradient are kept.  grad_hidden [R, H] (bf16) receives g . weight and
+ *   grad_weight [v, H] (optional; fp32 or bf16, weight_dtype) g^T . hidden,
+ *   both summed in fp32 over g rounded to bf16, written, not accumulated into.
+ *   The top logits: per row the k largest of the logits above -inf, the larger
+ *   first, equal ones by the smaller index; slots past them hold -1 and -inf;
+ *   lse[r] = log sum_v exp(y_v / temp_target) over all v columns.  With a map
+ *   d2t only the columns d2t[u] take part, each with the index u in [0,
+ *   v_draft) (the lse stays that of all columns).
+ *   loss_row, lse, top_idx ... hold R rows, contiguous; R < 2^24 (top logits:
+ *   2^22), k <= VSD_MAX_TOP.
  */
 #ifndef VSD_H
 #define VSD_H
@@ -314,6 +360,31 @@ typedef struct vsd_grad {
   void* grad_hidden;      /* fused: [R, H] bf16, required */
   float* grad_weight;     /* fused, optional: [V_d, H] fp32, g^T . hidden_d */
 } vsd_grad;
+
+/* Rows of the base losses and of the top logits (see above). */
+#define VSD_MAX_TOP 64
+typedef struct vsd_rows {
+  int64_t R;           /* 1 <= R < 2^24 */
+  int64_t ld;          /* row stride of the logits, elements (fused: unused) */
+  int32_t v;           /* vocabulary size, >= 1 */
+  int32_t dtype;       /* vsd_dtype of the logits (fused: VSD_BF16) */
+  int32_t hidden_dim;  /* fused LM head: H (multiple of 64); 0 otherwise */
+} vsd_rows;
+
+typedef struct vsd_loss_out {
+  float* loss_row;       /* [R] required */
+  float* lse;            /* [R] optional */
+  float* loss_total;     /* [1] optional */
+  int32_t* device_error; /* [1] required */
+} vsd_loss_out;
+
+typedef struct vsd_loss_grad {
+  void* grad_logits;     /* materialised: [R, ld], dtype of the logits; fused: NULL */
+  int64_t ld;            /* its row stride, elements */
+  void* grad_hidden;     /* fused: [R, H] bf16, required */
+  void* grad_weight;     /* fused, optional: [v, H] */
+  int32_t weight_dtype;  /* vsd_dtype of grad_weight */
+} vsd_loss_grad;
 
 /* E-step sampling (Alg. 1: z~ ~ q and z' ~ p; Alg. 2: z-bar greedy).
  * Writes tok_draft, tok_target, tok_greedy ([R] int32 each, draft-index
@@ -497,6 +568,37 @@ vsd_status vsd_score_workspace_bytes(const vsd_dims* dims, size_t* bytes);
  * materialised logits, the result slots of vsd_verify_paths (12 bytes a path).
  * The results are the same with and without it. */
 vsd_status vsd_score_workspace_best_bytes(const vsd_dims* dims, size_t* bytes);
+
+/* Softmax cross entropy of `rows` against labels ([R], in [0, v), -1: none),
+ * with its gradient unless grad is NULL.  `workspace` must hold
+ * vsd_loss_workspace_bytes(rows, 0, grad != NULL) bytes (16-B aligned; none for
+ * materialised logits). */
+vsd_status vsd_cross_entropy(const vsd_rows* rows, const vsd_src* draft, const int32_t* labels,
+                             const float* row_weight, float temp_draft, float loss_scale,
+                             const vsd_loss_out* out, const vsd_loss_grad* grad, void* workspace,
+                             size_t workspace_bytes, void* hip_stream);
+
+/* Distillation of `rows` from a teacher's k top logits ([R, k] indices in
+ * [0, v), -1: none, and logits of teacher_dtype), with its gradient unless grad
+ * is NULL.  `workspace`: vsd_loss_workspace_bytes(rows, k, grad != NULL). */
+vsd_status vsd_distill_loss(const vsd_rows* rows, const vsd_src* draft, int32_t k,
+                            const int32_t* teacher_idx, const void* teacher_logits, int32_t teacher_dtype,
+                            const float* teacher_lse, const float* row_weight, float temp_draft,
+                            float temp_target, float loss_scale, const vsd_loss_out* out,
+                            const vsd_loss_grad* grad, void* workspace, size_t workspace_bytes,
+                            void* hip_stream);
+
+/* The k largest logits of each row: top_idx and top_logits [R, k], lse [R]
+ * (optional).  Materialised logits only.  With a map, `workspace` must hold
+ * vsd_top_workspace_bytes(rows, 1) bytes; without one it may be NULL. */
+vsd_status vsd_top_logits(const vsd_rows* rows, const vsd_src* target, int32_t k, const int32_t* d2t,
+                          int32_t v_draft, float temp_target, int32_t* top_idx, float* top_logits,
+                          float* lse, void* workspace, size_t workspace_bytes, int32_t* device_error,
+                          void* hip_stream);
+
+/* Bytes of workspace the calls above need (host only). */
+vsd_status vsd_loss_workspace_bytes(const vsd_rows* rows, int32_t k, int32_t with_grad, size_t* bytes);
+vsd_status vsd_top_workspace_bytes(const vsd_rows* rows, int32_t with_map, size_t* bytes);
 
 const char* vsd_status_string(vsd_status status); /* static string */
 const char* vsd_last_error(void);                 /* thread-local detail */

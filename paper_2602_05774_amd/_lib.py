@@ -54,11 +54,28 @@ class VsdGrad(ctypes.Structure):
     _fields_ = [("grad_logits", c_vp), ("grad_hidden", c_vp), ("grad_weight", c_vp)]
 
 
+class VsdRows(ctypes.Structure):
+    _fields_ = [("R", c_i64), ("ld", c_i64), ("v", c_i32), ("dtype", c_i32), ("hidden_dim", c_i32)]
+
+
+class VsdLossOut(ctypes.Structure):
+    _fields_ = [("loss_row", c_vp), ("lse", c_vp), ("loss_total", c_vp), ("device_error", c_vp)]
+
+
+class VsdLossGrad(ctypes.Structure):
+    _fields_ = [("grad_logits", c_vp), ("ld", c_i64), ("grad_hidden", c_vp), ("grad_weight", c_vp),
+                ("weight_dtype", c_i32)]
+
+
+VSD_MAX_TOP = 64
+
 _lib = None
 
 EXPORTS = ("vsd_sample_paths", "vsd_score_paths", "vsd_sample_score_paths", "vsd_sample_score_paths_static",
            "vsd_weighted_loss_bwd",
            "vsd_sample_step", "vsd_score_paths_ctx", "vsd_weighted_loss_bwd_ctx", "vsd_verify_paths",
+           "vsd_cross_entropy", "vsd_distill_loss", "vsd_top_logits", "vsd_loss_workspace_bytes",
+           "vsd_top_workspace_bytes",
            "vsd_score_workspace_bytes", "vsd_score_workspace_best_bytes", "vsd_status_string", "vsd_last_error", "vsd_abi_version")
 
 
@@ -104,6 +121,19 @@ def load():
     for query in (lib.vsd_score_workspace_bytes, lib.vsd_score_workspace_best_bytes):
         query.argtypes = [P(VsdDims), P(ctypes.c_size_t)]
         query.restype = c_i32
+    lib.vsd_cross_entropy.argtypes = [P(VsdRows), P(VsdSrc), c_vp, c_vp, c_f32, c_f32, P(VsdLossOut), P(VsdLossGrad),
+                                      c_vp, ctypes.c_size_t, c_vp]
+    lib.vsd_cross_entropy.restype = c_i32
+    lib.vsd_distill_loss.argtypes = [P(VsdRows), P(VsdSrc), c_i32, c_vp, c_vp, c_i32, c_vp, c_vp, c_f32, c_f32, c_f32,
+                                     P(VsdLossOut), P(VsdLossGrad), c_vp, ctypes.c_size_t, c_vp]
+    lib.vsd_distill_loss.restype = c_i32
+    lib.vsd_top_logits.argtypes = [P(VsdRows), P(VsdSrc), c_i32, c_vp, c_i32, c_f32, c_vp, c_vp, c_vp, c_vp,
+                                   ctypes.c_size_t, c_vp, c_vp]
+    lib.vsd_top_logits.restype = c_i32
+    lib.vsd_loss_workspace_bytes.argtypes = [P(VsdRows), c_i32, c_i32, P(ctypes.c_size_t)]
+    lib.vsd_loss_workspace_bytes.restype = c_i32
+    lib.vsd_top_workspace_bytes.argtypes = [P(VsdRows), c_i32, P(ctypes.c_size_t)]
+    lib.vsd_top_workspace_bytes.restype = c_i32
     lib.vsd_status_string.argtypes = [c_i32]
     lib.vsd_status_string.restype = ctypes.c_char_p
     lib.vsd_last_error.argtypes = []

@@ -25,6 +25,7 @@
 // dH_d = g W_d and, when asked for, dW_d = g^T H_d (fp32).
 #include "vsd_device.hpp"
 #include "vsd_kernels.hpp"
+#include "vsd_loss.hpp"
 #include "vsd_topk.hpp"
 
 namespace vsd {
@@ -1557,6 +1558,8 @@ __global__ __launch_bounds__(kThreads, 1) void k_lm_gemm_tn(LmGemmTNArgs a) {
   });
 }
 
+#include "vsd_lm_loss.hpp"
+
 }  // namespace
 
 hipError_t launch_lm_inv(const int32_t* d2t, int Vd, int Vt, int32_t* inv, int32_t* err, uint32_t* clear, int nclear,
@@ -1629,6 +1632,56 @@ hipError_t launch_lm_bwd(const LmBwdArgs& a, hipStream_t s) {
   const int64_t nvt = (a.Vd + TM - 1) / TM;
   hipLaunchKernelGGL(big ? k_lm_gemm_tn<true> : k_lm_gemm_tn<false>, dim3((unsigned)(nvt * ((a.H + TN - 1) / TN))),
                      dim3(kThreads), 0, s, tn);
+  return hipGetLastError();
+}
+
+// (The grids are sized for every row in play; the kernels read how many are.)
+hipError_t launch_lm_loss(LmLossArgs a, bool weight_bf16, hipStream_t s) {
+  const bool distill = a.l.val != nullptr;
+  const int64_t R = a.l.R, nrt = (R + TM - 1) / TM;
+  const dim3 by_row((unsigned)((R + 3) / 4));
+  hipError_t e;
+  if (distill) {
+    hipLaunchKernelGGL(k_lm_loss_members, by_row, dim3(256), 0, s, a);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
+  hipLaunchKernelGGL(k_lm_loss_list, dim3((unsigned)((R + kListRows - 1) / kListRows)), dim3(kListRows), 0, s, a);
+  if ((e = hipGetLastError()) != hipSuccess) return e;
+  hipLaunchKernelGGL(k_lm_loss_pack, dim3((unsigned)((R + kLmLossPad + 3) / 4)), dim3(256), 0, s, a);
+  if ((e = hipGetLastError()) != hipSuccess) return e;
+  hipLaunchKernelGGL(k_lm_loss_fwd, dim3((unsigned)(nrt * a.nruns)), dim3(kThreads), 0, s, a);
+  if ((e = hipGetLastError()) != hipSuccess) return e;
+  if (distill)
+    hipLaunchKernelGGL(k_lm_loss_combine<true>, by_row, dim3(256), 0, s, a);
+  else
+    hipLaunchKernelGGL(k_lm_loss_combine<false>, by_row, dim3(256), 0, s, a);
+  if ((e = hipGetLastError()) != hipSuccess) return e;
+  if (a.dh == nullptr) return hipSuccess;
+  const int64_t nht = (a.H + TN - 1) / TN;
+  for (int64_t c0 = 0; c0 < a.l.V; c0 += a.piece) {
+    a.c0 = (int32_t)c0;
+    a.cols = (int32_t)(a.l.V - c0 < a.piece ? a.l.V - c0 : a.piece);
+    const int64_t nct = (a.cols + TN - 1) / TN;
+    if (distill) {
+      hipLaunchKernelGGL(k_lm_loss_g<true>, dim3((unsigned)(nrt * nct)), dim3(kThreads), 0, s, a);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+      hipLaunchKernelGGL(k_lm_loss_fix, by_row, dim3(256), 0, s, a);
+    } else {
+      hipLaunchKernelGGL(k_lm_loss_g<false>, dim3((unsigned)(nrt * nct)), dim3(kThreads), 0, s, a);
+    }
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+    hipLaunchKernelGGL(k_lm_loss_dh, dim3((unsigned)(nrt * nht * a.splits)), dim3(kThreads), 0, s, a);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+    if (a.dw != nullptr) {
+      const dim3 grid((unsigned)(nct * nht));
+      if (weight_bf16)
+        hipLaunchKernelGGL(k_lm_loss_dw<bf16_t>, grid, dim3(kThreads), 0, s, a);
+      else
+        hipLaunchKernelGGL(k_lm_loss_dw<float>, grid, dim3(kThreads), 0, s, a);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+  }
+  if (a.splits > 1) hipLaunchKernelGGL(k_lm_loss_dh_out, by_row, dim3(256), 0, s, a);
   return hipGetLastError();
 }
 

@@ -483,6 +483,210 @@ vsd_status static_scratch(void** ptr) {
   return VSD_OK;
 }
 
+// ------------------------------------------------------------ base losses ---
+// A launch counts its work-items in 32 bits: 256 a row for the losses, 1024 for
+// the top logits.
+constexpr int64_t kMaxTopRows = (int64_t)1 << 22;
+
+vsd_status check_rows_struct(const vsd_rows* rows) {
+  if (rows == nullptr) return fail(VSD_ERR_NULL_POINTER, "rows is NULL");
+  if (rows->R < 1 || rows->R >= kMaxRows)
+    return fail(VSD_ERR_INVALID_SHAPE, "R=%lld must be >= 1 and < 2^24", (long long)rows->R);
+  if (rows->v < 1) return fail(VSD_ERR_INVALID_SHAPE, "v=%d must be >= 1", rows->v);
+  if (rows->dtype != VSD_F32 && rows->dtype != VSD_BF16) return fail(VSD_ERR_INVALID_VALUE, "dtype=%d", rows->dtype);
+  const int32_t H = rows->hidden_dim;
+  if (H < 0 || H > kMaxHidden || H % 64 != 0)
+    return fail(VSD_ERR_INVALID_SHAPE, "hidden_dim=%d must be 0 or a multiple of 64 up to %d", H, kMaxHidden);
+  if (H > 0) {
+    if (rows->dtype != VSD_BF16) return fail(VSD_ERR_UNSUPPORTED, "the fused LM head takes bf16 operands only");
+    const int64_t nrt = (rows->R + vsd::kLmTile - 1) / vsd::kLmTile;
+    const int64_t nht = (H + vsd::kLmTile - 1) / vsd::kLmTile, vt = ((int64_t)rows->v + vsd::kLmTile - 1) / vsd::kLmTile;
+    if (nrt * std::max(nht, vt) >= kMaxLmWorkgroups || nht * vt >= kMaxLmWorkgroups)
+      return fail(VSD_ERR_INVALID_SHAPE, "fused LM head: R=%lld rows x v=%d x hidden_dim=%d too large",
+                  (long long)rows->R, rows->v, H);
+  }
+  return VSD_OK;
+}
+
+// One source over `rows`: logits with row stride ld, or a fused LM head.
+vsd_status check_rows_src(const vsd_rows* rows, const vsd_src* src, const char* name) {
+  if (rows->hidden_dim > 0) return check_fused_src(src, name);
+  vsd_dims d{};
+  d.dtype = rows->dtype;
+  return check_logits(&d, src, name, rows->ld, rows->v);
+}
+
+bool usable_temp(float t) { return finite_pos(t) && finite_pos(1.0f / t) && std::isfinite(vsd::kLog2e / t); }
+
+struct LossLayout {
+  size_t tag, at, rows, count, mid, mp, mstat, mx, hp, part, stat, g, acc, total;
+  int32_t run, nruns, piece, per, splits;
+};
+
+// The fused head's workspace (K = 0: cross entropy); materialised rows need none.
+LossLayout loss_layout(const vsd_rows* rows, int32_t K, bool grad) {
+  LossLayout w{};
+  const size_t R = (size_t)rows->R, H = (size_t)rows->hidden_dim;
+  if (H == 0) return w;
+  w.run = vsd::lm_loss_run(rows->R, rows->v);
+  w.nruns = vsd::lm_runs(rows->v, w.run);
+  w.piece = vsd::lm_loss_piece(rows->R, rows->v);
+  w.per = vsd::lm_loss_range(rows->R, rows->hidden_dim, w.piece);
+  w.splits = (std::min(w.piece, rows->v) + w.per - 1) / w.per;  // (every range of the first piece has columns)
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    const size_t here = at;
+    at += align_up(bytes);
+    return here;
+  };
+  w.count = take(sizeof(int32_t));
+  w.at = take(R * sizeof(int32_t));
+  w.rows = take(R * sizeof(int32_t));
+  if (K > 0) {
+    w.tag = take(R * sizeof(int32_t));
+    w.mid = take(R * K * sizeof(int32_t));
+    w.mp = take(R * K * sizeof(float));
+    w.mx = take(R * K * sizeof(float));
+    w.mstat = take(R * sizeof(float2));
+  }
+  const size_t padded = (size_t)vsd::lm_loss_pad(rows->R);
+  w.hp = take(padded * H * sizeof(uint16_t));
+  w.part = take(2 * (size_t)w.nruns * R * sizeof(float2));
+  w.stat = take(R * sizeof(float4));
+  if (grad) {
+    w.g = take(padded * (size_t)w.piece * sizeof(uint16_t));
+    if (w.splits > 1 || w.piece < rows->v) w.acc = take((size_t)w.splits * R * H * sizeof(float));
+  }
+  w.total = at;
+  return w;
+}
+
+vsd_status check_loss_out(const vsd_loss_out* out) {
+  if (out == nullptr) return fail(VSD_ERR_NULL_POINTER, "out is NULL");
+  if (out->loss_row == nullptr || out->device_error == nullptr)
+    return fail(VSD_ERR_NULL_POINTER, "out->loss_row and device_error are required");
+  return VSD_OK;
+}
+
+vsd_status check_loss_grad(const vsd_rows* rows, const vsd_loss_grad* grad) {
+  if (grad == nullptr) return VSD_OK;
+  if (rows->hidden_dim > 0) {
+    if (grad->grad_logits != nullptr)
+      return fail(VSD_ERR_UNSUPPORTED, "fused: the logits' gradient is not kept (grad_logits must be NULL)");
+    if (grad->grad_hidden == nullptr) return fail(VSD_ERR_NULL_POINTER, "fused: grad->grad_hidden is NULL");
+    if (!aligned16(grad->grad_hidden)) return fail(VSD_ERR_MISALIGNED, "grad_hidden not 16-byte aligned");
+    if (grad->grad_weight != nullptr) {
+      if (!aligned16(grad->grad_weight)) return fail(VSD_ERR_MISALIGNED, "grad_weight not 16-byte aligned");
+      if (grad->weight_dtype != VSD_F32 && grad->weight_dtype != VSD_BF16)
+        return fail(VSD_ERR_INVALID_VALUE, "weight_dtype=%d", grad->weight_dtype);
+    }
+    return VSD_OK;
+  }
+  if (grad->grad_hidden != nullptr || grad->grad_weight != nullptr)
+    return fail(VSD_ERR_UNSUPPORTED, "grad_hidden and grad_weight need a fused LM head (hidden_dim > 0)");
+  if (grad->grad_logits == nullptr) return fail(VSD_ERR_NULL_POINTER, "grad->grad_logits is NULL");
+  const int64_t es = rows->dtype == VSD_F32 ? 4 : 2;
+  if (grad->ld < rows->v) return fail(VSD_ERR_INVALID_SHAPE, "grad ld=%lld < v=%d", (long long)grad->ld, rows->v);
+  if (!aligned16(grad->grad_logits) || (grad->ld * es) % 16 != 0)
+    return fail(VSD_ERR_MISALIGNED, "grad_logits or its row stride not a multiple of 16 bytes");
+  return VSD_OK;
+}
+
+// Both losses: K = 0 is the cross entropy (idx: labels).
+vsd_status base_loss(const vsd_rows* rows, const vsd_src* src, int32_t K, const int32_t* idx, const void* val,
+                     int32_t val_dtype, const float* teacher_lse, const float* weight, float temp, float temp_target,
+                     float scale, const vsd_loss_out* out, const vsd_loss_grad* grad, void* workspace,
+                     size_t workspace_bytes, hipStream_t s) {
+  vsd_status st = check_rows_struct(rows);
+  if (st != VSD_OK) return st;
+  if ((st = check_rows_src(rows, src, "draft")) != VSD_OK) return st;
+  if (!usable_temp(temp) || !usable_temp(temp_target))
+    return fail(VSD_ERR_INVALID_VALUE, "temperatures must be finite, > 0 and have a finite reciprocal");
+  if (!std::isfinite(scale)) return fail(VSD_ERR_INVALID_VALUE, "loss_scale must be finite");
+  if ((st = check_loss_out(out)) != VSD_OK) return st;
+  if ((st = check_loss_grad(rows, grad)) != VSD_OK) return st;
+  vsd::LossArgs a{};
+  a.R = rows->R;
+  a.V = rows->v;
+  a.K = K > 0 ? K : 1;
+  a.idx = idx;
+  a.val = val;
+  a.val_bf16 = val_dtype == VSD_BF16;
+  a.teacher_lse = teacher_lse;
+  a.weight = weight;
+  a.inv_t = 1.0f / temp;
+  a.inv_tp = 1.0f / temp_target;
+  a.c = vsd::kLog2e / temp;
+  a.scale = scale;
+  a.loss = out->loss_row;
+  a.lse = out->lse;
+  a.err = out->device_error;
+  hipError_t e;
+  if (rows->hidden_dim == 0) {
+    a.X = src->logits;
+    a.ld = rows->ld;
+    if (grad != nullptr) {
+      a.G = grad->grad_logits;
+      a.ldg = grad->ld;
+    }
+    e = vsd::launch_row_loss(a, rows->dtype == VSD_BF16, s);
+    if (e != hipSuccess) return hip_fail(e, "k_row_loss launch");
+  } else {
+    const LossLayout w = loss_layout(rows, K, grad != nullptr);
+    if (workspace == nullptr || workspace_bytes < w.total)
+      return fail(VSD_ERR_WORKSPACE, "workspace of %zu bytes required, %zu given", w.total,
+                  workspace == nullptr ? (size_t)0 : workspace_bytes);
+    if (!aligned16(workspace)) return fail(VSD_ERR_MISALIGNED, "workspace not 16-byte aligned");
+    char* ws = static_cast<char*>(workspace);
+    vsd::LmLossArgs b{};
+    b.l = a;
+    b.h = src->hidden;
+    b.w = src->weight;
+    b.H = rows->hidden_dim;
+    b.run = w.run;
+    b.nruns = w.nruns;
+    b.piece = b.ldg = w.piece;
+    b.per = w.per;
+    b.splits = w.splits;
+    b.tag = K > 0 ? reinterpret_cast<int32_t*>(ws + w.tag) : const_cast<int32_t*>(idx);  // (labels are read only)
+    b.at = reinterpret_cast<int32_t*>(ws + w.at);
+    b.rows = reinterpret_cast<int32_t*>(ws + w.rows);
+    b.count = reinterpret_cast<int32_t*>(ws + w.count);
+    if (K > 0) {
+      b.mid = reinterpret_cast<int32_t*>(ws + w.mid);
+      b.mp = reinterpret_cast<float*>(ws + w.mp);
+      b.mx = reinterpret_cast<float*>(ws + w.mx);
+      b.mstat = reinterpret_cast<float2*>(ws + w.mstat);
+    }
+    b.hp = reinterpret_cast<uint16_t*>(ws + w.hp);
+    b.part = reinterpret_cast<float2*>(ws + w.part);
+    b.stat = reinterpret_cast<float4*>(ws + w.stat);
+    if (grad != nullptr) {
+      b.dh = grad->grad_hidden;
+      b.dw = grad->grad_weight;
+      b.g = reinterpret_cast<uint16_t*>(ws + w.g);
+      if (w.acc != 0) b.acc = reinterpret_cast<float*>(ws + w.acc);
+    }
+    e = vsd::launch_lm_loss(b, grad != nullptr && grad->weight_dtype == VSD_BF16, s);
+    if (e != hipSuccess) return hip_fail(e, "fused loss launch");
+  }
+  if (out->loss_total != nullptr) {
+    e = vsd::launch_row_total(out->loss_row, weight, rows->R, scale, out->loss_total, s);
+    if (e != hipSuccess) return hip_fail(e, "k_row_total launch");
+  }
+  return ok();
+}
+
+struct TopLayout {
+  size_t inv, mapped, total;
+};
+TopLayout top_layout(const vsd_rows* rows) {
+  TopLayout w{};
+  w.mapped = w.inv + align_up((size_t)rows->v * sizeof(int32_t));
+  w.total = w.mapped + align_up(((size_t)rows->v + 7) / 8);
+  return w;
+}
+
 }  // namespace
 
 extern "C" {
@@ -986,6 +1190,97 @@ vsd_status vsd_verify_paths(const vsd_dims* dims, const vsd_params* params, cons
   a.offset = offset;
   hipError_t e = vsd::launch_verify(a, dims->dtype == VSD_BF16, s);
   if (e != hipSuccess) return hip_fail(e, "k_verify launch");
+  return ok();
+}
+
+vsd_status vsd_cross_entropy(const vsd_rows* rows, const vsd_src* draft, const int32_t* labels,
+                             const float* row_weight, float temp_draft, float loss_scale, const vsd_loss_out* out,
+                             const vsd_loss_grad* grad, void* workspace, size_t workspace_bytes, void* hip_stream) {
+  if (labels == nullptr) return fail(VSD_ERR_NULL_POINTER, "labels are NULL");
+  return base_loss(rows, draft, 0, labels, nullptr, VSD_F32, nullptr, row_weight, temp_draft, 1.0f, loss_scale, out,
+                   grad, workspace, workspace_bytes, static_cast<hipStream_t>(hip_stream));
+}
+
+vsd_status vsd_distill_loss(const vsd_rows* rows, const vsd_src* draft, int32_t k, const int32_t* teacher_idx,
+                            const void* teacher_logits, int32_t teacher_dtype, const float* teacher_lse,
+                            const float* row_weight, float temp_draft, float temp_target, float loss_scale,
+                            const vsd_loss_out* out, const vsd_loss_grad* grad, void* workspace,
+                            size_t workspace_bytes, void* hip_stream) {
+  if (k < 1 || k > VSD_MAX_TOP)
+    return fail(VSD_ERR_INVALID_VALUE, "k=%d outside [1,%d]", k, VSD_MAX_TOP);
+  if (teacher_idx == nullptr || teacher_logits == nullptr)
+    return fail(VSD_ERR_NULL_POINTER, "teacher_idx and teacher_logits are required");
+  if (teacher_dtype != VSD_F32 && teacher_dtype != VSD_BF16)
+    return fail(VSD_ERR_INVALID_VALUE, "teacher_dtype=%d", teacher_dtype);
+  return base_loss(rows, draft, k, teacher_idx, teacher_logits, teacher_dtype, teacher_lse, row_weight, temp_draft,
+                   temp_target, loss_scale, out, grad, workspace, workspace_bytes,
+                   static_cast<hipStream_t>(hip_stream));
+}
+
+vsd_status vsd_loss_workspace_bytes(const vsd_rows* rows, int32_t k, int32_t with_grad, size_t* bytes) {
+  vsd_status st = check_rows_struct(rows);
+  if (st != VSD_OK) return st;
+  if (k < 0 || k > VSD_MAX_TOP) return fail(VSD_ERR_INVALID_VALUE, "k=%d outside [0,%d]", k, VSD_MAX_TOP);
+  if (bytes == nullptr) return fail(VSD_ERR_NULL_POINTER, "bytes is NULL");
+  *bytes = loss_layout(rows, k, with_grad != 0).total;
+  return ok();
+}
+
+vsd_status vsd_top_logits(const vsd_rows* rows, const vsd_src* target, int32_t k, const int32_t* d2t,
+                          int32_t v_draft, float temp_target, int32_t* top_idx, float* top_logits, float* lse,
+                          void* workspace, size_t workspace_bytes, int32_t* device_error, void* hip_stream) {
+  vsd_status st = check_rows_struct(rows);
+  if (st != VSD_OK) return st;
+  if (rows->hidden_dim > 0) return fail(VSD_ERR_UNSUPPORTED, "vsd_top_logits takes materialised logits");
+  if (rows->R >= kMaxTopRows)
+    return fail(VSD_ERR_INVALID_SHAPE, "R=%lld must be < 2^22", (long long)rows->R);
+  if ((st = check_rows_src(rows, target, "target")) != VSD_OK) return st;
+  if (k < 1 || k > VSD_MAX_TOP) return fail(VSD_ERR_INVALID_VALUE, "k=%d outside [1,%d]", k, VSD_MAX_TOP);
+  if (!usable_temp(temp_target))
+    return fail(VSD_ERR_INVALID_VALUE, "temp_target must be finite, > 0 and have a finite reciprocal");
+  if (top_idx == nullptr || top_logits == nullptr || device_error == nullptr)
+    return fail(VSD_ERR_NULL_POINTER, "top_idx, top_logits and device_error are required");
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  vsd::TopArgs a{};
+  hipError_t e;
+  if (d2t != nullptr) {
+    if (v_draft < 1 || v_draft > rows->v)
+      return fail(VSD_ERR_INVALID_SHAPE, "v_draft=%d outside [1,%d]", v_draft, rows->v);
+    if (!aligned16(d2t)) return fail(VSD_ERR_MISALIGNED, "d2t pointer not 16-byte aligned");
+    const TopLayout w = top_layout(rows);
+    if (workspace == nullptr || workspace_bytes < w.total)
+      return fail(VSD_ERR_WORKSPACE, "workspace of %zu bytes required, %zu given", w.total,
+                  workspace == nullptr ? (size_t)0 : workspace_bytes);
+    if (!aligned16(workspace)) return fail(VSD_ERR_MISALIGNED, "workspace not 16-byte aligned");
+    int32_t* inv = reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + w.inv);
+    uint8_t* mapped = reinterpret_cast<uint8_t*>(static_cast<char*>(workspace) + w.mapped);
+    e = vsd::launch_lm_inv(d2t, v_draft, rows->v, inv, device_error, nullptr, 0, s);
+    if (e != hipSuccess) return hip_fail(e, "k_lm_inv launch");
+    e = vsd::launch_top_bits(inv, rows->v, mapped, s);
+    if (e != hipSuccess) return hip_fail(e, "k_top_bits launch");
+    a.inv = inv;
+    a.mapped = mapped;
+  }
+  a.Y = target->logits;
+  a.R = rows->R;
+  a.ld = rows->ld;
+  a.V = rows->v;
+  a.K = k;
+  a.inv_t = 1.0f / temp_target;
+  a.c = vsd::kLog2e / temp_target;
+  a.idx = top_idx;
+  a.val = top_logits;
+  a.lse = lse;
+  e = vsd::launch_top_logits(a, rows->dtype == VSD_BF16, s);
+  if (e != hipSuccess) return hip_fail(e, "k_top_logits launch");
+  return ok();
+}
+
+vsd_status vsd_top_workspace_bytes(const vsd_rows* rows, int32_t with_map, size_t* bytes) {
+  vsd_status st = check_rows_struct(rows);
+  if (st != VSD_OK) return st;
+  if (bytes == nullptr) return fail(VSD_ERR_NULL_POINTER, "bytes is NULL");
+  *bytes = with_map != 0 ? top_layout(rows).total : 0;
   return ok();
 }
 

@@ -7,6 +7,7 @@
 namespace vsd {
 
 constexpr int kMaxL = 64;
+using bf16_store = uint16_t;  // bf16 storage
 
 struct SampleArgs {
   const void* X;             // [R, ld_d]
@@ -436,6 +437,107 @@ hipError_t launch_lm_combine(const LmCombineArgs& a, hipStream_t s);
 hipError_t launch_lm_kl_reset(const LmCombineArgs& a, hipStream_t s);
 hipError_t launch_lm_kl_redo(const LmCombineArgs& a, hipStream_t s);
 hipError_t launch_lm_bwd(const LmBwdArgs& a, hipStream_t s);
+
+// ------------------------------------------------------------ base losses ---
+constexpr int kMaxMembers = 64;  // members of a row: one lane each
+
+struct LossArgs {
+  const void* X;               // [R, ld] logits; LM head: null
+  void* G;                     // [R, ldg] gradient or null (may be X)
+  int64_t R, ld, ldg;
+  int32_t V, K;                // K: members per row (cross entropy: 1)
+  const int32_t* idx;          // [R] labels or [R, K] members' columns, -1: none
+  const void* val;             // [R, K] the members' teacher logits; null: cross entropy
+  int32_t val_bf16;
+  const float* teacher_lse;    // [R] or null: normalised over the row's members
+  const float* weight;         // [R] or null: 1
+  float inv_t, inv_tp, c;      // 1/T, 1/T_p, log2(e)/T
+  float scale;                 // loss_scale
+  float* loss;                 // [R]
+  float* lse;                  // [R] or null
+  int32_t* err;
+};
+
+// The K largest entries of a teacher's rows.
+struct TopArgs {
+  const void* Y;               // [R, ld]
+  int64_t R, ld;
+  int32_t V, K;
+  const int32_t* inv;          // [V] index of each column (-1: none) or null: the column
+  const uint8_t* mapped;       // one bit per column: inv >= 0
+  float inv_t, c;
+  int32_t* idx;                // [R, K]
+  float* val;                  // [R, K]
+  float* lse;                  // [R] or null
+};
+
+// The same losses through an LM head.
+constexpr int kLmLossPad = 64;  // rows in play are padded to whole stages of the products
+__host__ __device__ constexpr int64_t lm_loss_pad(int64_t n) { return (n + kLmLossPad - 1) / kLmLossPad * kLmLossPad; }
+
+struct LmLossArgs {
+  LossArgs l;                // members, weights, outputs; X, G: null
+  const void* h;             // [R, H] bf16
+  const void* w;             // [V, H] bf16
+  void* dh;                  // [R, H] bf16, or null: the loss only
+  void* dw;                  // [V, H] bf16 or fp32, or null
+  int32_t H;
+  int32_t run, nruns;        // vocabulary tiles per run of the forward, runs
+  int32_t piece;             // columns of a piece (a multiple of 256)
+  int32_t splits, per;       // ranges of a piece's columns in dh, columns of each (a multiple of 64)
+  int32_t c0, cols;          // the piece at hand
+  int32_t ldg;               // row stride of g
+  // workspace
+  int32_t* tag;              // [R] in play iff in [0, V) (and the weight is not 0): labels, or 0 / -1
+  int32_t* at;               // [R] place among the rows in play or -1
+  int32_t* rows;             // [R] the rows in play
+  int32_t* count;            // [1] how many
+  int32_t* mid;              // [R, K] members' columns
+  float* mp;                 // [R, K] their probabilities
+  float2* mstat;             // [R] sums of p and p log p
+  float* mx;                 // [rows in play, K] their logits
+  bf16_store* hp;            // [lm_loss_pad(R), H] hidden states of the rows in play
+  float2* part;              // [2 nruns, R] log-sum-exps of the runs, per wavefront group
+  float4* stat;              // [R] (m, kq, k, -) of the gradient
+  bf16_store* g;             // [lm_loss_pad(R), ldg] the piece's gradient
+  float* acc;                // [splits, R, H], or null: one piece and one range
+};
+
+// Vocabulary tiles that a forward workgroup walks: enough workgroups for two
+// rounds of the chip, and at most 16 tiles.
+inline int lm_loss_run(int64_t R, int V) {
+  const int64_t all = (R + kLmTile - 1) / kLmTile * lm_tiles(V);
+  const int64_t run = all / (2 * kLmCus);
+  return (int)(run < 1 ? 1 : run > kLmTilesPerSlice ? kLmTilesPerSlice : run);
+}
+// Columns of a piece: the whole vocabulary where its gradient fits 1 GiB, else
+// the largest power of two that does (at least 1024).
+constexpr int64_t kLmPieceBytes = 1ll << 30;
+inline int32_t lm_loss_piece(int64_t R, int V) {
+  const int64_t row = 2 * lm_loss_pad(R), all = (int64_t)lm_tiles(V) * kLmTile;
+  if (all * row <= kLmPieceBytes) return (int32_t)all;
+  int64_t piece = 1024;
+  while (2 * piece * row <= kLmPieceBytes) piece *= 2;
+  return (int32_t)(piece < all ? piece : all);
+}
+// Columns of one of the ranges that a piece is split into for dh: with fewer
+// tiles of dh than CUs, as many ranges as fill them, of at least four stages.
+inline int32_t lm_loss_range(int64_t R, int H, int32_t piece) {
+  const int64_t tiles = (R + kLmTile - 1) / kLmTile * ((H + kLmTile - 1) / kLmTile);
+  int64_t splits = kLmCus / tiles;
+  const int64_t most = piece / 256;
+  splits = splits > most ? most : splits;
+  if (splits < 2) return piece;
+  const int64_t stages = piece / 64;
+  return (int32_t)((stages + splits - 1) / splits * 64);
+}
+
+hipError_t launch_lm_loss(LmLossArgs a, bool weight_bf16, hipStream_t s);
+hipError_t launch_row_loss(const LossArgs& a, bool bf16, hipStream_t s);
+hipError_t launch_row_total(const float* loss, const float* weight, int64_t R, float scale, float* total,
+                            hipStream_t s);
+hipError_t launch_top_bits(const int32_t* inv, int V, uint8_t* mapped, hipStream_t s);
+hipError_t launch_top_logits(const TopArgs& a, bool bf16, hipStream_t s);
 
 hipError_t launch_sample(const SampleArgs& a, bool bf16, hipStream_t s);
 hipError_t launch_sample_step(const SampleStepArgs& a, bool bf16, hipStream_t s);

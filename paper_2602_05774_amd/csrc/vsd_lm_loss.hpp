@@ -1,0 +1,344 @@
+// The base losses through an LM head: logits x = h W^T formed tile by tile by
+// k_lmhead.hip's product loop (which includes this file after it) and consumed
+// in the accumulators.  Neither they nor their gradient are kept: g is formed a
+// piece of the vocabulary at a time, in bf16 (the operand type of the two
+// products that read it), and both add up in fp32.
+//
+//   rows     the rows that take part are listed and their hidden states copied
+//            to consecutive rows, followed by zero rows up to a multiple of 64:
+//            rows out of play then cost nothing and whatever they hold (padding)
+//            reaches no sum, and the weight's gradient has whole stages of rows
+//   forward  the rows' log-sum-exps over runs of vocabulary tiles; a combine
+//            joins the runs and forms the loss
+//   pieces   g of a piece, then dh += g W and dW = g^T h
+
+// The distillation's members, one wavefront per row (a lane each).
+__global__ __launch_bounds__(256) void k_lm_loss_members(LmLossArgs a) {
+  const int lane = threadIdx.x & 63;
+  const int64_t r = (int64_t)blockIdx.x * 4 + wave_id();
+  if (r >= a.l.R) return;
+  const Member e = load_member(a.l, r, lane);
+  const float mass = wave_sum(e.p), plogp = wave_sum(e.plogp);
+  if (lane < a.l.K) {
+    a.mid[r * a.l.K + lane] = e.id;
+    a.mp[r * a.l.K + lane] = e.p;
+  }
+  if (lane == 0) {
+    a.mstat[r] = make_float2(mass, plogp);
+    a.tag[r] = mass != 0.0f ? 0 : -1;
+  }
+}
+
+// at[r] = row r's place among the rows in play, or -1; the number of those
+// rows.  Every workgroup counts the rows before its own 1024.
+constexpr int kListRows = 1024;
+__global__ __launch_bounds__(kListRows) void k_lm_loss_list(LmLossArgs a) {
+  __shared__ int red[kListRows / kWave];
+  const int lane = threadIdx.x & 63, wave = wave_id();
+  auto in_play = [&](int64_t r) {
+    const int32_t t = a.tag[r];
+    if ((uint32_t)t >= (uint32_t)a.l.V) {
+      if (t != -1) report_error(a.l.err, VSD_DEVERR_TOKEN_RANGE);
+      return false;
+    }
+    return row_weight(a.l, r) != 0.0f;
+  };
+  const int64_t first = (int64_t)blockIdx.x * kListRows, r = first + threadIdx.x;
+  int before = 0;
+  for (int64_t k = threadIdx.x; k < first; k += kListRows) before += in_play(k) ? 1 : 0;
+  before = wave_sum_int(before);
+  if (lane == 0) red[wave] = before;
+  __syncthreads();
+  int place = 0;
+  for (int k = 0; k < kListRows / kWave; ++k) place += red[k];
+  __syncthreads();
+  const bool in = r < a.l.R && in_play(r);
+  const uint64_t has = __ballot(in);
+  if (lane == 0) red[wave] = __builtin_popcountll(has);
+  __syncthreads();
+  int total = place;
+  for (int k = 0; k < kListRows / kWave; ++k) {
+    if (k < wave) place += red[k];
+    total += red[k];
+  }
+  place += (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(has >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)has, 0u));
+  if (r < a.l.R) {
+    a.at[r] = in ? place : -1;
+    if (in) a.rows[place] = (int32_t)r;
+    if (!in) {
+      a.l.loss[r] = 0.0f;
+      if (a.l.lse != nullptr) a.l.lse[r] = 0.0f;
+    }
+  }
+  if (threadIdx.x == 0 && blockIdx.x == gridDim.x - 1) *a.count = total;
+}
+
+// The hidden states of the rows in play, consecutively; zero rows behind them;
+// a zero gradient for the other rows.  One wavefront per row.
+__global__ __launch_bounds__(256) void k_lm_loss_pack(LmLossArgs a) {
+  const int lane = threadIdx.x & 63;
+  const int64_t r = (int64_t)blockIdx.x * 4 + wave_id();
+  const uint4* from = nullptr;
+  uint4* to;
+  if (r < a.l.R) {
+    const int32_t place = a.at[r];
+    if (place >= 0) {
+      from = reinterpret_cast<const uint4*>(static_cast<const bf16_t*>(a.h) + r * a.H);
+      to = reinterpret_cast<uint4*>(a.hp + (int64_t)place * a.H);
+    } else {
+      if (a.dh == nullptr) return;
+      to = reinterpret_cast<uint4*>(static_cast<bf16_t*>(a.dh) + r * a.H);
+    }
+  } else {
+    const int64_t n = *a.count, place = n + (r - a.l.R);
+    if (place >= lm_loss_pad(n)) return;
+    to = reinterpret_cast<uint4*>(a.hp + place * a.H);
+  }
+  for (int k = lane; k < a.H / 8; k += kWave) to[k] = from != nullptr ? from[k] : make_uint4(0, 0, 0, 0);
+}
+
+// A run of vocabulary tiles against 256 rows: their log-sum-exps over the
+// columns of each wavefront group.
+__global__ __launch_bounds__(kThreads, 1) void k_lm_loss_fwd(LmLossArgs a) {
+  __shared__ __align__(16) bf16_t lds[2 * kBufElems];
+  const int64_t n = *a.count;
+  const int nrt = (int)((n + TM - 1) / TM);
+  if ((int64_t)blockIdx.x >= (int64_t)nrt * a.nruns) return;
+  int rt, run;
+  tile_of(blockIdx.x, nrt, a.nruns, rt, run);
+  const int64_t row0 = (int64_t)rt * TM, i = row0 + nt_lane_row();
+  const int tiles = (a.l.V + TN - 1) / TN, begin = run * a.run;
+  float m = kNegBig, s = 0.0f;
+  NtRows src{static_cast<const bf16_t*>(a.w), a.hp, a.l.V, row0, n, a.H, begin, min(tiles, begin + a.run)};
+  nt_stream(lds, src, [&](int tile, NtAcc& acc) {
+    nt_row_per_lane(acc);
+    if (i >= n) return;
+#pragma unroll 1
+    for (int ch = 0; ch < 16; ++ch) {
+      const int c = tile * TN + nt_chunk_col(ch);
+      if (c >= a.l.V) break;
+      float x[8];
+      nt_chunk(acc, ch, x);
+      if (c + 8 > a.l.V) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+          if (c + k >= a.l.V) x[k] = -INFINITY;
+      }
+      lse_add8(x, m, s, a.l.c);
+    }
+  });
+  if (i < n) a.part[((int64_t)run * 2 + (wave_id() >> 2)) * a.l.R + i] = make_float2(m, s);
+}
+
+// The runs joined, the members' logits (dot products), the loss, and what the
+// gradient needs: g_v = kq exp2((x_v - m) c) - k p_v.  One wavefront per row.
+template <bool DISTILL>
+__global__ __launch_bounds__(256) void k_lm_loss_combine(LmLossArgs a) {
+  const int lane = threadIdx.x & 63;
+  const int64_t i = (int64_t)blockIdx.x * 4 + wave_id();
+  if (i >= *a.count) return;
+  const int64_t r = a.rows[i];
+  float m = kNegBig, s = 0.0f;
+  for (int e = lane; e < 2 * a.nruns; e += kWave) {
+    const float2 p = a.part[(int64_t)e * a.l.R + i];
+    lse_join(m, s, p.x, p.y, a.l.c);
+  }
+  wave_lse(m, s, a.l.c);
+  const bf16_t* h = a.hp + i * a.H;
+  const bf16_t* W = static_cast<const bf16_t*>(a.w);
+  const bool live = s != 0.0f;
+  const float tail = logf(s);
+  float mass = 1.0f, loss;
+  if (DISTILL) {
+    const int K = a.l.K;
+    const int id = lane < K ? a.mid[r * K + lane] : -1;
+    const float p = lane < K ? a.mp[r * K + lane] : 0.0f;
+    float x = -INFINITY;
+    for (int k = 0; k < K; ++k) {
+      const int v = lane_i(id, k);
+      if (v < 0) continue;
+      const float xk = wave_dot(h, W + (int64_t)v * a.H, a.H, lane);
+      x = lane == k ? xk : x;
+    }
+    if (lane < K) a.mx[i * K + lane] = x;
+    const float2 ms = a.mstat[r];
+    mass = ms.x;
+    loss = ms.y - wave_sum(p != 0.0f ? p * ((x - m) * a.l.inv_t - tail) : 0.0f);
+  } else {
+    const float x = wave_dot(h, W + (int64_t)a.l.idx[r] * a.H, a.H, lane);
+    loss = tail - (x - m) * a.l.inv_t;
+  }
+  if (lane == 0) {
+    a.l.loss[r] = live ? loss : 0.0f;
+    if (a.l.lse != nullptr) a.l.lse[r] = live ? m * a.l.inv_t + tail : -INFINITY;
+    const float k = live ? a.l.scale * row_weight(a.l, r) * a.l.inv_t : 0.0f;
+    a.stat[i] = make_float4(m, live ? k * mass / s : 0.0f, k, 0.0f);
+  }
+}
+
+// g of one piece of the vocabulary (columns c0 .. c0 + cols - 1): a 256 x 256
+// tile per workgroup, zeros past the columns and in the rows that pad the
+// rows in play.
+template <bool DISTILL>
+__global__ __launch_bounds__(kThreads, 1) void k_lm_loss_g(LmLossArgs a) {
+  __shared__ __align__(16) bf16_t lds[2 * kBufElems];
+  const int64_t n = *a.count;
+  const int nrt = (int)((n + TM - 1) / TM), nct = (a.cols + TN - 1) / TN;
+  if ((int64_t)blockIdx.x >= (int64_t)nrt * nct) return;
+  int rt, ct;
+  tile_of(blockIdx.x, nrt, nct, rt, ct);
+  const int64_t row0 = (int64_t)rt * TM, i = row0 + nt_lane_row();
+  NtRows src{static_cast<const bf16_t*>(a.w) + (int64_t)a.c0 * a.H, a.hp, a.cols, row0, n, a.H, ct, ct + 1};
+  nt_stream(lds, src, [&](int tile, NtAcc& acc) {
+    nt_row_per_lane(acc);
+    if (i >= lm_loss_pad(n)) return;
+    const float4 st = i < n ? a.stat[i] : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    const int label = !DISTILL && i < n ? a.l.idx[a.rows[i]] - a.c0 : -1;
+    bf16_t* G = a.g + i * a.ldg;
+#pragma unroll 1
+    for (int ch = 0; ch < 16; ++ch) {
+      const int c = tile * TN + nt_chunk_col(ch);
+      float x[8], g[8];
+      nt_chunk(acc, ch, x);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        g[j] = st.y * lse_term(x[j], st.x, a.l.c) - (c + j == label ? st.z : 0.0f);
+        if (i >= n || c + j >= a.cols) g[j] = 0.0f;
+      }
+      store8(G + c, g);
+    }
+  });
+}
+
+// The distillation's members of that piece, each from its own logit and by the
+// first of the members that name the column.  One wavefront per row.
+__global__ __launch_bounds__(256) void k_lm_loss_fix(LmLossArgs a) {
+  const int lane = threadIdx.x & 63;
+  const int64_t i = (int64_t)blockIdx.x * 4 + wave_id();
+  if (i >= *a.count) return;
+  const int64_t r = a.rows[i];
+  const int K = a.l.K;
+  const int id = lane < K ? a.mid[r * K + lane] : -1;
+  const float p = lane < K ? a.mp[r * K + lane] : 0.0f;
+  float sum = 0.0f;
+  bool first = id >= a.c0 && id < a.c0 + a.cols;
+  for (int k = 0; k < K; ++k) {
+    const bool same = lane_i(id, k) == id;
+    sum += same ? lane_f(p, k) : 0.0f;
+    first = first && !(same && k < lane);
+  }
+  if (!first) return;
+  const float4 st = a.stat[i];
+  store1(a.g + i * a.ldg + (id - a.c0), st.y * lse_term(a.mx[i * K + lane], st.x, a.l.c) - st.z * sum);
+}
+
+// dh of a piece: 256 x 256 tiles of g W, the piece's columns in `splits` ranges
+// of `per` (few rows: more workgroups).  One piece and one range write the
+// rounded result; otherwise acc[range] holds the fp32 sums, which the last
+// piece (one range) or k_lm_loss_dh_out turns into the result.
+__global__ __launch_bounds__(kThreads, 1) void k_lm_loss_dh(LmLossArgs a) {
+  __shared__ __align__(16) bf16_t lds[2 * kBufElems];
+  const int lane = threadIdx.x & 63, w = wave_id();
+  const int64_t n = *a.count;
+  const int nrt = (int)((n + TM - 1) / TM), nct = (a.H + TN - 1) / TN;
+  const int64_t tiles = (int64_t)nrt * nct;
+  if ((int64_t)blockIdx.x >= tiles * a.splits) return;
+  const int z = (int)(blockIdx.x / tiles), k0 = z * a.per, K = min(a.per, a.cols - k0);
+  if (K <= 0) return;  // (a short last piece)
+  int rt, ct;
+  tile_of((int)(blockIdx.x % tiles), nrt, nct, rt, ct);
+  const int64_t row0 = (int64_t)rt * TM;
+  const int n0 = ct * TN;
+  const bool add = a.c0 > 0, out = a.splits == 1 && a.c0 + a.cols == a.l.V;
+  float* sums = a.acc != nullptr ? a.acc + (int64_t)z * a.l.R * a.H : nullptr;
+  NtTile<KRows<false>, false> src{{static_cast<const bf16_t*>(a.w) + (int64_t)(a.c0 + k0) * a.H, a.H, a.H, n0, K},
+                                  {a.g + k0, a.ldg, row0, n, K},
+                                  K};
+  nt_stream(lds, src, [&](int, NtAcc& acc) {
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      const int64_t i = row0 + g * 128 + (w & 3) * 32 + (lane & 31);
+      if (i >= n) continue;
+      bf16_t* D = static_cast<bf16_t*>(a.dh) + (int64_t)a.rows[i] * a.H;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int col = n0 + (q >> 1) * 128 + (w >> 2) * 64 + (lane >> 5) * 32 + (q & 1) * 16;
+        if (col >= a.H) continue;  // H and col are multiples of 16
+        const f32x16& c = acc[q >> 1][g][q & 1];
+#pragma unroll
+        for (int e = 0; e < 16; e += 8) {
+          float v[8] = {c[e], c[e + 1], c[e + 2], c[e + 3], c[e + 4], c[e + 5], c[e + 6], c[e + 7]};
+          if (add) {
+            float o[8];
+            load8(sums + i * a.H + col + e, o);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] += o[j];
+          }
+          if (out)
+            store8(D + col + e, v);
+          else
+            store8(sums + i * a.H + col + e, v);
+        }
+      }
+    }
+  });
+}
+
+__global__ __launch_bounds__(256) void k_lm_loss_dh_out(LmLossArgs a) {
+  const int lane = threadIdx.x & 63;
+  const int64_t i = (int64_t)blockIdx.x * 4 + wave_id();
+  if (i >= *a.count) return;
+  bf16_t* D = static_cast<bf16_t*>(a.dh) + (int64_t)a.rows[i] * a.H;
+  for (int k = lane * 8; k < a.H; k += kWave * 8) {
+    float v[8];
+    load8(a.acc + i * a.H + k, v);
+    for (int z = 1; z < a.splits; ++z) {
+      float o[8];
+      load8(a.acc + ((int64_t)z * a.l.R + i) * a.H + k, o);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] += o[j];
+    }
+    store8(D + k, v);
+  }
+}
+
+// dW of a piece: 256 x 256 tiles of g^T h over the rows in play (whole stages:
+// the rows behind them are zeros in both operands).
+template <typename T>
+__global__ __launch_bounds__(kThreads, 1) void k_lm_loss_dw(LmLossArgs a) {
+  __shared__ __align__(16) bf16_t lds[2 * kBufElems];
+  const int lane = threadIdx.x & 63, w = wave_id();
+  const int K = (int)lm_loss_pad(*a.count);
+  const int nrt = (a.cols + TM - 1) / TM;
+  int rt, ct;
+  tile_of(blockIdx.x, nrt, (a.H + TN - 1) / TN, rt, ct);
+  const int row0 = rt * TM, n0 = ct * TN;
+  T* D = static_cast<T*>(a.dw) + (int64_t)a.c0 * a.H;
+  auto write = [&](const NtAcc& acc) {
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      const int row = row0 + g * 128 + (w & 3) * 32 + (lane & 31);
+      if (row >= a.cols) continue;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int col = n0 + (q >> 1) * 128 + (w >> 2) * 64 + (lane >> 5) * 32 + (q & 1) * 16;
+        if (col >= a.H) continue;  // H and col are multiples of 16
+        const f32x16& c = acc[q >> 1][g][q & 1];
+#pragma unroll
+        for (int e = 0; e < 16; e += 8) {
+          const float v[8] = {c[e], c[e + 1], c[e + 2], c[e + 3], c[e + 4], c[e + 5], c[e + 6], c[e + 7]};
+          store8(D + (int64_t)row * a.H + col + e, v);
+        }
+      }
+    }
+  };
+  if (K == 0) {  // no row in play
+    NtAcc acc;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) acc[q >> 2][(q >> 1) & 1][q & 1] = f32x16{};
+    write(acc);
+    return;
+  }
+  NtTile<KMajor<false, false>, true> src{{a.hp, a.H, a.H, n0, K}, {a.g, a.ldg, a.ldg, row0, K}, K};
+  nt_stream(lds, src, [&](int, NtAcc& acc) { write(acc); });
+}

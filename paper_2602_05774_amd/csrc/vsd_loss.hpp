@@ -1,0 +1,93 @@
+// Shared by the base losses' kernels: a row's members (the label of the cross
+// entropy, the teacher's top logits of the distillation) and log-sum-exps.
+//
+// A row's log-sum-exp is held as (m, s): m its largest logit (raw), s the sum
+// of exp2((x - m) c), c = log2(e) / T.  The difference x - m is formed before
+// it is scaled: near the maximum, where the large probabilities are, it is
+// exact or nearly so, while x c - m c would carry half an ulp of the product.
+// A row that has seen nothing has m = -FLT_MAX and s = 0; a -inf logit adds 0
+// to it.  (s is finite or, from a NaN or +inf logit, NaN, and stays NaN.)
+#pragma once
+
+#include "vsd_device.hpp"
+#include "vsd_kernels.hpp"
+
+namespace vsd {
+
+__device__ __forceinline__ float lse_term(float x, float m, float c) {
+  return __builtin_amdgcn_exp2f((x - m) * c);
+}
+__device__ __forceinline__ void lse_join(float& m, float& s, float om, float os, float c) {
+  const float nm = fmaxf(m, om);
+  s = s * lse_term(m, nm, c) + os * lse_term(om, nm, c);
+  m = nm;
+}
+template <int CTRL>
+__device__ __forceinline__ void lse_step(float& m, float& s, float c) {
+  lse_join(m, s, dpp_f<CTRL>(m), dpp_f<CTRL>(s), c);
+}
+__device__ __forceinline__ void wave_lse(float& m, float& s, float c) {
+  lse_step<kDppQuad1>(m, s, c);
+  lse_step<kDppQuad2>(m, s, c);
+  lse_step<kDppHalfMirror>(m, s, c);
+  lse_step<kDppMirror>(m, s, c);
+  float rm = lane_f(m, 0), rs = lane_f(s, 0);
+#pragma unroll
+  for (int r = 1; r < 4; ++r) lse_join(rm, rs, lane_f(m, 16 * r), lane_f(s, 16 * r), c);
+  m = rm;
+  s = rs;
+}
+// Eight logits of a row.
+__device__ __forceinline__ void lse_add8(const float (&x)[8], float& m, float& s, float c) {
+  const float nm = fmaxf(m, max8(x));
+  s *= lse_term(m, nm, c);
+  m = nm;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) s += lse_term(x[k], m, c);
+}
+
+// One row's members, lane k holding member k: its column (-1: none), its
+// probability p and p log p.  Teacher values val / T_p are normalised over the
+// row's members or by the teacher's log-sum-exp.  A member of value -inf has
+// probability 0 and takes no further part.
+struct Member {
+  int id;
+  float p, plogp;
+};
+__device__ __forceinline__ Member load_member(const LossArgs& a, int64_t r, int lane) {
+  Member e{-1, 0.0f, 0.0f};
+  float v = -INFINITY;
+  if (lane < a.K) {
+    const int64_t at = r * a.K + lane;
+    e.id = a.idx[at];
+    if ((uint32_t)e.id >= (uint32_t)a.V) {
+      if (e.id != -1) report_error(a.err, VSD_DEVERR_TOKEN_RANGE);
+      e.id = -1;
+    } else {
+      v = (a.val_bf16 ? load1(static_cast<const bf16_t*>(a.val) + at) : static_cast<const float*>(a.val)[at]) * a.inv_tp;
+    }
+  }
+  const float top = wave_max(v);
+  const bool in = e.id >= 0 && v != -INFINITY;
+  float lp;
+  if (a.teacher_lse != nullptr) {
+    lp = v - a.teacher_lse[r];
+  } else {
+    const float sum = wave_sum(in ? expf(v - top) : 0.0f);
+    lp = (v - top) - logf(sum);
+  }
+  if (in) {
+    e.p = expf(lp);
+    e.plogp = e.p > 0.0f || e.p != e.p ? e.p * lp : 0.0f;
+  } else {
+    e.id = -1;
+  }
+  return e;
+}
+
+// Whether a row takes part by its weight.
+__device__ __forceinline__ float row_weight(const LossArgs& a, int64_t r) {
+  return a.weight != nullptr ? a.weight[r] : 1.0f;
+}
+
+}  // namespace vsd

@@ -1,0 +1,235 @@
+"""The base losses through an LM head against the float64 oracle, and the
+operators together as a training step uses them."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2602_05774_amd as vsd
+from oracle import losses as lo
+from tests import loss_bars as bars
+from tests.test_gpu_losses import _host, _members
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+BF = torch.bfloat16
+
+
+def _head(R, V, H, seed):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    h = (torch.randn(R, H, generator=g, device=DEV) * 1.5).to(BF)
+    w = (torch.randn(V, H, generator=g, device=DEV) * H ** -0.5 * 2).to(BF)
+    return h, w
+
+
+def _check(res, h, w, mem, weight, T, scale, V):
+    """Bars: a logit's sum of H exact products in float32, H u sum |h w| (any order); g is
+    rounded to bf16 (2^-8) and dh, dW are float32 sums of exact products with it
+    (n u sum |g| |w|), rounded once to their type."""
+    idx, p, plogp = mem
+    wt = None if weight is None else weight.cpu().numpy()
+    ref = lo.head(h, w, mem, wt, T, scale)
+    live = ref["live"]
+    hz = np.where(live[:, None], h, 0.0)
+    H = h.shape[1]
+    dx = H * bars.U * np.max(np.abs(hz) @ np.abs(w).T, axis=1) / T
+    x = hz @ w.T
+    m = np.where(live, x.max(1), 0.0)
+    runs = 2 * math.ceil(V / 256)
+    bar = bars.loss_bar(ref, x, idx, p, m, V, T, runs, dx)
+    loss = _host(res.loss_row)
+    assert np.all(np.abs(loss - ref["loss"]) <= bar), np.max(np.abs(loss - ref["loss"]) / bar)
+    assert np.all(loss[~live] == 0) and np.all(_host(res.lse)[~live] == 0)
+    assert np.all((np.abs(_host(res.lse) - ref["lse"]) <= bars.lse_bar(ref["lse"], m, V, T, runs, dx))[live])
+    wv = np.ones(len(h)) if wt is None else wt.astype(np.float64)
+    used = np.where(live, np.abs(wv), 0.0)
+    assert abs(float(res.loss_total) - ref["total"]) <= abs(scale) * np.sum(used * bar) + 2 * bars.U * abs(ref["total"])
+    if res.grad is None:
+        return
+    k = abs(scale) * used / T
+    gb = bars.grad_bar(ref, x, idx, p, m, V, T, k, "bf16", runs, dx[:, None])
+    ga = np.abs(ref["grad"]) + gb
+    dh = _host(res.grad.grad_hidden)
+    bh = gb @ np.abs(w) + V * bars.U * (ga @ np.abs(w))
+    bh += 2.0 ** -8 * (np.abs(ref["grad_hidden"]) + bh) + 1e-37
+    assert np.all(np.abs(dh - ref["grad_hidden"]) <= bh), np.max(np.abs(dh - ref["grad_hidden"]) / bh)
+    assert np.all(dh[~live] == 0)
+    if res.grad.grad_weight is not None:
+        half = 2.0 ** -8 if res.grad.grad_weight.dtype == BF else 2.0 ** -24
+        dw = _host(res.grad.grad_weight)
+        bw = gb.T @ np.abs(hz) + (len(h) + 64) * bars.U * (ga.T @ np.abs(hz))
+        bw += half * (np.abs(ref["grad_weight"]) + bw) + 1e-37
+        assert np.all(np.abs(dw - ref["grad_weight"]) <= bw), np.max(np.abs(dw - ref["grad_weight"]) / bw)
+
+
+SHAPES = [(1, 1, 64), (1, 300, 128), (5, 7, 64), (63, 256, 64), (64, 257, 192), (65, 1000, 320), (257, 5003, 128),
+          (600, 2049, 256), (48, 33000, 512), (1300, 700, 64)]
+
+
+@pytest.mark.parametrize("R,V,H", SHAPES)
+@pytest.mark.parametrize("dw", (False, torch.float32, BF))
+def test_cross_entropy(R, V, H, dw):
+    h, w = _head(R, V, H, 31)
+    labels = torch.randint(0, V, (R,), device=DEV, dtype=torch.int32)
+    weight = torch.rand(R, device=DEV) + 0.5
+    if R > 4:
+        labels[::3] = -1                      # out of play: whatever the rows hold
+        h[0] = math.nan
+        h[3, 5] = math.inf
+        weight[4] = 0.0
+        h[4] = math.nan
+        weight[0] = math.nan
+    ref_h = _host(h)
+    res = vsd.cross_entropy(vsd.LmHead(h, w), labels, weight, 0.8, 1.5, grad=True, weight_grad=dw)
+    assert int(res.device_error) == 0
+    mem = lo.label_members(labels.cpu().numpy())
+    _check(res, ref_h, _host(w), mem, weight, 0.8, 1.5, V)
+    only = vsd.cross_entropy(vsd.LmHead(h, w), labels, weight, 0.8, 1.5)
+    assert torch.equal(only.loss_row, res.loss_row) and torch.equal(only.lse, res.lse)
+
+
+@pytest.mark.parametrize("R,V,H,K", [(1, 5, 64, 2), (33, 300, 64, 64), (65, 1003, 128, 10), (300, 5003, 192, 33),
+                                     (20, 33000, 256, 16)])
+@pytest.mark.parametrize("lse", (False, True))
+def test_distillation(R, V, H, K, lse):
+    h, w = _head(R, V, H, 32)
+    mem, (idx, val, z) = _members(R, V, K, 5, lse, 1.25, dup=K in (33, 64))
+    weight = torch.rand(R, device=DEV) + 0.5
+    if R > 2:
+        h[2] = math.nan
+    res = vsd.distill_loss(vsd.LmHead(h, w), idx, val, z, weight, 0.8, 1.25, 0.5, grad=True, weight_grad=torch.float32)
+    assert int(res.device_error) == 0
+    _check(res, _host(h), _host(w), mem, weight, 0.8, 0.5, V)
+
+
+def test_no_row_in_play():
+    h, w = _head(70, 500, 128, 33)
+    h[:] = math.nan
+    labels = torch.full((70,), -1, dtype=torch.int32, device=DEV)
+    for R in (70, 1):
+        res = vsd.cross_entropy(vsd.LmHead(h[:R], w), labels[:R], grad=True, weight_grad=True)
+        assert float(res.loss_total) == 0 and torch.all(res.loss_row == 0) and torch.all(res.lse == 0)
+        assert torch.all(res.grad.grad_hidden == 0) and torch.all(res.grad.grad_weight == 0)
+
+
+def test_bad_labels_are_reported_and_skipped():
+    h, w = _head(4, 100, 64, 34)
+    labels = torch.tensor([5, 100, -2, 7], dtype=torch.int32, device=DEV)
+    res = vsd.cross_entropy(vsd.LmHead(h, w), labels, grad=True)
+    assert int(res.device_error) == 1 and torch.all(res.loss_row[1:3] == 0) and torch.all(res.grad.grad_hidden[1:3] == 0)
+
+
+@pytest.mark.parametrize("loss", ("ce", "distill"))
+def test_pieces(loss):
+    """More rows than one piece's gradient may hold: every row against the same rows of a
+    small call (one piece), the weight's gradient against float64 products on the device."""
+    R, V, H, K = 70001, 9001, 64, 6
+    assert vsd.loss_workspace_bytes(R, V, H, 0, True) < 2 * R * V
+    h, w = _head(R, V, H, 35)
+    labels = torch.randint(-1, V, (R,), device=DEV, dtype=torch.int32)
+    idx = torch.randint(0, V, (R, K), device=DEV, dtype=torch.int32)
+    val = torch.randn(R, K, device=DEV)
+
+    def call(s, **kw):
+        head = vsd.LmHead(h[s].contiguous(), w)
+        if loss == "ce":
+            return vsd.cross_entropy(head, labels[s].contiguous(), grad=True, **kw)
+        return vsd.distill_loss(head, idx[s].contiguous(), val[s].contiguous(), grad=True, **kw)
+
+    res = call(slice(0, R), weight_grad=torch.float32)
+    for s in (slice(0, 500), slice(40000, 40300), slice(R - 70, R)):
+        part = call(s)
+        assert torch.allclose(res.loss_row[s], part.loss_row, rtol=1e-5, atol=1e-6)
+        a, b = res.grad.grad_hidden[s].double(), part.grad.grad_hidden.double()
+        # each is one rounding (2^-8) from sums of the same bf16 g in another order
+        assert torch.all((a - b).abs() <= 2 ** -7 * b.abs() + 1e-4 * b.abs().amax())
+    dw = torch.zeros(V, H, dtype=torch.float64, device=DEV)
+    for lo_ in range(0, R, 10000):
+        s = slice(lo_, min(R, lo_ + 10000))
+        x = h[s].double() @ w.double().t()
+        g = torch.softmax(x, 1)
+        at = labels[s].long()[:, None] if loss == "ce" else idx[s].long()
+        p = (at >= 0).double() if loss == "ce" else torch.softmax(val[s].double(), 1)
+        g *= p.sum(1, keepdim=True)
+        g.scatter_add_(1, at.clamp(min=0), -p)
+        dw += g.t() @ h[s].double()
+    err = (res.grad.grad_weight.double() - dw).norm() / dw.norm()
+    assert err < 2 ** -8, float(err)  # every g is within 2^-8 of its value
+
+
+def test_captured_calls_and_a_kept_workspace():
+    R, V, H = 130, 3001, 128
+    h, w = _head(R, V, H, 36)
+    new = [_head(R, V, H, s)[0] for s in (37, 38)]
+    labels = torch.randint(-1, V, (R,), device=DEV, dtype=torch.int32)
+    idx = torch.randint(0, V, (R, 8), device=DEV, dtype=torch.int32)
+    val = torch.randn(R, 8, device=DEV)
+    ws = torch.full((vsd.loss_workspace_bytes(R, V, H, 8, True),), 255, dtype=torch.uint8, device=DEV)
+
+    def chain(ws=None):
+        c = vsd.cross_entropy(vsd.LmHead(h, w), labels, grad=True, weight_grad=True, workspace=ws)
+        d = vsd.distill_loss(vsd.LmHead(h, w), idx, val, grad=True, weight_grad=BF, workspace=ws)
+        return [*c[:3], *c.grad[::2], *d[:3], *d.grad[::2]]
+
+    ref = chain()
+    for a, b in zip(ref, chain(ws)):  # (whatever the workspace held)
+        assert torch.equal(a, b)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        outs = chain(ws)
+    for x in new:
+        h.copy_(x)
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(chain(), outs):
+            assert torch.equal(a, b)
+
+
+def test_gradient_buffers_and_refusals():
+    h, w = _head(20, 300, 64, 39)
+    labels = torch.randint(0, 300, (20,), device=DEV, dtype=torch.int32)
+    head = vsd.LmHead(h, w)
+    ref = vsd.cross_entropy(head, labels, grad=True, weight_grad=BF)
+    bufs = vsd.LmHeadGrad(torch.empty_like(h), None, torch.empty_like(w))
+    res = vsd.cross_entropy(head, labels, grad=bufs)
+    assert res.grad is bufs and torch.equal(bufs.grad_hidden, ref.grad.grad_hidden)
+    assert torch.equal(bufs.grad_weight, ref.grad.grad_weight)
+    assert ref.grad.grad_logits is None
+    for bad in (torch.empty_like(h), vsd.LmHeadGrad(torch.empty_like(h), torch.empty_like(h)),
+                vsd.LmHeadGrad(h.float(), None), vsd.LmHeadGrad(h[:3], None), vsd.LmHeadGrad(None, None),
+                vsd.LmHeadGrad(torch.empty_like(h), None, w.half())):
+        with pytest.raises(ValueError):
+            vsd.cross_entropy(head, labels, grad=bad)
+    with pytest.raises(ValueError):
+        vsd.cross_entropy(head, labels, weight_grad=True)
+    with pytest.raises(ValueError):
+        vsd.cross_entropy(head, labels, grad=True, workspace=torch.empty(4, device=DEV))
+
+
+def test_training_step_with_stored_teacher_logits():
+    """The teacher's rows give their top logits over the draft's tokens; the draft's
+    LM head is trained on them and on the data's labels; the two gradients add up."""
+    R, Vt, Vd, H, K = 150, 9000, 2500, 128, 12
+    h, w = _head(R, Vd, H, 40)
+    Y = (torch.randn(R, Vt, device=DEV) * 3).to(BF)
+    d2t = torch.randperm(Vt, device=DEV)[:Vd].sort().values.int()
+    labels = torch.randint(-1, Vd, (R,), device=DEV, dtype=torch.int32)
+    weight = torch.where(labels >= 0, 1.0 / (labels >= 0).sum(), 0.0)
+    top = vsd.top_logits(Y, K, d2t=d2t, temp_target=2.0)
+    head = vsd.LmHead(h, w)
+    kd = vsd.distill_loss(head, top.idx, top.logits, top.lse, temp_draft=2.0, temp_target=2.0, loss_scale=0.7 * 4 / R,
+                          grad=True, weight_grad=True)
+    ce = vsd.cross_entropy(head, labels, weight, loss_scale=0.3, grad=True, weight_grad=True)
+    dh = kd.grad.grad_hidden.double() + ce.grad.grad_hidden.double()
+    dw = kd.grad.grad_weight.double() + ce.grad.grad_weight.double()
+    y, hh, ww = _host(Y), _host(h), _host(w)
+    idx, val, lse = lo.top(y, K, d2t.cpu().numpy(), 2.0)
+    a = lo.head(hh, ww, lo.teacher_members(idx, val, lse, 2.0), None, 2.0, 0.7 * 4 / R)
+    b = lo.head(hh, ww, lo.label_members(labels.cpu().numpy()), weight.cpu().numpy(), 1.0, 0.3)
+    assert abs(float(kd.loss_total) - a["total"]) < 1e-5 * abs(a["total"])
+    assert abs(float(ce.loss_total) - b["total"]) < 1e-5 * abs(b["total"])
+    for got, ref in ((dh, a["grad_hidden"] + b["grad_hidden"]), (dw, a["grad_weight"] + b["grad_weight"])):
+        # each summand's elements are within 2^-8 (g) and 2^-8 (dh) of their values
+        assert np.linalg.norm(got.cpu().numpy() - ref) < 2 ** -6.5 * np.linalg.norm(ref)
