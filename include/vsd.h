@@ -366,7 +366,7 @@ typedef struct vsd_grad {
 typedef struct vsd_rows {
   int64_t R;           /* 1 <= R < 2^24 */
   int64_t ld;          /* row stride of the logits, elements (fused: unused) */
-  int32_t v;           /* vocabulary size, >= 1 */
+  int32_t v;           /* vocabulary size, 1 <= v <= 2^30 */
   int32_t dtype;       /* vsd_dtype of the logits (fused: VSD_BF16) */
   int32_t hidden_dim;  /* fused LM head: H (multiple of 64); 0 otherwise */
 } vsd_rows;
@@ -376,6 +376,8 @@ typedef struct vsd_loss_out {
   float* lse;            /* [R] optional */
   float* loss_total;     /* [1] optional */
   int32_t* device_error; /* [1] required */
+  int32_t* counter;      /* [1] optional: a word that is 0 before the call, and after it; with
+                            few rows the total then takes no launch of its own (same result) */
 } vsd_loss_out;
 
 typedef struct vsd_loss_grad {
@@ -589,8 +591,9 @@ vsd_status vsd_distill_loss(const vsd_rows* rows, const vsd_src* draft, int32_t 
                             void* hip_stream);
 
 /* The k largest logits of each row: top_idx and top_logits [R, k], lse [R]
- * (optional).  Materialised logits only.  With a map, `workspace` must hold
- * vsd_top_workspace_bytes(rows, 1) bytes; without one it may be NULL. */
+ * (optional).  Materialised logits only.  `workspace` must hold
+ * vsd_top_workspace_bytes(rows, k, d2t != NULL) bytes (16-B aligned; 0 for many
+ * rows without a map). */
 vsd_status vsd_top_logits(const vsd_rows* rows, const vsd_src* target, int32_t k, const int32_t* d2t,
                           int32_t v_draft, float temp_target, int32_t* top_idx, float* top_logits,
                           float* lse, void* workspace, size_t workspace_bytes, int32_t* device_error,
@@ -598,7 +601,7 @@ vsd_status vsd_top_logits(const vsd_rows* rows, const vsd_src* target, int32_t k
 
 /* Bytes of workspace the calls above need (host only). */
 vsd_status vsd_loss_workspace_bytes(const vsd_rows* rows, int32_t k, int32_t with_grad, size_t* bytes);
-vsd_status vsd_top_workspace_bytes(const vsd_rows* rows, int32_t with_map, size_t* bytes);
+vsd_status vsd_top_workspace_bytes(const vsd_rows* rows, int32_t k, int32_t with_map, size_t* bytes);
 
 const char* vsd_status_string(vsd_status status); /* static string */
 const char* vsd_last_error(void);                 /* thread-local detail */

@@ -5,8 +5,10 @@
 //   gradient       g_v = scale w / T (P q_v - sum_{k: i_k = v} p_k)
 // (the cross entropy is P = 1 with one member, the label).
 //
-// One workgroup per row: its log-sum-exp in one sweep, then, with the gradient,
-// a second sweep that writes g.  A row out of play is not read.
+// One workgroup per row.  With the gradient the row stays in registers (kNch
+// groups of eight columns per thread, all loads in flight at once) while its
+// log-sum-exp is formed, so the logits are read once and g is written once;
+// longer rows (kNch = 0) are read twice.  A row out of play is not read.
 #include "vsd_device.hpp"
 #include "vsd_kernels.hpp"
 #include "vsd_loss.hpp"
@@ -15,10 +17,8 @@ namespace vsd {
 
 namespace {
 
-constexpr int kThreads = 256;
-
-template <typename T, bool DISTILL, bool GRAD>
-__global__ __launch_bounds__(kThreads) void k_row_loss(LossArgs a) {
+template <typename T, bool DISTILL, bool GRAD, int kThreads, int kNch, bool kMore>
+__device__ __forceinline__ void row_loss(const LossArgs& a) {
   constexpr int kWaves = kThreads / kWave, kStep = kThreads * 8;
   __shared__ float red_m[kWaves], red_s[kWaves];
   __shared__ int sid[DISTILL ? kMaxMembers : 1];
@@ -29,6 +29,7 @@ __global__ __launch_bounds__(kThreads) void k_row_loss(LossArgs a) {
   const T* X = static_cast<const T*>(a.X) + r * a.ld;
   T* G = static_cast<T*>(a.G) + (GRAD ? r * a.ldg : 0);
   const float w = row_weight(a, r);
+  const int first = threadIdx.x * 8;
 
   // the row's members (every wavefront has the label; the first one the teacher's)
   Member e{-1, 1.0f, 0.0f};
@@ -56,14 +57,40 @@ __global__ __launch_bounds__(kThreads) void k_row_loss(LossArgs a) {
   if (wave == 0 && live && e.id >= 0) x_mine = load1(X + e.id);
 
   float m = kNegBig, s = 0.0f;
+  Raw8<T> row[kNch > 0 ? kNch : 1];
   if (live) {
-    int base = threadIdx.x * 8;
-    for (; base + 8 <= a.V; base += kStep) {
-      float x[8];
-      load8(X + base, x);
-      lse_add8(x, m, s, a.c);
+    if constexpr (kNch > 0) {
+#pragma unroll
+      for (int j = 0; j < kNch; ++j) load_cols(row[j], X, first + j * kStep, a.V);
+#pragma unroll
+      for (int j = 0; j < kNch; ++j) {
+        float x[8];
+        row[j].get(x);
+        lse_add8(x, m, s, a.c);
+      }
     }
-    for (int v = base; v < min(a.V, base + 8); ++v) lse_join(m, s, load1(X + v), 1.0f, a.c);
+    if constexpr (kMore) {  // what does not fit the registers
+      constexpr int U = 4;  // loads in flight per lane
+      int base = first + kNch * kStep;
+      for (; base + (U - 1) * kStep + 8 <= a.V; base += U * kStep) {
+        Raw8<T> q[U];
+#pragma unroll
+        for (int u = 0; u < U; ++u) q[u].load(X + base + u * kStep);
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          float x[8];
+          q[u].get(x);
+          lse_add8(x, m, s, a.c);
+        }
+      }
+      for (; base < a.V; base += kStep) {
+        Raw8<T> q;
+        float x[8];
+        load_cols(q, X, base, a.V);
+        q.get(x);
+        lse_add8(x, m, s, a.c);
+      }
+    }
     wave_lse(m, s, a.c);
     if (lane == 0) {
       red_m[wave] = m;
@@ -88,68 +115,152 @@ __global__ __launch_bounds__(kThreads) void k_row_loss(LossArgs a) {
     }
     if (DISTILL) loss = wave_sum(loss);
     if (lane == 0) {
-      a.loss[r] = loss;
+      // (with the total in this launch, another XCD's workgroup reads it)
+      __hip_atomic_store(a.loss + r, loss, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
       if (a.lse != nullptr) a.lse[r] = live ? m * a.inv_t + tail : empty ? -INFINITY : 0.0f;
     }
   }
   if (!GRAD) return;
 
-  const float k = a.scale * w * a.inv_t;
-  const float kq = live ? k * mass / s : 0.0f;
-  auto grad_of = [&](float x) { return live ? kq * lse_term(x, m, a.c) : 0.0f; };
-  const int label = DISTILL || !live ? -1 : e.id;
-  int base = threadIdx.x * 8;
-  for (; base + 8 <= a.V; base += kStep) {
-    float x[8] = {0, 0, 0, 0, 0, 0, 0, 0}, g[8];
-    if (live) load8(X + base, x);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) g[j] = grad_of(x[j]) - (base + j == label ? k : 0.0f);
-    store8(G + base, g);
+  if (!live) {
+    const float zero[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    int base = first;
+    for (; base + 8 <= a.V; base += kStep) store8(G + base, zero);
+    for (int v = base; v < min(a.V, base + 8); ++v) store1(G + v, 0.0f);
+    return;
   }
-  for (int v = base; v < min(a.V, base + 8); ++v)
-    store1(G + v, (live ? grad_of(load1(X + v)) : 0.0f) - (v == label ? k : 0.0f));
-  if (!DISTILL || !live) return;
+  const float k = a.scale * w * a.inv_t, kq = k * mass / s;
+  auto grad_of = [&](float x) { return kq * lse_term(x, m, a.c); };
+  const int label = DISTILL ? -1 : e.id;
+  auto write = [&](const Raw8<T>& q, int base) {
+    float x[8], g[8];
+    q.get(x);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) g[j] = grad_of(x[j]);
+    if ((uint32_t)(label - base) < 8u) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) g[j] -= base + j == label ? k : 0.0f;
+    }
+    if (base + 8 <= a.V) {
+      store8(G + base, g);
+    } else {
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (base + j < a.V) store1(G + base + j, g[j]);
+    }
+  };
+  if constexpr (kNch > 0) {
+#pragma unroll
+    for (int j = 0; j < kNch; ++j)
+      if (first + j * kStep < a.V) write(row[j], first + j * kStep);
+  }
+  if constexpr (kMore) {
+    constexpr int U = 2;
+    int base = first + kNch * kStep;
+    for (; base + (U - 1) * kStep + 8 <= a.V; base += U * kStep) {
+      Raw8<T> q[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) q[u].load(X + base + u * kStep);
+#pragma unroll
+      for (int u = 0; u < U; ++u) write(q[u], base + u * kStep);
+    }
+    for (; base < a.V; base += kStep) {
+      Raw8<T> q;
+      load_cols(q, X, base, a.V);
+      write(q, base);
+    }
+  }
+  if (!DISTILL) return;
   // the members' columns again, each from its own logit and by the first of
   // the members that name it, so that every element is rounded once
   __syncthreads();
   if (wave != 0 || e.id < 0) return;
   float p = 0.0f;
-  bool first = true;
+  bool mine = true;
   for (int j = 0; j < a.K; ++j) {
     const bool same = sid[j] == e.id;
     p += same ? sp[j] : 0.0f;
-    first = first && !(same && j < lane);
+    mine = mine && !(same && j < lane);
   }
-  if (first) store1(G + e.id, grad_of(x_mine) - k * p);
+  if (mine) store1(G + e.id, grad_of(x_mine) - k * p);
 }
 
-// loss_scale sum_r w_r l_r over a call's rows, in a fixed order (64-bit sums:
-// one thread adds R / 1024 rows).
+// loss_scale sum_r w_r l_r over a call's rows, in 64 bits and in one order
+// whatever workgroup forms it: 1024 partial sums of every 1024th row, then
+// those (of 64 consecutive ones a tree, of the 16 results a chain).
 constexpr int kTotalThreads = 1024;
+template <int kThreads>
+__device__ __forceinline__ void row_total(const float* loss, const float* weight, int64_t R, float scale,
+                                          float* total) {
+  __shared__ double part[kTotalThreads / kWave];
+  constexpr int U = 8;  // rows in flight per thread
+  for (int t = threadIdx.x; t < kTotalThreads; t += kThreads) {
+    double acc = 0.0;
+    for (int64_t r0 = t; r0 < R; r0 += U * kTotalThreads) {
+      float l[U], w[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int64_t r = r0 + u * kTotalThreads;
+        l[u] = r < R ? __hip_atomic_load(loss + r, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0.0f;
+        w[u] = r < R && weight != nullptr ? weight[r] : 1.0f;
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) acc += l[u] != 0.0f ? (double)l[u] * w[u] : 0.0;  // (out of play: any weight)
+    }
+    for (int n = kWave / 2; n > 0; n /= 2) acc += __shfl_xor(acc, n);
+    if ((threadIdx.x & 63) == 0) part[t / kWave] = acc;
+  }
+  __syncthreads();
+  if (threadIdx.x != 0) return;
+  double acc = part[0];
+  for (int k = 1; k < kTotalThreads / kWave; ++k) acc += part[k];
+  *total = (float)(acc * scale);
+}
+
 __global__ __launch_bounds__(kTotalThreads) void k_row_total(const float* loss, const float* weight, int64_t R,
                                                              float scale, float* total) {
-  __shared__ double part[kTotalThreads];
-  double acc = 0.0;
-  for (int64_t r = threadIdx.x; r < R; r += kTotalThreads) {
-    const float l = loss[r];
-    if (l != 0.0f) acc += (double)l * (weight != nullptr ? weight[r] : 1.0f);  // (a row out of play has any weight)
-  }
-  part[threadIdx.x] = acc;
-  for (int n = kTotalThreads / 2; n > 0; n /= 2) {
-    __syncthreads();
-    if ((int)threadIdx.x < n) part[threadIdx.x] += part[threadIdx.x + n];
-  }
-  if (threadIdx.x == 0) *total = (float)(part[0] * scale);
+  row_total<kTotalThreads>(loss, weight, R, scale, total);
 }
 
+template <typename T, bool DISTILL, bool GRAD, int kThreads, int kNch, bool kMore>
+__global__ __launch_bounds__(kThreads) void k_row_loss(LossArgs a) {
+  row_loss<T, DISTILL, GRAD, kThreads, kNch, kMore>(a);
+  if (a.total == nullptr) return;
+  // the last workgroup to come here forms the total
+  __shared__ int last;
+  if (threadIdx.x == 0)  // (the first lane of the wavefront that stored the row's loss)
+    last = __hip_atomic_fetch_add(a.counter, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == (int)gridDim.x - 1;
+  __syncthreads();
+  if (!last) return;
+  if (threadIdx.x == 0) *a.counter = 0;
+  row_total<kThreads>(a.loss, a.weight, a.R, a.scale, a.total);
+}
+
+template <typename T, bool DISTILL, bool GRAD, int kThreads, int kNch, bool kMore = kNch == 0>
+hipError_t launch_n(const LossArgs& a, hipStream_t s) {
+  hipLaunchKernelGGL((k_row_loss<T, DISTILL, GRAD, kThreads, kNch, kMore>), dim3((unsigned)a.R), dim3(kThreads), 0, s,
+                     a);
+  return hipGetLastError();
+}
+
+// Threads per row and whether it stays in registers.
 template <typename T, bool DISTILL>
 hipError_t launch_t(const LossArgs& a, hipStream_t s) {
-  const dim3 grid((unsigned)a.R);
-  if (a.G != nullptr)
-    hipLaunchKernelGGL((k_row_loss<T, DISTILL, true>), grid, dim3(kThreads), 0, s, a);
-  else
-    hipLaunchKernelGGL((k_row_loss<T, DISTILL, false>), grid, dim3(kThreads), 0, s, a);
-  return hipGetLastError();
+  if (a.G == nullptr) {
+    if (a.V <= 2048) return launch_n<T, DISTILL, false, 64, 0>(a, s);
+    if (a.R <= 512 && a.V > 8192) return launch_n<T, DISTILL, false, 1024, 0>(a, s);
+    return launch_n<T, DISTILL, false, 256, 0>(a, s);
+  }
+  constexpr bool kWide = sizeof(T) == 4;
+  constexpr int kFull = kWide ? 8 : 16;
+  if (a.V <= 2048) return launch_n<T, DISTILL, true, 64, 4>(a, s);
+  if (a.V <= 4096) return launch_n<T, DISTILL, true, kWide ? 256 : 128, kWide ? 2 : 4>(a, s);
+  if (a.V <= 8192) return launch_n<T, DISTILL, true, kWide ? 512 : 256, kWide ? 2 : 4>(a, s);
+  if (a.V <= 16384) return launch_n<T, DISTILL, true, kWide ? 1024 : 512, kWide ? 2 : 4>(a, s);
+  if (a.V <= 32768) return launch_n<T, DISTILL, true, kWide ? 1024 : 512, kWide ? 4 : 8>(a, s);
+  if (a.V <= 65536) return launch_n<T, DISTILL, true, 1024, 8>(a, s);
+  if (a.V <= kFull * 8192) return launch_n<T, DISTILL, true, 1024, kFull>(a, s);
+  return launch_n<T, DISTILL, true, 1024, kFull, true>(a, s);
 }
 
 }  // namespace

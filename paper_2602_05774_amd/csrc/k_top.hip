@@ -1,12 +1,15 @@
 // The K largest logits of a row, their indices and the row's log-sum-exp.
 //
-// One workgroup per row.  The first sweep forms the log-sum-exp and every
-// thread's largest entry.  The K-th largest of some threads' maxima is a lower
-// bound of the row's K-th entry, so the second sweep lists the entries that
-// reach it (few more than K) in LDS, and each listed entry's place is the
-// number of entries that beat it.  Order: the larger value first, equal values
-// by the smaller index.  A row with more entries at the bound than the list
-// holds (long runs of equal logits) gets its K-th entry by bisection instead.
+// One workgroup per row, one sweep: it forms the log-sum-exp and, per thread, the
+// largest entry of each of up to 16 groups of its columns.  The K-th largest of
+// some threads' maxima is a lower bound of the row's K-th entry, so the members
+// are among the entries that reach it, in the groups whose maximum does (few
+// more than K): those groups are read again, the entries listed in LDS, and an
+// entry's place is the number of entries that beat it.  Order: the larger value
+// first, equal values by the smaller index.  A row with more groups or entries
+// at the bound than the lists hold (long runs of equal logits) gets its K-th
+// entry by bisection instead.  Few long rows are split into segments, a workgroup
+// each, whose results a second launch joins.
 #include "vsd_device.hpp"
 #include "vsd_kernels.hpp"
 #include "vsd_loss.hpp"
@@ -15,21 +18,56 @@ namespace vsd {
 
 namespace {
 
-constexpr int kThreads = 1024, kWaves = kThreads / kWave;
-constexpr int kCap = 2048;   // listed entries
-constexpr int kMostTop = kMaxMembers;
-// maxima that each wavefront contributes to the bound: together more than K
-__device__ __forceinline__ int maxima_of(int K) { return (K + kWaves - 1) / kWaves + 1; }
-constexpr int kMaxima = kWaves * ((kMostTop + kWaves - 1) / kWaves + 1);
+constexpr int kU = 4;  // loads of 8 columns in flight per thread
+// LDS lists.  Rows of at most 2048 columns (one wavefront, one group a thread)
+// have short ones, so that eight of their wavefronts fit a SIMD.
+template <int kThreads>
+struct Lists {
+  static constexpr bool kShort = kThreads == kWave;
+  static constexpr int kGroups = kShort ? 1 : 16;      // per thread
+  static constexpr int kGroupCap = kShort ? 64 : 1024; // listed groups
+  static constexpr int kCap = kShort ? 512 : 2048;     // listed entries
+};
+constexpr int kShortCols = kWave * 8 * kU;
+constexpr int kRoundsK = 16;  // members up to which the bound comes from rounds of wavefront maxima
+// maxima that each of W wavefronts contributes to it: together more than K
+__host__ __device__ constexpr int maxima_of(int K, int W) { return (K + W - 1) / W + 1; }
 
-__device__ __forceinline__ bool beats(float v, int i, float ov, int oi) { return v > ov || (v == ov && i < oi); }
-
-// A value as an integer in the same order (-0 = +0).
+// A value as an integer in the same order (-0 = +0), and back.
 __device__ __forceinline__ uint32_t order_of(float x) {
   const uint32_t u = __float_as_uint(x + 0.0f);
   return (u & 0x80000000u) != 0u ? ~u : u | 0x80000000u;
 }
+__device__ __forceinline__ float value_of(uint32_t o) {
+  return __uint_as_float((o & 0x80000000u) != 0u ? o & 0x7FFFFFFFu : ~o);
+}
+// An entry as one integer: the larger value, then the smaller index, is the
+// larger key.  0 is below every entry.
+__device__ __forceinline__ uint64_t key_of(float x, int index) {
+  return (uint64_t)order_of(x) << 32 | (uint32_t)~index;
+}
+__device__ __forceinline__ int index_in(uint64_t key) { return (int)~(uint32_t)key; }
+__device__ __forceinline__ float value_in(uint64_t key) { return value_of((uint32_t)(key >> 32)); }
+// How many of keys[0 .. n) (n even, 16-byte aligned) are larger.
+__device__ __forceinline__ int rank_of(uint64_t key, const uint64_t* keys, int n) {
+  int rank = 0;
+  for (int j = 0; j < n; j += 2) {
+    const ulonglong2 k = *reinterpret_cast<const ulonglong2*>(keys + j);
+    rank += (k.x > key ? 1 : 0) + (k.y > key ? 1 : 0);
+  }
+  return rank;
+}
 
+__device__ __forceinline__ uint32_t wave_max_u32(uint32_t v) {
+  v = max(v, (uint32_t)dpp_i<kDppQuad1>((int)v));
+  v = max(v, (uint32_t)dpp_i<kDppQuad2>((int)v));
+  v = max(v, (uint32_t)dpp_i<kDppHalfMirror>((int)v));
+  v = max(v, (uint32_t)dpp_i<kDppMirror>((int)v));
+  return max(max((uint32_t)lane_i((int)v, 0), (uint32_t)lane_i((int)v, 16)),
+             max((uint32_t)lane_i((int)v, 32), (uint32_t)lane_i((int)v, 48)));
+}
+
+template <int kWaves>
 __device__ __forceinline__ int block_sum(int v, int* red) {
   const int s = wave_sum_int(v);
   __syncthreads();
@@ -41,98 +79,169 @@ __device__ __forceinline__ int block_sum(int v, int* red) {
   return t;
 }
 
-template <typename T, bool MAP>
+template <typename T, bool MAP, int kThreads>
 __global__ __launch_bounds__(kThreads) void k_top_logits(TopArgs a) {
-  constexpr int kStep = kThreads * 8;
+  constexpr int kWaves = kThreads / kWave, kStep = kThreads * 8;
+  constexpr int kGroups = Lists<kThreads>::kGroups, kGroupCap = Lists<kThreads>::kGroupCap,
+                kCap = Lists<kThreads>::kCap;
+  constexpr int kShared = kGroups * kThreads > 2 * kCap ? kGroups * kThreads : 2 * kCap;
   __shared__ float red_m[kWaves], red_s[kWaves];
   __shared__ int red_i[kWaves];
-  __shared__ float maxima[kMaxima];
+  __shared__ __align__(16) uint32_t maxima[kThreads];
   __shared__ float bound;
-  __shared__ float cv[kCap];
-  __shared__ int ci[kCap];
-  __shared__ int count;
+  __shared__ __align__(16) float shared[kShared];  // the groups' maxima, later the listed entries' keys
+  __shared__ int groups[kGroupCap];
+  __shared__ int ngroups, count;
+  uint64_t* const keys = reinterpret_cast<uint64_t*>(shared);
   const int lane = threadIdx.x & 63, wave = wave_id();
-  const int64_t r = blockIdx.x;
-  const T* Y = static_cast<const T*>(a.Y) + r * a.ld;
-  // every entry that may be a member (finite, its column mapped), by f(value, column)
-  auto sweep = [&](auto&& f) {
-    int base = threadIdx.x * 8;
-    for (; base + 8 <= a.V; base += kStep) {
-      float x[8];
-      load8(Y + base, x);
-      const uint32_t in = MAP ? a.mapped[base >> 3] : 0xFFu;
+  const int64_t r = blockIdx.x / (unsigned)a.segs;
+  const int seg = blockIdx.x % (unsigned)a.segs, from = seg * a.seg_cols;  // columns are counted from `from`
+  const int V = min(a.V - from, a.seg_cols);
+  const T* Y = static_cast<const T*>(a.Y) + r * a.ld + from;
+  const int first = threadIdx.x * 8;
+  auto index_of = [&](int col) { return MAP ? a.inv[from + col] : from + col; };
+  auto mask_of = [&](int base) { return MAP ? (uint32_t)a.mapped[(from + base) >> 3] : 0xFFu; };
+  // every entry of eight columns that may be a member (above -inf, its column mapped), by f(value, column)
+  auto entries = [&](int base, auto&& f) {
+    if (base >= V) return;
+    Raw8<T> q;
+    float x[8];
+    load_cols(q, Y, base, V);
+    q.get(x);
+    const uint32_t in = mask_of(base);
 #pragma unroll
-      for (int k = 0; k < 8; ++k)
-        if (((in >> k) & 1u) != 0u && x[k] > -INFINITY) f(x[k], base + k);
-    }
-    for (int v = base; v < min(a.V, base + 8); ++v) {
-      const float x = load1(Y + v);
-      if ((!MAP || (a.mapped[v >> 3] >> (v & 7) & 1) != 0) && x > -INFINITY) f(x, v);
-    }
+    for (int k = 0; k < 8; ++k)
+      if (((in >> k) & 1u) != 0u && x[k] > -INFINITY) f(x[k], base + k);
   };
-  auto index_of = [&](int col) { return MAP ? a.inv[col] : col; };
+  auto sweep = [&](auto&& f) {
+    for (int base = first; base < V; base += kStep) entries(base, f);
+  };
 
+  // the sweep: kU * kStep columns an iteration, `per_group` iterations a group
+  const int iters = (V + kU * kStep - 1) / (kU * kStep);
+  const int per_group = (iters + kGroups - 1) / kGroups;
   float m = kNegBig, s = 0.0f, best = -INFINITY;
-  {
-    int base = threadIdx.x * 8;
-    for (; base + 8 <= a.V; base += kStep) {
-      float x[8];
-      load8(Y + base, x);
-      lse_add8(x, m, s, a.c);
+  for (int g = 0, it = 0; it < iters; ++g) {
+    float top = -INFINITY;
+    for (int j = 0; j < per_group && it < iters; ++j, ++it) {
+      const int base = first + it * kU * kStep;
+      Raw8<T> q[kU];
+      uint32_t in[kU];
+      if ((it + 1) * kU * kStep <= V) {
+#pragma unroll
+        for (int u = 0; u < kU; ++u) {
+          q[u].load(Y + base + u * kStep);
+          if (MAP) in[u] = mask_of(base + u * kStep);
+        }
+      } else {
+#pragma unroll
+        for (int u = 0; u < kU; ++u) {
+          load_cols(q[u], Y, base + u * kStep, V);
+          if (MAP) in[u] = base + u * kStep < V ? mask_of(base + u * kStep) : 0u;
+        }
+      }
+#pragma unroll
+      for (int u = 0; u < kU; ++u) {
+        float x[8];
+        q[u].get(x);
+        lse_add8(x, m, s, a.c);
+        if (MAP) {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) x[k] = ((in[u] >> k) & 1u) != 0u ? x[k] : -INFINITY;
+        }
+        top = fmaxf(top, max8(x));
+      }
     }
-    for (int v = base; v < min(a.V, base + 8); ++v) lse_join(m, s, load1(Y + v), 1.0f, a.c);
+    shared[g * kThreads + threadIdx.x] = top;
+    best = fmaxf(best, top);
   }
-  sweep([&](float x, int) { best = fmaxf(best, x); });
+  const int used = (iters + per_group - 1) / per_group;
   wave_lse(m, s, a.c);
-  const int per = maxima_of(a.K);
-  for (int t = 0; t < per; ++t) {
-    const float top = wave_max(best);
-    const uint64_t has = __ballot(best == top);
-    if (lane == (int)__builtin_ctzll(has)) best = -INFINITY;
-    if (lane == 0) maxima[wave * per + t] = top;
+  // the bound: the K-th largest of the threads' maxima (many members: counted
+  // over all of them), or of some per wavefront that has columns.  Equal maxima
+  // are told apart by the low byte, which gives way to the thread: the bound is
+  // at most that much lower (not at all for bf16 logits).
+  const bool rounds = a.K <= kRoundsK;
+  const int per = rounds ? maxima_of(a.K, min(kWaves, (V + kWave * 8 - 1) / (kWave * 8))) : kWave;
+  static_assert(maxima_of(kRoundsK, 1) <= kWave && kThreads <= 256, "a wavefront has that many, a byte names a thread");
+  uint32_t left = (order_of(best) & ~0xFFu) | threadIdx.x;
+  if (rounds) {
+    for (int t = 0; t < per; ++t) {
+      const uint32_t top = wave_max_u32(left);
+      if (left == top) left = 0u;
+      if (lane == 0) maxima[wave * per + t] = top;
+    }
+  } else {
+    maxima[threadIdx.x] = left;
   }
   if (lane == 0) {
     red_m[wave] = m;
     red_s[wave] = s;
   }
-  if (threadIdx.x == 0) count = 0;
+  if (threadIdx.x == 0) ngroups = count = 0;
   __syncthreads();
-  if (wave == 0) {
-    if (a.lse != nullptr) {
-      m = red_m[0];
-      s = red_s[0];
-#pragma unroll
-      for (int k = 1; k < kWaves; ++k) lse_join(m, s, red_m[k], red_s[k], a.c);
-      if (lane == 0) a.lse[r] = s == 0.0f ? -INFINITY : m * a.inv_t + logf(s);
+  const int nmax = kWaves * per;
+  if ((int)threadIdx.x < nmax) {
+    const uint32_t mine = maxima[threadIdx.x];
+    int rank = 0;
+    if (rounds) {
+      for (int j = 0; j < nmax; ++j) rank += maxima[j] > mine ? 1 : 0;
+    } else {
+#pragma unroll 4
+      for (int j = 0; j < kThreads; j += 4) {
+        const uint4 o = *reinterpret_cast<const uint4*>(maxima + j);
+        rank += (o.x > mine ? 1 : 0) + (o.y > mine ? 1 : 0) + (o.z > mine ? 1 : 0) + (o.w > mine ? 1 : 0);
+      }
     }
-    const int n = kWaves * per;
-    for (int i = lane; i < n; i += kWave) {
-      const float v = maxima[i];
-      int rank = 0;
-      for (int j = 0; j < n; ++j) rank += beats(maxima[j], j, v, i) ? 1 : 0;
-      if (rank == a.K - 1) bound = v;
+    if (rank == a.K - 1) {
+      const float v = value_of(mine & ~0xFFu);
+      bound = v == v ? v : -INFINITY;  // (a thread without an entry: -inf without its low byte is no number)
+    }
+  }
+  if (wave == 0) {
+    m = red_m[0];
+    s = red_s[0];
+#pragma unroll
+    for (int k = 1; k < kWaves; ++k) lse_join(m, s, red_m[k], red_s[k], a.c);
+    if (lane == 0) {
+      if (a.segs > 1)
+        a.plse[blockIdx.x] = make_float2(m, s);
+      else if (a.lse != nullptr)
+        a.lse[r] = s == 0.0f ? -INFINITY : m * a.inv_t + logf(s);
     }
   }
   __syncthreads();
   const float least = bound;
-  sweep([&](float x, int col) {
-    if (x >= least) {
-      const int at = atomicAdd(&count, 1);
-      if (at < kCap) {
-        cv[at] = x;
-        ci[at] = index_of(col);
+  if (best >= least && best > -INFINITY)
+    for (int g = 0; g < used; ++g)
+      if (shared[g * kThreads + threadIdx.x] >= least) {
+        const int at = atomicAdd(&ngroups, 1);
+        if (at < kGroupCap) groups[at] = g * kThreads + threadIdx.x;
       }
+  __syncthreads();
+  const bool crowded = ngroups > kGroupCap;
+  auto list = [&](float x, int col) {
+    const int at = atomicAdd(&count, 1);
+    if (at < kCap) keys[at] = key_of(x, index_of(col));
+  };
+  if (!crowded) {
+    const int chunks = per_group * kU, items = ngroups * chunks;
+    for (int i = threadIdx.x; i < items; i += kThreads) {
+      const int id = groups[i / chunks], g = id / kThreads, t = id % kThreads;
+      entries((g * chunks + i % chunks) * kStep + t * 8, [&](float x, int col) {
+        if (x >= least) list(x, col);
+      });
     }
-  });
+  }
   __syncthreads();
   int n = count;
-  if (n > kCap) {
+  if (crowded || n > kCap) {
     // the K-th entry's value, bit by bit, then the index up to which entries of
     // that value are members
     auto counted = [&](auto&& f) {
       int c = 0;
       sweep([&](float x, int col) { c += f(x, col) ? 1 : 0; });
-      return block_sum(c, red_i);
+      return block_sum<kWaves>(c, red_i);
     };
     uint32_t kth = 0;
     for (int b = 31; b >= 0; --b) {
@@ -150,30 +259,72 @@ __global__ __launch_bounds__(kThreads) void k_top_logits(TopArgs a) {
     __syncthreads();
     sweep([&](float x, int col) {
       const uint32_t o = order_of(x);
-      if (o > kth || (o == kth && index_of(col) <= last)) {
-        const int at = atomicAdd(&count, 1);
-        if (at < kCap) {
-          cv[at] = x;
-          ci[at] = index_of(col);
-        }
-      }
+      if (o > kth || (o == kth && index_of(col) <= last)) list(x, col);
     });
     __syncthreads();
     n = min(count, kCap);
   }
+  if (threadIdx.x == 0 && (n & 1) != 0) keys[n] = 0;  // (kCap is even)
+  __syncthreads();
+  int32_t* const idx = (a.segs > 1 ? a.pidx : a.idx) + (int64_t)blockIdx.x * a.K;
+  float* const val = (a.segs > 1 ? a.pval : a.val) + (int64_t)blockIdx.x * a.K;
   for (int i = threadIdx.x; i < n; i += kThreads) {
-    const float v = cv[i];
-    const int id = ci[i];
-    int rank = 0;
-    for (int j = 0; j < n; ++j) rank += beats(cv[j], ci[j], v, id) ? 1 : 0;
+    const uint64_t key = keys[i];
+    const int rank = rank_of(key, keys, (n + 1) & ~1);
     if (rank < a.K) {
-      a.idx[r * a.K + rank] = id;
-      a.val[r * a.K + rank] = v;
+      idx[rank] = index_in(key);
+      val[rank] = value_in(key);
     }
   }
-  if ((int)threadIdx.x >= n && (int)threadIdx.x < a.K) {
-    a.idx[r * a.K + threadIdx.x] = -1;
-    a.val[r * a.K + threadIdx.x] = -INFINITY;
+  for (int i = n + (int)threadIdx.x; i < a.K; i += kThreads) {
+    idx[i] = -1;
+    val[i] = -INFINITY;
+  }
+}
+
+// A row's K largest from its segments' lists (each in order): an entry's place is
+// its place in its own list and, by bisection, the entries of the others that
+// beat it (all lists at once, so that the steps' reads do not wait for each other).
+constexpr int kJoinThreads = 1024;
+__global__ __launch_bounds__(kJoinThreads) void k_top_join(TopArgs a) {
+  __shared__ uint64_t keys[kTopSegs * kMaxMembers], out[kMaxMembers];
+  static_assert(kTopSegs * kMaxMembers <= kJoinThreads, "an entry per thread");
+  const int64_t r = blockIdx.x;
+  const int K = a.K, n = a.segs * K, i = threadIdx.x;
+  if (wave_id() == kJoinThreads / kWave - 1 && a.lse != nullptr) {
+    const int lane = i & 63;
+    const float2 p = lane < a.segs ? a.plse[r * a.segs + lane] : make_float2(kNegBig, 0.0f);
+    float m = p.x, s = p.y;
+    wave_lse(m, s, a.c);
+    if (lane == 0) a.lse[r] = s == 0.0f ? -INFINITY : m * a.inv_t + logf(s);
+  }
+  if (i < n) {
+    const int id = a.pidx[r * n + i];
+    keys[i] = id < 0 ? 0 : key_of(a.pval[r * n + i], id);
+  }
+  if (i < K) out[i] = 0;
+  __syncthreads();
+  if (i < n && keys[i] != 0) {
+    const uint64_t key = keys[i];
+    int lo[kTopSegs];  // entries before it beat this one
+#pragma unroll
+    for (int g = 0; g < kTopSegs; ++g) lo[g] = 0;
+    for (int step = kMaxMembers; step > 0; step /= 2) {
+#pragma unroll
+      for (int g = 0; g < kTopSegs; ++g) {
+        const int at = lo[g] + step;
+        if (g < a.segs && at <= K && keys[g * K + at - 1] > key) lo[g] = at;
+      }
+    }
+    int rank = 0;
+#pragma unroll
+    for (int g = 0; g < kTopSegs; ++g) rank += lo[g];
+    if (rank < K) out[rank] = key;
+  }
+  __syncthreads();
+  if (i < K) {
+    a.idx[r * K + i] = out[i] != 0 ? index_in(out[i]) : -1;
+    a.val[r * K + i] = out[i] != 0 ? value_in(out[i]) : -INFINITY;
   }
 }
 
@@ -186,14 +337,23 @@ __global__ __launch_bounds__(256) void k_top_bits(const int32_t* inv, int V, uin
   mapped[b] = (uint8_t)bits;
 }
 
+template <typename T, int kThreads>
+hipError_t launch_n(const TopArgs& a, hipStream_t s) {
+  const dim3 grid((unsigned)(a.R * a.segs));
+  if (a.inv != nullptr)
+    hipLaunchKernelGGL((k_top_logits<T, true, kThreads>), grid, dim3(kThreads), 0, s, a);
+  else
+    hipLaunchKernelGGL((k_top_logits<T, false, kThreads>), grid, dim3(kThreads), 0, s, a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess || a.segs == 1) return e;
+  hipLaunchKernelGGL(k_top_join, dim3((unsigned)a.R), dim3(kJoinThreads), 0, s, a);
+  return hipGetLastError();
+}
+
 template <typename T>
 hipError_t launch_t(const TopArgs& a, hipStream_t s) {
-  const dim3 grid((unsigned)a.R);
-  if (a.inv != nullptr)
-    hipLaunchKernelGGL((k_top_logits<T, true>), grid, dim3(kThreads), 0, s, a);
-  else
-    hipLaunchKernelGGL((k_top_logits<T, false>), grid, dim3(kThreads), 0, s, a);
-  return hipGetLastError();
+  if (a.V <= kShortCols && a.K <= kRoundsK) return launch_n<T, kWave>(a, s);
+  return launch_n<T, 256>(a, s);
 }
 
 }  // namespace

@@ -456,7 +456,12 @@ struct LossArgs {
   float* loss;                 // [R]
   float* lse;                  // [R] or null
   int32_t* err;
+  float* total;                // [1], or null: formed by launch_row_total
+  int32_t* counter;            // [1] zero (with total): workgroups that are done
 };
+// Rows up to which the last workgroup of the row kernel forms the total: each
+// workgroup then ends with an atomic add.
+constexpr int64_t kTotalRows = 1024;
 
 // The K largest entries of a teacher's rows.
 struct TopArgs {
@@ -469,7 +474,20 @@ struct TopArgs {
   int32_t* idx;                // [R, K]
   float* val;                  // [R, K]
   float* lse;                  // [R] or null
+  // few rows: a row's columns in `segs` segments of `seg_cols` (a multiple of 8),
+  // whose results a second launch joins
+  int32_t segs, seg_cols;
+  int32_t* pidx;               // [R, segs, K]
+  float* pval;                 // [R, segs, K]
+  float2* plse;                // [R, segs]
 };
+// Segments of a row: four workgroups per CU, of at least 4096 columns each.
+constexpr int kTopSegs = 16;
+inline int top_segs(int64_t R, int V) {
+  int64_t n = 1024 / R;
+  n = n > V / 4096 ? V / 4096 : n;
+  return (int)(n < 1 ? 1 : n > kTopSegs ? kTopSegs : n);
+}
 
 // The same losses through an LM head.
 constexpr int kLmLossPad = 64;  // rows in play are padded to whole stages of the products

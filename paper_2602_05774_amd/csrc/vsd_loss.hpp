@@ -46,6 +46,62 @@ __device__ __forceinline__ void lse_add8(const float (&x)[8], float& m, float& s
   for (int k = 0; k < 8; ++k) s += lse_term(x[k], m, c);
 }
 
+// Eight consecutive logits as they lie in memory.
+template <typename T>
+struct Raw8;
+template <>
+struct Raw8<bf16_t> {
+  uint4 a;
+  __device__ __forceinline__ void load(const bf16_t* p) { a = *reinterpret_cast<const uint4*>(p); }
+  __device__ __forceinline__ void clear() { a = make_uint4(0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u, 0xFF80FF80u); }
+  __device__ __forceinline__ void get(float (&v)[8]) const {
+    v[0] = bf16_lo(a.x); v[1] = bf16_hi(a.x);
+    v[2] = bf16_lo(a.y); v[3] = bf16_hi(a.y);
+    v[4] = bf16_lo(a.z); v[5] = bf16_hi(a.z);
+    v[6] = bf16_lo(a.w); v[7] = bf16_hi(a.w);
+  }
+  __device__ __forceinline__ void load_part(const bf16_t* p, int n) {
+    uint32_t w[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) w[k] = k < n ? p[k] : 0xFF80u;
+    a = make_uint4(w[0] | w[1] << 16, w[2] | w[3] << 16, w[4] | w[5] << 16, w[6] | w[7] << 16);
+  }
+};
+template <>
+struct Raw8<float> {
+  float4 a, b;
+  __device__ __forceinline__ void load(const float* p) {
+    a = reinterpret_cast<const float4*>(p)[0];
+    b = reinterpret_cast<const float4*>(p)[1];
+  }
+  __device__ __forceinline__ void clear() {
+    a = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+    b = a;
+  }
+  __device__ __forceinline__ void get(float (&v)[8]) const {
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+    v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+  }
+  __device__ __forceinline__ void load_part(const float* p, int n) {
+    float w[8];
+#pragma unroll
+    for (int k = 0; k < 8; ++k) w[k] = k < n ? p[k] : -INFINITY;
+    a = make_float4(w[0], w[1], w[2], w[3]);
+    b = make_float4(w[4], w[5], w[6], w[7]);
+  }
+};
+// Columns base .. base + 7 of a row of V columns, -inf past its end (nothing is
+// read there).
+template <typename T>
+__device__ __forceinline__ void load_cols(Raw8<T>& x, const T* row, int base, int V) {
+  if (base + 8 <= V)
+    x.load(row + base);
+  else if (base < V)
+    x.load_part(row + base, V - base);
+  else
+    x.clear();
+}
+
 // One row's members, lane k holding member k: its column (-1: none), its
 // probability p and p log p.  Teacher values val / T_p are normalised over the
 // row's members or by the teacher's log-sum-exp.  A member of value -inf has

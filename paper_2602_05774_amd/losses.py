@@ -9,6 +9,7 @@ Rows are [R, v] logits with unit column stride (a column range of a wider
 buffer is fine: base address and row stride are multiples of 16 bytes), or an
 LmHead(hidden [R, H], weight [v, H]), whose logits are neither stored nor kept.
 """
+import contextlib
 import ctypes
 import functools
 from typing import NamedTuple, Optional, Union
@@ -88,10 +89,15 @@ def _query_loss(R, v, hidden_dim, k, grad):
     return n.value
 
 
-def top_workspace_bytes(v, with_map=True):
-    """Workspace bytes of top_logits over rows of v logits."""
-    rows, n = _lib.VsdRows(1, v, v, VSD_BF16, 0), ctypes.c_size_t(0)
-    _lib.check(_lib.load().vsd_top_workspace_bytes(ctypes.byref(rows), int(with_map), ctypes.byref(n)))
+def top_workspace_bytes(R, v, k, with_map=True):
+    """Workspace bytes of top_logits over R rows of v logits."""
+    return _query_top(R, v, k, bool(with_map))
+
+
+@functools.lru_cache(maxsize=256)
+def _query_top(R, v, k, with_map):
+    rows, n = _lib.VsdRows(R, v, v, VSD_BF16, 0), ctypes.c_size_t(0)
+    _lib.check(_lib.load().vsd_top_workspace_bytes(ctypes.byref(rows), k, int(with_map), ctypes.byref(n)))
     return n.value
 
 
@@ -107,11 +113,23 @@ def _workspace(need, given, dev):
     return torch.empty(need, dtype=torch.uint8, device=dev)
 
 
-def _error_word(given, dev):
-    if given is None:
-        return torch.zeros(1, dtype=torch.int32, device=dev)
-    _check("device_error", given, torch.int32, (1,), dev)
-    return given
+# Zeroed words [error, counter] of one call each, made 256 at a time per device
+# and stream (a fill a call took 4 of its 21 us on the host); a word is handed out
+# once.  A captured call gets a fill of its own, which its graph repeats.
+_words = {}
+
+
+def _call_words(dev, stream):
+    """A zeroed [1] int32 tensor with a zeroed word behind it."""
+    if torch.cuda.is_current_stream_capturing():
+        return torch.zeros(2, dtype=torch.int32, device=dev)[:1]
+    try:
+        return _words[dev.index, stream].pop()
+    except (KeyError, IndexError):
+        made = list(torch.zeros(256, 2, dtype=torch.int32, device=dev).narrow(1, 0, 1).unbind(0))
+        mine = made.pop()
+        _words[dev.index, stream] = made
+        return mine
 
 
 def _gradient(X, rows, dev, grad, weight_grad):
@@ -140,11 +158,23 @@ def _gradient(X, rows, dev, grad, weight_grad):
         raise ValueError("weight_grad needs an LmHead source")
     if grad is True:
         per16 = 16 // X.element_size()
-        grad = torch.empty(rows.R, (rows.v + per16 - 1) // per16 * per16, dtype=X.dtype, device=dev)[:, :rows.v]
+        ld = (rows.v + per16 - 1) // per16 * per16
+        grad = torch.empty(rows.R, ld, dtype=X.dtype, device=dev)
+        if ld != rows.v:
+            grad = grad[:, :rows.v]
+        return grad, _lib.VsdLossGrad(grad.data_ptr(), ld, None, None, VSD_F32)
     if (not isinstance(grad, torch.Tensor) or grad.shape != X.shape or grad.dtype != X.dtype or grad.device != dev
             or (grad.stride(1) != 1 and grad.shape[1] != 1)):
         raise ValueError("grad must match the logits in shape, dtype and device, with unit column stride")
     return grad, _lib.VsdLossGrad(grad.data_ptr(), _row_stride(grad), None, None, VSD_F32)
+
+
+_here = contextlib.nullcontext()
+
+
+def _device(dev):
+    """Makes the tensors' device the current one, as kernel launches need."""
+    return _here if torch.cuda.current_device() == dev.index else torch.cuda.device(dev)
 
 
 def _loss(X, k, dev, rows, src, call, grad, weight_grad, row_weight, workspace, device_error):
@@ -161,14 +191,21 @@ def _loss(X, k, dev, rows, src, call, grad, weight_grad, row_weight, workspace, 
     else:
         result, g = _gradient(X, rows, dev, grad, weight_grad)
     out = torch.empty(2 * R + 1, dtype=torch.float32, device=dev)
-    err = _error_word(device_error, dev)
+    loss_row, lse, total = torch.split_with_sizes(out, (R, R, 1))
+    stream = _stream(dev)
+    words = _call_words(dev, stream)
+    if device_error is None:
+        err = words
+    else:
+        _check("device_error", device_error, torch.int32, (1,), dev)
+        err = device_error
     need = _query_loss(R, rows.v, rows.hidden_dim, k, g is not None) if rows.hidden_dim else 0
     ws = _workspace(need, workspace, dev)
     at = out.data_ptr()
-    lo = _lib.VsdLossOut(at, at + 4 * R, at + 8 * R, err.data_ptr())
+    lo = _lib.VsdLossOut(at, at + 4 * R, at + 8 * R, err.data_ptr(), words.data_ptr() + 4)
     _lib.check(call(ctypes.byref(rows), ctypes.byref(src), _ptr(row_weight), ctypes.byref(lo),
-                    None if g is None else ctypes.byref(g), _ptr(ws), need, _stream(dev)))
-    return LossResult(out[:R], out[R:2 * R], out[2 * R:], result, err)
+                    None if g is None else ctypes.byref(g), _ptr(ws), need, stream))
+    return LossResult(loss_row, lse, total, result, err)
 
 
 def cross_entropy(X, labels, row_weight=None, temp_draft=1.0, loss_scale=1.0, grad=None, weight_grad=False,
@@ -191,7 +228,7 @@ def cross_entropy(X, labels, row_weight=None, temp_draft=1.0, loss_scale=1.0, gr
     def call(r, s, weight, out, g, ws, need, stream):
         return lib.vsd_cross_entropy(r, s, labels.data_ptr(), weight, temp_draft, loss_scale, out, g, ws, need, stream)
 
-    with torch.cuda.device(dev):
+    with _device(dev):
         return _loss(X, 0, dev, rows, src, call, grad, weight_grad, row_weight, workspace, device_error)
 
 
@@ -222,7 +259,7 @@ def distill_loss(X, teacher_idx, teacher_logits, teacher_lse=None, row_weight=No
                                     _dtype_code(teacher_logits), _ptr(teacher_lse), weight, temp_draft, temp_target,
                                     loss_scale, out, g, ws, need, stream)
 
-    with torch.cuda.device(dev):
+    with _device(dev):
         return _loss(X, k, dev, rows, src, call, grad, weight_grad, row_weight, workspace, device_error)
 
 
@@ -244,13 +281,16 @@ def top_logits(Y, k, d2t=None, temp_target=1.0, workspace=None, device_error=Non
         raise ValueError(f"k={k} outside [1, {VSD_MAX_TOP}]")
     if d2t is not None:
         _check("d2t", d2t, torch.int32, (d2t.numel(),), dev)
-    with torch.cuda.device(dev):
-        out = torch.empty(R * (2 * k + 1), dtype=torch.float32, device=dev)
-        idx, val, lse = out[:R * k].view(torch.int32).view(R, k), out[R * k:2 * R * k].view(R, k), out[2 * R * k:]
-        err = _error_word(device_error, dev)
-        need = top_workspace_bytes(rows.v) if d2t is not None else 0
+    with _device(dev):
+        idx = torch.empty(R, k, dtype=torch.int32, device=dev)
+        val = torch.empty(R, k, dtype=torch.float32, device=dev)
+        lse = torch.empty(R, dtype=torch.float32, device=dev)
+        stream = _stream(dev)
+        err = _call_words(dev, stream) if device_error is None else device_error
+        _check("device_error", err, torch.int32, (1,), dev)
+        need = _query_top(R, rows.v, k, d2t is not None)
         ws = _workspace(need, workspace, dev)
         _lib.check(lib.vsd_top_logits(ctypes.byref(rows), ctypes.byref(src), k, _ptr(d2t),
                                       0 if d2t is None else d2t.numel(), temp_target, idx.data_ptr(), val.data_ptr(),
-                                      lse.data_ptr(), _ptr(ws), need, err.data_ptr(), _stream(dev)))
+                                      lse.data_ptr(), _ptr(ws), need, err.data_ptr(), stream))
     return TopLogits(idx, val, lse, err)
