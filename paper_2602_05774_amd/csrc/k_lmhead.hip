@@ -23,10 +23,14 @@
 // logits are recomputed tile by tile; g = loss_scale/T_q ((a+b) q - a e_z~ -
 // b e_z') is written in bf16 (the gradient with respect to the logits); then
 // dH_d = g W_d and, when asked for, dW_d = g^T H_d (fp32).
+#include <type_traits>
+
 #include "vsd_device.hpp"
 #include "vsd_kernels.hpp"
 #include "vsd_loss.hpp"
 #include "vsd_topk.hpp"
+
+
 
 namespace vsd {
 
@@ -1638,18 +1642,23 @@ hipError_t launch_lm_bwd(const LmBwdArgs& a, hipStream_t s) {
 // (The grids are sized for every row in play; the kernels read how many are.)
 hipError_t launch_lm_loss(LmLossArgs a, bool weight_bf16, hipStream_t s) {
   const bool distill = a.l.val != nullptr;
-  const int64_t R = a.l.R, nrt = (R + TM - 1) / TM;
+  const int64_t R = a.l.R, nrt = (R + TM - 1) / TM, nht = (a.H + TN - 1) / TN;
   const dim3 by_row((unsigned)((R + 3) / 4));
+  auto runs = [&](int V) {  // workgroups of a launch that walks runs of V columns' tiles
+    const int64_t all = nrt * lm_tiles(V), most = nrt > kLmLossRuns ? nrt : kLmLossRuns;
+    return dim3((unsigned)(all < most ? all : most));
+  };
   hipError_t e;
   if (distill) {
     hipLaunchKernelGGL(k_lm_loss_members, by_row, dim3(256), 0, s, a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
+  a.cols = a.l.V < a.piece ? a.l.V : a.piece;
   hipLaunchKernelGGL(k_lm_loss_list, dim3((unsigned)((R + kListRows - 1) / kListRows)), dim3(kListRows), 0, s, a);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   hipLaunchKernelGGL(k_lm_loss_pack, dim3((unsigned)((R + kLmLossPad + 3) / 4)), dim3(256), 0, s, a);
   if ((e = hipGetLastError()) != hipSuccess) return e;
-  hipLaunchKernelGGL(k_lm_loss_fwd, dim3((unsigned)(nrt * a.nruns)), dim3(kThreads), 0, s, a);
+  hipLaunchKernelGGL(k_lm_loss_fwd, runs(a.l.V), dim3(kThreads), 0, s, a);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   if (distill)
     hipLaunchKernelGGL(k_lm_loss_combine<true>, by_row, dim3(256), 0, s, a);
@@ -1657,31 +1666,38 @@ hipError_t launch_lm_loss(LmLossArgs a, bool weight_bf16, hipStream_t s) {
     hipLaunchKernelGGL(k_lm_loss_combine<false>, by_row, dim3(256), 0, s, a);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   if (a.dh == nullptr) return hipSuccess;
-  const int64_t nht = (a.H + TN - 1) / TN;
   for (int64_t c0 = 0; c0 < a.l.V; c0 += a.piece) {
     a.c0 = (int32_t)c0;
     a.cols = (int32_t)(a.l.V - c0 < a.piece ? a.l.V - c0 : a.piece);
-    const int64_t nct = (a.cols + TN - 1) / TN;
     if (distill) {
-      hipLaunchKernelGGL(k_lm_loss_g<true>, dim3((unsigned)(nrt * nct)), dim3(kThreads), 0, s, a);
+      hipLaunchKernelGGL(k_lm_loss_g<true>, runs(a.cols), dim3(kThreads), 0, s, a);
       if ((e = hipGetLastError()) != hipSuccess) return e;
       hipLaunchKernelGGL(k_lm_loss_fix, by_row, dim3(256), 0, s, a);
     } else {
-      hipLaunchKernelGGL(k_lm_loss_g<false>, dim3((unsigned)(nrt * nct)), dim3(kThreads), 0, s, a);
+      hipLaunchKernelGGL(k_lm_loss_g<false>, runs(a.cols), dim3(kThreads), 0, s, a);
     }
     if ((e = hipGetLastError()) != hipSuccess) return e;
-    hipLaunchKernelGGL(k_lm_loss_dh, dim3((unsigned)(nrt * nht * a.splits)), dim3(kThreads), 0, s, a);
+    const int64_t one = nrt * nht, split = one * kLmLossSplits < kLmLossDh ? one * kLmLossSplits : kLmLossDh;
+    const int64_t dh = one > split ? one : split, dw1 = a.dw != nullptr ? (int64_t)lm_tiles(a.cols) * nht : 0;
+    const int64_t dw = a.wacc != nullptr ? (dw1 * kLmLossSplits < kLmLossDw ? dw1 * kLmLossSplits : kLmLossDw) : dw1;
+    const dim3 grid((unsigned)(dh + dw));
+    if (a.dw == nullptr)
+      hipLaunchKernelGGL(k_lm_loss_grads<void>, grid, dim3(kThreads), 0, s, a);
+    else if (weight_bf16)
+      hipLaunchKernelGGL(k_lm_loss_grads<bf16_t>, grid, dim3(kThreads), 0, s, a);
+    else
+      hipLaunchKernelGGL(k_lm_loss_grads<float>, grid, dim3(kThreads), 0, s, a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
-    if (a.dw != nullptr) {
-      const dim3 grid((unsigned)(nct * nht));
+    if (a.wacc != nullptr) {
+      const dim3 by_eight((unsigned)(((int64_t)a.cols * a.H / 8 + 255) / 256));
       if (weight_bf16)
-        hipLaunchKernelGGL(k_lm_loss_dw<bf16_t>, grid, dim3(kThreads), 0, s, a);
+        hipLaunchKernelGGL(k_lm_loss_dw_out<bf16_t>, by_eight, dim3(256), 0, s, a);
       else
-        hipLaunchKernelGGL(k_lm_loss_dw<float>, grid, dim3(kThreads), 0, s, a);
+        hipLaunchKernelGGL(k_lm_loss_dw_out<float>, by_eight, dim3(256), 0, s, a);
       if ((e = hipGetLastError()) != hipSuccess) return e;
     }
   }
-  if (a.splits > 1) hipLaunchKernelGGL(k_lm_loss_dh_out, by_row, dim3(256), 0, s, a);
+  hipLaunchKernelGGL(k_lm_loss_dh_out, by_row, dim3(256), 0, s, a);
   return hipGetLastError();
 }
 

@@ -521,8 +521,8 @@ vsd_status check_rows_src(const vsd_rows* rows, const vsd_src* src, const char* 
 bool usable_temp(float t) { return finite_pos(t) && finite_pos(1.0f / t) && std::isfinite(vsd::kLog2e / t); }
 
 struct LossLayout {
-  size_t tag, at, rows, count, mid, mp, mstat, mx, hp, part, stat, g, acc, total;
-  int32_t run, nruns, piece, per, splits;
+  size_t tag, at, rows, plan, mid, mp, mstat, mx, hp, part, stat, g, acc, wacc, total;
+  int32_t piece;
 };
 
 // The fused head's workspace (K = 0: cross entropy); materialised rows need none.
@@ -530,18 +530,14 @@ LossLayout loss_layout(const vsd_rows* rows, int32_t K, bool grad) {
   LossLayout w{};
   const size_t R = (size_t)rows->R, H = (size_t)rows->hidden_dim;
   if (H == 0) return w;
-  w.run = vsd::lm_loss_run(rows->R, rows->v);
-  w.nruns = vsd::lm_runs(rows->v, w.run);
   w.piece = vsd::lm_loss_piece(rows->R, rows->v);
-  w.per = vsd::lm_loss_range(rows->R, rows->hidden_dim, w.piece);
-  w.splits = (std::min(w.piece, rows->v) + w.per - 1) / w.per;  // (every range of the first piece has columns)
   size_t at = 0;
   auto take = [&](size_t bytes) {
     const size_t here = at;
     at += align_up(bytes);
     return here;
   };
-  w.count = take(sizeof(int32_t));
+  w.plan = take(sizeof(vsd::LmLossPlan));
   w.at = take(R * sizeof(int32_t));
   w.rows = take(R * sizeof(int32_t));
   if (K > 0) {
@@ -553,11 +549,13 @@ LossLayout loss_layout(const vsd_rows* rows, int32_t K, bool grad) {
   }
   const size_t padded = (size_t)vsd::lm_loss_pad(rows->R);
   w.hp = take(padded * H * sizeof(uint16_t));
-  w.part = take(2 * (size_t)w.nruns * R * sizeof(float2));
+  w.part = take((size_t)vsd::lm_loss_parts(rows->R, rows->v) * sizeof(float2));
   w.stat = take(R * sizeof(float4));
   if (grad) {
-    w.g = take(padded * (size_t)w.piece * sizeof(uint16_t));
-    if (w.splits > 1 || w.piece < rows->v) w.acc = take((size_t)w.splits * R * H * sizeof(float));
+    w.g = take(padded * (size_t)vsd::lm_loss_ldg(w.piece) * sizeof(uint16_t));
+    w.acc = take((size_t)vsd::lm_loss_sums(rows->R, rows->hidden_dim) * sizeof(float));
+    const int64_t wsums = vsd::lm_loss_wsums(rows->v, rows->hidden_dim, w.piece);
+    if (wsums > 0) w.wacc = take((size_t)wsums * sizeof(float));
   }
   w.total = at;
   return w;
@@ -649,15 +647,12 @@ vsd_status base_loss(const vsd_rows* rows, const vsd_src* src, int32_t K, const 
     b.h = src->hidden;
     b.w = src->weight;
     b.H = rows->hidden_dim;
-    b.run = w.run;
-    b.nruns = w.nruns;
-    b.piece = b.ldg = w.piece;
-    b.per = w.per;
-    b.splits = w.splits;
+    b.piece = w.piece;
+    b.ldg = vsd::lm_loss_ldg(w.piece);
     b.tag = K > 0 ? reinterpret_cast<int32_t*>(ws + w.tag) : const_cast<int32_t*>(idx);  // (labels are read only)
     b.at = reinterpret_cast<int32_t*>(ws + w.at);
     b.rows = reinterpret_cast<int32_t*>(ws + w.rows);
-    b.count = reinterpret_cast<int32_t*>(ws + w.count);
+    b.plan = reinterpret_cast<vsd::LmLossPlan*>(ws + w.plan);
     if (K > 0) {
       b.mid = reinterpret_cast<int32_t*>(ws + w.mid);
       b.mp = reinterpret_cast<float*>(ws + w.mp);
@@ -671,7 +666,8 @@ vsd_status base_loss(const vsd_rows* rows, const vsd_src* src, int32_t K, const 
       b.dh = grad->grad_hidden;
       b.dw = grad->grad_weight;
       b.g = reinterpret_cast<uint16_t*>(ws + w.g);
-      if (w.acc != 0) b.acc = reinterpret_cast<float*>(ws + w.acc);
+      b.acc = reinterpret_cast<float*>(ws + w.acc);
+      if (grad->grad_weight != nullptr && w.wacc != 0) b.wacc = reinterpret_cast<float*>(ws + w.wacc);
     }
     e = vsd::launch_lm_loss(b, grad != nullptr && grad->weight_dtype == VSD_BF16, s);
     if (e != hipSuccess) return hip_fail(e, "fused loss launch");

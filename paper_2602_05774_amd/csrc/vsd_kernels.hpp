@@ -493,6 +493,15 @@ inline int top_segs(int64_t R, int V) {
 constexpr int kLmLossPad = 64;  // rows in play are padded to whole stages of the products
 __host__ __device__ constexpr int64_t lm_loss_pad(int64_t n) { return (n + kLmLossPad - 1) / kLmLossPad * kLmLossPad; }
 
+// Made on the device, where the number of rows in play is known.
+struct LmLossPlan {
+  int32_t n;                 // rows in play
+  int32_t fwd_run, fwd_runs; // vocabulary tiles that a workgroup of the forward walks, runs
+  int32_t g_run;             // the same of a piece's gradient
+  int32_t per, splits;       // dh: columns of a range of a piece (a multiple of 64), ranges
+  int32_t dw_per, dw_splits; // dW: rows of a range of the rows in play (a multiple of 64), ranges
+};
+
 struct LmLossArgs {
   LossArgs l;                // members, weights, outputs; X, G: null
   const void* h;             // [R, H] bf16
@@ -500,34 +509,30 @@ struct LmLossArgs {
   void* dh;                  // [R, H] bf16, or null: the loss only
   void* dw;                  // [V, H] bf16 or fp32, or null
   int32_t H;
-  int32_t run, nruns;        // vocabulary tiles per run of the forward, runs
   int32_t piece;             // columns of a piece (a multiple of 256)
-  int32_t splits, per;       // ranges of a piece's columns in dh, columns of each (a multiple of 64)
-  int32_t c0, cols;          // the piece at hand
+  int32_t c0, cols;          // the piece at hand (the list: piece's columns in the first one)
   int32_t ldg;               // row stride of g
   // workspace
   int32_t* tag;              // [R] in play iff in [0, V) (and the weight is not 0): labels, or 0 / -1
   int32_t* at;               // [R] place among the rows in play or -1
   int32_t* rows;             // [R] the rows in play
-  int32_t* count;            // [1] how many
+  LmLossPlan* plan;          // [1] how many, and how their products are divided
   int32_t* mid;              // [R, K] members' columns
   float* mp;                 // [R, K] their probabilities
   float2* mstat;             // [R] sums of p and p log p
   float* mx;                 // [rows in play, K] their logits
   bf16_store* hp;            // [lm_loss_pad(R), H] hidden states of the rows in play
-  float2* part;              // [2 nruns, R] log-sum-exps of the runs, per wavefront group
+  float2* part;              // [2 runs, rows in play] log-sum-exps, per wavefront group
   float4* stat;              // [R] (m, kq, k, -) of the gradient
   bf16_store* g;             // [lm_loss_pad(R), ldg] the piece's gradient
-  float* acc;                // [splits, R, H], or null: one piece and one range
+  float* acc;                // [splits, rows in play, H] sums of dh
+  float* wacc;               // [dw_splits, cols, H] sums of dW, or null: one range
 };
 
-// Vocabulary tiles that a forward workgroup walks: enough workgroups for two
-// rounds of the chip, and at most 16 tiles.
-inline int lm_loss_run(int64_t R, int V) {
-  const int64_t all = (R + kLmTile - 1) / kLmTile * lm_tiles(V);
-  const int64_t run = all / (2 * kLmCus);
-  return (int)(run < 1 ? 1 : run > kLmTilesPerSlice ? kLmTilesPerSlice : run);
-}
+// Most workgroups of a launch that walk runs of tiles (or one per row tile), of
+// the dh products and of the dW products (or one per tile).
+constexpr int kLmLossRuns = 4 * kLmCus, kLmLossDh = 10 * kLmCus, kLmLossDw = 2 * kLmCus;
+constexpr int kLmLossSplits = 32;  // most ranges of a product's depth
 // Columns of a piece: the whole vocabulary where its gradient fits 1 GiB, else
 // the largest power of two that does (at least 1024).
 constexpr int64_t kLmPieceBytes = 1ll << 30;
@@ -538,16 +543,26 @@ inline int32_t lm_loss_piece(int64_t R, int V) {
   while (2 * piece * row <= kLmPieceBytes) piece *= 2;
   return (int32_t)(piece < all ? piece : all);
 }
-// Columns of one of the ranges that a piece is split into for dh: with fewer
-// tiles of dh than CUs, as many ranges as fill them, of at least four stages.
-inline int32_t lm_loss_range(int64_t R, int H, int32_t piece) {
-  const int64_t tiles = (R + kLmTile - 1) / kLmTile * ((H + kLmTile - 1) / kLmTile);
-  int64_t splits = kLmCus / tiles;
-  const int64_t most = piece / 256;
-  splits = splits > most ? most : splits;
-  if (splits < 2) return piece;
-  const int64_t stages = piece / 64;
-  return (int32_t)((stages + splits - 1) / splits * 64);
+// Row stride of its gradient: not a power of two, whose rows would share their
+// memory channels.
+inline int32_t lm_loss_ldg(int32_t piece) { return piece + 128; }
+// Entries of the forward's log-sum-exps: two per run and row in play.
+inline int64_t lm_loss_parts(int64_t R, int V) {
+  const int64_t all = R * lm_tiles(V), runs = (int64_t)kLmLossRuns * kLmTile;
+  return 2 * (all < runs ? all : runs > R ? runs : R);
+}
+// fp32 sums of dW, of every range (0: its tiles are too many for more than one).
+inline int64_t lm_loss_wsums(int V, int H, int32_t piece) {
+  const int64_t cols = V < piece ? V : piece, tiles = (int64_t)lm_tiles((int)cols) * lm_tiles(H);
+  if (2 * tiles > kLmLossDw) return 0;
+  const int64_t most = kLmLossDw / tiles;
+  return (most < kLmLossSplits ? most : kLmLossSplits) * cols * H;
+}
+// fp32 sums of dh, of every range.
+inline int64_t lm_loss_sums(int64_t R, int H) {
+  const int64_t tiles = (int64_t)kLmLossDh * kLmTile * kLmTile;
+  const int64_t most = kLmLossSplits * R * H;
+  return most < tiles ? most : tiles > R * H ? tiles : R * H;
 }
 
 hipError_t launch_lm_loss(LmLossArgs a, bool weight_bf16, hipStream_t s);

@@ -29,8 +29,43 @@ __global__ __launch_bounds__(256) void k_lm_loss_members(LmLossArgs a) {
   }
 }
 
+// How the products of n rows in play are divided among the CUs, a workgroup on
+// each at a time.  A lane tries one division; the cheapest (in 64-deep product
+// stages, every workgroup costing a few more) wins.  One wavefront.
+constexpr float kRunCost = 6.0f;  // stages' time of a workgroup's first loads and of its end
+// Tiles per run, so that nrt row tiles x runs fill whole rounds.
+__device__ int plan_runs(int nrt, int tiles, int stages, int lane) {
+  const int most = min(tiles, max(1, kLmLossRuns / nrt));
+  float best = -INFINITY;
+  int at = 0x7FFFFFFF;
+  for (int runs = lane + 1; runs <= most; runs += kWave) {
+    const int rounds = (nrt * runs + kLmCus - 1) / kLmCus, run = (tiles + runs - 1) / runs;
+    argmax_merge(best, at, -(float)rounds * ((float)run * stages + kRunCost), run);
+  }
+  wave_argmax(best, at);
+  return at;
+}
+// Ranges of the depth (`stages`) of a product of so many tiles.  Next to another
+// product's `beside` stages no range may take longer than all of them over all
+// CUs; alone, whole rounds.
+__device__ int plan_splits(int64_t tiles, int stages, float beside, int limit, int lane) {
+  const int most = (int)min((int64_t)min(stages, kLmLossSplits), max((int64_t)1, limit / tiles));
+  float best = -INFINITY;
+  int at = 0x7FFFFFFF;
+  const int splits = lane + 1;
+  if (splits <= most) {
+    const float each = (float)((stages + splits - 1) / splits) + kRunCost;
+    const float cost = beside > 0.0f ? fmaxf(each, ((float)tiles * splits * each + beside) / kLmCus)
+                                     : (float)((tiles * splits + kLmCus - 1) / kLmCus) * each;
+    best = -cost;
+    at = splits;
+  }
+  wave_argmax(best, at);
+  return at;
+}
+
 // at[r] = row r's place among the rows in play, or -1; the number of those
-// rows.  Every workgroup counts the rows before its own 1024.
+// rows and their plan.  Every workgroup counts the rows before its own 1024.
 constexpr int kListRows = 1024;
 __global__ __launch_bounds__(kListRows) void k_lm_loss_list(LmLossArgs a) {
   __shared__ int red[kListRows / kWave];
@@ -70,7 +105,29 @@ __global__ __launch_bounds__(kListRows) void k_lm_loss_list(LmLossArgs a) {
       if (a.l.lse != nullptr) a.l.lse[r] = 0.0f;
     }
   }
-  if (threadIdx.x == 0 && blockIdx.x == gridDim.x - 1) *a.count = total;
+  if (wave != 0 || blockIdx.x != gridDim.x - 1) return;
+  LmLossPlan p{total, 0, 0, 0, 0, 1, 0, 1};
+  if (total > 0) {
+    const int nrt = (total + TM - 1) / TM, tiles = (a.l.V + TN - 1) / TN, stages = a.H / TK;
+    p.fwd_run = plan_runs(nrt, tiles, stages, lane);
+    p.fwd_runs = (tiles + p.fwd_run - 1) / p.fwd_run;
+    if (a.dh != nullptr) {
+      const int ct = (a.cols + TN - 1) / TN, ht = (a.H + TN - 1) / TN, deep = (a.cols + TK - 1) / TK;
+      p.g_run = plan_runs(nrt, ct, stages, lane);
+      const int wdeep = (total + TK - 1) / TK;  // (whole stages: the rows are padded)
+      const float dh = (float)nrt * ht * ((float)deep + kRunCost);
+      const float dw = a.dw != nullptr ? (float)ct * ht * ((float)wdeep + kRunCost) : 0.0f;
+      const int splits = plan_splits((int64_t)nrt * ht, deep, dw, kLmLossDh, lane);
+      p.per = (deep + splits - 1) / splits * TK;
+      p.splits = (a.cols + p.per - 1) / p.per;  // (every range of the first piece has columns)
+      if (a.wacc != nullptr) {
+        const int wsplits = plan_splits((int64_t)ct * ht, wdeep, dh, kLmLossDw, lane);
+        p.dw_per = (wdeep + wsplits - 1) / wsplits * TK;
+        p.dw_splits = (wdeep * TK + p.dw_per - 1) / p.dw_per;
+      }
+    }
+  }
+  if (lane == 0) *a.plan = p;
 }
 
 // The hidden states of the rows in play, consecutively; zero rows behind them;
@@ -90,7 +147,7 @@ __global__ __launch_bounds__(256) void k_lm_loss_pack(LmLossArgs a) {
       to = reinterpret_cast<uint4*>(static_cast<bf16_t*>(a.dh) + r * a.H);
     }
   } else {
-    const int64_t n = *a.count, place = n + (r - a.l.R);
+    const int64_t n = a.plan->n, place = n + (r - a.l.R);
     if (place >= lm_loss_pad(n)) return;
     to = reinterpret_cast<uint4*>(a.hp + place * a.H);
   }
@@ -101,15 +158,15 @@ __global__ __launch_bounds__(256) void k_lm_loss_pack(LmLossArgs a) {
 // columns of each wavefront group.
 __global__ __launch_bounds__(kThreads, 1) void k_lm_loss_fwd(LmLossArgs a) {
   __shared__ __align__(16) bf16_t lds[2 * kBufElems];
-  const int64_t n = *a.count;
-  const int nrt = (int)((n + TM - 1) / TM);
-  if ((int64_t)blockIdx.x >= (int64_t)nrt * a.nruns) return;
+  const int64_t n = a.plan->n;
+  const int nrt = (int)((n + TM - 1) / TM), runs = a.plan->fwd_runs, length = a.plan->fwd_run;
+  if ((int64_t)blockIdx.x >= (int64_t)nrt * runs) return;
   int rt, run;
-  tile_of(blockIdx.x, nrt, a.nruns, rt, run);
+  tile_of(blockIdx.x, nrt, runs, rt, run);
   const int64_t row0 = (int64_t)rt * TM, i = row0 + nt_lane_row();
-  const int tiles = (a.l.V + TN - 1) / TN, begin = run * a.run;
+  const int tiles = (a.l.V + TN - 1) / TN, begin = run * length;
   float m = kNegBig, s = 0.0f;
-  NtRows src{static_cast<const bf16_t*>(a.w), a.hp, a.l.V, row0, n, a.H, begin, min(tiles, begin + a.run)};
+  NtRows src{static_cast<const bf16_t*>(a.w), a.hp, a.l.V, row0, n, a.H, begin, min(tiles, begin + length)};
   nt_stream(lds, src, [&](int tile, NtAcc& acc) {
     nt_row_per_lane(acc);
     if (i >= n) return;
@@ -127,7 +184,7 @@ __global__ __launch_bounds__(kThreads, 1) void k_lm_loss_fwd(LmLossArgs a) {
       lse_add8(x, m, s, a.l.c);
     }
   });
-  if (i < n) a.part[((int64_t)run * 2 + (wave_id() >> 2)) * a.l.R + i] = make_float2(m, s);
+  if (i < n) a.part[((int64_t)run * 2 + (wave_id() >> 2)) * n + i] = make_float2(m, s);
 }
 
 // The runs joined, the members' logits (dot products), the loss, and what the
@@ -136,11 +193,12 @@ template <bool DISTILL>
 __global__ __launch_bounds__(256) void k_lm_loss_combine(LmLossArgs a) {
   const int lane = threadIdx.x & 63;
   const int64_t i = (int64_t)blockIdx.x * 4 + wave_id();
-  if (i >= *a.count) return;
+  const int64_t n = a.plan->n;
+  if (i >= n) return;
   const int64_t r = a.rows[i];
   float m = kNegBig, s = 0.0f;
-  for (int e = lane; e < 2 * a.nruns; e += kWave) {
-    const float2 p = a.part[(int64_t)e * a.l.R + i];
+  for (int e = lane; e < 2 * a.plan->fwd_runs; e += kWave) {
+    const float2 p = a.part[(int64_t)e * n + i];
     lse_join(m, s, p.x, p.y, a.l.c);
   }
   wave_lse(m, s, a.l.c);
@@ -176,19 +234,22 @@ __global__ __launch_bounds__(256) void k_lm_loss_combine(LmLossArgs a) {
   }
 }
 
-// g of one piece of the vocabulary (columns c0 .. c0 + cols - 1): a 256 x 256
-// tile per workgroup, zeros past the columns and in the rows that pad the
-// rows in play.
+// g of one piece of the vocabulary (columns c0 .. c0 + cols - 1): a run of
+// 256 x 256 tiles per workgroup, zeros past the columns and in the rows that pad
+// the rows in play.
 template <bool DISTILL>
 __global__ __launch_bounds__(kThreads, 1) void k_lm_loss_g(LmLossArgs a) {
   __shared__ __align__(16) bf16_t lds[2 * kBufElems];
-  const int64_t n = *a.count;
+  const int64_t n = a.plan->n;
   const int nrt = (int)((n + TM - 1) / TM), nct = (a.cols + TN - 1) / TN;
-  if ((int64_t)blockIdx.x >= (int64_t)nrt * nct) return;
-  int rt, ct;
-  tile_of(blockIdx.x, nrt, nct, rt, ct);
+  if (n == 0) return;
+  const int length = a.plan->g_run, runs = (nct + length - 1) / length;
+  if ((int64_t)blockIdx.x >= (int64_t)nrt * runs) return;
+  int rt, run;
+  tile_of(blockIdx.x, nrt, runs, rt, run);
   const int64_t row0 = (int64_t)rt * TM, i = row0 + nt_lane_row();
-  NtRows src{static_cast<const bf16_t*>(a.w) + (int64_t)a.c0 * a.H, a.hp, a.cols, row0, n, a.H, ct, ct + 1};
+  NtRows src{static_cast<const bf16_t*>(a.w) + (int64_t)a.c0 * a.H, a.hp, a.cols, row0, n, a.H, run * length,
+             min(nct, (run + 1) * length)};
   nt_stream(lds, src, [&](int tile, NtAcc& acc) {
     nt_row_per_lane(acc);
     if (i >= lm_loss_pad(n)) return;
@@ -215,7 +276,7 @@ __global__ __launch_bounds__(kThreads, 1) void k_lm_loss_g(LmLossArgs a) {
 __global__ __launch_bounds__(256) void k_lm_loss_fix(LmLossArgs a) {
   const int lane = threadIdx.x & 63;
   const int64_t i = (int64_t)blockIdx.x * 4 + wave_id();
-  if (i >= *a.count) return;
+  if (i >= a.plan->n) return;
   const int64_t r = a.rows[i];
   const int K = a.l.K;
   const int id = lane < K ? a.mid[r * K + lane] : -1;
@@ -233,24 +294,21 @@ __global__ __launch_bounds__(256) void k_lm_loss_fix(LmLossArgs a) {
 }
 
 // dh of a piece: 256 x 256 tiles of g W, the piece's columns in `splits` ranges
-// of `per` (few rows: more workgroups).  One piece and one range write the
-// rounded result; otherwise acc[range] holds the fp32 sums, which the last
-// piece (one range) or k_lm_loss_dh_out turns into the result.
-__global__ __launch_bounds__(kThreads, 1) void k_lm_loss_dh(LmLossArgs a) {
-  __shared__ __align__(16) bf16_t lds[2 * kBufElems];
+// of `per`.  One piece and one range write the rounded result; otherwise
+// acc[range] holds the fp32 sums, which the last piece (one range) or
+// k_lm_loss_dh_out turns into the result.
+__device__ __forceinline__ void lm_loss_dh(const LmLossArgs& a, bf16_t* lds, int pid, int nrt) {
   const int lane = threadIdx.x & 63, w = wave_id();
-  const int64_t n = *a.count;
-  const int nrt = (int)((n + TM - 1) / TM), nct = (a.H + TN - 1) / TN;
-  const int64_t tiles = (int64_t)nrt * nct;
-  if ((int64_t)blockIdx.x >= tiles * a.splits) return;
-  const int z = (int)(blockIdx.x / tiles), k0 = z * a.per, K = min(a.per, a.cols - k0);
+  const int64_t n = a.plan->n;
+  const int nct = (a.H + TN - 1) / TN, per = a.plan->per, tiles = nrt * nct;
+  const int z = pid / tiles, k0 = z * per, K = min(per, a.cols - k0);
   if (K <= 0) return;  // (a short last piece)
   int rt, ct;
-  tile_of((int)(blockIdx.x % tiles), nrt, nct, rt, ct);
+  tile_of(pid % tiles, nrt, nct, rt, ct);
   const int64_t row0 = (int64_t)rt * TM;
   const int n0 = ct * TN;
-  const bool add = a.c0 > 0, out = a.splits == 1 && a.c0 + a.cols == a.l.V;
-  float* sums = a.acc != nullptr ? a.acc + (int64_t)z * a.l.R * a.H : nullptr;
+  const bool add = a.c0 > 0, out = a.plan->splits == 1 && a.c0 + a.cols == a.l.V;
+  float* sums = a.acc + (int64_t)z * n * a.H;
   NtTile<KRows<false>, false> src{{static_cast<const bf16_t*>(a.w) + (int64_t)(a.c0 + k0) * a.H, a.H, a.H, n0, K},
                                   {a.g + k0, a.ldg, row0, n, K},
                                   K};
@@ -284,37 +342,21 @@ __global__ __launch_bounds__(kThreads, 1) void k_lm_loss_dh(LmLossArgs a) {
   });
 }
 
-__global__ __launch_bounds__(256) void k_lm_loss_dh_out(LmLossArgs a) {
-  const int lane = threadIdx.x & 63;
-  const int64_t i = (int64_t)blockIdx.x * 4 + wave_id();
-  if (i >= *a.count) return;
-  bf16_t* D = static_cast<bf16_t*>(a.dh) + (int64_t)a.rows[i] * a.H;
-  for (int k = lane * 8; k < a.H; k += kWave * 8) {
-    float v[8];
-    load8(a.acc + i * a.H + k, v);
-    for (int z = 1; z < a.splits; ++z) {
-      float o[8];
-      load8(a.acc + ((int64_t)z * a.l.R + i) * a.H + k, o);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] += o[j];
-    }
-    store8(D + k, v);
-  }
-}
-
 // dW of a piece: 256 x 256 tiles of g^T h over the rows in play (whole stages:
-// the rows behind them are zeros in both operands).
+// the rows behind them are zeros in both operands), the rows in `dw_splits` ranges
+// where the tiles are few: their fp32 sums then go to wacc and k_lm_loss_dw_out
+// adds them.
 template <typename T>
-__global__ __launch_bounds__(kThreads, 1) void k_lm_loss_dw(LmLossArgs a) {
-  __shared__ __align__(16) bf16_t lds[2 * kBufElems];
+__device__ __forceinline__ void lm_loss_dw(const LmLossArgs& a, bf16_t* lds, int pid) {
   const int lane = threadIdx.x & 63, w = wave_id();
-  const int K = (int)lm_loss_pad(*a.count);
-  const int nrt = (a.cols + TM - 1) / TM;
+  const int all = (int)lm_loss_pad(a.plan->n), splits = a.plan->dw_splits;
+  const int nrt = (a.cols + TM - 1) / TM, nct = (a.H + TN - 1) / TN;
+  const int z = splits > 1 ? pid / (nrt * nct) : 0, k0 = z * a.plan->dw_per;
+  const int K = splits > 1 ? min(a.plan->dw_per, all - k0) : all;
   int rt, ct;
-  tile_of(blockIdx.x, nrt, (a.H + TN - 1) / TN, rt, ct);
+  tile_of(splits > 1 ? pid % (nrt * nct) : pid, nrt, nct, rt, ct);
   const int row0 = rt * TM, n0 = ct * TN;
-  T* D = static_cast<T*>(a.dw) + (int64_t)a.c0 * a.H;
-  auto write = [&](const NtAcc& acc) {
+  auto write_to = [&](auto* D, const NtAcc& acc) {
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
       const int row = row0 + g * 128 + (w & 3) * 32 + (lane & 31);
@@ -332,6 +374,12 @@ __global__ __launch_bounds__(kThreads, 1) void k_lm_loss_dw(LmLossArgs a) {
       }
     }
   };
+  auto write = [&](const NtAcc& acc) {
+    if (splits > 1)
+      write_to(a.wacc + (int64_t)z * a.cols * a.H, acc);
+    else
+      write_to(static_cast<T*>(a.dw) + (int64_t)a.c0 * a.H, acc);
+  };
   if (K == 0) {  // no row in play
     NtAcc acc;
 #pragma unroll
@@ -339,6 +387,58 @@ __global__ __launch_bounds__(kThreads, 1) void k_lm_loss_dw(LmLossArgs a) {
     write(acc);
     return;
   }
-  NtTile<KMajor<false, false>, true> src{{a.hp, a.H, a.H, n0, K}, {a.g, a.ldg, a.ldg, row0, K}, K};
+  NtTile<KMajor<false, false>, true> src{{a.hp + (int64_t)k0 * a.H, a.H, a.H, n0, K},
+                                         {a.g + (int64_t)k0 * a.ldg, a.ldg, a.ldg, row0, K},
+                                         K};
   nt_stream(lds, src, [&](int, NtAcc& acc) { write(acc); });
+}
+
+// The two products that read a piece's g in one launch: dh's few long ones
+// first, dW's many short ones (T: its type; void: none) fill the CUs behind them.
+template <typename T>
+__global__ __launch_bounds__(kThreads, 1) void k_lm_loss_grads(LmLossArgs a) {
+  __shared__ __align__(16) bf16_t lds[2 * kBufElems];
+  const int nrt = (int)((a.plan->n + TM - 1) / TM), nht = (a.H + TN - 1) / TN;
+  const int64_t ndh = (int64_t)nrt * nht * a.plan->splits, pid = blockIdx.x;
+  if (pid < ndh) {
+    lm_loss_dh(a, lds, (int)pid, nrt);
+    return;
+  }
+  if constexpr (!std::is_void_v<T>) {
+    if (pid - ndh < (int64_t)((a.cols + TM - 1) / TM) * nht * a.plan->dw_splits) lm_loss_dw<T>(a, lds, (int)(pid - ndh));
+  }
+}
+
+__global__ __launch_bounds__(256) void k_lm_loss_dh_out(LmLossArgs a) {
+  const int lane = threadIdx.x & 63;
+  const int64_t i = (int64_t)blockIdx.x * 4 + wave_id(), n = a.plan->n;
+  if (i >= n || a.plan->splits == 1) return;
+  bf16_t* D = static_cast<bf16_t*>(a.dh) + (int64_t)a.rows[i] * a.H;
+  for (int k = lane * 8; k < a.H; k += kWave * 8) {
+    float v[8];
+    load8(a.acc + i * a.H + k, v);
+    for (int z = 1; z < a.plan->splits; ++z) {
+      float o[8];
+      load8(a.acc + ((int64_t)z * n + i) * a.H + k, o);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] += o[j];
+    }
+    store8(D + k, v);
+  }
+}
+
+template <typename T>
+__global__ __launch_bounds__(256) void k_lm_loss_dw_out(LmLossArgs a) {
+  const int splits = a.plan->dw_splits;
+  const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8, all = (int64_t)a.cols * a.H;
+  if (splits == 1 || at >= all) return;
+  float v[8];
+  load8(a.wacc + at, v);
+  for (int z = 1; z < splits; ++z) {
+    float o[8];
+    load8(a.wacc + z * all + at, o);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] += o[j];
+  }
+  store8(static_cast<T*>(a.dw) + (int64_t)a.c0 * a.H + at, v);
 }
