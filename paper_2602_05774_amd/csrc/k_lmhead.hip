@@ -1648,35 +1648,49 @@ hipError_t launch_lm_loss(LmLossArgs a, bool weight_bf16, hipStream_t s) {
     const int64_t all = nrt * lm_tiles(V), most = nrt > kLmLossRuns ? nrt : kLmLossRuns;
     return dim3((unsigned)(all < most ? all : most));
   };
+  const bool few = lm_few(R);
+  const auto few_fwd = R <= 32 ? k_lm_loss_few<1> : R <= 64 ? k_lm_loss_few<2> : k_lm_loss_few<4>;
+  const auto few_g =
+      distill ? (R <= 32 ? k_lm_loss_few_g<1, true> : R <= 64 ? k_lm_loss_few_g<2, true> : k_lm_loss_few_g<4, true>)
+              : (R <= 32 ? k_lm_loss_few_g<1, false> : R <= 64 ? k_lm_loss_few_g<2, false> : k_lm_loss_few_g<4, false>);
   hipError_t e;
   if (distill) {
     hipLaunchKernelGGL(k_lm_loss_members, by_row, dim3(256), 0, s, a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
-  a.cols = a.l.V < a.piece ? a.l.V : a.piece;
-  hipLaunchKernelGGL(k_lm_loss_list, dim3((unsigned)((R + kListRows - 1) / kListRows)), dim3(kListRows), 0, s, a);
-  if ((e = hipGetLastError()) != hipSuccess) return e;
-  hipLaunchKernelGGL(k_lm_loss_pack, dim3((unsigned)((R + kLmLossPad + 3) / 4)), dim3(256), 0, s, a);
-  if ((e = hipGetLastError()) != hipSuccess) return e;
-  hipLaunchKernelGGL(k_lm_loss_fwd, runs(a.l.V), dim3(kThreads), 0, s, a);
-  if ((e = hipGetLastError()) != hipSuccess) return e;
-  if (distill)
-    hipLaunchKernelGGL(k_lm_loss_combine<true>, by_row, dim3(256), 0, s, a);
+  if (few && a.dh == nullptr) {
+    a.plan = nullptr;
+  } else {
+    a.cols = a.l.V < a.piece ? a.l.V : a.piece;
+    hipLaunchKernelGGL(k_lm_loss_list, dim3((unsigned)((R + kListRows - 1) / kListRows)), dim3(kListRows), 0, s, a);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+    hipLaunchKernelGGL(k_lm_loss_pack, dim3((unsigned)((R + kLmLossPad + 3) / 4)), dim3(256), 0, s, a);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
+  if (few)
+    hipLaunchKernelGGL(few_fwd, dim3((unsigned)lm_few_groups(a.l.V)), dim3(kFewThreads), 0, s, a);
   else
-    hipLaunchKernelGGL(k_lm_loss_combine<false>, by_row, dim3(256), 0, s, a);
+    hipLaunchKernelGGL(k_lm_loss_fwd, runs(a.l.V), dim3(kThreads), 0, s, a);
+  if ((e = hipGetLastError()) != hipSuccess) return e;
+  if (few)
+    hipLaunchKernelGGL(distill ? k_lm_loss_few_combine<true> : k_lm_loss_few_combine<false>, dim3((unsigned)R), dim3(256),
+                       0, s, a);
+  else
+    hipLaunchKernelGGL(distill ? k_lm_loss_combine<true> : k_lm_loss_combine<false>, by_row, dim3(256), 0, s, a);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   if (a.dh == nullptr) return hipSuccess;
   for (int64_t c0 = 0; c0 < a.l.V; c0 += a.piece) {
     a.c0 = (int32_t)c0;
     a.cols = (int32_t)(a.l.V - c0 < a.piece ? a.l.V - c0 : a.piece);
-    if (distill) {
-      hipLaunchKernelGGL(k_lm_loss_g<true>, runs(a.cols), dim3(kThreads), 0, s, a);
-      if ((e = hipGetLastError()) != hipSuccess) return e;
-      hipLaunchKernelGGL(k_lm_loss_fix, by_row, dim3(256), 0, s, a);
-    } else {
-      hipLaunchKernelGGL(k_lm_loss_g<false>, runs(a.cols), dim3(kThreads), 0, s, a);
-    }
+    if (few)
+      hipLaunchKernelGGL(few_g, dim3((unsigned)(lm_tiles(a.cols) * (kLmTile / kLmFewCols))), dim3(kFewThreads), 0, s, a);
+    else
+      hipLaunchKernelGGL(distill ? k_lm_loss_g<true> : k_lm_loss_g<false>, runs(a.cols), dim3(kThreads), 0, s, a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
+    if (distill) {
+      hipLaunchKernelGGL(k_lm_loss_fix, by_row, dim3(256), 0, s, a);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
     const int64_t one = nrt * nht, split = one * kLmLossSplits < kLmLossDh ? one * kLmLossSplits : kLmLossDh;
     const int64_t dh = one > split ? one : split, dw1 = a.dw != nullptr ? (int64_t)lm_tiles(a.cols) * nht : 0;
     const int64_t dw = a.wacc != nullptr ? (dw1 * kLmLossSplits < kLmLossDw ? dw1 * kLmLossSplits : kLmLossDw) : dw1;
@@ -1697,7 +1711,7 @@ hipError_t launch_lm_loss(LmLossArgs a, bool weight_bf16, hipStream_t s) {
       if ((e = hipGetLastError()) != hipSuccess) return e;
     }
   }
-  hipLaunchKernelGGL(k_lm_loss_dh_out, by_row, dim3(256), 0, s, a);
+  hipLaunchKernelGGL(k_lm_loss_dh_out, dim3((unsigned)((R * a.H / 8 + 255) / 256)), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 

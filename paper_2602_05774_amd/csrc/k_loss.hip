@@ -185,38 +185,6 @@ __device__ __forceinline__ void row_loss(const LossArgs& a) {
   if (mine) store1(G + e.id, grad_of(x_mine) - k * p);
 }
 
-// loss_scale sum_r w_r l_r over a call's rows, in 64 bits and in one order
-// whatever workgroup forms it: 1024 partial sums of every 1024th row, then
-// those (of 64 consecutive ones a tree, of the 16 results a chain).
-constexpr int kTotalThreads = 1024;
-template <int kThreads>
-__device__ __forceinline__ void row_total(const float* loss, const float* weight, int64_t R, float scale,
-                                          float* total) {
-  __shared__ double part[kTotalThreads / kWave];
-  constexpr int U = 8;  // rows in flight per thread
-  for (int t = threadIdx.x; t < kTotalThreads; t += kThreads) {
-    double acc = 0.0;
-    for (int64_t r0 = t; r0 < R; r0 += U * kTotalThreads) {
-      float l[U], w[U];
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int64_t r = r0 + u * kTotalThreads;
-        l[u] = r < R ? __hip_atomic_load(loss + r, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0.0f;
-        w[u] = r < R && weight != nullptr ? weight[r] : 1.0f;
-      }
-#pragma unroll
-      for (int u = 0; u < U; ++u) acc += l[u] != 0.0f ? (double)l[u] * w[u] : 0.0;  // (out of play: any weight)
-    }
-    for (int n = kWave / 2; n > 0; n /= 2) acc += __shfl_xor(acc, n);
-    if ((threadIdx.x & 63) == 0) part[t / kWave] = acc;
-  }
-  __syncthreads();
-  if (threadIdx.x != 0) return;
-  double acc = part[0];
-  for (int k = 1; k < kTotalThreads / kWave; ++k) acc += part[k];
-  *total = (float)(acc * scale);
-}
-
 __global__ __launch_bounds__(kTotalThreads) void k_row_total(const float* loss, const float* weight, int64_t R,
                                                              float scale, float* total) {
   row_total<kTotalThreads>(loss, weight, R, scale, total);
@@ -225,15 +193,7 @@ __global__ __launch_bounds__(kTotalThreads) void k_row_total(const float* loss, 
 template <typename T, bool DISTILL, bool GRAD, int kThreads, int kNch, bool kMore>
 __global__ __launch_bounds__(kThreads) void k_row_loss(LossArgs a) {
   row_loss<T, DISTILL, GRAD, kThreads, kNch, kMore>(a);
-  if (a.total == nullptr) return;
-  // the last workgroup to come here forms the total
-  __shared__ int last;
-  if (threadIdx.x == 0)  // (the first lane of the wavefront that stored the row's loss)
-    last = __hip_atomic_fetch_add(a.counter, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == (int)gridDim.x - 1;
-  __syncthreads();
-  if (!last) return;
-  if (threadIdx.x == 0) *a.counter = 0;
-  row_total<kThreads>(a.loss, a.weight, a.R, a.scale, a.total);
+  total_by_last<kThreads>(a);
 }
 
 template <typename T, bool DISTILL, bool GRAD, int kThreads, int kNch, bool kMore = kNch == 0>

@@ -643,6 +643,10 @@ vsd_status base_loss(const vsd_rows* rows, const vsd_src* src, int32_t K, const 
     if (!aligned16(workspace)) return fail(VSD_ERR_MISALIGNED, "workspace not 16-byte aligned");
     char* ws = static_cast<char*>(workspace);
     vsd::LmLossArgs b{};
+    if (out->loss_total != nullptr && out->counter != nullptr && rows->R <= vsd::kTotalRows) {
+      a.total = out->loss_total;
+      a.counter = out->counter;
+    }
     b.l = a;
     b.h = src->hidden;
     b.w = src->weight;

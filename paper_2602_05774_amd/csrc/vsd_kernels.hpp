@@ -516,13 +516,15 @@ struct LmLossArgs {
   int32_t* tag;              // [R] in play iff in [0, V) (and the weight is not 0): labels, or 0 / -1
   int32_t* at;               // [R] place among the rows in play or -1
   int32_t* rows;             // [R] the rows in play
-  LmLossPlan* plan;          // [1] how many, and how their products are divided
+  LmLossPlan* plan;          // [1] how many, and how their products are divided; null: the
+                             // loss of few rows, taken as they lie
   int32_t* mid;              // [R, K] members' columns
   float* mp;                 // [R, K] their probabilities
   float2* mstat;             // [R] sums of p and p log p
   float* mx;                 // [rows in play, K] their logits
   bf16_store* hp;            // [lm_loss_pad(R), H] hidden states of the rows in play
-  float2* part;              // [2 runs, rows in play] log-sum-exps, per wavefront group
+  float2* part;              // [2 runs, rows in play] log-sum-exps, per wavefront group (few
+                             // rows: [rows in play, 2 groups of columns])
   float4* stat;              // [R] (m, kq, k, -) of the gradient
   bf16_store* g;             // [lm_loss_pad(R), ldg] the piece's gradient
   float* acc;                // [splits, rows in play, H] sums of dh
@@ -546,8 +548,13 @@ inline int32_t lm_loss_piece(int64_t R, int V) {
 // Row stride of its gradient: not a power of two, whose rows would share their
 // memory channels.
 inline int32_t lm_loss_ldg(int32_t piece) { return piece + 128; }
+// Few rows: a product whose tiles are 64 columns of W and all rows.
+constexpr int kLmFewRows = 128, kLmFewCols = 64;
+__host__ __device__ constexpr bool lm_few(int64_t R) { return R <= kLmFewRows; }
+__host__ __device__ constexpr int lm_few_groups(int V) { return (V + kLmFewCols - 1) / kLmFewCols; }
 // Entries of the forward's log-sum-exps: two per run and row in play.
 inline int64_t lm_loss_parts(int64_t R, int V) {
+  if (lm_few(R)) return 2 * R * lm_few_groups(V);
   const int64_t all = R * lm_tiles(V), runs = (int64_t)kLmLossRuns * kLmTile;
   return 2 * (all < runs ? all : runs > R ? runs : R);
 }

@@ -187,51 +187,280 @@ __global__ __launch_bounds__(kThreads, 1) void k_lm_loss_fwd(LmLossArgs a) {
   if (i < n) a.part[((int64_t)run * 2 + (wave_id() >> 2)) * n + i] = make_float2(m, s);
 }
 
+// Few rows (at most 32 kG): the products x = h W^T of 64 columns with every row.
+// Four wavefronts, each with 32 of the columns and half of a stage's depth (64).
+// Bound by the stream of W: stages of W (8 KB) and of the rows (4 KB kG, from L2)
+// are loaded straight into a ring in LDS, as nt_stream does (eight consecutive
+// lanes a row's 128 bytes; operands loaded from memory in the matrix cores'
+// layout, one row per lane, took the address unit a cycle per lane: 48 rows of
+// 32 000 x 4096 in 86 us).  One barrier per stage: before it a wavefront
+// has waited for its loads of the stage and finished reading the one before, whose
+// place the next loads take.  Past the end the last stage is loaded again.
+// take(g, c, x) consumes a lane's 16 logits of row 32 g + lane % 32: x[e] is
+// column c + 8 (e / 4) + e % 4 (the first two wavefronts).
+template <int kG>
+struct Few {
+  static constexpr int kRing = kG == 1 ? 6 : kG == 2 ? 4 : 3;
+  static constexpr int kStage = (kLmFewCols + 32 * kG) * TK;  // elements
+  static constexpr int kLds = kRing * kStage;
+  static_assert(kLds * 2 >= 2 * kG * 16 * kWave * 4, "the halves' sums fit the ring");
+  static_assert(kLds * 2 * 2 <= 160 * 1024, "two workgroups fit the LDS");
+};
+constexpr int kFewThreads = 256;
+template <int kG, class Take>
+__device__ __forceinline__ void lm_few_products(const bf16_t* h, int n, const bf16_t* W, int V, int H, bf16_t* lds,
+                                                Take&& take) {
+  constexpr int kRing = Few<kG>::kRing, kStage = Few<kG>::kStage, kLoads = 2 + kG;  // per wavefront and stage
+  const int lane = threadIdx.x & 63, wave = wave_id(), half = wave >> 1;
+  const int first = blockIdx.x * kLmFewCols, c0 = first + (wave & 1) * 32;
+  const int cols = __builtin_amdgcn_readfirstlane(max(0, min(V - first, kLmFewCols)));  // (scalar, as a descriptor)
+  const auto wr = row_rsrc(W + (int64_t)first * H, (uint32_t)cols * (uint32_t)H * 2u);
+  const auto hr = row_rsrc(h, (uint32_t)n * (uint32_t)H * 2u);
+  int wo[2], ho[kG];  // the lane's byte offset: eight rows per load
+#pragma unroll
+  for (int j = 0; j < 2; ++j) {
+    const int r = (wave * 2 + j) * 8 + (lane >> 3);
+    wo[j] = (r * H + (((lane & 7) ^ swz_v(r)) << 3)) * 2;
+  }
+#pragma unroll
+  for (int j = 0; j < kG; ++j) {
+    const int r = (wave * kG + j) * 8 + (lane >> 3);
+    ho[j] = (r * H + (((lane & 7) ^ swz_v(r)) << 3)) * 2;
+  }
+  const int stages = H / TK;
+  auto load = [&](int stage, int slot) {
+    const int k = __builtin_amdgcn_readfirstlane(min(stage, stages - 1) * TK * 2);
+    bf16_t* const to = lds + slot * kStage;
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(wr, (lds_void*)(to + (wave * 2 + j) * 8 * TK), 16, wo[j], k, 0, 0);
+#pragma unroll
+    for (int j = 0; j < kG; ++j)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(hr, (lds_void*)(to + (kLmFewCols + (wave * kG + j) * 8) * TK), 16, ho[j],
+                                               k, 0, 0);
+  };
+  f32x16 acc[kG];
+#pragma unroll
+  for (int g = 0; g < kG; ++g) acc[g] = f32x16{};
+  const int row = lane & 31;
+  auto frag = [&](int slot, int r, int j) {  // 16 K values from step j of this wavefront's half
+    const int c = half * 4 + j * 2 + (lane >> 5);
+    return *reinterpret_cast<const bf16x8*>(lds + slot * kStage + r * TK + ((c ^ swz_v(r)) << 3));
+  };
+#pragma unroll
+  for (int u = 0; u < kRing - 1; ++u) load(u, u);
+  int slot = 0;
+  for (int t = 0; t < stages; ++t) {
+    wait_loads<(kRing - 2) * kLoads>();
+    phase_barrier();
+    load(t + kRing - 1, slot == 0 ? kRing - 1 : slot - 1);
+    bf16x8 fw[2], fh[kG][2];
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      fw[j] = frag(slot, (wave & 1) * 32 + row, j);
+#pragma unroll
+      for (int g = 0; g < kG; ++g) fh[g][j] = frag(slot, kLmFewCols + g * 32 + row, j);
+    }
+    wait_lds();
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int g = 0; g < kG; ++g) acc[g] = mfma(fw[j], fh[g][j], acc[g]);
+    slot = slot + 1 == kRing ? 0 : slot + 1;
+  }
+  wait_loads<0>();  // the repeated loads have landed ...
+  __syncthreads();  // ... in every wavefront: the ring is free
+  // the two halves of the depth
+  float* mine = reinterpret_cast<float*>(lds) + (wave & 1) * kG * 16 * kWave + lane;
+  if (half == 1) {
+#pragma unroll
+    for (int g = 0; g < kG; ++g)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) mine[(g * 16 + e) * kWave] = acc[g][e];
+  }
+  __syncthreads();
+  if (half == 1) return;
+#pragma unroll
+  for (int g = 0; g < kG; ++g) {
+    float x[16];
+#pragma unroll
+    for (int e = 0; e < 16; ++e) x[e] = acc[g][e] + mine[(g * 16 + e) * kWave];
+    take(g, c0 + 4 * (lane >> 5), x);
+  }
+}
+
+template <int kG>
+__global__ __launch_bounds__(kFewThreads, 2) void k_lm_loss_few(LmLossArgs a) {
+  __shared__ __align__(16) bf16_t lds[Few<kG>::kLds];
+  const int lane = threadIdx.x & 63, n = a.plan != nullptr ? a.plan->n : (int)a.l.R;
+  if (n == 0) return;
+  lm_few_products<kG>(a.plan != nullptr ? a.hp : static_cast<const bf16_t*>(a.h), n, static_cast<const bf16_t*>(a.w),
+                      a.l.V, a.H, lds, [&](int g, int c, float (&x)[16]) {
+                        float m = kNegBig, s = 0.0f;
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) {
+                          if (c + 8 * (e / 4) + e % 4 >= a.l.V) x[e] = -INFINITY;
+                          m = fmaxf(m, x[e]);
+                        }
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) s += lse_term(x[e], m, a.l.c);
+                        lse_join(m, s, __shfl_xor(m, 32), __shfl_xor(s, 32), a.l.c);
+                        const int i = g * 32 + lane;
+                        if (lane < 32 && i < n)
+                          a.part[(int64_t)i * 2 * lm_few_groups(a.l.V) + blockIdx.x * 2 + wave_id()] = make_float2(m, s);
+                      });
+}
+
+// The same products for g of a piece.
+static_assert(kLmLossPad <= 64, "one row group's rows and as many behind them");
+template <int kG, bool DISTILL>
+__global__ __launch_bounds__(kFewThreads, 2) void k_lm_loss_few_g(LmLossArgs a) {
+  __shared__ __align__(16) bf16_t lds[Few<kG>::kLds];
+  const int lane = threadIdx.x & 63, n = a.plan->n, pad = (int)lm_loss_pad(n);
+  if (n == 0) return;
+  lm_few_products<kG>(a.hp, n, static_cast<const bf16_t*>(a.w) + (int64_t)a.c0 * a.H, a.cols, a.H, lds,
+                      [&](int g, int c, float (&x)[16]) {
+                        const int i = g * 32 + (lane & 31);
+                        if (i >= pad) return;
+                        const float4 st = i < n ? a.stat[i] : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+                        const int label = !DISTILL && i < n ? a.l.idx[a.rows[i]] - a.c0 : -1;
+                        bf16_t* G = a.g + (int64_t)i * a.ldg;
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                          float v[4];
+#pragma unroll
+                          for (int j = 0; j < 4; ++j) {
+                            const int col = c + 8 * q + j;
+                            v[j] = st.y * lse_term(x[q * 4 + j], st.x, a.l.c) - (col == label ? st.z : 0.0f);
+                            if (i >= n || col >= a.cols) v[j] = 0.0f;
+                          }
+                          *reinterpret_cast<uint2*>(G + c + 8 * q) =
+                              make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
+                          if (kG * 32 < kLmLossPad)  // (the rows in play are padded past this tile's)
+                            *reinterpret_cast<uint2*>(G + (int64_t)kG * 32 * a.ldg + c + 8 * q) = make_uint2(0, 0);
+                        }
+                      });
+}
+
 // The runs joined, the members' logits (dot products), the loss, and what the
 // gradient needs: g_v = kq exp2((x_v - m) c) - k p_v.  One wavefront per row.
+// What a row's loss and gradient are made of, by all lanes of a wavefront: (m, s)
+// and the logit of a lane's member (cross entropy: every lane the label's).
 template <bool DISTILL>
-__global__ __launch_bounds__(256) void k_lm_loss_combine(LmLossArgs a) {
+__device__ __forceinline__ void lm_loss_finish(const LmLossArgs& a, int64_t i, int64_t r, float m, float s, float x) {
   const int lane = threadIdx.x & 63;
-  const int64_t i = (int64_t)blockIdx.x * 4 + wave_id();
-  const int64_t n = a.plan->n;
-  if (i >= n) return;
-  const int64_t r = a.rows[i];
-  float m = kNegBig, s = 0.0f;
-  for (int e = lane; e < 2 * a.plan->fwd_runs; e += kWave) {
-    const float2 p = a.part[(int64_t)e * n + i];
-    lse_join(m, s, p.x, p.y, a.l.c);
-  }
-  wave_lse(m, s, a.l.c);
-  const bf16_t* h = a.hp + i * a.H;
-  const bf16_t* W = static_cast<const bf16_t*>(a.w);
   const bool live = s != 0.0f;
   const float tail = logf(s);
   float mass = 1.0f, loss;
   if (DISTILL) {
     const int K = a.l.K;
-    const int id = lane < K ? a.mid[r * K + lane] : -1;
     const float p = lane < K ? a.mp[r * K + lane] : 0.0f;
-    float x = -INFINITY;
-    for (int k = 0; k < K; ++k) {
-      const int v = lane_i(id, k);
-      if (v < 0) continue;
-      const float xk = wave_dot(h, W + (int64_t)v * a.H, a.H, lane);
-      x = lane == k ? xk : x;
-    }
     if (lane < K) a.mx[i * K + lane] = x;
     const float2 ms = a.mstat[r];
     mass = ms.x;
     loss = ms.y - wave_sum(p != 0.0f ? p * ((x - m) * a.l.inv_t - tail) : 0.0f);
   } else {
-    const float x = wave_dot(h, W + (int64_t)a.l.idx[r] * a.H, a.H, lane);
     loss = tail - (x - m) * a.l.inv_t;
   }
   if (lane == 0) {
-    a.l.loss[r] = live ? loss : 0.0f;
+    // (with the total in this launch, another XCD's workgroup reads it)
+    __hip_atomic_store(a.l.loss + r, live ? loss : 0.0f, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     if (a.l.lse != nullptr) a.l.lse[r] = live ? m * a.l.inv_t + tail : -INFINITY;
     const float k = live ? a.l.scale * row_weight(a.l, r) * a.l.inv_t : 0.0f;
     a.stat[i] = make_float4(m, live ? k * mass / s : 0.0f, k, 0.0f);
   }
+}
+
+template <bool DISTILL>
+__global__ __launch_bounds__(256) void k_lm_loss_combine(LmLossArgs a) {
+  const int lane = threadIdx.x & 63;
+  const int64_t i = (int64_t)blockIdx.x * 4 + wave_id(), n = a.plan->n;
+  if (i < n) {
+    const int64_t r = a.rows[i];
+    float m = kNegBig, s = 0.0f;
+    for (int e = lane; e < 2 * a.plan->fwd_runs; e += kWave) {
+      const float2 p = a.part[(int64_t)e * n + i];
+      lse_join(m, s, p.x, p.y, a.l.c);
+    }
+    wave_lse(m, s, a.l.c);
+    const bf16_t* h = a.hp + i * a.H;
+    const bf16_t* W = static_cast<const bf16_t*>(a.w);
+    float x = -INFINITY;
+    if (DISTILL) {
+      const int K = a.l.K, id = lane < K ? a.mid[r * K + lane] : -1;
+      for (int k = 0; k < K; ++k) {
+        const int v = lane_i(id, k);
+        if (v < 0) continue;
+        const float xk = wave_dot(h, W + (int64_t)v * a.H, a.H, lane);
+        x = lane == k ? xk : x;
+      }
+    } else {
+      x = wave_dot(h, W + (int64_t)a.l.idx[r] * a.H, a.H, lane);
+    }
+    lm_loss_finish<DISTILL>(a, i, r, m, s, x);
+  }
+  if (a.l.total == nullptr) return;
+  __syncthreads();
+  total_by_last<256>(a.l);
+}
+
+// The same of few rows, a workgroup per row (two partial sums for every 64
+// columns).  Without a plan every row is here, in play or not.
+template <bool DISTILL>
+__global__ __launch_bounds__(256) void k_lm_loss_few_combine(LmLossArgs a) {
+  __shared__ float red_m[4], red_s[4], xs[DISTILL ? kMaxMembers : 1];
+  const int lane = threadIdx.x & 63, wave = wave_id();
+  const int64_t i = blockIdx.x;
+  bool in = i < (a.plan != nullptr ? a.plan->n : (int)a.l.R);
+  const int64_t r = a.plan != nullptr && in ? a.rows[i] : i;
+  if (a.plan == nullptr) {
+    const int32_t t = a.tag[r];
+    in = (uint32_t)t < (uint32_t)a.l.V && row_weight(a.l, r) != 0.0f;
+    if (!in && threadIdx.x == 0) {
+      if (t != -1 && (uint32_t)t >= (uint32_t)a.l.V) report_error(a.l.err, VSD_DEVERR_TOKEN_RANGE);
+      __hip_atomic_store(a.l.loss + r, 0.0f, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      if (a.l.lse != nullptr) a.l.lse[r] = 0.0f;
+    }
+  }
+  if (in) {
+    const int parts = 2 * lm_few_groups(a.l.V);
+    const float2* part = a.part + i * parts;
+    float m = kNegBig, s = 0.0f;
+    constexpr int U = 8;  // in flight per thread
+    for (int e0 = threadIdx.x; e0 < parts; e0 += U * 256) {
+      float2 p[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) p[u] = e0 + u * 256 < parts ? part[e0 + u * 256] : make_float2(kNegBig, 0.0f);
+#pragma unroll
+      for (int u = 0; u < U; ++u) lse_join(m, s, p[u].x, p[u].y, a.l.c);
+    }
+    wave_lse(m, s, a.l.c);
+    if (lane == 0) {
+      red_m[wave] = m;
+      red_s[wave] = s;
+    }
+    const bf16_t* h = a.plan != nullptr ? a.hp + i * a.H : static_cast<const bf16_t*>(a.h) + r * a.H;
+    const bf16_t* W = static_cast<const bf16_t*>(a.w);
+    if (DISTILL) {
+      for (int k = wave; k < a.l.K; k += 4) {
+        const int v = __builtin_amdgcn_readfirstlane(a.mid[r * a.l.K + k]);
+        const float x = v >= 0 ? wave_dot(h, W + (int64_t)v * a.H, a.H, lane) : -INFINITY;
+        if (lane == 0) xs[k] = x;
+      }
+    } else if (wave == 0) {
+      const float x = wave_dot(h, W + (int64_t)a.l.idx[r] * a.H, a.H, lane);
+      if (lane == 0) xs[0] = x;
+    }
+    __syncthreads();
+    if (wave == 0) {
+      m = red_m[0];
+      s = red_s[0];
+#pragma unroll
+      for (int k = 1; k < 4; ++k) lse_join(m, s, red_m[k], red_s[k], a.l.c);
+      lm_loss_finish<DISTILL>(a, i, r, m, s, !DISTILL ? xs[0] : lane < a.l.K ? xs[lane] : -INFINITY);
+    }
+  }
+  total_by_last<256>(a.l);
 }
 
 // g of one piece of the vocabulary (columns c0 .. c0 + cols - 1): a run of
@@ -409,22 +638,21 @@ __global__ __launch_bounds__(kThreads, 1) void k_lm_loss_grads(LmLossArgs a) {
   }
 }
 
+// The ranges' sums of dh, eight columns per thread.
 __global__ __launch_bounds__(256) void k_lm_loss_dh_out(LmLossArgs a) {
-  const int lane = threadIdx.x & 63;
-  const int64_t i = (int64_t)blockIdx.x * 4 + wave_id(), n = a.plan->n;
-  if (i >= n || a.plan->splits == 1) return;
-  bf16_t* D = static_cast<bf16_t*>(a.dh) + (int64_t)a.rows[i] * a.H;
-  for (int k = lane * 8; k < a.H; k += kWave * 8) {
-    float v[8];
-    load8(a.acc + i * a.H + k, v);
-    for (int z = 1; z < a.plan->splits; ++z) {
-      float o[8];
-      load8(a.acc + ((int64_t)z * n + i) * a.H + k, o);
+  const int splits = a.plan->splits;
+  const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8, all = (int64_t)a.plan->n * a.H;
+  if (splits == 1 || at >= all) return;
+  float v[8];
+  load8(a.acc + at, v);
+#pragma unroll 4
+  for (int z = 1; z < splits; ++z) {
+    float o[8];
+    load8(a.acc + z * all + at, o);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] += o[j];
-    }
-    store8(D + k, v);
+    for (int j = 0; j < 8; ++j) v[j] += o[j];
   }
+  store8(static_cast<bf16_t*>(a.dh) + (int64_t)a.rows[at / a.H] * a.H + at % a.H, v);
 }
 
 template <typename T>
@@ -434,6 +662,7 @@ __global__ __launch_bounds__(256) void k_lm_loss_dw_out(LmLossArgs a) {
   if (splits == 1 || at >= all) return;
   float v[8];
   load8(a.wacc + at, v);
+#pragma unroll 4
   for (int z = 1; z < splits; ++z) {
     float o[8];
     load8(a.wacc + z * all + at, o);

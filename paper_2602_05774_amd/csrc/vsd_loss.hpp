@@ -146,4 +146,51 @@ __device__ __forceinline__ float row_weight(const LossArgs& a, int64_t r) {
   return a.weight != nullptr ? a.weight[r] : 1.0f;
 }
 
+// loss_scale sum_r w_r l_r over a call's rows, in 64 bits and in one order
+// whatever workgroup forms it: 1024 partial sums of every 1024th row, then
+// those (of 64 consecutive ones a tree, of the 16 results a chain).
+constexpr int kTotalThreads = 1024;
+template <int kThreads>
+__device__ __forceinline__ void row_total(const float* loss, const float* weight, int64_t R, float scale,
+                                          float* total) {
+  __shared__ double part[kTotalThreads / kWave];
+  constexpr int U = 8;  // rows in flight per thread
+  for (int t = threadIdx.x; t < kTotalThreads; t += kThreads) {
+    double acc = 0.0;
+    for (int64_t r0 = t; r0 < R; r0 += U * kTotalThreads) {
+      float l[U], w[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int64_t r = r0 + u * kTotalThreads;
+        l[u] = r < R ? __hip_atomic_load(loss + r, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0.0f;
+        w[u] = r < R && weight != nullptr ? weight[r] : 1.0f;
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) acc += l[u] != 0.0f ? (double)l[u] * w[u] : 0.0;  // (out of play: any weight)
+    }
+    for (int n = kWave / 2; n > 0; n /= 2) acc += __shfl_xor(acc, n);
+    if ((threadIdx.x & 63) == 0) part[t / kWave] = acc;
+  }
+  __syncthreads();
+  if (threadIdx.x != 0) return;
+  double acc = part[0];
+  for (int k = 1; k < kTotalThreads / kWave; ++k) acc += part[k];
+  *total = (float)(acc * scale);
+}
+
+// The last of a launch's workgroups to come here forms the total (its thread 0
+// having stored the losses of its own rows device-wide, or after a barrier that
+// follows such stores).
+template <int kThreads>
+__device__ __forceinline__ void total_by_last(const LossArgs& a) {
+  if (a.total == nullptr) return;
+  __shared__ int last;
+  if (threadIdx.x == 0)
+    last = __hip_atomic_fetch_add(a.counter, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == (int)gridDim.x - 1;
+  __syncthreads();
+  if (!last) return;
+  if (threadIdx.x == 0) *a.counter = 0;
+  row_total<kThreads>(a.loss, a.weight, a.R, a.scale, a.total);
+}
+
 }  // namespace vsd

@@ -64,7 +64,7 @@ def _check(res, h, w, mem, weight, T, scale, V):
         assert np.all(np.abs(dw - ref["grad_weight"]) <= bw), np.max(np.abs(dw - ref["grad_weight"]) / bw)
 
 
-SHAPES = [(1, 1, 64), (1, 300, 128), (5, 7, 64), (63, 256, 64), (64, 257, 192), (65, 1000, 320), (257, 5003, 128),
+SHAPES = [(1, 1, 64), (1, 300, 128), (20, 515, 192), (33, 4099, 128), (100, 1000, 576), (5, 7, 64), (63, 256, 64), (64, 257, 192), (65, 1000, 320), (257, 5003, 128),
           (600, 2049, 256), (48, 33000, 512), (1300, 700, 64)]
 
 
@@ -159,8 +159,9 @@ def test_pieces(loss):
     assert err < 2 ** -8, float(err)  # every g is within 2^-8 of its value
 
 
-def test_captured_calls_and_a_kept_workspace():
-    R, V, H = 130, 3001, 128
+@pytest.mark.parametrize("R", (3, 20, 50, 100, 130, 1500))
+def test_captured_calls_and_a_kept_workspace(R):
+    V, H = 3001, 128
     h, w = _head(R, V, H, 36)
     new = [_head(R, V, H, s)[0] for s in (37, 38)]
     labels = torch.randint(-1, V, (R,), device=DEV, dtype=torch.int32)
