@@ -1673,8 +1673,8 @@ hipError_t launch_lm_loss(LmLossArgs a, bool weight_bf16, hipStream_t s) {
     hipLaunchKernelGGL(k_lm_loss_fwd, runs(a.l.V), dim3(kThreads), 0, s, a);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   if (few)
-    hipLaunchKernelGGL(distill ? k_lm_loss_few_combine<true> : k_lm_loss_few_combine<false>, dim3((unsigned)R), dim3(256),
-                       0, s, a);
+    hipLaunchKernelGGL(distill ? k_lm_loss_few_combine<true> : k_lm_loss_few_combine<false>, dim3((unsigned)R),
+                       dim3(distill ? FewCombine<true>::kThreads : FewCombine<false>::kThreads), 0, s, a);
   else
     hipLaunchKernelGGL(distill ? k_lm_loss_combine<true> : k_lm_loss_combine<false>, by_row, dim3(256), 0, s, a);
   if ((e = hipGetLastError()) != hipSuccess) return e;

@@ -407,8 +407,13 @@ __global__ __launch_bounds__(256) void k_lm_loss_combine(LmLossArgs a) {
 // The same of few rows, a workgroup per row (two partial sums for every 64
 // columns).  Without a plan every row is here, in play or not.
 template <bool DISTILL>
-__global__ __launch_bounds__(256) void k_lm_loss_few_combine(LmLossArgs a) {
-  __shared__ float red_m[4], red_s[4], xs[DISTILL ? kMaxMembers : 1];
+struct FewCombine {
+  static constexpr int kThreads = DISTILL ? 1024 : 256;  // (a wavefront per few members)
+};
+template <bool DISTILL>
+__global__ __launch_bounds__(FewCombine<DISTILL>::kThreads) void k_lm_loss_few_combine(LmLossArgs a) {
+  constexpr int kThreads = FewCombine<DISTILL>::kThreads, kWaves = kThreads / kWave;
+  __shared__ float red_m[kWaves], red_s[kWaves], xs[DISTILL ? kMaxMembers : 1];
   const int lane = threadIdx.x & 63, wave = wave_id();
   const int64_t i = blockIdx.x;
   bool in = i < (a.plan != nullptr ? a.plan->n : (int)a.l.R);
@@ -427,10 +432,11 @@ __global__ __launch_bounds__(256) void k_lm_loss_few_combine(LmLossArgs a) {
     const float2* part = a.part + i * parts;
     float m = kNegBig, s = 0.0f;
     constexpr int U = 8;  // in flight per thread
-    for (int e0 = threadIdx.x; e0 < parts; e0 += U * 256) {
+    for (int e0 = threadIdx.x; e0 < parts; e0 += U * kThreads) {
       float2 p[U];
 #pragma unroll
-      for (int u = 0; u < U; ++u) p[u] = e0 + u * 256 < parts ? part[e0 + u * 256] : make_float2(kNegBig, 0.0f);
+      for (int u = 0; u < U; ++u)
+        p[u] = e0 + u * kThreads < parts ? part[e0 + u * kThreads] : make_float2(kNegBig, 0.0f);
 #pragma unroll
       for (int u = 0; u < U; ++u) lse_join(m, s, p[u].x, p[u].y, a.l.c);
     }
@@ -442,7 +448,7 @@ __global__ __launch_bounds__(256) void k_lm_loss_few_combine(LmLossArgs a) {
     const bf16_t* h = a.plan != nullptr ? a.hp + i * a.H : static_cast<const bf16_t*>(a.h) + r * a.H;
     const bf16_t* W = static_cast<const bf16_t*>(a.w);
     if (DISTILL) {
-      for (int k = wave; k < a.l.K; k += 4) {
+      for (int k = wave; k < a.l.K; k += kWaves) {
         const int v = __builtin_amdgcn_readfirstlane(a.mid[r * a.l.K + k]);
         const float x = v >= 0 ? wave_dot(h, W + (int64_t)v * a.H, a.H, lane) : -INFINITY;
         if (lane == 0) xs[k] = x;
@@ -456,11 +462,11 @@ __global__ __launch_bounds__(256) void k_lm_loss_few_combine(LmLossArgs a) {
       m = red_m[0];
       s = red_s[0];
 #pragma unroll
-      for (int k = 1; k < 4; ++k) lse_join(m, s, red_m[k], red_s[k], a.l.c);
+      for (int k = 1; k < kWaves; ++k) lse_join(m, s, red_m[k], red_s[k], a.l.c);
       lm_loss_finish<DISTILL>(a, i, r, m, s, !DISTILL ? xs[0] : lane < a.l.K ? xs[lane] : -INFINITY);
     }
   }
-  total_by_last<256>(a.l);
+  total_by_last<kThreads>(a.l);
 }
 
 // g of one piece of the vocabulary (columns c0 .. c0 + cols - 1): a run of
@@ -482,20 +488,30 @@ __global__ __launch_bounds__(kThreads, 1) void k_lm_loss_g(LmLossArgs a) {
   nt_stream(lds, src, [&](int tile, NtAcc& acc) {
     nt_row_per_lane(acc);
     if (i >= lm_loss_pad(n)) return;
+    const uint32_t keep = i < n ? ~0u : 0u;  // (what lies behind the rows in play gives zeros, whatever x is)
     const float4 st = i < n ? a.stat[i] : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     const int label = !DISTILL && i < n ? a.l.idx[a.rows[i]] - a.c0 : -1;
+    const float c = a.l.c, mc = st.x * a.l.c;  // (its rounding is 2^-24 |m c| of g, which is rounded to 2^-8)
     bf16_t* G = a.g + i * a.ldg;
 #pragma unroll 1
     for (int ch = 0; ch < 16; ++ch) {
-      const int c = tile * TN + nt_chunk_col(ch);
+      const int col = tile * TN + nt_chunk_col(ch);
       float x[8], g[8];
       nt_chunk(acc, ch, x);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        g[j] = st.y * lse_term(x[j], st.x, a.l.c) - (c + j == label ? st.z : 0.0f);
-        if (i >= n || c + j >= a.cols) g[j] = 0.0f;
+      for (int j = 0; j < 8; ++j) g[j] = st.y * __builtin_amdgcn_exp2f(fmaf(x[j], c, -mc));
+      if (!DISTILL && (uint32_t)(label - col) < 8u) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) g[j] -= col + j == label ? st.z : 0.0f;
       }
-      store8(G + c, g);
+      if (col + 8 > a.cols) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (col + j >= a.cols) g[j] = 0.0f;
+      }
+      *reinterpret_cast<uint4*>(G + col) =
+          make_uint4(pack_bf16x2(g[0], g[1]) & keep, pack_bf16x2(g[2], g[3]) & keep, pack_bf16x2(g[4], g[5]) & keep,
+                     pack_bf16x2(g[6], g[7]) & keep);
     }
   });
 }
