@@ -240,7 +240,9 @@
  *   d2t only the columns d2t[u] take part, each with the index u in [0,
  *   v_draft) (the lse stays that of all columns).
  *   loss_row, lse, top_idx ... hold R rows, contiguous; R < 2^24 (top logits:
- *   2^22), k <= VSD_MAX_TOP.
+ *   2^22), k <= VSD_MAX_TOP, temperatures in [1e-30, 1e30].  Calls that may
+ *   overlap on the device need workspaces (and counters) of their own; a
+ *   workspace may hold anything before a call.
  */
 #ifndef VSD_H
 #define VSD_H

@@ -31,19 +31,13 @@ __device__ __forceinline__ void row_loss(const LossArgs& a) {
   const float w = row_weight(a, r);
   const int first = threadIdx.x * 8;
 
-  // the row's members (every wavefront has the label; the first one the teacher's)
+  // the row's members: every wavefront has the label, or whether there are any (the
+  // teacher's probabilities are formed while the logits are on their way)
   Member e{-1, 1.0f, 0.0f};
   float mass = 1.0f;
   if (DISTILL) {
-    if (wave == 0) {
-      e = load_member(a, r, lane);
-      const float total = wave_sum(e.p);
-      sid[lane] = e.id;
-      sp[lane] = e.p;
-      if (lane == 0) sum_p = total;
-    }
-    __syncthreads();
-    mass = sum_p;
+    e.id = member_id(a, r, lane);
+    mass = __ballot(e.id >= 0) != 0ull ? 1.0f : 0.0f;
   } else {
     e.id = a.idx[r];
     if ((uint32_t)e.id >= (uint32_t)a.V) {
@@ -54,14 +48,38 @@ __device__ __forceinline__ void row_loss(const LossArgs& a) {
   bool live = mass != 0.0f && w != 0.0f;
   // the members' logits: read ahead of the sweeps' barrier, since G may be X
   float x_mine = -INFINITY;
-  if (wave == 0 && live && e.id >= 0) x_mine = load1(X + e.id);
+  MemberValue value{-INFINITY, 0.0f};
+  if (wave == 0 && live) {
+    if (DISTILL) value = load_value(a, r, lane, e.id);
+    if (e.id >= 0) x_mine = load1(X + e.id);
+  }
 
   float m = kNegBig, s = 0.0f;
   Raw8<T> row[kNch > 0 ? kNch : 1];
+  auto members = [&]() {
+    if (!DISTILL || wave != 0) return;
+    e = member_of(a, e.id, value);
+    const float total = wave_sum(e.p);
+    sid[lane] = e.id;
+    sp[lane] = e.p;
+    if (lane == 0) sum_p = total;
+  };
+  // The first wavefront's probabilities: while the row is on its way, but for rows of
+  // 512 threads x 8 before it is asked for (us, before / meanwhile: 16 384 x 32 000
+  // bf16 399 / 417, 4096 x 128 256 490 / 457, 9930 x 4673 68 / 66, 4000 x 9000
+  // float32 89 / 85).
+  constexpr bool kMembersFirst = DISTILL && kThreads == 512 && kNch == 8;
   if (live) {
+    if constexpr (kMembersFirst) {
+      members();
+      __syncthreads();
+    }
     if constexpr (kNch > 0) {
 #pragma unroll
       for (int j = 0; j < kNch; ++j) load_cols(row[j], X, first + j * kStep, a.V);
+    }
+    if constexpr (!kMembersFirst) members();
+    if constexpr (kNch > 0) {
 #pragma unroll
       for (int j = 0; j < kNch; ++j) {
         float x[8];
@@ -101,7 +119,9 @@ __device__ __forceinline__ void row_loss(const LossArgs& a) {
     s = red_s[0];
 #pragma unroll
     for (int k = 1; k < kWaves; ++k) lse_join(m, s, red_m[k], red_s[k], a.c);
+    if (DISTILL) mass = sum_p;
   }
+  live = live && mass != 0.0f;
   const bool empty = live && s == 0.0f;  // no logit above -inf
   live = live && !empty;
 
@@ -196,38 +216,51 @@ __global__ __launch_bounds__(kThreads) void k_row_loss(LossArgs a) {
   total_by_last<kThreads>(a);
 }
 
-template <typename T, bool DISTILL, bool GRAD, int kThreads, int kNch, bool kMore = kNch == 0>
-hipError_t launch_n(const LossArgs& a, hipStream_t s) {
-  hipLaunchKernelGGL((k_row_loss<T, DISTILL, GRAD, kThreads, kNch, kMore>), dim3((unsigned)a.R), dim3(kThreads), 0, s,
-                     a);
+template <typename T, bool DISTILL, bool GRAD>
+hipError_t launch_t(const LossArgs& a, hipStream_t s) {
+  const RowThreads t = row_loss_threads(a.R, a.V, sizeof(T) == 4, GRAD);
+  void (*kernel)(LossArgs) = nullptr;
+  auto use = [&](int threads, int chunks, bool more, void (*k)(LossArgs)) {
+    if (t.threads == threads && t.chunks == chunks && t.more == more) kernel = k;
+  };
+  if constexpr (!GRAD) {
+    use(64, 0, true, k_row_loss<T, DISTILL, false, 64, 0, true>);
+    use(256, 0, true, k_row_loss<T, DISTILL, false, 256, 0, true>);
+    use(1024, 0, true, k_row_loss<T, DISTILL, false, 1024, 0, true>);
+  } else {
+    use(64, 4, false, k_row_loss<T, DISTILL, true, 64, 4, false>);
+    use(256, 0, true, k_row_loss<T, DISTILL, true, 256, 0, true>);
+    use(1024, 8, false, k_row_loss<T, DISTILL, true, 1024, 8, false>);
+    if constexpr (sizeof(T) == 4) {
+      use(256, 2, false, k_row_loss<T, DISTILL, true, 256, 2, false>);
+      use(512, 2, false, k_row_loss<T, DISTILL, true, 512, 2, false>);
+      use(1024, 2, false, k_row_loss<T, DISTILL, true, 1024, 2, false>);
+      use(1024, 4, false, k_row_loss<T, DISTILL, true, 1024, 4, false>);
+      use(1024, 8, true, k_row_loss<T, DISTILL, true, 1024, 8, true>);
+    } else {
+      use(128, 4, false, k_row_loss<T, DISTILL, true, 128, 4, false>);
+      use(256, 4, false, k_row_loss<T, DISTILL, true, 256, 4, false>);
+      use(512, 4, false, k_row_loss<T, DISTILL, true, 512, 4, false>);
+      use(512, 8, false, k_row_loss<T, DISTILL, true, 512, 8, false>);
+      use(1024, 16, false, k_row_loss<T, DISTILL, true, 1024, 16, false>);
+      use(1024, 16, true, k_row_loss<T, DISTILL, true, 1024, 16, true>);
+    }
+  }
+  if (kernel == nullptr) return hipErrorInvalidConfiguration;  // (row_loss_threads names one of these)
+  hipLaunchKernelGGL(kernel, dim3((unsigned)a.R), dim3((unsigned)t.threads), 0, s, a);
   return hipGetLastError();
 }
 
-// Threads per row and whether it stays in registers.
 template <typename T, bool DISTILL>
-hipError_t launch_t(const LossArgs& a, hipStream_t s) {
-  if (a.G == nullptr) {
-    if (a.V <= 2048) return launch_n<T, DISTILL, false, 64, 0>(a, s);
-    if (a.R <= 512 && a.V > 8192) return launch_n<T, DISTILL, false, 1024, 0>(a, s);
-    return launch_n<T, DISTILL, false, 256, 0>(a, s);
-  }
-  constexpr bool kWide = sizeof(T) == 4;
-  constexpr int kFull = kWide ? 8 : 16;
-  if (a.V <= 2048) return launch_n<T, DISTILL, true, 64, 4>(a, s);
-  if (a.V <= 4096) return launch_n<T, DISTILL, true, kWide ? 256 : 128, kWide ? 2 : 4>(a, s);
-  if (a.V <= 8192) return launch_n<T, DISTILL, true, kWide ? 512 : 256, kWide ? 2 : 4>(a, s);
-  if (a.V <= 16384) return launch_n<T, DISTILL, true, kWide ? 1024 : 512, kWide ? 2 : 4>(a, s);
-  if (a.V <= 32768) return launch_n<T, DISTILL, true, kWide ? 1024 : 512, kWide ? 4 : 8>(a, s);
-  if (a.V <= 65536) return launch_n<T, DISTILL, true, 1024, 8>(a, s);
-  if (a.V <= kFull * 8192) return launch_n<T, DISTILL, true, 1024, kFull>(a, s);
-  return launch_n<T, DISTILL, true, 1024, kFull, true>(a, s);
+hipError_t launch_d(const LossArgs& a, hipStream_t s) {
+  return a.G != nullptr ? launch_t<T, DISTILL, true>(a, s) : launch_t<T, DISTILL, false>(a, s);
 }
 
 }  // namespace
 
 hipError_t launch_row_loss(const LossArgs& a, bool bf16, hipStream_t s) {
-  if (a.val != nullptr) return bf16 ? launch_t<bf16_t, true>(a, s) : launch_t<float, true>(a, s);
-  return bf16 ? launch_t<bf16_t, false>(a, s) : launch_t<float, false>(a, s);
+  if (a.val != nullptr) return bf16 ? launch_d<bf16_t, true>(a, s) : launch_d<float, true>(a, s);
+  return bf16 ? launch_d<bf16_t, false>(a, s) : launch_d<float, false>(a, s);
 }
 
 hipError_t launch_row_total(const float* loss, const float* weight, int64_t R, float scale, float* total,

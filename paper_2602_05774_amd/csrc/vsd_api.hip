@@ -503,7 +503,8 @@ vsd_status check_rows_struct(const vsd_rows* rows) {
     if (rows->dtype != VSD_BF16) return fail(VSD_ERR_UNSUPPORTED, "the fused LM head takes bf16 operands only");
     const int64_t nrt = (rows->R + vsd::kLmTile - 1) / vsd::kLmTile;
     const int64_t nht = (H + vsd::kLmTile - 1) / vsd::kLmTile, vt = ((int64_t)rows->v + vsd::kLmTile - 1) / vsd::kLmTile;
-    if (nrt * std::max(nht, vt) >= kMaxLmWorkgroups || nht * vt >= kMaxLmWorkgroups)
+    if (nrt * std::max(nht, vt) >= kMaxLmWorkgroups || nht * vt >= kMaxLmWorkgroups ||
+        rows->R * H >= ((int64_t)1 << 35))  // (a work-item per eight of them)
       return fail(VSD_ERR_INVALID_SHAPE, "fused LM head: R=%lld rows x v=%d x hidden_dim=%d too large",
                   (long long)rows->R, rows->v, H);
   }
@@ -518,7 +519,8 @@ vsd_status check_rows_src(const vsd_rows* rows, const vsd_src* src, const char* 
   return check_logits(&d, src, name, rows->ld, rows->v);
 }
 
-bool usable_temp(float t) { return finite_pos(t) && finite_pos(1.0f / t) && std::isfinite(vsd::kLog2e / t); }
+// Logits times log2(e) / t must stay finite.
+bool usable_temp(float t) { return std::isfinite(t) && t >= 1e-30f && t <= 1e30f; }
 
 struct LossLayout {
   size_t tag, at, rows, plan, mid, mp, mstat, mx, hp, part, stat, g, acc, wacc, total;
@@ -601,7 +603,7 @@ vsd_status base_loss(const vsd_rows* rows, const vsd_src* src, int32_t K, const 
   if (st != VSD_OK) return st;
   if ((st = check_rows_src(rows, src, "draft")) != VSD_OK) return st;
   if (!usable_temp(temp) || !usable_temp(temp_target))
-    return fail(VSD_ERR_INVALID_VALUE, "temperatures must be finite, > 0 and have a finite reciprocal");
+    return fail(VSD_ERR_INVALID_VALUE, "temperatures must lie in [1e-30, 1e30]");
   if (!std::isfinite(scale)) return fail(VSD_ERR_INVALID_VALUE, "loss_scale must be finite");
   if ((st = check_loss_out(out)) != VSD_OK) return st;
   if ((st = check_loss_grad(rows, grad)) != VSD_OK) return st;
@@ -1262,7 +1264,7 @@ vsd_status vsd_top_logits(const vsd_rows* rows, const vsd_src* target, int32_t k
   if ((st = check_rows_src(rows, target, "target")) != VSD_OK) return st;
   if (k < 1 || k > VSD_MAX_TOP) return fail(VSD_ERR_INVALID_VALUE, "k=%d outside [1,%d]", k, VSD_MAX_TOP);
   if (!usable_temp(temp_target))
-    return fail(VSD_ERR_INVALID_VALUE, "temp_target must be finite, > 0 and have a finite reciprocal");
+    return fail(VSD_ERR_INVALID_VALUE, "temp_target must lie in [1e-30, 1e30]");
   if (top_idx == nullptr || top_logits == nullptr || device_error == nullptr)
     return fail(VSD_ERR_NULL_POINTER, "top_idx, top_logits and device_error are required");
   hipStream_t s = static_cast<hipStream_t>(hip_stream);

@@ -459,9 +459,49 @@ struct LossArgs {
   float* total;                // [1], or null: formed by launch_row_total
   int32_t* counter;            // [1] zero (with total): workgroups that are done
 };
-// Rows up to which the last workgroup of the row kernel forms the total: each
-// workgroup then ends with an atomic add.
-constexpr int64_t kTotalRows = 1024;
+// Rows up to which the last workgroup of the row kernel forms the total.  Each
+// workgroup then ends with an atomic add on one word (about 35 ns one after the
+// other), which up to here takes no longer than a launch on the GPU and spares the
+// host's 3 us; us of a replayed graph, launch / atomics, float32 with gradient:
+// 64 rows of 1000 19.2 / 19.4, 192 rows 18.5 / 24.4, 1000 rows 17.8 / 52.5.
+constexpr int64_t kTotalRows = 64;
+
+// Threads per row of the losses on materialised logits.  With the gradient a row
+// stays in registers: 32 columns a thread (float32: 16), 64 for 512 threads
+// (32 for 1024), and, what 1024 threads do not hold (131 072 columns, float32:
+// 65 536), the rest of it is read twice.  A launch counts its work-items in 32
+// bits: past 2^22 rows, 256 threads that read the row twice.
+// us of cross_entropy by threads x groups of eight columns:
+//   gradient, bf16    65 536 x 500      256 x 1  141     64 x 4    78
+//                     65 536 x 2000     256 x 1  194     64 x 4   118
+//                     65 536 x 4000     256 x 4  269    128 x 8   235   128 x 4  214
+//                     16 384 x 8000     256 x 4  111    128 x 8   115   512 x 2  124
+//                     16 384 x 16 000   512 x 4  201    256 x 8   211   512 x 8  243
+//                     16 384 x 32 000   512 x 8  403    read twice 494
+//                      8192 x 128 256  1024 x 16 810    read twice 1266
+//            float32  16 384 x 8000     512 x 2  201    256 x 4   226   128 x 8  245
+//                      8192 x 32 000   1024 x 4  410    512 x 8   422   read twice 593
+//                      2048 x 128 256  1024 x 8 and the rest twice 478, all twice 640
+//   loss only, bf16     512 x 128 256  1024      36     256        43
+//                      1024 x 128 256  1024      52     256        57
+//                     65 536 x 2000      64      80     256       130
+struct RowThreads {
+  int threads, chunks;  // chunks: groups of eight columns that a thread keeps
+  bool more;            // the row is longer than they hold
+};
+constexpr int64_t kMaxWideRows = ((int64_t)1 << 22) - 1;
+inline RowThreads row_loss_threads(int64_t R, int V, bool wide, bool grad) {
+  if (V <= 2048) return {64, grad ? 4 : 0, !grad};
+  if (!grad) return {R <= 512 && V > 8192 ? 1024 : 256, 0, true};
+  if (V <= 4096) return wide ? RowThreads{256, 2, false} : RowThreads{128, 4, false};
+  if (R > kMaxWideRows) return {256, 0, true};
+  if (V <= 8192) return wide ? RowThreads{512, 2, false} : RowThreads{256, 4, false};
+  if (V <= 16384) return wide ? RowThreads{1024, 2, false} : RowThreads{512, 4, false};
+  if (V <= 32768) return wide ? RowThreads{1024, 4, false} : RowThreads{512, 8, false};
+  if (V <= 65536) return {1024, 8, false};
+  if (!wide && V <= 131072) return {1024, 16, false};
+  return {1024, wide ? 8 : 16, true};
+}
 
 // The K largest entries of a teacher's rows.
 struct TopArgs {

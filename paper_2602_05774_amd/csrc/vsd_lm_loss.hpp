@@ -17,7 +17,8 @@ __global__ __launch_bounds__(256) void k_lm_loss_members(LmLossArgs a) {
   const int lane = threadIdx.x & 63;
   const int64_t r = (int64_t)blockIdx.x * 4 + wave_id();
   if (r >= a.l.R) return;
-  const Member e = load_member(a.l, r, lane);
+  const int id = member_id(a.l, r, lane);
+  const Member e = member_of(a.l, id, load_value(a.l, r, lane, id));
   const float mass = wave_sum(e.p), plogp = wave_sum(e.plogp);
   if (lane < a.l.K) {
     a.mid[r * a.l.K + lane] = e.id;
@@ -491,7 +492,8 @@ __global__ __launch_bounds__(kThreads, 1) void k_lm_loss_g(LmLossArgs a) {
     const uint32_t keep = i < n ? ~0u : 0u;  // (what lies behind the rows in play gives zeros, whatever x is)
     const float4 st = i < n ? a.stat[i] : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     const int label = !DISTILL && i < n ? a.l.idx[a.rows[i]] - a.c0 : -1;
-    const float c = a.l.c, mc = st.x * a.l.c;  // (its rounding is 2^-24 |m c| of g, which is rounded to 2^-8)
+    // kq exp2((x - m) c) with one rounding in the exponent: that of m c goes into kq
+    const float c = a.l.c, mc = st.x * a.l.c, kq = st.y * __builtin_amdgcn_exp2f(-fmaf(st.x, c, -mc));
     bf16_t* G = a.g + i * a.ldg;
 #pragma unroll 1
     for (int ch = 0; ch < 16; ++ch) {
@@ -499,7 +501,7 @@ __global__ __launch_bounds__(kThreads, 1) void k_lm_loss_g(LmLossArgs a) {
       float x[8], g[8];
       nt_chunk(acc, ch, x);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) g[j] = st.y * __builtin_amdgcn_exp2f(fmaf(x[j], c, -mc));
+      for (int j = 0; j < 8; ++j) g[j] = kq * __builtin_amdgcn_exp2f(fmaf(x[j], c, -mc));
       if (!DISTILL && (uint32_t)(label - col) < 8u) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) g[j] -= col + j == label ? st.z : 0.0f;

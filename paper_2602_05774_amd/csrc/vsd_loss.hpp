@@ -110,27 +110,34 @@ struct Member {
   int id;
   float p, plogp;
 };
-__device__ __forceinline__ Member load_member(const LossArgs& a, int64_t r, int lane) {
-  Member e{-1, 0.0f, 0.0f};
-  float v = -INFINITY;
-  if (lane < a.K) {
+__device__ __forceinline__ int member_id(const LossArgs& a, int64_t r, int lane) {
+  const int id = lane < a.K ? a.idx[r * a.K + lane] : -1;
+  if ((uint32_t)id < (uint32_t)a.V) return id;
+  if (id != -1) report_error(a.err, VSD_DEVERR_TOKEN_RANGE);
+  return -1;
+}
+// What lane k needs for member k: its teacher logit / T_p and the teacher's log-sum-exp.
+struct MemberValue {
+  float v, lse;
+};
+__device__ __forceinline__ MemberValue load_value(const LossArgs& a, int64_t r, int lane, int id) {
+  MemberValue m{-INFINITY, a.teacher_lse != nullptr ? a.teacher_lse[r] : 0.0f};
+  if (id >= 0) {
     const int64_t at = r * a.K + lane;
-    e.id = a.idx[at];
-    if ((uint32_t)e.id >= (uint32_t)a.V) {
-      if (e.id != -1) report_error(a.err, VSD_DEVERR_TOKEN_RANGE);
-      e.id = -1;
-    } else {
-      v = (a.val_bf16 ? load1(static_cast<const bf16_t*>(a.val) + at) : static_cast<const float*>(a.val)[at]) * a.inv_tp;
-    }
+    m.v = (a.val_bf16 ? load1(static_cast<const bf16_t*>(a.val) + at) : static_cast<const float*>(a.val)[at]) * a.inv_tp;
   }
-  const float top = wave_max(v);
-  const bool in = e.id >= 0 && v != -INFINITY;
+  return m;
+}
+__device__ __forceinline__ Member member_of(const LossArgs& a, int id, const MemberValue& m) {
+  Member e{id, 0.0f, 0.0f};
+  const bool in = id >= 0 && m.v != -INFINITY;
   float lp;
   if (a.teacher_lse != nullptr) {
-    lp = v - a.teacher_lse[r];
+    lp = m.v - m.lse;
   } else {
-    const float sum = wave_sum(in ? expf(v - top) : 0.0f);
-    lp = (v - top) - logf(sum);
+    const float top = wave_max(m.v);
+    const float sum = wave_sum(in ? expf(m.v - top) : 0.0f);
+    lp = (m.v - top) - logf(sum);
   }
   if (in) {
     e.p = expf(lp);

@@ -126,7 +126,8 @@ def _call_words(dev, stream):
     try:
         return _words[dev.index, stream].pop()
     except (KeyError, IndexError):
-        made = list(torch.zeros(256, 2, dtype=torch.int32, device=dev).narrow(1, 0, 1).unbind(0))
+        with torch.inference_mode(False):
+            made = list(torch.zeros(256, 2, dtype=torch.int32, device=dev).narrow(1, 0, 1).unbind(0))
         mine = made.pop()
         _words[dev.index, stream] = made
         return mine

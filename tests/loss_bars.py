@@ -47,8 +47,7 @@ def loss_bar(o, x, idx, p, m, V, T, runs=0, dx=0.0):
 
 
 def grad_bar(o, x, idx, p, m, V, T, k, kind, runs=0, dx=0.0):
-    """|gradient error| per element; k [R] = |scale w / T|.  (LM head, runs > 0: the
-    exponent is x c - m c in one rounding, with m c rounded before.)"""
+    """|gradient error| per element; k [R] = |scale w / T|."""
     a = np.minimum(np.abs((x - m[:, None]) / T) / math.log(2), 300)
     q = o["q"] * p.sum(1, keepdims=True)
     with np.errstate(divide="ignore"):
@@ -59,6 +58,6 @@ def grad_bar(o, x, idx, p, m, V, T, k, kind, runs=0, dx=0.0):
         np.add.at(mem[r], idx[r][on], p[r][on] * (lp_err[r][on] + 64 * U))
     mass_err = np.sum(p * lp_err, axis=1, keepdims=True)
     with np.errstate(invalid="ignore"):
-        soft = np.where(q > 0, q * (sum_rel(V, runs) + (2 * U * np.abs(m / T)[:, None] if runs else 0.0) + 3 * U * a * math.log(2) + 10 * U + 2 * dx), 0.0)
+        soft = np.where(q > 0, q * (sum_rel(V, runs) + 3 * U * a * math.log(2) + 10 * U + 2 * dx), 0.0)
     err = k[:, None] * (soft + o["q"] * mass_err + mem)
     return err * 1.01 + HALF[kind] * (np.abs(o["grad"]) + err) + TINY

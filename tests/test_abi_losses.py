@@ -71,7 +71,7 @@ def test_bad_sources(lib, call):
     assert call(lib, src=HEAD) == 6                       # a head needs hidden_dim
 
 
-@pytest.mark.parametrize("temp", (0.0, -1.0, float("inf"), float("nan"), 1e-45))
+@pytest.mark.parametrize("temp", (0.0, -1.0, float("inf"), float("nan"), 1e-45, 1e31))
 def test_bad_temperatures(lib, temp):
     assert _ce(lib, temp=temp) == 3 and _top(lib, temp=temp) == 3
     assert _kd(lib, temps=(temp, 1.0)) == 3 and _kd(lib, temps=(1.0, temp)) == 3
@@ -133,13 +133,15 @@ def test_workspaces(lib):
 @pytest.mark.parametrize("R,v,H", ((1, 1, 64), (6144, 128256, 4096), (70000, 9000, 64), (1 << 20, 50000, 1024),
                                    (48, 32000, 4096), (300, 257, 65536)))
 def test_workspace_is_bounded_by_its_parts(lib, R, v, H):
-    """Never the logits of a large batch: at most about 1 GiB of their gradient,
-    the hidden states, the fp32 sums and small per-row records."""
+    """Never the logits of a large batch: about 1 GiB of their gradient at most, the hidden
+    states, the products' fp32 partial sums (32 ranges or 2560 and 512 tiles of 256 x 256) and
+    small per-row records."""
     got = vsd.loss_workspace_bytes(R, v, H, 16, True)
-    pad = (R + 63) // 64 * 64
-    ranges = max(1, 256 // (-(-R // 256) * -(-H // 256)))
-    assert got <= max(1 << 30, pad * 2 * 1024) + pad * 256 * 2 + R * H * (2 + 4 * ranges) + 64 * H * 2 \
-        + R * (16 * 12 + 64 + 16 * (-(-v // 256))) + 16 * 256
+    pad, tiles = (R + 63) // 64 * 64, -(-v // 256)
+    g = max(1 << 30, pad * 2 * 1024) + pad * 2 * (256 + 128)
+    dh = 4 * min(32 * R * H, max(2560 << 16, R * H))
+    parts = 16 * max(R, min(1024 * 256, R * tiles), R * -(-v // 64) if R <= 128 else 0)
+    assert got <= g + dh + 4 * (512 << 16) + pad * H * 2 + parts + R * (16 * 12 + 64) + 16 * 256
 
 
 def test_binding_refuses_host_tensors():
