@@ -593,9 +593,9 @@ vsd_status vsd_distill_loss(const vsd_rows* rows, const vsd_src* draft, int32_t 
                             void* hip_stream);
 
 /* The k largest logits of each row: top_idx and top_logits [R, k], lse [R]
- * (optional).  Materialised logits only.  `workspace` must hold
- * vsd_top_workspace_bytes(rows, k, d2t != NULL) bytes (16-B aligned; 0 for many
- * rows without a map). */
+ * (optional).  Materialised logits only.  With a map, `workspace` must
+ * hold vsd_top_workspace_bytes(rows, 1) bytes (16-B aligned); without one it may
+ * be NULL. */
 vsd_status vsd_top_logits(const vsd_rows* rows, const vsd_src* target, int32_t k, const int32_t* d2t,
                           int32_t v_draft, float temp_target, int32_t* top_idx, float* top_logits,
                           float* lse, void* workspace, size_t workspace_bytes, int32_t* device_error,
@@ -603,7 +603,7 @@ vsd_status vsd_top_logits(const vsd_rows* rows, const vsd_src* target, int32_t k
 
 /* Bytes of workspace the calls above need (host only). */
 vsd_status vsd_loss_workspace_bytes(const vsd_rows* rows, int32_t k, int32_t with_grad, size_t* bytes);
-vsd_status vsd_top_workspace_bytes(const vsd_rows* rows, int32_t k, int32_t with_map, size_t* bytes);
+vsd_status vsd_top_workspace_bytes(const vsd_rows* rows, int32_t with_map, size_t* bytes);
 
 const char* vsd_status_string(vsd_status status); /* static string */
 const char* vsd_last_error(void);                 /* thread-local detail */

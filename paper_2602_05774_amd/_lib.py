@@ -133,7 +133,7 @@ def load():
     lib.vsd_top_logits.restype = c_i32
     lib.vsd_loss_workspace_bytes.argtypes = [P(VsdRows), c_i32, c_i32, P(ctypes.c_size_t)]
     lib.vsd_loss_workspace_bytes.restype = c_i32
-    lib.vsd_top_workspace_bytes.argtypes = [P(VsdRows), c_i32, c_i32, P(ctypes.c_size_t)]
+    lib.vsd_top_workspace_bytes.argtypes = [P(VsdRows), c_i32, P(ctypes.c_size_t)]
     lib.vsd_top_workspace_bytes.restype = c_i32
     lib.vsd_status_string.argtypes = [c_i32]
     lib.vsd_status_string.restype = ctypes.c_char_p

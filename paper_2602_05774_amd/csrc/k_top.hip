@@ -8,8 +8,9 @@
 // entry's place is the number of entries that beat it.  Order: the larger value
 // first, equal values by the smaller index.  A row with more groups or entries
 // at the bound than the lists hold (long runs of equal logits) gets its K-th
-// entry by bisection instead.  Few long rows are split into segments, a workgroup
-// each, whose results a second launch joins.
+// entry by bisection instead.  (Few long rows in segments of at least 4096 columns, a
+// workgroup each, and a second launch that joined them: 24 rows of 128 256 in 23.5
+// instead of 25.4 us, 24 rows of 32 000 in 22.1 instead of 18.0: not kept.)
 #include "vsd_device.hpp"
 #include "vsd_kernels.hpp"
 #include "vsd_loss.hpp"
@@ -19,8 +20,8 @@ namespace vsd {
 namespace {
 
 constexpr int kU = 4;  // loads of 8 columns in flight per thread
-// LDS lists.  Rows of at most 2048 columns (one wavefront, one group a thread)
-// have short ones, so that eight of their wavefronts fit a SIMD.
+// LDS lists.  Short rows (one wavefront, one group a thread) have short ones, so
+// that eight of their wavefronts fit a SIMD.
 template <int kThreads>
 struct Lists {
   static constexpr bool kShort = kThreads == kWave;
@@ -28,8 +29,15 @@ struct Lists {
   static constexpr int kGroupCap = kShort ? 64 : 1024; // listed groups
   static constexpr int kCap = kShort ? 512 : 2048;     // listed entries
 };
-constexpr int kShortCols = kWave * 8 * kU;
-constexpr int kRoundsK = 16;  // members up to which the bound comes from rounds of wavefront maxima
+// Rows for one wavefront: with more members the K-th of its 64 maxima is far below
+// the row's (us, one wavefront / four: 65 536 x 1000 K = 10 83 / 248, K = 32
+// 113 / 399, K = 64 686 / 485; 8192 x 4000 K = 16 33 / 45, K = 32 40 / 65;
+// 8192 x 8000 K = 16 50 / 48; 16 384 x 32 000 367 / 195).
+constexpr int kShortCols = 4096, kShortK = 32;
+// Members up to which four wavefronts' bound comes from rounds of wavefront maxima
+// instead of a count over all threads' (us, rounds / count: 8192 x 4000, K = 16,
+// 46.5 / 62.1; 8192 x 32 000 108 / 115; one wavefront, 65 536 x 1000, K = 10, 93 / 86).
+constexpr int kRoundsK = 16;
 // maxima that each of W wavefronts contributes to it: together more than K
 __host__ __device__ constexpr int maxima_of(int K, int W) { return (K + W - 1) / W + 1; }
 
@@ -94,13 +102,12 @@ __global__ __launch_bounds__(kThreads) void k_top_logits(TopArgs a) {
   __shared__ int ngroups, count;
   uint64_t* const keys = reinterpret_cast<uint64_t*>(shared);
   const int lane = threadIdx.x & 63, wave = wave_id();
-  const int64_t r = blockIdx.x / (unsigned)a.segs;
-  const int seg = blockIdx.x % (unsigned)a.segs, from = seg * a.seg_cols;  // columns are counted from `from`
-  const int V = min(a.V - from, a.seg_cols);
-  const T* Y = static_cast<const T*>(a.Y) + r * a.ld + from;
+  const int64_t r = blockIdx.x;
+  const int V = a.V;
+  const T* Y = static_cast<const T*>(a.Y) + r * a.ld;
   const int first = threadIdx.x * 8;
-  auto index_of = [&](int col) { return MAP ? a.inv[from + col] : from + col; };
-  auto mask_of = [&](int base) { return MAP ? (uint32_t)a.mapped[(from + base) >> 3] : 0xFFu; };
+  auto index_of = [&](int col) { return MAP ? a.inv[col] : col; };
+  auto mask_of = [&](int base) { return MAP ? (uint32_t)a.mapped[base >> 3] : 0xFFu; };
   // every entry of eight columns that may be a member (above -inf, its column mapped), by f(value, column)
   auto entries = [&](int base, auto&& f) {
     if (base >= V) return;
@@ -161,7 +168,7 @@ __global__ __launch_bounds__(kThreads) void k_top_logits(TopArgs a) {
   // over all of them), or of some per wavefront that has columns.  Equal maxima
   // are told apart by the low byte, which gives way to the thread: the bound is
   // at most that much lower (not at all for bf16 logits).
-  const bool rounds = a.K <= kRoundsK;
+  const bool rounds = kWaves > 1 && a.K <= kRoundsK;
   const int per = rounds ? maxima_of(a.K, min(kWaves, (V + kWave * 8 - 1) / (kWave * 8))) : kWave;
   static_assert(maxima_of(kRoundsK, 1) <= kWave && kThreads <= 256, "a wavefront has that many, a byte names a thread");
   uint32_t left = (order_of(best) & ~0xFFu) | threadIdx.x;
@@ -203,12 +210,7 @@ __global__ __launch_bounds__(kThreads) void k_top_logits(TopArgs a) {
     s = red_s[0];
 #pragma unroll
     for (int k = 1; k < kWaves; ++k) lse_join(m, s, red_m[k], red_s[k], a.c);
-    if (lane == 0) {
-      if (a.segs > 1)
-        a.plse[blockIdx.x] = make_float2(m, s);
-      else if (a.lse != nullptr)
-        a.lse[r] = s == 0.0f ? -INFINITY : m * a.inv_t + logf(s);
-    }
+    if (lane == 0 && a.lse != nullptr) a.lse[r] = s == 0.0f ? -INFINITY : m * a.inv_t + logf(s);
   }
   __syncthreads();
   const float least = bound;
@@ -266,8 +268,8 @@ __global__ __launch_bounds__(kThreads) void k_top_logits(TopArgs a) {
   }
   if (threadIdx.x == 0 && (n & 1) != 0) keys[n] = 0;  // (kCap is even)
   __syncthreads();
-  int32_t* const idx = (a.segs > 1 ? a.pidx : a.idx) + (int64_t)blockIdx.x * a.K;
-  float* const val = (a.segs > 1 ? a.pval : a.val) + (int64_t)blockIdx.x * a.K;
+  int32_t* const idx = a.idx + r * a.K;
+  float* const val = a.val + r * a.K;
   for (int i = threadIdx.x; i < n; i += kThreads) {
     const uint64_t key = keys[i];
     const int rank = rank_of(key, keys, (n + 1) & ~1);
@@ -282,52 +284,6 @@ __global__ __launch_bounds__(kThreads) void k_top_logits(TopArgs a) {
   }
 }
 
-// A row's K largest from its segments' lists (each in order): an entry's place is
-// its place in its own list and, by bisection, the entries of the others that
-// beat it (all lists at once, so that the steps' reads do not wait for each other).
-constexpr int kJoinThreads = 1024;
-__global__ __launch_bounds__(kJoinThreads) void k_top_join(TopArgs a) {
-  __shared__ uint64_t keys[kTopSegs * kMaxMembers], out[kMaxMembers];
-  static_assert(kTopSegs * kMaxMembers <= kJoinThreads, "an entry per thread");
-  const int64_t r = blockIdx.x;
-  const int K = a.K, n = a.segs * K, i = threadIdx.x;
-  if (wave_id() == kJoinThreads / kWave - 1 && a.lse != nullptr) {
-    const int lane = i & 63;
-    const float2 p = lane < a.segs ? a.plse[r * a.segs + lane] : make_float2(kNegBig, 0.0f);
-    float m = p.x, s = p.y;
-    wave_lse(m, s, a.c);
-    if (lane == 0) a.lse[r] = s == 0.0f ? -INFINITY : m * a.inv_t + logf(s);
-  }
-  if (i < n) {
-    const int id = a.pidx[r * n + i];
-    keys[i] = id < 0 ? 0 : key_of(a.pval[r * n + i], id);
-  }
-  if (i < K) out[i] = 0;
-  __syncthreads();
-  if (i < n && keys[i] != 0) {
-    const uint64_t key = keys[i];
-    int lo[kTopSegs];  // entries before it beat this one
-#pragma unroll
-    for (int g = 0; g < kTopSegs; ++g) lo[g] = 0;
-    for (int step = kMaxMembers; step > 0; step /= 2) {
-#pragma unroll
-      for (int g = 0; g < kTopSegs; ++g) {
-        const int at = lo[g] + step;
-        if (g < a.segs && at <= K && keys[g * K + at - 1] > key) lo[g] = at;
-      }
-    }
-    int rank = 0;
-#pragma unroll
-    for (int g = 0; g < kTopSegs; ++g) rank += lo[g];
-    if (rank < K) out[rank] = key;
-  }
-  __syncthreads();
-  if (i < K) {
-    a.idx[r * K + i] = out[i] != 0 ? index_in(out[i]) : -1;
-    a.val[r * K + i] = out[i] != 0 ? value_in(out[i]) : -INFINITY;
-  }
-}
-
 __global__ __launch_bounds__(256) void k_top_bits(const int32_t* inv, int V, uint8_t* mapped) {
   const int b = blockIdx.x * 256 + threadIdx.x;
   if (b >= (V + 7) / 8) return;
@@ -339,20 +295,17 @@ __global__ __launch_bounds__(256) void k_top_bits(const int32_t* inv, int V, uin
 
 template <typename T, int kThreads>
 hipError_t launch_n(const TopArgs& a, hipStream_t s) {
-  const dim3 grid((unsigned)(a.R * a.segs));
+  const dim3 grid((unsigned)a.R);
   if (a.inv != nullptr)
     hipLaunchKernelGGL((k_top_logits<T, true, kThreads>), grid, dim3(kThreads), 0, s, a);
   else
     hipLaunchKernelGGL((k_top_logits<T, false, kThreads>), grid, dim3(kThreads), 0, s, a);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess || a.segs == 1) return e;
-  hipLaunchKernelGGL(k_top_join, dim3((unsigned)a.R), dim3(kJoinThreads), 0, s, a);
   return hipGetLastError();
 }
 
 template <typename T>
 hipError_t launch_t(const TopArgs& a, hipStream_t s) {
-  if (a.V <= kShortCols && a.K <= kRoundsK) return launch_n<T, kWave>(a, s);
+  if (a.V <= kShortCols && a.K <= kShortK) return launch_n<T, kWave>(a, s);
   return launch_n<T, 256>(a, s);
 }
 

@@ -686,31 +686,12 @@ vsd_status base_loss(const vsd_rows* rows, const vsd_src* src, int32_t K, const 
 }
 
 struct TopLayout {
-  size_t inv, mapped, pidx, pval, plse, total;
-  int32_t segs;
+  size_t inv, mapped, total;
 };
-// The inverse map and its bits (with a map), then the segments' results (rows in
-// more than one).
-TopLayout top_layout(const vsd_rows* rows, int32_t k, bool map) {
+TopLayout top_layout(const vsd_rows* rows) {
   TopLayout w{};
-  size_t at = 0;
-  auto take = [&](size_t bytes) {
-    const size_t here = at;
-    at += align_up(bytes);
-    return here;
-  };
-  if (map) {
-    w.inv = take((size_t)rows->v * sizeof(int32_t));
-    w.mapped = take(((size_t)rows->v + 7) / 8);
-  }
-  w.segs = vsd::top_segs(rows->R, rows->v);
-  if (w.segs > 1) {
-    const size_t n = (size_t)rows->R * w.segs;
-    w.pidx = take(n * k * sizeof(int32_t));
-    w.pval = take(n * k * sizeof(float));
-    w.plse = take(n * sizeof(float2));
-  }
-  w.total = at;
+  w.mapped = w.inv + align_up((size_t)rows->v * sizeof(int32_t));
+  w.total = w.mapped + align_up(((size_t)rows->v + 7) / 8);
   return w;
 }
 
@@ -1274,25 +1255,13 @@ vsd_status vsd_top_logits(const vsd_rows* rows, const vsd_src* target, int32_t k
     if (v_draft < 1 || v_draft > rows->v)
       return fail(VSD_ERR_INVALID_SHAPE, "v_draft=%d outside [1,%d]", v_draft, rows->v);
     if (!aligned16(d2t)) return fail(VSD_ERR_MISALIGNED, "d2t pointer not 16-byte aligned");
-  }
-  const TopLayout w = top_layout(rows, k, d2t != nullptr);
-  if (w.total > 0) {
+    const TopLayout w = top_layout(rows);
     if (workspace == nullptr || workspace_bytes < w.total)
       return fail(VSD_ERR_WORKSPACE, "workspace of %zu bytes required, %zu given", w.total,
                   workspace == nullptr ? (size_t)0 : workspace_bytes);
     if (!aligned16(workspace)) return fail(VSD_ERR_MISALIGNED, "workspace not 16-byte aligned");
-  }
-  char* ws = static_cast<char*>(workspace);
-  a.segs = w.segs;
-  a.seg_cols = ((rows->v + w.segs - 1) / w.segs + 7) / 8 * 8;  // (the last one's columns: at least 4096 - 8 w.segs)
-  if (w.segs > 1) {
-    a.pidx = reinterpret_cast<int32_t*>(ws + w.pidx);
-    a.pval = reinterpret_cast<float*>(ws + w.pval);
-    a.plse = reinterpret_cast<float2*>(ws + w.plse);
-  }
-  if (d2t != nullptr) {
-    int32_t* inv = reinterpret_cast<int32_t*>(ws + w.inv);
-    uint8_t* mapped = reinterpret_cast<uint8_t*>(ws + w.mapped);
+    int32_t* inv = reinterpret_cast<int32_t*>(static_cast<char*>(workspace) + w.inv);
+    uint8_t* mapped = reinterpret_cast<uint8_t*>(static_cast<char*>(workspace) + w.mapped);
     e = vsd::launch_lm_inv(d2t, v_draft, rows->v, inv, device_error, nullptr, 0, s);
     if (e != hipSuccess) return hip_fail(e, "k_lm_inv launch");
     e = vsd::launch_top_bits(inv, rows->v, mapped, s);
@@ -1315,12 +1284,11 @@ vsd_status vsd_top_logits(const vsd_rows* rows, const vsd_src* target, int32_t k
   return ok();
 }
 
-vsd_status vsd_top_workspace_bytes(const vsd_rows* rows, int32_t k, int32_t with_map, size_t* bytes) {
+vsd_status vsd_top_workspace_bytes(const vsd_rows* rows, int32_t with_map, size_t* bytes) {
   vsd_status st = check_rows_struct(rows);
   if (st != VSD_OK) return st;
-  if (k < 1 || k > VSD_MAX_TOP) return fail(VSD_ERR_INVALID_VALUE, "k=%d outside [1,%d]", k, VSD_MAX_TOP);
   if (bytes == nullptr) return fail(VSD_ERR_NULL_POINTER, "bytes is NULL");
-  *bytes = top_layout(rows, k, with_map != 0).total;
+  *bytes = with_map != 0 ? top_layout(rows).total : 0;
   return ok();
 }
 

@@ -482,8 +482,10 @@ constexpr int64_t kTotalRows = 64;
 //            float32  16 384 x 8000     512 x 2  201    256 x 4   226   128 x 8  245
 //                      8192 x 32 000   1024 x 4  410    512 x 8   422   read twice 593
 //                      2048 x 128 256  1024 x 8 and the rest twice 478, all twice 640
-//   loss only, bf16     512 x 128 256  1024      36     256        43
-//                      1024 x 128 256  1024      52     256        57
+//   loss only, bf16      48 x 128 256  1024      21.1   256        23.1
+//                       256 x 128 256  1024      25.9   256        27.1
+//                       512 x 128 256  1024      36.0   256        33.3
+//                      1024 x 32 000   1024      31.6   256        25.3
 //                     65 536 x 2000      64      80     256       130
 struct RowThreads {
   int threads, chunks;  // chunks: groups of eight columns that a thread keeps
@@ -492,7 +494,7 @@ struct RowThreads {
 constexpr int64_t kMaxWideRows = ((int64_t)1 << 22) - 1;
 inline RowThreads row_loss_threads(int64_t R, int V, bool wide, bool grad) {
   if (V <= 2048) return {64, grad ? 4 : 0, !grad};
-  if (!grad) return {R <= 512 && V > 8192 ? 1024 : 256, 0, true};
+  if (!grad) return {R <= 256 && V > 65536 ? 1024 : 256, 0, true};
   if (V <= 4096) return wide ? RowThreads{256, 2, false} : RowThreads{128, 4, false};
   if (R > kMaxWideRows) return {256, 0, true};
   if (V <= 8192) return wide ? RowThreads{512, 2, false} : RowThreads{256, 4, false};
@@ -514,20 +516,7 @@ struct TopArgs {
   int32_t* idx;                // [R, K]
   float* val;                  // [R, K]
   float* lse;                  // [R] or null
-  // few rows: a row's columns in `segs` segments of `seg_cols` (a multiple of 8),
-  // whose results a second launch joins
-  int32_t segs, seg_cols;
-  int32_t* pidx;               // [R, segs, K]
-  float* pval;                 // [R, segs, K]
-  float2* plse;                // [R, segs]
 };
-// Segments of a row: four workgroups per CU, of at least 4096 columns each.
-constexpr int kTopSegs = 16;
-inline int top_segs(int64_t R, int V) {
-  int64_t n = 1024 / R;
-  n = n > V / 4096 ? V / 4096 : n;
-  return (int)(n < 1 ? 1 : n > kTopSegs ? kTopSegs : n);
-}
 
 // The same losses through an LM head.
 constexpr int kLmLossPad = 64;  // rows in play are padded to whole stages of the products

@@ -89,15 +89,11 @@ def _query_loss(R, v, hidden_dim, k, grad):
     return n.value
 
 
-def top_workspace_bytes(R, v, k, with_map=True):
-    """Workspace bytes of top_logits over R rows of v logits."""
-    return _query_top(R, v, k, bool(with_map))
-
-
 @functools.lru_cache(maxsize=256)
-def _query_top(R, v, k, with_map):
-    rows, n = _lib.VsdRows(R, v, v, VSD_BF16, 0), ctypes.c_size_t(0)
-    _lib.check(_lib.load().vsd_top_workspace_bytes(ctypes.byref(rows), k, int(with_map), ctypes.byref(n)))
+def top_workspace_bytes(v):
+    """Workspace bytes of top_logits over rows of v logits with a map (none without)."""
+    rows, n = _lib.VsdRows(1, v, v, VSD_BF16, 0), ctypes.c_size_t(0)
+    _lib.check(_lib.load().vsd_top_workspace_bytes(ctypes.byref(rows), 1, ctypes.byref(n)))
     return n.value
 
 
@@ -289,7 +285,7 @@ def top_logits(Y, k, d2t=None, temp_target=1.0, workspace=None, device_error=Non
         stream = _stream(dev)
         err = _call_words(dev, stream) if device_error is None else device_error
         _check("device_error", err, torch.int32, (1,), dev)
-        need = _query_top(R, rows.v, k, d2t is not None)
+        need = top_workspace_bytes(rows.v) if d2t is not None else 0
         ws = _workspace(need, workspace, dev)
         _lib.check(lib.vsd_top_logits(ctypes.byref(rows), ctypes.byref(src), k, _ptr(d2t),
                                       0 if d2t is None else d2t.numel(), temp_target, idx.data_ptr(), val.data_ptr(),
