@@ -1662,9 +1662,12 @@ hipError_t launch_lm_loss(LmLossArgs a, bool weight_bf16, hipStream_t s) {
     a.plan = nullptr;
   } else {
     a.cols = a.l.V < a.piece ? a.l.V : a.piece;
-    hipLaunchKernelGGL(k_lm_loss_list, dim3((unsigned)((R + kListRows - 1) / kListRows)), dim3(kListRows), 0, s, a);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
-    hipLaunchKernelGGL(k_lm_loss_pack, dim3((unsigned)((R + kLmLossPad + 3) / 4)), dim3(256), 0, s, a);
+    if (R > kListRows) {
+      hipLaunchKernelGGL(k_lm_loss_list, dim3((unsigned)((R + kListRows - 1) / kListRows)), dim3(kListRows), 0, s, a);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+    hipLaunchKernelGGL(R > kListRows ? k_lm_loss_pack<false> : k_lm_loss_pack<true>,
+                       dim3((unsigned)((R + kLmLossPad + 3) / 4)), dim3(256), 0, s, a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
   if (few)
@@ -1678,7 +1681,8 @@ hipError_t launch_lm_loss(LmLossArgs a, bool weight_bf16, hipStream_t s) {
   else
     hipLaunchKernelGGL(distill ? k_lm_loss_combine<true> : k_lm_loss_combine<false>, by_row, dim3(256), 0, s, a);
   if ((e = hipGetLastError()) != hipSuccess) return e;
-  if (a.dh == nullptr) return hipSuccess;
+  const bool total = a.l.total != nullptr && a.l.counter == nullptr;
+  if (a.dh == nullptr) return total ? launch_row_total(a.l, s) : hipSuccess;
   for (int64_t c0 = 0; c0 < a.l.V; c0 += a.piece) {
     a.c0 = (int32_t)c0;
     a.cols = (int32_t)(a.l.V - c0 < a.piece ? a.l.V - c0 : a.piece);
@@ -1702,17 +1706,16 @@ hipError_t launch_lm_loss(LmLossArgs a, bool weight_bf16, hipStream_t s) {
     else
       hipLaunchKernelGGL(k_lm_loss_grads<float>, grid, dim3(kThreads), 0, s, a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
-    if (a.wacc != nullptr) {
-      const dim3 by_eight((unsigned)(((int64_t)a.cols * a.H / 8 + 255) / 256));
-      if (weight_bf16)
-        hipLaunchKernelGGL(k_lm_loss_dw_out<bf16_t>, by_eight, dim3(256), 0, s, a);
-      else
-        hipLaunchKernelGGL(k_lm_loss_dw_out<float>, by_eight, dim3(256), 0, s, a);
+    const bool last = c0 + a.piece >= a.l.V;
+    a.out_dh = last ? (int32_t)((R * a.H / 8 + 255) / 256) : 0;
+    a.out_dw = a.wacc != nullptr ? (int32_t)(((int64_t)a.cols * a.H / 8 + 255) / 256) : 0;
+    const dim3 rest((unsigned)(a.out_dh + a.out_dw + (last && total ? 1 : 0)));
+    if (rest.x > 0) {
+      hipLaunchKernelGGL(weight_bf16 ? k_lm_loss_out<bf16_t> : k_lm_loss_out<float>, rest, dim3(256), 0, s, a);
       if ((e = hipGetLastError()) != hipSuccess) return e;
     }
   }
-  hipLaunchKernelGGL(k_lm_loss_dh_out, dim3((unsigned)((R * a.H / 8 + 255) / 256)), dim3(256), 0, s, a);
-  return hipGetLastError();
+  return hipSuccess;
 }
 
 }  // namespace vsd

@@ -259,13 +259,17 @@ hipError_t launch_d(const LossArgs& a, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_row_loss(const LossArgs& a, bool bf16, hipStream_t s) {
-  if (a.val != nullptr) return bf16 ? launch_d<bf16_t, true>(a, s) : launch_d<float, true>(a, s);
-  return bf16 ? launch_d<bf16_t, false>(a, s) : launch_d<float, false>(a, s);
+  hipError_t e;
+  if (a.val != nullptr)
+    e = bf16 ? launch_d<bf16_t, true>(a, s) : launch_d<float, true>(a, s);
+  else
+    e = bf16 ? launch_d<bf16_t, false>(a, s) : launch_d<float, false>(a, s);
+  if (e != hipSuccess || a.total == nullptr || a.counter != nullptr) return e;
+  return launch_row_total(a, s);
 }
 
-hipError_t launch_row_total(const float* loss, const float* weight, int64_t R, float scale, float* total,
-                            hipStream_t s) {
-  hipLaunchKernelGGL(k_row_total, dim3(1), dim3(kTotalThreads), 0, s, loss, weight, R, scale, total);
+hipError_t launch_row_total(const LossArgs& a, hipStream_t s) {
+  hipLaunchKernelGGL(k_row_total, dim3(1), dim3(kTotalThreads), 0, s, a.loss, a.weight, a.R, a.scale, a.total);
   return hipGetLastError();
 }
 

@@ -623,6 +623,8 @@ vsd_status base_loss(const vsd_rows* rows, const vsd_src* src, int32_t K, const 
   a.loss = out->loss_row;
   a.lse = out->lse;
   a.err = out->device_error;
+  a.total = out->loss_total;
+  a.counter = rows->R <= vsd::kTotalRows ? out->counter : nullptr;
   hipError_t e;
   if (rows->hidden_dim == 0) {
     a.X = src->logits;
@@ -630,10 +632,6 @@ vsd_status base_loss(const vsd_rows* rows, const vsd_src* src, int32_t K, const 
     if (grad != nullptr) {
       a.G = grad->grad_logits;
       a.ldg = grad->ld;
-    }
-    if (out->loss_total != nullptr && out->counter != nullptr && rows->R <= vsd::kTotalRows) {
-      a.total = out->loss_total;
-      a.counter = out->counter;
     }
     e = vsd::launch_row_loss(a, rows->dtype == VSD_BF16, s);
     if (e != hipSuccess) return hip_fail(e, "k_row_loss launch");
@@ -645,10 +643,6 @@ vsd_status base_loss(const vsd_rows* rows, const vsd_src* src, int32_t K, const 
     if (!aligned16(workspace)) return fail(VSD_ERR_MISALIGNED, "workspace not 16-byte aligned");
     char* ws = static_cast<char*>(workspace);
     vsd::LmLossArgs b{};
-    if (out->loss_total != nullptr && out->counter != nullptr && rows->R <= vsd::kTotalRows) {
-      a.total = out->loss_total;
-      a.counter = out->counter;
-    }
     b.l = a;
     b.h = src->hidden;
     b.w = src->weight;
@@ -677,10 +671,6 @@ vsd_status base_loss(const vsd_rows* rows, const vsd_src* src, int32_t K, const 
     }
     e = vsd::launch_lm_loss(b, grad != nullptr && grad->weight_dtype == VSD_BF16, s);
     if (e != hipSuccess) return hip_fail(e, "fused loss launch");
-  }
-  if (out->loss_total != nullptr && a.total == nullptr) {
-    e = vsd::launch_row_total(out->loss_row, weight, rows->R, scale, out->loss_total, s);
-    if (e != hipSuccess) return hip_fail(e, "k_row_total launch");
   }
   return ok();
 }

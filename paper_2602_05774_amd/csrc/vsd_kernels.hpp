@@ -456,8 +456,9 @@ struct LossArgs {
   float* loss;                 // [R]
   float* lse;                  // [R] or null
   int32_t* err;
-  float* total;                // [1], or null: formed by launch_row_total
-  int32_t* counter;            // [1] zero (with total): workgroups that are done
+  float* total;                // [1], or null
+  int32_t* counter;            // [1] zero: workgroups that are done; null: the total by a launch
+                               // of its own or beside other work
 };
 // Rows up to which the last workgroup of the row kernel forms the total.  Each
 // workgroup then ends with an atomic add on one word (about 35 ns one after the
@@ -558,6 +559,7 @@ struct LmLossArgs {
   bf16_store* g;             // [lm_loss_pad(R), ldg] the piece's gradient
   float* acc;                // [splits, rows in play, H] sums of dh
   float* wacc;               // [dw_splits, cols, H] sums of dW, or null: one range
+  int32_t out_dh, out_dw;    // workgroups of the closing launch for dh and dW (then one for the total)
 };
 
 // Most workgroups of a launch that walk runs of tiles (or one per row tile), of
@@ -603,8 +605,7 @@ inline int64_t lm_loss_sums(int64_t R, int H) {
 
 hipError_t launch_lm_loss(LmLossArgs a, bool weight_bf16, hipStream_t s);
 hipError_t launch_row_loss(const LossArgs& a, bool bf16, hipStream_t s);
-hipError_t launch_row_total(const float* loss, const float* weight, int64_t R, float scale, float* total,
-                            hipStream_t s);
+hipError_t launch_row_total(const LossArgs& a, hipStream_t s);
 hipError_t launch_top_bits(const int32_t* inv, int V, uint8_t* mapped, hipStream_t s);
 hipError_t launch_top_logits(const TopArgs& a, bool bf16, hipStream_t s);
 

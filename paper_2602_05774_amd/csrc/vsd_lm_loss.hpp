@@ -65,57 +65,17 @@ __device__ int plan_splits(int64_t tiles, int stages, float beside, int limit, i
   return at;
 }
 
-// at[r] = row r's place among the rows in play, or -1; the number of those
-// rows and their plan.  Every workgroup counts the rows before its own 1024.
-constexpr int kListRows = 1024;
-__global__ __launch_bounds__(kListRows) void k_lm_loss_list(LmLossArgs a) {
-  __shared__ int red[kListRows / kWave];
-  const int lane = threadIdx.x & 63, wave = wave_id();
-  auto in_play = [&](int64_t r) {
-    const int32_t t = a.tag[r];
-    if ((uint32_t)t >= (uint32_t)a.l.V) {
-      if (t != -1) report_error(a.l.err, VSD_DEVERR_TOKEN_RANGE);
-      return false;
-    }
-    return row_weight(a.l, r) != 0.0f;
-  };
-  const int64_t first = (int64_t)blockIdx.x * kListRows, r = first + threadIdx.x;
-  int before = 0;
-  for (int64_t k = threadIdx.x; k < first; k += kListRows) before += in_play(k) ? 1 : 0;
-  before = wave_sum_int(before);
-  if (lane == 0) red[wave] = before;
-  __syncthreads();
-  int place = 0;
-  for (int k = 0; k < kListRows / kWave; ++k) place += red[k];
-  __syncthreads();
-  const bool in = r < a.l.R && in_play(r);
-  const uint64_t has = __ballot(in);
-  if (lane == 0) red[wave] = __builtin_popcountll(has);
-  __syncthreads();
-  int total = place;
-  for (int k = 0; k < kListRows / kWave; ++k) {
-    if (k < wave) place += red[k];
-    total += red[k];
-  }
-  place += (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(has >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)has, 0u));
-  if (r < a.l.R) {
-    a.at[r] = in ? place : -1;
-    if (in) a.rows[place] = (int32_t)r;
-    if (!in) {
-      a.l.loss[r] = 0.0f;
-      if (a.l.lse != nullptr) a.l.lse[r] = 0.0f;
-    }
-  }
-  if (wave != 0 || blockIdx.x != gridDim.x - 1) return;
-  LmLossPlan p{total, 0, 0, 0, 0, 1, 0, 1};
-  if (total > 0) {
-    const int nrt = (total + TM - 1) / TM, tiles = (a.l.V + TN - 1) / TN, stages = a.H / TK;
+// The plan of n rows in play, by one wavefront.
+__device__ void make_plan(const LmLossArgs& a, int n, int lane) {
+  LmLossPlan p{n, 0, 0, 0, 0, 1, 0, 1};
+  if (n > 0) {
+    const int nrt = (n + TM - 1) / TM, tiles = (a.l.V + TN - 1) / TN, stages = a.H / TK;
     p.fwd_run = plan_runs(nrt, tiles, stages, lane);
     p.fwd_runs = (tiles + p.fwd_run - 1) / p.fwd_run;
     if (a.dh != nullptr) {
       const int ct = (a.cols + TN - 1) / TN, ht = (a.H + TN - 1) / TN, deep = (a.cols + TK - 1) / TK;
       p.g_run = plan_runs(nrt, ct, stages, lane);
-      const int wdeep = (total + TK - 1) / TK;  // (whole stages: the rows are padded)
+      const int wdeep = (n + TK - 1) / TK;  // (whole stages: the rows are padded)
       const float dh = (float)nrt * ht * ((float)deep + kRunCost);
       const float dw = a.dw != nullptr ? (float)ct * ht * ((float)wdeep + kRunCost) : 0.0f;
       const int splits = plan_splits((int64_t)nrt * ht, deep, dw, kLmLossDh, lane);
@@ -130,16 +90,99 @@ __global__ __launch_bounds__(kListRows) void k_lm_loss_list(LmLossArgs a) {
   }
   if (lane == 0) *a.plan = p;
 }
+__device__ __forceinline__ bool in_play(const LmLossArgs& a, int64_t r) {
+  const int32_t t = a.tag[r];
+  if ((uint32_t)t >= (uint32_t)a.l.V) {
+    if (t != -1) report_error(a.l.err, VSD_DEVERR_TOKEN_RANGE);
+    return false;
+  }
+  return row_weight(a.l, r) != 0.0f;
+}
+__device__ __forceinline__ void out_of_play(const LmLossArgs& a, int64_t r) {
+  a.l.loss[r] = 0.0f;
+  if (a.l.lse != nullptr) a.l.lse[r] = 0.0f;
+}
 
-// The hidden states of the rows in play, consecutively; zero rows behind them;
-// a zero gradient for the other rows.  One wavefront per row.
+// at[r] = row r's place among the rows in play, or -1; the rows in play and their
+// plan.  Every workgroup counts the rows before its own 1024.
+constexpr int kListRows = 1024;
+__global__ __launch_bounds__(kListRows) void k_lm_loss_list(LmLossArgs a) {
+  __shared__ int red[kListRows / kWave];
+  const int lane = threadIdx.x & 63, wave = wave_id();
+  const int64_t first = (int64_t)blockIdx.x * kListRows, r = first + threadIdx.x;
+  int before = 0;
+  for (int64_t k = threadIdx.x; k < first; k += kListRows) before += in_play(a, k) ? 1 : 0;
+  before = wave_sum_int(before);
+  if (lane == 0) red[wave] = before;
+  __syncthreads();
+  int place = 0;
+  for (int k = 0; k < kListRows / kWave; ++k) place += red[k];
+  __syncthreads();
+  const bool in = r < a.l.R && in_play(a, r);
+  const uint64_t has = __ballot(in);
+  if (lane == 0) red[wave] = __builtin_popcountll(has);
+  __syncthreads();
+  int total = place;
+  for (int k = 0; k < kListRows / kWave; ++k) {
+    if (k < wave) place += red[k];
+    total += red[k];
+  }
+  place += (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(has >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)has, 0u));
+  if (r < a.l.R) {
+    a.at[r] = in ? place : -1;
+    if (in)
+      a.rows[place] = (int32_t)r;
+    else
+      out_of_play(a, r);
+  }
+  if (wave == 0 && blockIdx.x == gridDim.x - 1) make_plan(a, total, lane);
+}
+
+// The hidden states of the rows in play, consecutively; zero rows behind them; a
+// zero gradient for the other rows.  One wavefront per row.  LIST (at most 1024
+// rows): every workgroup finds the rows in play itself, and the first one writes
+// what the list would.
+template <bool LIST>
 __global__ __launch_bounds__(256) void k_lm_loss_pack(LmLossArgs a) {
-  const int lane = threadIdx.x & 63;
-  const int64_t r = (int64_t)blockIdx.x * 4 + wave_id();
+  __shared__ uint64_t in[LIST ? kListRows / kWave : 1];
+  const int lane = threadIdx.x & 63, wave = wave_id();
+  const int64_t r = (int64_t)blockIdx.x * 4 + wave;
+  auto place_of = [&](int k, int& n) {  // row k's place or -1, the rows in play
+    int place = 0;
+    n = 0;
+    for (int w = 0; w < kListRows / kWave; ++w) {
+      const int c = __builtin_popcountll(in[w]);
+      place += w < k / kWave ? c : 0;
+      n += c;
+    }
+    if (k >= kListRows) return -1;
+    const uint64_t mine = in[k / kWave], bit = 1ull << (k % kWave);
+    return (mine & bit) != 0 ? place + __builtin_popcountll(mine & (bit - 1)) : -1;
+  };
+  if (LIST) {
+    for (int k = threadIdx.x; k < kListRows; k += 256) {
+      const uint64_t has = __ballot(k < a.l.R && in_play(a, k));
+      if (lane == 0) in[k / kWave] = has;
+    }
+    __syncthreads();
+    if (blockIdx.x == 0) {
+      int n;
+      for (int k = threadIdx.x; k < (int)a.l.R; k += 256) {
+        const int place = place_of(k, n);
+        if (place >= 0)
+          a.rows[place] = k;
+        else
+          out_of_play(a, k);
+      }
+      place_of(0, n);
+      if (wave == 0) make_plan(a, n, lane);
+    }
+  }
+  int n = 0;
   const uint4* from = nullptr;
   uint4* to;
   if (r < a.l.R) {
-    const int32_t place = a.at[r];
+    const int32_t place = LIST ? place_of((int)r, n) : a.at[r];
     if (place >= 0) {
       from = reinterpret_cast<const uint4*>(static_cast<const bf16_t*>(a.h) + r * a.H);
       to = reinterpret_cast<uint4*>(a.hp + (int64_t)place * a.H);
@@ -148,7 +191,11 @@ __global__ __launch_bounds__(256) void k_lm_loss_pack(LmLossArgs a) {
       to = reinterpret_cast<uint4*>(static_cast<bf16_t*>(a.dh) + r * a.H);
     }
   } else {
-    const int64_t n = a.plan->n, place = n + (r - a.l.R);
+    if (LIST)
+      place_of(0, n);
+    else
+      n = a.plan->n;
+    const int64_t place = n + (r - a.l.R);
     if (place >= lm_loss_pad(n)) return;
     to = reinterpret_cast<uint4*>(a.hp + place * a.H);
   }
@@ -400,7 +447,7 @@ __global__ __launch_bounds__(256) void k_lm_loss_combine(LmLossArgs a) {
     }
     lm_loss_finish<DISTILL>(a, i, r, m, s, x);
   }
-  if (a.l.total == nullptr) return;
+  if (a.l.counter == nullptr) return;
   __syncthreads();
   total_by_last<256>(a.l);
 }
@@ -431,23 +478,27 @@ __global__ __launch_bounds__(FewCombine<DISTILL>::kThreads) void k_lm_loss_few_c
   if (in) {
     const int parts = 2 * lm_few_groups(a.l.V);
     const float2* part = a.part + i * parts;
+    const bf16_t* h = a.plan != nullptr ? a.hp + i * a.H : static_cast<const bf16_t*>(a.h) + r * a.H;
+    const bf16_t* W = static_cast<const bf16_t*>(a.w);
+    // the cross entropy's first wavefront has the label's logit meanwhile
+    constexpr int kFirst = DISTILL ? 0 : 1, kSumming = kThreads - kFirst * kWave;
     float m = kNegBig, s = 0.0f;
-    constexpr int U = 8;  // in flight per thread
-    for (int e0 = threadIdx.x; e0 < parts; e0 += U * kThreads) {
-      float2 p[U];
+    if (wave >= kFirst) {
+      constexpr int U = 8;  // in flight per thread
+      for (int e0 = threadIdx.x - kFirst * kWave; e0 < parts; e0 += U * kSumming) {
+        float2 p[U];
 #pragma unroll
-      for (int u = 0; u < U; ++u)
-        p[u] = e0 + u * kThreads < parts ? part[e0 + u * kThreads] : make_float2(kNegBig, 0.0f);
+        for (int u = 0; u < U; ++u)
+          p[u] = e0 + u * kSumming < parts ? part[e0 + u * kSumming] : make_float2(kNegBig, 0.0f);
 #pragma unroll
-      for (int u = 0; u < U; ++u) lse_join(m, s, p[u].x, p[u].y, a.l.c);
+        for (int u = 0; u < U; ++u) lse_join(m, s, p[u].x, p[u].y, a.l.c);
+      }
+      wave_lse(m, s, a.l.c);
     }
-    wave_lse(m, s, a.l.c);
     if (lane == 0) {
       red_m[wave] = m;
       red_s[wave] = s;
     }
-    const bf16_t* h = a.plan != nullptr ? a.hp + i * a.H : static_cast<const bf16_t*>(a.h) + r * a.H;
-    const bf16_t* W = static_cast<const bf16_t*>(a.w);
     if (DISTILL) {
       for (int k = wave; k < a.l.K; k += kWaves) {
         const int v = __builtin_amdgcn_readfirstlane(a.mid[r * a.l.K + k]);
@@ -543,7 +594,7 @@ __global__ __launch_bounds__(256) void k_lm_loss_fix(LmLossArgs a) {
 // dh of a piece: 256 x 256 tiles of g W, the piece's columns in `splits` ranges
 // of `per`.  One piece and one range write the rounded result; otherwise
 // acc[range] holds the fp32 sums, which the last piece (one range) or
-// k_lm_loss_dh_out turns into the result.
+// k_lm_loss_out turns into the result.
 __device__ __forceinline__ void lm_loss_dh(const LmLossArgs& a, bf16_t* lds, int pid, int nrt) {
   const int lane = threadIdx.x & 63, w = wave_id();
   const int64_t n = a.plan->n;
@@ -591,7 +642,7 @@ __device__ __forceinline__ void lm_loss_dh(const LmLossArgs& a, bf16_t* lds, int
 
 // dW of a piece: 256 x 256 tiles of g^T h over the rows in play (whole stages:
 // the rows behind them are zeros in both operands), the rows in `dw_splits` ranges
-// where the tiles are few: their fp32 sums then go to wacc and k_lm_loss_dw_out
+// where the tiles are few: their fp32 sums then go to wacc and k_lm_loss_out
 // adds them.
 template <typename T>
 __device__ __forceinline__ void lm_loss_dw(const LmLossArgs& a, bf16_t* lds, int pid) {
@@ -656,36 +707,32 @@ __global__ __launch_bounds__(kThreads, 1) void k_lm_loss_grads(LmLossArgs a) {
   }
 }
 
-// The ranges' sums of dh, eight columns per thread.
-__global__ __launch_bounds__(256) void k_lm_loss_dh_out(LmLossArgs a) {
-  const int splits = a.plan->splits;
-  const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8, all = (int64_t)a.plan->n * a.H;
-  if (splits == 1 || at >= all) return;
-  float v[8];
-  load8(a.acc + at, v);
-#pragma unroll 4
-  for (int z = 1; z < splits; ++z) {
-    float o[8];
-    load8(a.acc + z * all + at, o);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] += o[j];
-  }
-  store8(static_cast<bf16_t*>(a.dh) + (int64_t)a.rows[at / a.H] * a.H + at % a.H, v);
-}
-
+// What is left after the products, eight columns per thread: the ranges' sums of dh
+// (out_dh workgroups), those of a piece's dW (out_dw; T: its type), the total.
 template <typename T>
-__global__ __launch_bounds__(256) void k_lm_loss_dw_out(LmLossArgs a) {
-  const int splits = a.plan->dw_splits;
-  const int64_t at = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 8, all = (int64_t)a.cols * a.H;
+__global__ __launch_bounds__(256) void k_lm_loss_out(LmLossArgs a) {
+  const int64_t b = blockIdx.x;
+  if (b >= a.out_dh + a.out_dw) {
+    row_total<256>(a.l.loss, a.l.weight, a.l.R, a.l.scale, a.l.total);
+    return;
+  }
+  const bool dh = b < a.out_dh;
+  const int splits = dh ? a.plan->splits : a.plan->dw_splits;
+  const int64_t at = ((b - (dh ? 0 : a.out_dh)) * 256 + threadIdx.x) * 8;
+  const int64_t all = (dh ? (int64_t)a.plan->n : (int64_t)a.cols) * a.H;
   if (splits == 1 || at >= all) return;
+  const float* sums = dh ? a.acc : a.wacc;
   float v[8];
-  load8(a.wacc + at, v);
+  load8(sums + at, v);
 #pragma unroll 4
   for (int z = 1; z < splits; ++z) {
     float o[8];
-    load8(a.wacc + z * all + at, o);
+    load8(sums + z * all + at, o);
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] += o[j];
   }
-  store8(static_cast<T*>(a.dw) + (int64_t)a.c0 * a.H + at, v);
+  if (dh)
+    store8(static_cast<bf16_t*>(a.dh) + (int64_t)a.rows[at / a.H] * a.H + at % a.H, v);
+  else
+    store8(static_cast<T*>(a.dw) + (int64_t)a.c0 * a.H + at, v);
 }

@@ -190,7 +190,7 @@ __device__ __forceinline__ void row_total(const float* loss, const float* weight
 // follows such stores).
 template <int kThreads>
 __device__ __forceinline__ void total_by_last(const LossArgs& a) {
-  if (a.total == nullptr) return;
+  if (a.total == nullptr || a.counter == nullptr) return;
   __shared__ int last;
   if (threadIdx.x == 0)
     last = __hip_atomic_fetch_add(a.counter, 1, __ATOMIC_ACQ_REL, __HIP_MEMORY_SCOPE_AGENT) == (int)gridDim.x - 1;
