@@ -1681,8 +1681,13 @@ hipError_t launch_lm_loss(LmLossArgs a, bool weight_bf16, hipStream_t s) {
   else
     hipLaunchKernelGGL(distill ? k_lm_loss_combine<true> : k_lm_loss_combine<false>, by_row, dim3(256), 0, s, a);
   if ((e = hipGetLastError()) != hipSuccess) return e;
-  const bool total = a.l.total != nullptr && a.l.counter == nullptr;
-  if (a.dh == nullptr) return total ? launch_row_total(a.l, s) : hipSuccess;
+  // the total of many rows wants more threads than the closing launch has
+  bool total = a.l.total != nullptr && a.l.counter == nullptr;
+  if (total && (a.dh == nullptr || R > kListRows)) {
+    if ((e = launch_row_total(a.l, s)) != hipSuccess) return e;
+    total = false;
+  }
+  if (a.dh == nullptr) return hipSuccess;
   for (int64_t c0 = 0; c0 < a.l.V; c0 += a.piece) {
     a.c0 = (int32_t)c0;
     a.cols = (int32_t)(a.l.V - c0 < a.piece ? a.l.V - c0 : a.piece);

@@ -88,24 +88,34 @@ __device__ __forceinline__ void row_loss(const LossArgs& a) {
       }
     }
     if constexpr (kMore) {  // what does not fit the registers
-      constexpr int U = 4;  // loads in flight per lane
-      int base = first + kNch * kStep;
-      for (; base + (U - 1) * kStep + 8 <= a.V; base += U * kStep) {
-        Raw8<T> q[U];
+      constexpr int U = 4;  // loads of a step; the next one's are in flight
+      Raw8<T> q[2][U];
+      const int from = kNch * kStep, whole = (a.V - from) / (U * kStep);
+      auto load = [&](Raw8<T>(&c)[U], int it) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) q[u].load(X + base + u * kStep);
+        for (int u = 0; u < U; ++u) c[u].load(X + from + first + (it * U + u) * kStep);
+      };
+      auto take = [&](const Raw8<T>(&c)[U]) {
 #pragma unroll
         for (int u = 0; u < U; ++u) {
           float x[8];
-          q[u].get(x);
+          c[u].get(x);
           lse_add8(x, m, s, a.c);
         }
+      };
+      if (whole > 0) load(q[0], 0);
+      for (int it = 0; it < whole; it += 2) {  // (no load depends on a branch)
+        load(q[1], min(it + 1, whole - 1));
+        take(q[0]);
+        if (it + 1 == whole) break;
+        load(q[0], min(it + 2, whole - 1));
+        take(q[1]);
       }
-      for (; base < a.V; base += kStep) {
-        Raw8<T> q;
+      for (int base = from + whole * U * kStep + first; base < a.V; base += kStep) {
+        Raw8<T> c;
         float x[8];
-        load_cols(q, X, base, a.V);
-        q.get(x);
+        load_cols(c, X, base, a.V);
+        c.get(x);
         lse_add8(x, m, s, a.c);
       }
     }

@@ -124,42 +124,63 @@ __global__ __launch_bounds__(kThreads) void k_top_logits(TopArgs a) {
     for (int base = first; base < V; base += kStep) entries(base, f);
   };
 
-  // the sweep: kU * kStep columns an iteration, `per_group` iterations a group
-  const int iters = (V + kU * kStep - 1) / (kU * kStep);
+  // the sweep: kU * kStep columns an iteration, the next one's loads in flight
+  // (whole iterations: no load depends on a branch), `per_group` iterations a group
+  const int iters = (V + kU * kStep - 1) / (kU * kStep), whole = V / (kU * kStep);
   const int per_group = (iters + kGroups - 1) / kGroups;
-  float m = kNegBig, s = 0.0f, best = -INFINITY;
-  for (int g = 0, it = 0; it < iters; ++g) {
-    float top = -INFINITY;
-    for (int j = 0; j < per_group && it < iters; ++j, ++it) {
-      const int base = first + it * kU * kStep;
-      Raw8<T> q[kU];
-      uint32_t in[kU];
-      if ((it + 1) * kU * kStep <= V) {
+  float m = kNegBig, s = 0.0f, best = -INFINITY, top = -INFINITY;
+  int group = 0, in_group = 0;
+  struct Cols {
+    Raw8<T> q[kU];
+    uint32_t in[kU];
+  } cols[2];
+  auto load = [&](Cols& c, int it) {
+    const int base = first + it * kU * kStep;
 #pragma unroll
-        for (int u = 0; u < kU; ++u) {
-          q[u].load(Y + base + u * kStep);
-          if (MAP) in[u] = mask_of(base + u * kStep);
-        }
-      } else {
-#pragma unroll
-        for (int u = 0; u < kU; ++u) {
-          load_cols(q[u], Y, base + u * kStep, V);
-          if (MAP) in[u] = base + u * kStep < V ? mask_of(base + u * kStep) : 0u;
-        }
-      }
-#pragma unroll
-      for (int u = 0; u < kU; ++u) {
-        float x[8];
-        q[u].get(x);
-        lse_add8(x, m, s, a.c);
-        if (MAP) {
-#pragma unroll
-          for (int k = 0; k < 8; ++k) x[k] = ((in[u] >> k) & 1u) != 0u ? x[k] : -INFINITY;
-        }
-        top = fmaxf(top, max8(x));
-      }
+    for (int u = 0; u < kU; ++u) {
+      c.q[u].load(Y + base + u * kStep);
+      if (MAP) c.in[u] = mask_of(base + u * kStep);
     }
-    shared[g * kThreads + threadIdx.x] = top;
+  };
+  auto take = [&](const Cols& c) {
+#pragma unroll
+    for (int u = 0; u < kU; ++u) {
+      float x[8];
+      c.q[u].get(x);
+      lse_add8(x, m, s, a.c);
+      if (MAP) {
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[k] = ((c.in[u] >> k) & 1u) != 0u ? x[k] : -INFINITY;
+      }
+      top = fmaxf(top, max8(x));
+    }
+    if (++in_group == per_group) {
+      shared[group * kThreads + threadIdx.x] = top;
+      best = fmaxf(best, top);
+      top = -INFINITY;
+      in_group = 0;
+      ++group;
+    }
+  };
+  if (whole > 0) load(cols[0], 0);
+  for (int it = 0; it < whole; it += 2) {
+    load(cols[1], min(it + 1, whole - 1));
+    take(cols[0]);
+    if (it + 1 == whole) break;
+    load(cols[0], min(it + 2, whole - 1));
+    take(cols[1]);
+  }
+  if (whole < iters) {
+    const int base = first + whole * kU * kStep;
+#pragma unroll
+    for (int u = 0; u < kU; ++u) {
+      load_cols(cols[0].q[u], Y, base + u * kStep, V);
+      cols[0].in[u] = MAP && base + u * kStep < V ? mask_of(base + u * kStep) : 0u;
+    }
+    take(cols[0]);
+  }
+  if (in_group > 0) {
+    shared[group * kThreads + threadIdx.x] = top;
     best = fmaxf(best, top);
   }
   const int used = (iters + per_group - 1) / per_group;
