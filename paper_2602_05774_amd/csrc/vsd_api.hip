@@ -503,8 +503,10 @@ vsd_status check_rows_struct(const vsd_rows* rows) {
     if (rows->dtype != VSD_BF16) return fail(VSD_ERR_UNSUPPORTED, "the fused LM head takes bf16 operands only");
     const int64_t nrt = (rows->R + vsd::kLmTile - 1) / vsd::kLmTile;
     const int64_t nht = (H + vsd::kLmTile - 1) / vsd::kLmTile, vt = ((int64_t)rows->v + vsd::kLmTile - 1) / vsd::kLmTile;
-    if (nrt * std::max(nht, vt) >= kMaxLmWorkgroups || nht * vt >= kMaxLmWorkgroups ||
-        rows->R * H >= ((int64_t)1 << 35))  // (a work-item per eight of them)
+    // 512 work-items a tile of logits, or of both gradients (and their ranges) in one
+    // launch; 256 for 64 columns; one for eight elements of dh
+    if (nrt * vt >= kMaxLmWorkgroups || nht * (nrt + vt) + vsd::kLmLossDh + vsd::kLmLossDw >= kMaxLmWorkgroups ||
+        rows->v > kMaxVocab / 2 || rows->R * H >= ((int64_t)1 << 34))
       return fail(VSD_ERR_INVALID_SHAPE, "fused LM head: R=%lld rows x v=%d x hidden_dim=%d too large",
                   (long long)rows->R, rows->v, H);
   }
@@ -570,7 +572,7 @@ vsd_status check_loss_out(const vsd_loss_out* out) {
   return VSD_OK;
 }
 
-vsd_status check_loss_grad(const vsd_rows* rows, const vsd_loss_grad* grad) {
+vsd_status check_loss_grad(const vsd_rows* rows, const vsd_src* src, const vsd_loss_grad* grad) {
   if (grad == nullptr) return VSD_OK;
   if (rows->hidden_dim > 0) {
     if (grad->grad_logits != nullptr)
@@ -578,6 +580,8 @@ vsd_status check_loss_grad(const vsd_rows* rows, const vsd_loss_grad* grad) {
     if (grad->grad_hidden == nullptr) return fail(VSD_ERR_NULL_POINTER, "fused: grad->grad_hidden is NULL");
     if (!aligned16(grad->grad_hidden)) return fail(VSD_ERR_MISALIGNED, "grad_hidden not 16-byte aligned");
     if (grad->grad_weight != nullptr) {
+      if (grad->grad_weight == src->weight)
+        return fail(VSD_ERR_INVALID_VALUE, "grad_weight must not be the weight");
       if (!aligned16(grad->grad_weight)) return fail(VSD_ERR_MISALIGNED, "grad_weight not 16-byte aligned");
       if (grad->weight_dtype != VSD_F32 && grad->weight_dtype != VSD_BF16)
         return fail(VSD_ERR_INVALID_VALUE, "weight_dtype=%d", grad->weight_dtype);
@@ -589,6 +593,8 @@ vsd_status check_loss_grad(const vsd_rows* rows, const vsd_loss_grad* grad) {
   if (grad->grad_logits == nullptr) return fail(VSD_ERR_NULL_POINTER, "grad->grad_logits is NULL");
   const int64_t es = rows->dtype == VSD_F32 ? 4 : 2;
   if (grad->ld < rows->v) return fail(VSD_ERR_INVALID_SHAPE, "grad ld=%lld < v=%d", (long long)grad->ld, rows->v);
+  if (grad->grad_logits == src->logits && grad->ld != rows->ld)
+    return fail(VSD_ERR_INVALID_VALUE, "a gradient in the logits' place has their row stride");
   if (!aligned16(grad->grad_logits) || (grad->ld * es) % 16 != 0)
     return fail(VSD_ERR_MISALIGNED, "grad_logits or its row stride not a multiple of 16 bytes");
   return VSD_OK;
@@ -606,7 +612,7 @@ vsd_status base_loss(const vsd_rows* rows, const vsd_src* src, int32_t K, const 
     return fail(VSD_ERR_INVALID_VALUE, "temperatures must lie in [1e-30, 1e30]");
   if (!std::isfinite(scale)) return fail(VSD_ERR_INVALID_VALUE, "loss_scale must be finite");
   if ((st = check_loss_out(out)) != VSD_OK) return st;
-  if ((st = check_loss_grad(rows, grad)) != VSD_OK) return st;
+  if ((st = check_loss_grad(rows, src, grad)) != VSD_OK) return st;
   vsd::LossArgs a{};
   a.R = rows->R;
   a.V = rows->v;

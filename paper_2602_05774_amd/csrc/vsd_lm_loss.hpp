@@ -390,10 +390,9 @@ __global__ __launch_bounds__(kFewThreads, 2) void k_lm_loss_few_g(LmLossArgs a) 
                       });
 }
 
-// The runs joined, the members' logits (dot products), the loss, and what the
-// gradient needs: g_v = kq exp2((x_v - m) c) - k p_v.  One wavefront per row.
-// What a row's loss and gradient are made of, by all lanes of a wavefront: (m, s)
-// and the logit of a lane's member (cross entropy: every lane the label's).
+// A row's loss and what its gradient needs, g_v = kq exp2((x_v - m) c) - k p_v, by
+// all lanes of a wavefront from (m, s) and the logit of a lane's member (cross
+// entropy: every lane the label's).
 template <bool DISTILL>
 __device__ __forceinline__ void lm_loss_finish(const LmLossArgs& a, int64_t i, int64_t r, float m, float s, float x) {
   const int lane = threadIdx.x & 63;
@@ -419,6 +418,7 @@ __device__ __forceinline__ void lm_loss_finish(const LmLossArgs& a, int64_t i, i
   }
 }
 
+// The runs joined and the members' logits (dot products).  One wavefront per row.
 template <bool DISTILL>
 __global__ __launch_bounds__(256) void k_lm_loss_combine(LmLossArgs a) {
   const int lane = threadIdx.x & 63;

@@ -29,8 +29,7 @@ def _head(**kw):
 
 LOGITS, HEAD = _lib.VsdSrc(FAKE, None, None), _lib.VsdSrc(None, FAKE, FAKE)
 OUT = _lib.VsdLossOut(FAKE, FAKE, FAKE, FAKE)
-GRAD = _lib.VsdLossGrad(FAKE, 1000, None, None, 0)
-HGRAD = _lib.VsdLossGrad(None, 0, FAKE, FAKE, 0)
+HGRAD = _lib.VsdLossGrad(None, 0, FAKE, FAKE + 16, 0)
 
 
 def _ref(x):
@@ -85,14 +84,17 @@ def test_bad_outputs_and_gradients(lib):
         assert call(lib, grad=_lib.VsdLossGrad(None, 1000, None, None, 0)) == 1
         assert call(lib, grad=_lib.VsdLossGrad(FAKE + 4, 1000, None, None, 0)) == 4
         assert call(lib, grad=_lib.VsdLossGrad(FAKE, 999, None, None, 0)) == 2
-        assert call(lib, grad=_lib.VsdLossGrad(FAKE, 1002, None, None, 0)) == 4
+        assert call(lib, grad=_lib.VsdLossGrad(FAKE + 16, 1002, None, None, 0)) == 4
         assert call(lib, grad=_lib.VsdLossGrad(FAKE, 1000, FAKE, None, 0)) == 6
-        hg = lambda **kw: _lib.VsdLossGrad(**{**dict(grad_hidden=FAKE, grad_weight=FAKE), **kw})  # noqa: E731
+        hg = lambda **kw: _lib.VsdLossGrad(**{**dict(grad_hidden=FAKE, grad_weight=FAKE + 16), **kw})  # noqa: E731
+        # in the logits' place: their stride, the check of which comes before the alignment's
+        assert call(lib, grad=_lib.VsdLossGrad(FAKE, 1002, None, None, 0)) == 3
         head = dict(rows=_head(), src=HEAD, ws=FAKE, n=1 << 40)
         assert call(lib, **head, grad=hg(grad_hidden=None)) == 1
         assert call(lib, **head, grad=hg(grad_hidden=FAKE + 8)) == 4
         assert call(lib, **head, grad=hg(grad_weight=FAKE + 8)) == 4
         assert call(lib, **head, grad=hg(weight_dtype=2)) == 3
+        assert call(lib, **head, grad=hg(grad_weight=FAKE)) == 3    # the weight itself
         assert call(lib, **head, grad=hg(grad_logits=FAKE)) == 6
     assert _ce(lib, labels=None) == 1
     assert _ce(lib, scale=float("inf")) == 3
@@ -137,6 +139,12 @@ def test_workspace_is_bounded_by_its_parts(lib, R, v, H):
     dh = 4 * min(32 * R * H, max(2560 << 16, R * H))
     parts = 16 * max(R, min(1024 * 256, R * tiles), R * -(-v // 64) if R <= 128 else 0)
     assert got <= g + dh + 4 * (512 << 16) + pad * H * 2 + parts + R * (16 * 12 + 64) + 16 * 256
+
+
+@pytest.mark.parametrize("kw", (dict(R=(1 << 24) - 1, v=1 << 20), dict(v=(1 << 29) + 1, hidden_dim=64),
+                                dict(R=1 << 23, v=8, hidden_dim=4096), dict(R=1 << 20, v=1 << 26, hidden_dim=64)))
+def test_fused_launches_stay_within_32_bits(lib, kw):
+    assert _ce(lib, rows=_head(**kw), src=HEAD, ws=FAKE, n=1 << 50) == 2
 
 
 def test_binding_refuses_host_tensors():
