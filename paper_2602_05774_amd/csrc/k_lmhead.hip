@@ -1648,7 +1648,8 @@ hipError_t launch_lm_loss(LmLossArgs a, bool weight_bf16, hipStream_t s) {
     const int64_t all = nrt * lm_tiles(V), most = nrt > kLmLossRuns ? nrt : kLmLossRuns;
     return dim3((unsigned)(all < most ? all : most));
   };
-  const bool few = lm_few(R);
+  const bool few = lm_few(R, a.l.V), by_workgroup = few || (distill && R <= kLmFewMost);
+  const unsigned few_rows = (unsigned)((R + kLmFewRows - 1) / kLmFewRows);
   const auto few_fwd = R <= 32 ? k_lm_loss_few<1> : R <= 64 ? k_lm_loss_few<2> : k_lm_loss_few<4>;
   const auto few_g =
       distill ? (R <= 32 ? k_lm_loss_few_g<1, true> : R <= 64 ? k_lm_loss_few_g<2, true> : k_lm_loss_few_g<4, true>)
@@ -1671,13 +1672,13 @@ hipError_t launch_lm_loss(LmLossArgs a, bool weight_bf16, hipStream_t s) {
     if ((e = hipGetLastError()) != hipSuccess) return e;
   }
   if (few)
-    hipLaunchKernelGGL(few_fwd, dim3((unsigned)lm_few_groups(a.l.V)), dim3(kFewThreads), 0, s, a);
+    hipLaunchKernelGGL(few_fwd, dim3((unsigned)lm_few_groups(a.l.V), few_rows), dim3(kFewThreads), 0, s, a);
   else
     hipLaunchKernelGGL(k_lm_loss_fwd, runs(a.l.V), dim3(kThreads), 0, s, a);
   if ((e = hipGetLastError()) != hipSuccess) return e;
-  if (few)
-    hipLaunchKernelGGL(distill ? k_lm_loss_few_combine<true> : k_lm_loss_few_combine<false>, dim3((unsigned)R),
-                       dim3(distill ? FewCombine<true>::kThreads : FewCombine<false>::kThreads), 0, s, a);
+  if (by_workgroup)
+    hipLaunchKernelGGL(distill ? k_lm_loss_row_combine<true> : k_lm_loss_row_combine<false>, dim3((unsigned)R),
+                       dim3(distill ? RowCombine<true>::kThreads : RowCombine<false>::kThreads), 0, s, a);
   else
     hipLaunchKernelGGL(distill ? k_lm_loss_combine<true> : k_lm_loss_combine<false>, by_row, dim3(256), 0, s, a);
   if ((e = hipGetLastError()) != hipSuccess) return e;
@@ -1692,7 +1693,8 @@ hipError_t launch_lm_loss(LmLossArgs a, bool weight_bf16, hipStream_t s) {
     a.c0 = (int32_t)c0;
     a.cols = (int32_t)(a.l.V - c0 < a.piece ? a.l.V - c0 : a.piece);
     if (few)
-      hipLaunchKernelGGL(few_g, dim3((unsigned)(lm_tiles(a.cols) * (kLmTile / kLmFewCols))), dim3(kFewThreads), 0, s, a);
+      hipLaunchKernelGGL(few_g, dim3((unsigned)(lm_tiles(a.cols) * (kLmTile / kLmFewCols)), few_rows),
+                         dim3(kFewThreads), 0, s, a);
     else
       hipLaunchKernelGGL(distill ? k_lm_loss_g<true> : k_lm_loss_g<false>, runs(a.cols), dim3(kThreads), 0, s, a);
     if ((e = hipGetLastError()) != hipSuccess) return e;

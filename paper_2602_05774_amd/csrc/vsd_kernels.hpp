@@ -579,13 +579,21 @@ inline int32_t lm_loss_piece(int64_t R, int V) {
 // Row stride of its gradient: not a power of two, whose rows would share their
 // memory channels.
 inline int32_t lm_loss_ldg(int32_t piece) { return piece + 128; }
-// Few rows: a product whose tiles are 64 columns of W and all rows.
-constexpr int kLmFewRows = 128, kLmFewCols = 64;
-__host__ __device__ constexpr bool lm_few(int64_t R) { return R <= kLmFewRows; }
+// Few rows: a product whose tiles are 64 columns of W and up to 128 rows.  For up to
+// 128 rows, whose time is that of reading W, and for up to 1024 as long as these
+// tiles are at most two per CU: 256 x 256 tiles would leave most CUs idle.  Loss and
+// both gradients with those and with these: 132 rows of 512 x 3456, 54 members, 303
+// and 117 us; 256 of 8000 x 4096, 234 and 143; 1000 of 2000 x 1024, 137 and 109;
+// the loss alone of 256 of 16 000 x 4096 (two per CU), 97.8 and 62.6.
+constexpr int kLmFewRows = 128, kLmFewCols = 64, kLmFewMost = 1024;
 __host__ __device__ constexpr int lm_few_groups(int V) { return (V + kLmFewCols - 1) / kLmFewCols; }
+__host__ __device__ constexpr bool lm_few(int64_t R, int V) {
+  return R <= kLmFewRows ||
+         (R <= kLmFewMost && (R + kLmFewRows - 1) / kLmFewRows * lm_few_groups(V) <= 2 * kLmCus);
+}
 // Entries of the forward's log-sum-exps: two per run and row in play.
 inline int64_t lm_loss_parts(int64_t R, int V) {
-  if (lm_few(R)) return 2 * R * lm_few_groups(V);
+  if (lm_few(R, V)) return 2 * R * lm_few_groups(V);
   const int64_t all = R * lm_tiles(V), runs = (int64_t)kLmLossRuns * kLmTile;
   return 2 * (all < runs ? all : runs > R ? runs : R);
 }

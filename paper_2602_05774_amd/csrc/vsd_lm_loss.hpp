@@ -235,7 +235,7 @@ __global__ __launch_bounds__(kThreads, 1) void k_lm_loss_fwd(LmLossArgs a) {
   if (i < n) a.part[((int64_t)run * 2 + (wave_id() >> 2)) * n + i] = make_float2(m, s);
 }
 
-// Few rows (at most 32 kG): the products x = h W^T of 64 columns with every row.
+// Few rows: the products x = h W^T of 64 columns with 32 kG rows.
 // Four wavefronts, each with 32 of the columns and half of a stage's depth (64).
 // Bound by the stream of W: stages of W (8 KB) and of the rows (4 KB kG, from L2)
 // are loaded straight into a ring in LDS, as nt_stream does (eight consecutive
@@ -337,13 +337,15 @@ __device__ __forceinline__ void lm_few_products(const bf16_t* h, int n, const bf
   }
 }
 
+// (blockIdx.y: 32 kG rows; more than one of them only with kG = 4)
 template <int kG>
 __global__ __launch_bounds__(kFewThreads, 2) void k_lm_loss_few(LmLossArgs a) {
   __shared__ __align__(16) bf16_t lds[Few<kG>::kLds];
-  const int lane = threadIdx.x & 63, n = a.plan != nullptr ? a.plan->n : (int)a.l.R;
-  if (n == 0) return;
-  lm_few_products<kG>(a.plan != nullptr ? a.hp : static_cast<const bf16_t*>(a.h), n, static_cast<const bf16_t*>(a.w),
-                      a.l.V, a.H, lds, [&](int g, int c, float (&x)[16]) {
+  const int lane = threadIdx.x & 63, n = a.plan != nullptr ? a.plan->n : (int)a.l.R, row0 = blockIdx.y * 32 * kG;
+  if (row0 >= n) return;
+  const bf16_t* h = a.plan != nullptr ? a.hp : static_cast<const bf16_t*>(a.h);
+  lm_few_products<kG>(h + (int64_t)row0 * a.H, min(n - row0, 32 * kG), static_cast<const bf16_t*>(a.w), a.l.V, a.H, lds,
+                      [&](int g, int c, float (&x)[16]) {
                         float m = kNegBig, s = 0.0f;
 #pragma unroll
                         for (int e = 0; e < 16; ++e) {
@@ -353,22 +355,23 @@ __global__ __launch_bounds__(kFewThreads, 2) void k_lm_loss_few(LmLossArgs a) {
 #pragma unroll
                         for (int e = 0; e < 16; ++e) s += lse_term(x[e], m, a.l.c);
                         lse_join(m, s, __shfl_xor(m, 32), __shfl_xor(s, 32), a.l.c);
-                        const int i = g * 32 + lane;
+                        const int i = row0 + g * 32 + lane;
                         if (lane < 32 && i < n)
                           a.part[(int64_t)i * 2 * lm_few_groups(a.l.V) + blockIdx.x * 2 + wave_id()] = make_float2(m, s);
                       });
 }
 
 // The same products for g of a piece.
-static_assert(kLmLossPad <= 64, "one row group's rows and as many behind them");
+static_assert(kLmLossPad <= 64 && kLmFewRows % kLmLossPad == 0, "the padding of 32 rows is 32 more, of 128 none");
 template <int kG, bool DISTILL>
 __global__ __launch_bounds__(kFewThreads, 2) void k_lm_loss_few_g(LmLossArgs a) {
   __shared__ __align__(16) bf16_t lds[Few<kG>::kLds];
-  const int lane = threadIdx.x & 63, n = a.plan->n, pad = (int)lm_loss_pad(n);
-  if (n == 0) return;
-  lm_few_products<kG>(a.hp, n, static_cast<const bf16_t*>(a.w) + (int64_t)a.c0 * a.H, a.cols, a.H, lds,
+  const int lane = threadIdx.x & 63, n = a.plan->n, pad = (int)lm_loss_pad(n), row0 = blockIdx.y * 32 * kG;
+  if (row0 >= n) return;
+  lm_few_products<kG>(a.hp + (int64_t)row0 * a.H, min(n - row0, 32 * kG),
+                      static_cast<const bf16_t*>(a.w) + (int64_t)a.c0 * a.H, a.cols, a.H, lds,
                       [&](int g, int c, float (&x)[16]) {
-                        const int i = g * 32 + (lane & 31);
+                        const int i = row0 + g * 32 + (lane & 31);
                         if (i >= pad) return;
                         const float4 st = i < n ? a.stat[i] : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
                         const int label = !DISTILL && i < n ? a.l.idx[a.rows[i]] - a.c0 : -1;
@@ -452,15 +455,18 @@ __global__ __launch_bounds__(256) void k_lm_loss_combine(LmLossArgs a) {
   total_by_last<256>(a.l);
 }
 
-// The same of few rows, a workgroup per row (two partial sums for every 64
-// columns).  Without a plan every row is here, in play or not.
+// The same by a workgroup per row, for up to 1024 rows: few rows have two partial
+// sums for every 64 columns, and the distillation's dot products want many
+// wavefronts (500 rows of 5000 x 512 with 16 members, few rows' products included:
+// 43.5 -> 30.6 us; 500 of 32 000 x 2048 with 64, the other products: 174 -> 99.6).
+// Without a plan every row is here, in play or not.
 template <bool DISTILL>
-struct FewCombine {
+struct RowCombine {
   static constexpr int kThreads = DISTILL ? 1024 : 256;  // (a wavefront per few members)
 };
 template <bool DISTILL>
-__global__ __launch_bounds__(FewCombine<DISTILL>::kThreads) void k_lm_loss_few_combine(LmLossArgs a) {
-  constexpr int kThreads = FewCombine<DISTILL>::kThreads, kWaves = kThreads / kWave;
+__global__ __launch_bounds__(RowCombine<DISTILL>::kThreads) void k_lm_loss_row_combine(LmLossArgs a) {
+  constexpr int kThreads = RowCombine<DISTILL>::kThreads, kWaves = kThreads / kWave;
   __shared__ float red_m[kWaves], red_s[kWaves], xs[DISTILL ? kMaxMembers : 1];
   const int lane = threadIdx.x & 63, wave = wave_id();
   const int64_t i = blockIdx.x;
@@ -476,8 +482,10 @@ __global__ __launch_bounds__(FewCombine<DISTILL>::kThreads) void k_lm_loss_few_c
     }
   }
   if (in) {
-    const int parts = 2 * lm_few_groups(a.l.V);
-    const float2* part = a.part + i * parts;
+    const bool few = lm_few(a.l.R, a.l.V);
+    const int parts = 2 * (few ? lm_few_groups(a.l.V) : a.plan->fwd_runs);
+    const float2* part = a.part + i * (few ? parts : 1);
+    const int64_t next = few ? 1 : a.plan->n;  // from one partial sum to the next
     const bf16_t* h = a.plan != nullptr ? a.hp + i * a.H : static_cast<const bf16_t*>(a.h) + r * a.H;
     const bf16_t* W = static_cast<const bf16_t*>(a.w);
     // the cross entropy's first wavefront has the label's logit meanwhile
@@ -489,7 +497,7 @@ __global__ __launch_bounds__(FewCombine<DISTILL>::kThreads) void k_lm_loss_few_c
         float2 p[U];
 #pragma unroll
         for (int u = 0; u < U; ++u)
-          p[u] = e0 + u * kSumming < parts ? part[e0 + u * kSumming] : make_float2(kNegBig, 0.0f);
+          p[u] = e0 + u * kSumming < parts ? part[(e0 + u * kSumming) * next] : make_float2(kNegBig, 0.0f);
 #pragma unroll
         for (int u = 0; u < U; ++u) lse_join(m, s, p[u].x, p[u].y, a.l.c);
       }

@@ -137,7 +137,7 @@ def test_workspace_is_bounded_by_its_parts(lib, R, v, H):
     pad, tiles = (R + 63) // 64 * 64, -(-v // 256)
     g = max(1 << 30, pad * 2 * 1024) + pad * 2 * (256 + 128)
     dh = 4 * min(32 * R * H, max(2560 << 16, R * H))
-    parts = 16 * max(R, min(1024 * 256, R * tiles), R * -(-v // 64) if R <= 128 else 0)
+    parts = 16 * max(R, min(1024 * 256, R * tiles), R * -(-v // 64) if R <= 128 else 512 * 128)
     assert got <= g + dh + 4 * (512 << 16) + pad * H * 2 + parts + R * (16 * 12 + 64) + 16 * 256
 
 
