@@ -1651,9 +1651,6 @@ hipError_t launch_lm_loss(LmLossArgs a, bool weight_bf16, hipStream_t s) {
   const bool few = lm_few(R, a.l.V), by_workgroup = few || (distill && R <= kLmFewMost);
   const unsigned few_rows = (unsigned)((R + kLmFewRows - 1) / kLmFewRows);
   const auto few_fwd = R <= 32 ? k_lm_loss_few<1> : R <= 64 ? k_lm_loss_few<2> : k_lm_loss_few<4>;
-  const auto few_g =
-      distill ? (R <= 32 ? k_lm_loss_few_g<1, true> : R <= 64 ? k_lm_loss_few_g<2, true> : k_lm_loss_few_g<4, true>)
-              : (R <= 32 ? k_lm_loss_few_g<1, false> : R <= 64 ? k_lm_loss_few_g<2, false> : k_lm_loss_few_g<4, false>);
   hipError_t e;
   if (distill) {
     hipLaunchKernelGGL(k_lm_loss_members, by_row, dim3(256), 0, s, a);
@@ -1692,13 +1689,15 @@ hipError_t launch_lm_loss(LmLossArgs a, bool weight_bf16, hipStream_t s) {
   for (int64_t c0 = 0; c0 < a.l.V; c0 += a.piece) {
     a.c0 = (int32_t)c0;
     a.cols = (int32_t)(a.l.V - c0 < a.piece ? a.l.V - c0 : a.piece);
-    if (few)
-      hipLaunchKernelGGL(few_g, dim3((unsigned)(lm_tiles(a.cols) * (kLmTile / kLmFewCols)), few_rows),
-                         dim3(kFewThreads), 0, s, a);
+    if (a.x != nullptr)
+      hipLaunchKernelGGL(distill ? k_lm_loss_few_g<true> : k_lm_loss_few_g<false>,
+                         dim3((unsigned)((lm_tiles(a.cols) * kLmTile + kFewGCols - 1) / kFewGCols),
+                              (unsigned)lm_loss_pad(R)),
+                         dim3(256), 0, s, a);
     else
       hipLaunchKernelGGL(distill ? k_lm_loss_g<true> : k_lm_loss_g<false>, runs(a.cols), dim3(kThreads), 0, s, a);
     if ((e = hipGetLastError()) != hipSuccess) return e;
-    if (distill) {
+    if (distill && a.x == nullptr) {
       hipLaunchKernelGGL(k_lm_loss_fix, by_row, dim3(256), 0, s, a);
       if ((e = hipGetLastError()) != hipSuccess) return e;
     }

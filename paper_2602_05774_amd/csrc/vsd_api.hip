@@ -525,7 +525,7 @@ vsd_status check_rows_src(const vsd_rows* rows, const vsd_src* src, const char* 
 bool usable_temp(float t) { return std::isfinite(t) && t >= 1e-30f && t <= 1e30f; }
 
 struct LossLayout {
-  size_t tag, at, rows, plan, mid, mp, mstat, mx, hp, part, stat, g, acc, wacc, total;
+  size_t tag, at, rows, plan, mid, mp, mstat, mx, hp, part, stat, x, g, acc, wacc, total;
   int32_t piece;
 };
 
@@ -556,6 +556,7 @@ LossLayout loss_layout(const vsd_rows* rows, int32_t K, bool grad) {
   w.part = take((size_t)vsd::lm_loss_parts(rows->R, rows->v) * sizeof(float2));
   w.stat = take(R * sizeof(float4));
   if (grad) {
+    if (vsd::lm_few_keeps(rows->R, rows->v)) w.x = take(R * (size_t)vsd::lm_few_ldx(rows->v) * sizeof(float));
     w.g = take(padded * (size_t)vsd::lm_loss_ldg(w.piece) * sizeof(uint16_t));
     w.acc = take((size_t)vsd::lm_loss_sums(rows->R, rows->hidden_dim) * sizeof(float));
     const int64_t wsums = vsd::lm_loss_wsums(rows->v, rows->hidden_dim, w.piece);
@@ -671,6 +672,7 @@ vsd_status base_loss(const vsd_rows* rows, const vsd_src* src, int32_t K, const 
     if (grad != nullptr) {
       b.dh = grad->grad_hidden;
       b.dw = grad->grad_weight;
+      if (w.x != 0) b.x = reinterpret_cast<float*>(ws + w.x);
       b.g = reinterpret_cast<uint16_t*>(ws + w.g);
       b.acc = reinterpret_cast<float*>(ws + w.acc);
       if (grad->grad_weight != nullptr && w.wacc != 0) b.wacc = reinterpret_cast<float*>(ws + w.wacc);

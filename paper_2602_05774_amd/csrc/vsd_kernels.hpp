@@ -556,6 +556,7 @@ struct LmLossArgs {
   float2* part;              // [2 runs, rows in play] log-sum-exps, per wavefront group (few
                              // rows: [rows in play, 2 groups of columns])
   float4* stat;              // [R] (m, kq, k, -) of the gradient
+  float* x;                  // [rows in play, lm_few_ldx(V)] logits of few rows with a gradient, or null
   bf16_store* g;             // [lm_loss_pad(R), ldg] the piece's gradient
   float* acc;                // [splits, rows in play, H] sums of dh
   float* wacc;               // [dw_splits, cols, H] sums of dW, or null: one range
@@ -591,6 +592,10 @@ __host__ __device__ constexpr bool lm_few(int64_t R, int V) {
   return R <= kLmFewRows ||
          (R <= kLmFewMost && (R + kLmFewRows - 1) / kLmFewRows * lm_few_groups(V) <= 2 * kLmCus);
 }
+// Few rows' logits (fp32) are kept for the gradient up to 256 MB, which the last
+// cache holds; beyond that g comes of products again.
+__host__ __device__ constexpr int64_t lm_few_ldx(int V) { return (int64_t)lm_few_groups(V) * kLmFewCols; }
+constexpr bool lm_few_keeps(int64_t R, int V) { return lm_few(R, V) && R * lm_few_ldx(V) <= 1ll << 26; }
 // Entries of the forward's log-sum-exps: two per run and row in play.
 inline int64_t lm_loss_parts(int64_t R, int V) {
   if (lm_few(R, V)) return 2 * R * lm_few_groups(V);

@@ -338,6 +338,10 @@ __device__ __forceinline__ void lm_few_products(const bf16_t* h, int n, const bf
 }
 
 // (blockIdx.y: 32 kG rows; more than one of them only with kG = 4)
+// With a gradient the logits are kept (lm_few_keeps), as its g needs them: W is the
+// most that few rows read, and products again for g cost more than 8 bytes per logit
+// (loss and dh of 16 rows of 128 256 x 4096: 631 us, so 435; 48 of 32 000 x 4096: 163
+// and 127; with dW, 132 of 512 x 3456: 118 and 94).
 template <int kG>
 __global__ __launch_bounds__(kFewThreads, 2) void k_lm_loss_few(LmLossArgs a) {
   __shared__ __align__(16) bf16_t lds[Few<kG>::kLds];
@@ -346,6 +350,14 @@ __global__ __launch_bounds__(kFewThreads, 2) void k_lm_loss_few(LmLossArgs a) {
   const bf16_t* h = a.plan != nullptr ? a.hp : static_cast<const bf16_t*>(a.h);
   lm_few_products<kG>(h + (int64_t)row0 * a.H, min(n - row0, 32 * kG), static_cast<const bf16_t*>(a.w), a.l.V, a.H, lds,
                       [&](int g, int c, float (&x)[16]) {
+                        const int i = row0 + g * 32 + (lane & 31);
+                        if (a.x != nullptr && i < n) {
+                          float* X = a.x + (int64_t)i * lm_few_ldx(a.l.V) + c;
+#pragma unroll
+                          for (int q = 0; q < 4; ++q)
+                            *reinterpret_cast<float4*>(X + 8 * q) =
+                                make_float4(x[q * 4], x[q * 4 + 1], x[q * 4 + 2], x[q * 4 + 3]);
+                        }
                         float m = kNegBig, s = 0.0f;
 #pragma unroll
                         for (int e = 0; e < 16; ++e) {
@@ -355,41 +367,8 @@ __global__ __launch_bounds__(kFewThreads, 2) void k_lm_loss_few(LmLossArgs a) {
 #pragma unroll
                         for (int e = 0; e < 16; ++e) s += lse_term(x[e], m, a.l.c);
                         lse_join(m, s, __shfl_xor(m, 32), __shfl_xor(s, 32), a.l.c);
-                        const int i = row0 + g * 32 + lane;
                         if (lane < 32 && i < n)
                           a.part[(int64_t)i * 2 * lm_few_groups(a.l.V) + blockIdx.x * 2 + wave_id()] = make_float2(m, s);
-                      });
-}
-
-// The same products for g of a piece.
-static_assert(kLmLossPad <= 64 && kLmFewRows % kLmLossPad == 0, "the padding of 32 rows is 32 more, of 128 none");
-template <int kG, bool DISTILL>
-__global__ __launch_bounds__(kFewThreads, 2) void k_lm_loss_few_g(LmLossArgs a) {
-  __shared__ __align__(16) bf16_t lds[Few<kG>::kLds];
-  const int lane = threadIdx.x & 63, n = a.plan->n, pad = (int)lm_loss_pad(n), row0 = blockIdx.y * 32 * kG;
-  if (row0 >= n) return;
-  lm_few_products<kG>(a.hp + (int64_t)row0 * a.H, min(n - row0, 32 * kG),
-                      static_cast<const bf16_t*>(a.w) + (int64_t)a.c0 * a.H, a.cols, a.H, lds,
-                      [&](int g, int c, float (&x)[16]) {
-                        const int i = row0 + g * 32 + (lane & 31);
-                        if (i >= pad) return;
-                        const float4 st = i < n ? a.stat[i] : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-                        const int label = !DISTILL && i < n ? a.l.idx[a.rows[i]] - a.c0 : -1;
-                        bf16_t* G = a.g + (int64_t)i * a.ldg;
-#pragma unroll
-                        for (int q = 0; q < 4; ++q) {
-                          float v[4];
-#pragma unroll
-                          for (int j = 0; j < 4; ++j) {
-                            const int col = c + 8 * q + j;
-                            v[j] = st.y * lse_term(x[q * 4 + j], st.x, a.l.c) - (col == label ? st.z : 0.0f);
-                            if (i >= n || col >= a.cols) v[j] = 0.0f;
-                          }
-                          *reinterpret_cast<uint2*>(G + c + 8 * q) =
-                              make_uint2(pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]));
-                          if (kG * 32 < kLmLossPad)  // (the rows in play are padded past this tile's)
-                            *reinterpret_cast<uint2*>(G + (int64_t)kG * 32 * a.ldg + c + 8 * q) = make_uint2(0, 0);
-                        }
                       });
 }
 
@@ -577,18 +556,15 @@ __global__ __launch_bounds__(kThreads, 1) void k_lm_loss_g(LmLossArgs a) {
   });
 }
 
-// The distillation's members of that piece, each from its own logit and by the
-// first of the members that name the column.  One wavefront per row.
-__global__ __launch_bounds__(256) void k_lm_loss_fix(LmLossArgs a) {
-  const int lane = threadIdx.x & 63;
-  const int64_t i = (int64_t)blockIdx.x * 4 + wave_id();
-  if (i >= a.plan->n) return;
+// A row's members in columns [lo, hi), each from its own logit and by the first of
+// the members that name the column.  By a wavefront.
+__device__ __forceinline__ void lm_loss_fix(const LmLossArgs& a, int64_t i, int lo, int hi) {
+  const int lane = threadIdx.x & 63, K = a.l.K;
   const int64_t r = a.rows[i];
-  const int K = a.l.K;
   const int id = lane < K ? a.mid[r * K + lane] : -1;
   const float p = lane < K ? a.mp[r * K + lane] : 0.0f;
   float sum = 0.0f;
-  bool first = id >= a.c0 && id < a.c0 + a.cols;
+  bool first = id >= lo && id < hi;
   for (int k = 0; k < K; ++k) {
     const bool same = lane_i(id, k) == id;
     sum += same ? lane_f(p, k) : 0.0f;
@@ -597,6 +573,38 @@ __global__ __launch_bounds__(256) void k_lm_loss_fix(LmLossArgs a) {
   if (!first) return;
   const float4 st = a.stat[i];
   store1(a.g + i * a.ldg + (id - a.c0), st.y * lse_term(a.mx[i * K + lane], st.x, a.l.c) - st.z * sum);
+}
+
+// The distillation's members of that piece.  One wavefront per row.
+__global__ __launch_bounds__(256) void k_lm_loss_fix(LmLossArgs a) {
+  const int64_t i = (int64_t)blockIdx.x * 4 + wave_id();
+  if (i < a.plan->n) lm_loss_fix(a, i, a.c0, a.c0 + a.cols);
+}
+
+// g of a piece from the logits that few rows' products left: 2048 columns of row
+// blockIdx.y per workgroup.  Bound by 6 bytes per element.
+constexpr int kFewGCols = 8 * 256;
+template <bool DISTILL>
+__global__ __launch_bounds__(256) void k_lm_loss_few_g(LmLossArgs a) {
+  const int n = a.plan->n, i = blockIdx.y, first = blockIdx.x * kFewGCols, col = first + threadIdx.x * 8;
+  if (i >= (int)lm_loss_pad(n)) return;
+  if (col < (a.cols + kLmTile - 1) / kLmTile * kLmTile) {
+    float g[8] = {0, 0, 0, 0, 0, 0, 0, 0};
+    if (i < n && col < a.cols) {
+      const float4* X = reinterpret_cast<const float4*>(a.x + (int64_t)i * lm_few_ldx(a.l.V) + a.c0 + col);
+      const float4 lo = X[0], hi = X[1], st = a.stat[i];
+      const float x[8] = {lo.x, lo.y, lo.z, lo.w, hi.x, hi.y, hi.z, hi.w};
+      const int label = DISTILL ? -1 : a.l.idx[a.rows[i]] - a.c0;
+#pragma unroll
+      for (int j = 0; j < 8; ++j)
+        if (col + j < a.cols) g[j] = st.y * lse_term(x[j], st.x, a.l.c) - (col + j == label ? st.z : 0.0f);
+    }
+    *reinterpret_cast<uint4*>(a.g + (int64_t)i * a.ldg + col) =
+        make_uint4(pack_bf16x2(g[0], g[1]), pack_bf16x2(g[2], g[3]), pack_bf16x2(g[4], g[5]), pack_bf16x2(g[6], g[7]));
+  }
+  if (!DISTILL || i >= n) return;
+  __syncthreads();  // (the row's stores before its members')
+  if (wave_id() == 0) lm_loss_fix(a, i, a.c0 + first, a.c0 + min(first + kFewGCols, a.cols));
 }
 
 // dh of a piece: 256 x 256 tiles of g W, the piece's columns in `splits` ranges

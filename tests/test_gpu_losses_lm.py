@@ -123,6 +123,54 @@ def test_bad_labels_are_reported_and_skipped():
     assert int(res.device_error) == 1 and torch.all(res.loss_row[1:3] == 0) and torch.all(res.grad.grad_hidden[1:3] == 0)
 
 
+@pytest.mark.parametrize("R,V", ((2, 9000001), (100, 700001)))
+@pytest.mark.parametrize("loss", ("ce", "distill"))
+def test_few_rows_of_a_very_large_vocabulary(loss, R, V):
+    """The logits that few rows keep, cut into two pieces (2 rows), and more of them than are
+    kept (100 rows): against float64 on the device."""
+    H, K = 64, 6
+    h, w = _head(R, V, H, 39)
+    g_ = torch.Generator(device=DEV).manual_seed(40)
+    labels = torch.randint(V - 2000, V, (R,), device=DEV, dtype=torch.int32, generator=g_)
+    idx = torch.randint(0, V, (R, K), device=DEV, dtype=torch.int32, generator=g_)
+    idx[:, 0] = V - 1
+    val = torch.randn(R, K, device=DEV, generator=g_)
+    labels[1], idx[1] = -1, -1
+    head = vsd.LmHead(h, w)
+    if loss == "ce":
+        res = vsd.cross_entropy(head, labels, grad=True, weight_grad=torch.float32)
+    else:
+        res = vsd.distill_loss(head, idx, val, grad=True, weight_grad=torch.float32)
+    lse, parts = torch.full((R,), float("-inf"), dtype=torch.float64, device=DEV), range(0, V, 1 << 20)
+    for lo_ in parts:
+        lse = torch.logaddexp(lse, torch.logsumexp(h.double() @ w[lo_:lo_ + (1 << 20)].double().t(), 1))
+    at = labels[:, None].long() if loss == "ce" else idx.long()
+    p = torch.ones(R, 1, dtype=torch.float64, device=DEV) if loss == "ce" else torch.softmax(val.double(), 1)
+    p = torch.where(at >= 0, p, 0.0)
+    live = p.sum(1, keepdim=True)
+    x = (h.double()[:, None] * w[at.clamp(min=0)].double()).sum(2)
+    want = (p * (lse[:, None] - x)).sum(1)
+    if loss == "distill":
+        want += torch.xlogy(p, p).sum(1)
+    # the largest number of partial sums that one thread joins, four roundings each
+    t = (V / (32 * 192) + 64) * 4 * 2 ** -24
+    assert torch.all((res.loss_row.double() - want).abs() <= t + 2 ** -20 * want.abs())
+    # every g is one rounding from its value, and its softmax within t of the exact one
+    dh, bar = torch.zeros(2, R, H, dtype=torch.float64, device=DEV)
+    for lo_ in parts:
+        wp = w[lo_:lo_ + (1 << 20)].double()
+        q = torch.exp(h.double() @ wp.t() - lse[:, None]) * live
+        g = q.clone()
+        here = (at >= lo_) & (at < lo_ + len(wp))
+        g.scatter_add_(1, (at - lo_).clamp(0, len(wp) - 1), torch.where(here, -p, 0.0))
+        off = 2 ** -8 * g.abs() + t * q
+        dh += g @ wp
+        bar += off @ wp.abs()
+        dw = res.grad.grad_weight[lo_:lo_ + (1 << 20)].double()
+        assert torch.all((dw - g.t() @ h.double()).abs() <= off.t() @ h.double().abs() + 1e-30), lo_
+    assert torch.all((res.grad.grad_hidden.double() - dh).abs() <= bar + 2 ** -8 * dh.abs())
+
+
 @pytest.mark.parametrize("loss", ("ce", "distill"))
 def test_pieces(loss):
     """More rows than one piece's gradient may hold: every row against the same rows of a
