@@ -1648,7 +1648,7 @@ hipError_t launch_lm_loss(LmLossArgs a, bool weight_bf16, hipStream_t s) {
     const int64_t all = nrt * lm_tiles(V), most = nrt > kLmLossRuns ? nrt : kLmLossRuns;
     return dim3((unsigned)(all < most ? all : most));
   };
-  const bool few = lm_few(R, a.l.V), by_workgroup = few || (distill && R <= kLmFewMost);
+  const bool few = lm_few(R, a.l.V), by_workgroup = lm_by_workgroup(R, a.l.V, distill ? a.l.K : 0, a.H);
   const unsigned few_rows = (unsigned)((R + kLmFewRows - 1) / kLmFewRows);
   const auto few_fwd = R <= 32 ? k_lm_loss_few<1> : R <= 64 ? k_lm_loss_few<2> : k_lm_loss_few<4>;
   hipError_t e;

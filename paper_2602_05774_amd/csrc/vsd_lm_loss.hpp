@@ -434,10 +434,9 @@ __global__ __launch_bounds__(256) void k_lm_loss_combine(LmLossArgs a) {
   total_by_last<256>(a.l);
 }
 
-// The same by a workgroup per row, for up to 1024 rows: few rows have two partial
-// sums for every 64 columns, and the distillation's dot products want many
-// wavefronts (500 rows of 5000 x 512 with 16 members, few rows' products included:
-// 43.5 -> 30.6 us; 500 of 32 000 x 2048 with 64, the other products: 174 -> 99.6).
+// The same by a workgroup per row (lm_by_workgroup): few rows have two partial sums
+// for every 64 columns, and the distillation's dot products want many wavefronts (500
+// rows of 32 000 x 2048 with 64 members: 174 -> 99.6 us).
 // Without a plan every row is here, in play or not.
 template <bool DISTILL>
 struct RowCombine {

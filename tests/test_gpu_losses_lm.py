@@ -93,7 +93,7 @@ def test_cross_entropy(R, V, H, dw):
 
 @pytest.mark.parametrize("R,V,H,K", [(1, 5, 64, 2), (33, 300, 64, 64), (65, 1003, 128, 10), (300, 5003, 192, 33),
                                      (20, 33000, 256, 16), (132, 512, 256, 54), (900, 6000, 64, 20),
-                                     (1100, 400, 64, 5)])
+                                     (1100, 400, 64, 5), (530, 20000, 192, 60)])
 @pytest.mark.parametrize("lse", (False, True))
 def test_distillation(R, V, H, K, lse):
     h, w = _head(R, V, H, 32)
