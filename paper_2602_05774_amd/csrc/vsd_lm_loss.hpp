@@ -1,6 +1,6 @@
 // The base losses through an LM head: logits x = h W^T formed tile by tile by
 // k_lmhead.hip's product loop (which includes this file after it) and consumed
-// in the accumulators.  Neither they nor their gradient are kept: g is formed a
+// in the accumulators.  Neither they (but for few rows) nor their gradient are kept: g is formed a
 // piece of the vocabulary at a time, in bf16 (the operand type of the two
 // products that read it), and both add up in fp32.
 //
