@@ -596,14 +596,15 @@ __host__ __device__ constexpr bool lm_few(int64_t R, int V) {
 // cache holds; beyond that g comes of products again.
 __host__ __device__ constexpr int64_t lm_few_ldx(int V) { return (int64_t)lm_few_groups(V) * kLmFewCols; }
 constexpr bool lm_few_keeps(int64_t R, int V) { return lm_few(R, V) && R * lm_few_ldx(V) <= 1ll << 26; }
-// Rows joined by a workgroup each, which the distillation's dot products want, not by
-// a wavefront (K members; 0: cross entropy).  The loss of R rows of 32 000 x H by a
-// wavefront and by a workgroup, us: R = 300, H = 2048, 1 and 16 members, 77.2 and
-// 77.1, 98.7 and 78.5; 1000, H = 256, 16 members, 58.6 and 59.9; 1000, H = 2048, 4 and
-// 8 members, 140.7 and 142.3, 146.6 and 143.1; 4000, H = 2048, 16 and 64 members, 491
-// and 491, 632 and 586; 9001 of 8000 x 512 with 64, 199 and 248.
+// Rows joined by a workgroup each, not by a wavefront: few rows, and the
+// distillation's dot products (K members; 0: cross entropy) where the rows are no
+// more than two workgroups per CU or long and many.  The loss of R rows of 32 000 x H
+// by a wavefront and by a workgroup, us: R = 200, H = 2048, 16 and 64 members, 74.3
+// and 68.9, 95.7 and 75.8; 400, H = 256, 2 and 64, 38.0 and 39.7, 50.7 and 43.5; 700,
+// H = 2048, 2 and 64, 116 and 121, 145 and 143; 2000, H = 4096, 16 and 64, 481 and
+// 479, 615 and 585; 4000, H = 256, 64, 133 and 167; H = 2048, 64, 616 and 586.
 constexpr bool lm_by_workgroup(int64_t R, int V, int K, int H) {
-  return lm_few(R, V) || (K > 0 && (R <= 512 || (int64_t)K * H >= 16 * R) && R < 1 << 20);  // (32-bit launch)
+  return lm_few(R, V) || (K > 0 && (R <= 2 * kLmCus || ((int64_t)K * H >= 1 << 17 && R < 1 << 20)));  // (32-bit launch)
 }
 // Entries of the forward's log-sum-exps: two per run and row in play.
 inline int64_t lm_loss_parts(int64_t R, int V) {
