@@ -309,6 +309,107 @@ __global__ __launch_bounds__(kThreads) void k_top_logits(TopArgs a) {
   }
 }
 
+// Rows of up to 512 kNch columns, one wavefront each: the row stays in registers as
+// integers in the values' order (bf16: 16 bits of them; 0: no entry) and the K-th
+// largest is found bit by bit, a count of all entries per bit, until exactly K are
+// at or above it.  Bound by those counts (ballots): the lists' bound is worth little
+// where K is near the number of groups.
+// us, lists / this, by columns and K: 65 536 rows of 300 bf16, 4 79 / 69, 40 1065 / 87;
+// of 500 float32, 20 106 / 76; of 1000 bf16, 10 85 / 143, 64 483 / 151; of 2000, 64
+// 480 / 280; 10 rows of 400, 10 17.8 / 17.7, of 1000, 64 19.4 / 19.7, of 2000, 40 17.9 /
+// 26.7 (four chunks' counts one after another: only many rows hide them).
+constexpr int kManyShort = 1024;
+constexpr int kShortRows = 4;  // per workgroup
+template <typename T, bool MAP, int kNch>
+__global__ __launch_bounds__(kShortRows * kWave) void k_top_short(TopArgs a) {
+  constexpr int kBits = sizeof(T) == 2 ? 16 : 32, kDown = 32 - kBits;
+  __shared__ __align__(16) uint64_t all_keys[kShortRows][VSD_MAX_TOP];
+  const int lane = threadIdx.x & 63, V = a.V, K = a.K;
+  const int64_t r = (int64_t)blockIdx.x * kShortRows + wave_id();
+  if (r >= a.R) return;
+  uint64_t* const keys = all_keys[wave_id()];
+  const T* Y = static_cast<const T*>(a.Y) + r * a.ld;
+  auto col_of = [&](int j) { return (j >> 3) * 512 + lane * 8 + (j & 7); };
+  Raw8<T> q[kNch];
+  uint32_t in[kNch];
+#pragma unroll
+  for (int u = 0; u < kNch; ++u) {
+    const int base = u * 512 + lane * 8;
+    load_cols(q[u], Y, base, V);
+    in[u] = !MAP ? 0xFFu : base < V ? (uint32_t)a.mapped[base >> 3] : 0u;
+  }
+  uint32_t o[kNch * 8];
+  float m = kNegBig, s = 0.0f;
+#pragma unroll
+  for (int u = 0; u < kNch; ++u) {
+    float x[8];
+    q[u].get(x);
+    lse_add8(x, m, s, a.c);
+#pragma unroll
+    for (int k = 0; k < 8; ++k)
+      o[u * 8 + k] = ((in[u] >> k) & 1u) != 0u && x[k] > -INFINITY ? order_of(x[k]) >> kDown : 0u;
+  }
+  wave_lse(m, s, a.c);
+  if (lane == 0 && a.lse != nullptr) a.lse[r] = s == 0.0f ? -INFINITY : m * a.inv_t + logf(s);
+  auto counted = [&](auto&& f) {
+    int c = 0;
+#pragma unroll
+    for (int j = 0; j < kNch * 8; ++j) c += __builtin_popcountll(__ballot(f(j)));
+    return c;
+  };
+  uint32_t kth = 1;
+  bool exact = counted([&](int j) { return o[j] >= 1u; }) <= K;
+  if (!exact) {
+    kth = 0;
+    for (int b = kBits - 1; b >= 0 && !exact; --b) {
+      const uint32_t t = kth | (1u << b);
+      const int c = counted([&](int j) { return o[j] >= t; });
+      if (c >= K) kth = t;
+      exact = c == K;
+    }
+  }
+  // more entries of the K-th's value than places: the smallest index with enough of
+  // them up to it
+  int last = 0x7FFFFFFF;
+  if (!exact) {
+    const int need = K - counted([&](int j) { return o[j] > kth; }), bits = 32 - __builtin_clz(V);
+    auto index_if = [&](int j) { return o[j] != kth ? 0x7FFFFFFF : MAP ? a.inv[col_of(j)] : col_of(j); };
+    last = (1 << bits) - 1;  // (every index is below V)
+    for (int b = bits - 1; b >= 0; --b) {
+      const int t = last & ~(1 << b);
+      if (counted([&](int j) { return index_if(j) <= t; }) >= need) last = t;
+    }
+  }
+  int n = 0;
+#pragma unroll
+  for (int j = 0; j < kNch * 8; ++j) {
+    bool member = o[j] >= kth;
+    const uint64_t maybe = __ballot(member);
+    if (maybe == 0ull) continue;
+    const int index = !member ? 0 : MAP ? a.inv[col_of(j)] : col_of(j);
+    member = member && (o[j] > kth || index <= last);
+    const uint64_t who = __ballot(member);
+    // (bf16: the value's lower half is zeros below the order's, ones where it is negative)
+    const uint32_t order = kDown == 0 || o[j] >= 0x8000u ? o[j] << kDown : o[j] << kDown | 0xFFFFu;
+    if (member) keys[n + __builtin_popcountll(who & ((1ull << lane) - 1))] = (uint64_t)order << 32 | (uint32_t)~index;
+    n += __builtin_popcountll(who);
+  }
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+  if (lane >= K) return;
+  if (lane >= n) {
+    a.idx[r * K + lane] = -1;
+    a.val[r * K + lane] = -INFINITY;
+    return;
+  }
+  const uint64_t key = keys[lane];
+  int rank = 0;
+  for (int j = 0; j < n; ++j) rank += keys[j] > key ? 1 : 0;
+  a.idx[r * K + rank] = index_in(key);
+  a.val[r * K + rank] = value_in(key);
+}
+
 __global__ __launch_bounds__(256) void k_top_bits(const int32_t* inv, int V, uint8_t* mapped) {
   const int b = blockIdx.x * 256 + threadIdx.x;
   if (b >= (V + 7) / 8) return;
@@ -328,8 +429,21 @@ hipError_t launch_n(const TopArgs& a, hipStream_t s) {
   return hipGetLastError();
 }
 
+template <typename T, int kNch>
+hipError_t launch_short(const TopArgs& a, hipStream_t s) {
+  const dim3 grid((unsigned)((a.R + kShortRows - 1) / kShortRows));
+  if (a.inv != nullptr)
+    hipLaunchKernelGGL((k_top_short<T, true, kNch>), grid, dim3(kShortRows * kWave), 0, s, a);
+  else
+    hipLaunchKernelGGL((k_top_short<T, false, kNch>), grid, dim3(kShortRows * kWave), 0, s, a);
+  return hipGetLastError();
+}
+
 template <typename T>
 hipError_t launch_t(const TopArgs& a, hipStream_t s) {
+  if (a.V <= 512) return launch_short<T, 1>(a, s);
+  if (a.V <= 1024 && a.K > kShortK) return launch_short<T, 2>(a, s);
+  if (a.V <= 2048 && a.K > kShortK && a.R >= kManyShort) return launch_short<T, 4>(a, s);
   if (a.V <= kShortCols && a.K <= kShortK) return launch_n<T, kWave>(a, s);
   return launch_n<T, 256>(a, s);
 }

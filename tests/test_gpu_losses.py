@@ -300,6 +300,25 @@ def test_top_logits_of_ties(V, kind, mapped):
         _check_top(_host(Y), vsd.top_logits(Y, k, d2t=d2t), k, d2t)
 
 
+@pytest.mark.parametrize("R,V", ((1030, 300), (1024, 700), (1025, 1025), (2000, 2048), (1023, 1900)))
+@pytest.mark.parametrize("kind", ("bf16", "f32"))
+@pytest.mark.parametrize("mapped", (False, True))
+def test_top_logits_of_many_short_rows(R, V, kind, mapped):
+    """Rows that stay in a wavefront: values of both signs, equal ones across the K-th place,
+    fewer entries than K, none."""
+    _, Y = _rows(R, V, kind, 33)
+    g = torch.Generator(device=DEV).manual_seed(34)
+    Y[: R // 2] = torch.randint(-3, 4, (R // 2, V), generator=g, device=DEV).to(Y.dtype)
+    Y[0] = -7.0
+    Y[1] = -math.inf
+    Y[2, 30:] = -math.inf
+    Y[3] = -torch.rand(V, generator=g, device=DEV).to(Y.dtype)
+    Y[4] = torch.where(torch.arange(V, device=DEV) % 2 == 0, 0.0, -0.0).to(Y.dtype)
+    d2t = torch.randperm(V, device=DEV, generator=g)[: V * 9 // 10].int() if mapped else None
+    for k in (1, 33, 64):
+        _check_top(_host(Y), vsd.top_logits(Y, k, d2t=d2t), k, d2t)
+
+
 def test_top_logits_of_a_bad_map():
     _, Y = _rows(2, 64, "f32", 24)
     for bad, code in (([3, 3, 5, 1], 4), ([3, 64, 5, 1], 2), ([3, -1, 5, 1], 2)):
