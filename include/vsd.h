@@ -231,8 +231,8 @@
  *   be the logits' own buffer; its padding columns are not touched.  Fused LM
  *   head (rows->hidden_dim > 0): the logits are formed tile by tile, and again,
  *   a piece of the vocabulary at a time, for the gradient; neither they nor
- *   their gradient are kept (the logits of up to 1024 rows are, in the
- *   workspace, up to 256 MB of them).  grad_hidden [R, H] (bf16) receives g . weight and
+ *   their gradient are kept (the logits of few rows, or of a small vocabulary
+ *   and up to 8192 rows, are, in the workspace: 256 MB at most).  grad_hidden [R, H] (bf16) receives g . weight and
  *   grad_weight [v, H] (optional; fp32 or bf16, weight_dtype) g^T . hidden,
  *   both summed in fp32 over g rounded to bf16, written, not accumulated into.
  *   The top logits: per row the k largest of the logits above -inf, the larger

@@ -1649,6 +1649,14 @@ hipError_t launch_lm_loss(LmLossArgs a, bool weight_bf16, hipStream_t s) {
     return dim3((unsigned)(all < most ? all : most));
   };
   const bool few = lm_few(R, a.l.V), by_workgroup = lm_by_workgroup(R, a.l.V, distill ? a.l.K : 0, a.H);
+  // The distillation's join has 16 wavefronts a row, or, where its many rows fill the
+  // chip, four: the loss of R rows of V x H, K members, us, 16 / 4: 600 of 5000 x 1024,
+  // 16 and 64, 39.8 / 39.0, 47.3 / 52.7; 1000 of 2000 x 1024, 4 and 64, 33.6 / 29.5, 43.9 /
+  // 46.8; 4000 of 900 x 256, 4 and 64, 49.9 / 32.1, 69.7 / 54.4.
+  const bool wide_join = !few || R <= 2 * kLmCus || (R <= 4 * kLmCus && a.l.K > 32);
+  const auto row_join = !distill    ? k_lm_loss_row_combine<false, 256>
+                        : wide_join ? k_lm_loss_row_combine<true, 1024>
+                                    : k_lm_loss_row_combine<true, 256>;
   const unsigned few_rows = (unsigned)((R + kLmFewRows - 1) / kLmFewRows);
   const auto few_fwd = R <= 32 ? k_lm_loss_few<1> : R <= 64 ? k_lm_loss_few<2> : k_lm_loss_few<4>;
   hipError_t e;
@@ -1674,8 +1682,7 @@ hipError_t launch_lm_loss(LmLossArgs a, bool weight_bf16, hipStream_t s) {
     hipLaunchKernelGGL(k_lm_loss_fwd, runs(a.l.V), dim3(kThreads), 0, s, a);
   if ((e = hipGetLastError()) != hipSuccess) return e;
   if (by_workgroup)
-    hipLaunchKernelGGL(distill ? k_lm_loss_row_combine<true> : k_lm_loss_row_combine<false>, dim3((unsigned)R),
-                       dim3(distill ? RowCombine<true>::kThreads : RowCombine<false>::kThreads), 0, s, a);
+    hipLaunchKernelGGL(row_join, dim3((unsigned)R), dim3(distill && wide_join ? 1024 : 256), 0, s, a);
   else
     hipLaunchKernelGGL(distill ? k_lm_loss_combine<true> : k_lm_loss_combine<false>, by_row, dim3(256), 0, s, a);
   if ((e = hipGetLastError()) != hipSuccess) return e;

@@ -581,12 +581,13 @@ inline int32_t lm_loss_piece(int64_t R, int V) {
 // memory channels.
 inline int32_t lm_loss_ldg(int32_t piece) { return piece + 128; }
 // Few rows: a product whose tiles are 64 columns of W and up to 128 rows.  For up to
-// 128 rows, whose time is that of reading W, and for up to 1024 as long as these
+// 128 rows, whose time is that of reading W, and for up to 8192 as long as these
 // tiles are at most two per CU: 256 x 256 tiles would leave most CUs idle.  Loss and
 // both gradients with those and with these: 132 rows of 512 x 3456, 54 members, 303
 // and 117 us; 256 of 8000 x 4096, 234 and 143; 1000 of 2000 x 1024, 137 and 109;
-// the loss alone of 256 of 16 000 x 4096 (two per CU), 97.8 and 62.6.
-constexpr int kLmFewRows = 128, kLmFewCols = 64, kLmFewMost = 1024;
+// 4000 of 1000 x 2048, 179 and 129; 8000 of 256 x 512, dh only, 107 and 92; the loss
+// alone of 256 of 16 000 x 4096 (two per CU), 97.8 and 62.6.
+constexpr int kLmFewRows = 128, kLmFewCols = 64, kLmFewMost = 8192;
 __host__ __device__ constexpr int lm_few_groups(int V) { return (V + kLmFewCols - 1) / kLmFewCols; }
 __host__ __device__ constexpr bool lm_few(int64_t R, int V) {
   return R <= kLmFewRows ||

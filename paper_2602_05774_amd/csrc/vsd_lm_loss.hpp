@@ -473,16 +473,12 @@ __global__ __launch_bounds__(256) void k_lm_loss_combine(LmLossArgs a) {
 }
 
 // The same by a workgroup per row (lm_by_workgroup): few rows have two partial sums
-// for every 64 columns, and the distillation's dot products want many wavefronts (500
+// for every 64 columns one after another, and the distillation's dot products want many wavefronts (500
 // rows of 32 000 x 2048 with 64 members: 174 -> 99.6 us).
 // Without a plan every row is here, in play or not.
-template <bool DISTILL>
-struct RowCombine {
-  static constexpr int kThreads = DISTILL ? 1024 : 256;  // (a wavefront per few members)
-};
-template <bool DISTILL>
-__global__ __launch_bounds__(RowCombine<DISTILL>::kThreads) void k_lm_loss_row_combine(LmLossArgs a) {
-  constexpr int kThreads = RowCombine<DISTILL>::kThreads, kWaves = kThreads / kWave;
+template <bool DISTILL, int kThreads>
+__global__ __launch_bounds__(kThreads) void k_lm_loss_row_combine(LmLossArgs a) {
+  constexpr int kWaves = kThreads / kWave;
   __shared__ float red_m[kWaves], red_s[kWaves], xs[DISTILL ? kMaxMembers : 1];
   const int lane = threadIdx.x & 63, wave = wave_id();
   const int64_t i = blockIdx.x;

@@ -8,7 +8,7 @@ tensors lie on one device.
 Rows are [R, v] logits with unit column stride (a column range of a wider
 buffer is fine: base address and row stride are multiples of 16 bytes), or an
 LmHead(hidden [R, H], weight [v, H]), whose logits are not kept (those of
-few rows lie in the workspace, 256 MB at most).
+few rows or of a small vocabulary lie in the workspace, 256 MB at most).
 """
 import contextlib
 import ctypes

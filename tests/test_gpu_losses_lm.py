@@ -66,7 +66,7 @@ def _check(res, h, w, mem, weight, T, scale, V):
 
 SHAPES = [(1, 1, 64), (1, 300, 128), (20, 515, 192), (33, 4099, 128), (100, 1000, 576), (5, 7, 64), (63, 256, 64), (64, 257, 192), (65, 1000, 320), (257, 5003, 128),
           (600, 2049, 256), (48, 33000, 512), (1300, 700, 64), (132, 512, 448), (1000, 130, 192), (1025, 130, 64),
-          (900, 6000, 64)]
+          (900, 6000, 64), (2000, 300, 64), (5000, 500, 128), (8193, 130, 64)]
 
 
 @pytest.mark.parametrize("R,V,H", SHAPES)
@@ -93,7 +93,8 @@ def test_cross_entropy(R, V, H, dw):
 
 @pytest.mark.parametrize("R,V,H,K", [(1, 5, 64, 2), (33, 300, 64, 64), (65, 1003, 128, 10), (300, 5003, 192, 33),
                                      (20, 33000, 256, 16), (132, 512, 256, 54), (900, 6000, 64, 20),
-                                     (1100, 400, 64, 5), (530, 20000, 192, 60)])
+                                     (1100, 400, 64, 5), (530, 20000, 192, 60), (700, 900, 128, 40),
+                                     (2000, 300, 64, 64)])
 @pytest.mark.parametrize("lse", (False, True))
 def test_distillation(R, V, H, K, lse):
     h, w = _head(R, V, H, 32)

@@ -29,7 +29,7 @@ def test_row_loss_launch(tmp_path):
         assert t[2] or t[0] * 8 * t[1] >= v
 
 
-@pytest.mark.parametrize("R", (1, 100, 128, 129, 500, 1024, 6144, 70001, 300000))
+@pytest.mark.parametrize("R", (1, 100, 128, 129, 500, 1024, 6144, 8192, 8193, 70001, 300000))
 @pytest.mark.parametrize("V", (1, 300, 32000, 128256))
 @pytest.mark.parametrize("H", (64, 1024, 4096))
 def test_partial_sums_fit_their_regions(tmp_path, R, V, H):
@@ -45,7 +45,7 @@ def test_partial_sums_fit_their_regions(tmp_path, R, V, H):
     cols = min(V, piece)
     for n in ns:
         nrt, nht, tiles = math.ceil(n / 256), math.ceil(H / 256), math.ceil(V / 256)
-        few = R <= 128 or (R <= 1024 and math.ceil(R / 128) * math.ceil(V / 64) <= 512)
+        few = R <= 128 or (R <= 8192 and math.ceil(R / 128) * math.ceil(V / 64) <= 512)
         runs = math.ceil(V / 64) if few else min(tiles, max(1, runs_max // nrt))
         assert 2 * runs * n <= parts
         splits = min(math.ceil(cols / 64), splits_max, max(1, dh_max // (nrt * nht)))
