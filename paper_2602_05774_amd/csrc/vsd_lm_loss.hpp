@@ -563,8 +563,8 @@ __global__ __launch_bounds__(kThreads, 1) void k_lm_loss_g(LmLossArgs a) {
     const uint32_t keep = i < n ? ~0u : 0u;  // (what lies behind the rows in play gives zeros, whatever x is)
     const float4 st = i < n ? a.stat[i] : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     const int label = !DISTILL && i < n ? a.l.idx[a.rows[i]] - a.c0 : -1;
-    // kq exp2((x - m) c) with one rounding in the exponent: that of m c goes into kq
-    const float c = a.l.c, mc = st.x * a.l.c, kq = st.y * __builtin_amdgcn_exp2f(-fmaf(st.x, c, -mc));
+    // (x c - m c in one operation saved no time, 2961 and 2968 us for both gradients of 9001
+    // rows of 32 000 x 2048, and is no number where m c or its rounding leaves float32's range)
     bf16_t* G = a.g + i * a.ldg;
 #pragma unroll 1
     for (int ch = 0; ch < 16; ++ch) {
@@ -572,7 +572,7 @@ __global__ __launch_bounds__(kThreads, 1) void k_lm_loss_g(LmLossArgs a) {
       float x[8], g[8];
       nt_chunk(acc, ch, x);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) g[j] = kq * __builtin_amdgcn_exp2f(fmaf(x[j], c, -mc));
+      for (int j = 0; j < 8; ++j) g[j] = st.y * lse_term(x[j], st.x, a.l.c);
       if (!DISTILL && (uint32_t)(label - col) < 8u) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) g[j] -= col + j == label ? st.z : 0.0f;
