@@ -1648,7 +1648,8 @@ hipError_t launch_lm_loss(LmLossArgs a, bool weight_bf16, hipStream_t s) {
     const int64_t all = nrt * lm_tiles(V), most = nrt > kLmLossRuns ? nrt : kLmLossRuns;
     return dim3((unsigned)(all < most ? all : most));
   };
-  const bool few = lm_few(R, a.l.V), by_workgroup = lm_by_workgroup(R, a.l.V, distill ? a.l.K : 0, a.H);
+  const bool few = lm_few_forward(R, a.l.V, a.dh != nullptr);
+  const bool by_workgroup = lm_by_workgroup(R, a.l.V, distill ? a.l.K : 0, a.H);
   // The distillation's join has 16 wavefronts a row, or, where its many rows fill the
   // chip, four: the loss of R rows of V x H, K members, us, 16 / 4: 600 of 5000 x 1024,
   // 16 and 64, 39.8 / 39.0, 47.3 / 52.7; 1000 of 2000 x 1024, 4 and 64, 33.6 / 29.5, 43.9 /

@@ -594,9 +594,17 @@ __host__ __device__ constexpr bool lm_few(int64_t R, int V) {
          (R <= kLmFewMost && (R + kLmFewRows - 1) / kLmFewRows * lm_few_groups(V) <= 2 * kLmCus);
 }
 // Few rows' logits (fp32) are kept for the gradient up to 256 MB, which the last
-// cache holds; beyond that g comes of products again.
+// cache holds; beyond that g comes of products again, and so do the sums that it
+// refers to: a row's maximum from sums in another order is not that of its x, which
+// a small temperature turns into any number (100 rows of 700 001 x 64 with gradients,
+// sums of 64-column products and of those, 592 and 580 us; 128 of
+// 600 000 x 4096, 3345 and 3114).
 __host__ __device__ constexpr int64_t lm_few_ldx(int V) { return (int64_t)lm_few_groups(V) * kLmFewCols; }
-constexpr bool lm_few_keeps(int64_t R, int V) { return lm_few(R, V) && R * lm_few_ldx(V) <= 1ll << 26; }
+__host__ __device__ constexpr bool lm_few_keeps(int64_t R, int V) { return lm_few(R, V) && R * lm_few_ldx(V) <= 1ll << 26; }
+// Whether the forward's products are those of few rows.
+__host__ __device__ constexpr bool lm_few_forward(int64_t R, int V, bool grad) {
+  return grad ? lm_few_keeps(R, V) : lm_few(R, V);
+}
 // Rows joined by a workgroup each, not by a wavefront: few rows, and the
 // distillation's dot products (K members; 0: cross entropy) where the rows are no
 // more than two workgroups per CU or long and many.  The loss of R rows of 32 000 x H
@@ -607,7 +615,8 @@ constexpr bool lm_few_keeps(int64_t R, int V) { return lm_few(R, V) && R * lm_fe
 constexpr bool lm_by_workgroup(int64_t R, int V, int K, int H) {
   return lm_few(R, V) || (K > 0 && (R <= 2 * kLmCus || ((int64_t)K * H >= 1 << 17 && R < 1 << 20)));  // (32-bit launch)
 }
-// Entries of the forward's log-sum-exps: two per run and row in play.
+// Entries of the forward's log-sum-exps: two per run and row in play (few rows: and
+// group of columns, which are more than the runs of another forward).
 inline int64_t lm_loss_parts(int64_t R, int V) {
   if (lm_few(R, V)) return 2 * R * lm_few_groups(V);
   const int64_t all = R * lm_tiles(V), runs = (int64_t)kLmLossRuns * kLmTile;

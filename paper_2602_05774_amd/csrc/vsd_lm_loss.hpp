@@ -494,7 +494,7 @@ __global__ __launch_bounds__(kThreads) void k_lm_loss_row_combine(LmLossArgs a) 
     }
   }
   if (in) {
-    const bool few = lm_few(a.l.R, a.l.V);
+    const bool few = lm_few_forward(a.l.R, a.l.V, a.dh != nullptr);
     const int parts = 2 * (few ? lm_few_groups(a.l.V) : a.plan->fwd_runs);
     const float2* part = a.part + i * (few ? parts : 1);
     const int64_t next = few ? 1 : a.plan->n;  // from one partial sum to the next
