@@ -232,7 +232,10 @@
  *   head (rows->hidden_dim > 0): the logits are formed tile by tile, and again,
  *   a piece of the vocabulary at a time, for the gradient; neither they nor
  *   their gradient are kept (the logits of few rows, or of a small vocabulary
- *   and up to 8192 rows, are, in the workspace: 256 MB at most).  grad_hidden [R, H] (bf16) receives g . weight and
+ *   and up to 8192 rows, are, in the workspace: 256 MB at most).  A logit is an
+ *   fp32 sum of H products, a member's in an order of its own (and at most the
+ *   row's largest logit): what its rounding is over T is the accuracy of the
+ *   results.  grad_hidden [R, H] (bf16) receives g . weight and
  *   grad_weight [v, H] (optional; fp32 or bf16, weight_dtype) g^T . hidden,
  *   both summed in fp32 over g rounded to bf16, written, not accumulated into.
  *   The top logits: per row the k largest of the logits above -inf, the larger

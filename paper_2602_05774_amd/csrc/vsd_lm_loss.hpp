@@ -387,6 +387,9 @@ __device__ __forceinline__ void lm_loss_finish(const LmLossArgs& a, int64_t i, i
   const int lane = threadIdx.x & 63;
   const bool live = s != 0.0f;
   const float tail = logf(s);
+  // a member's dot product, rounded in another order than the sums behind m, is not above
+  // the row's largest logit (a NaN stays one)
+  x = x > m ? m : x;
   float mass = 1.0f, loss;
   if (DISTILL) {
     const int K = a.l.K;

@@ -136,3 +136,26 @@ def test_few_rows_of_a_very_large_vocabulary_at_a_small_temperature():
     bar = (2.0 ** -8 * 1.01 * (a.abs() + b.abs()) / T + 2.0 ** -8 * dh.abs()) * 1.01
     off = (res.grad.grad_hidden.double() - dh).abs()
     assert torch.all((off <= bar)[sure]), (off / bar)[sure].amax(1)
+
+
+@pytest.mark.parametrize("R,V,H", AGAIN + KEPT)
+@pytest.mark.parametrize("T", (1e-4, 1e-6, 1e-9, 1e-30))
+def test_members_are_never_above_the_largest_logit(R, V, H, T):
+    """Labels and members at the rows' largest logits, whose own dot products may come out above
+    the maximum: no log q is above 0 and no q above 1."""
+    h, w = _head(R, V, H, 56)
+    x = h.double() @ w.double().t()
+    idx = x.topk(6, dim=1).indices.int()
+    labels = idx[:, 0].contiguous()
+    head = vsd.LmHead(h, w)
+    ce = vsd.cross_entropy(head, labels, temp_draft=T, grad=True, weight_grad=torch.float32)
+    assert torch.all(ce.loss_row >= 0)
+    _check(ce, _host(h), _host(w), lo.label_members(labels.cpu().numpy()), None, T, 1.0, V)
+    val = torch.randn(R, 6, device=DEV, generator=torch.Generator(device=DEV).manual_seed(57)).sort(dim=1, descending=True).values
+    mem = lo.teacher_members(idx.cpu().numpy(), val.double().cpu().numpy())
+    kd = vsd.distill_loss(head, idx, val, temp_draft=T, grad=True, weight_grad=torch.float32)
+    # sum p log p >= -log 6, each term to a few roundings (bars.loss_bar: 140), and no log q above 0
+    assert torch.all(kd.loss_row >= -math.log(6) - 1000 * bars.U)
+    for t in (*ce[:3], *ce.grad[::2], *kd[:3], *kd.grad[::2]):
+        assert torch.isfinite(t).all()
+    _check(kd, _host(h), _host(w), mem, None, T, 1.0, V)
