@@ -150,6 +150,8 @@ def _gradient(X, rows, dev, grad, weight_grad):
             _check("grad_weight", gw, gw.dtype, (v, H), dev)
         if grad.grad_hidden is None:
             raise ValueError("grad_hidden is required")
+        if weight_grad and gw is None:
+            raise ValueError("weight_grad needs grad=True, or a grad_weight to fill")
         return grad, _lib.VsdLossGrad(None, 0, grad.grad_hidden.data_ptr(), _ptr(gw),
                                       VSD_BF16 if gw is not None and gw.dtype == torch.bfloat16 else VSD_F32)
     if weight_grad:
