@@ -615,6 +615,7 @@ __host__ __device__ constexpr bool lm_few_forward(int64_t R, int V, bool grad) {
 constexpr bool lm_by_workgroup(int64_t R, int V, int K, int H) {
   return lm_few(R, V) || (K > 0 && (R <= 2 * kLmCus || ((int64_t)K * H >= 1 << 17 && R < 1 << 20)));  // (32-bit launch)
 }
+static_assert(kTotalRows <= kLmFewRows, "the total of so few rows is formed where a workgroup joins a row");
 // Entries of the forward's log-sum-exps: two per run and row in play (few rows: and
 // group of columns, which are more than the runs of another forward).
 inline int64_t lm_loss_parts(int64_t R, int V) {

@@ -442,37 +442,33 @@ template <bool DISTILL>
 __global__ __launch_bounds__(256) void k_lm_loss_combine(LmLossArgs a) {
   const int lane = threadIdx.x & 63;
   const int64_t i = (int64_t)blockIdx.x * 4 + wave_id(), n = a.plan->n;
-  if (i < n) {
-    const int64_t r = a.rows[i];
-    float m = kNegBig, s = 0.0f;
-    for (int e = lane; e < 2 * a.plan->fwd_runs; e += kWave) {
-      const float2 p = a.part[(int64_t)e * n + i];
-      lse_join(m, s, p.x, p.y, a.l.c);
-    }
-    wave_lse(m, s, a.l.c);
-    const bf16_t* h = a.hp + i * a.H;
-    const bf16_t* W = static_cast<const bf16_t*>(a.w);
-    float x = -INFINITY;
-    if (DISTILL) {
-      const int K = a.l.K, id = lane < K ? a.mid[r * K + lane] : -1;
-      constexpr int U = 4;
-      for (int k = 0; k < K; k += U) {
-        int v[U];
-        float xk[U];
-#pragma unroll
-        for (int u = 0; u < U; ++u) v[u] = lane_i(id, min(k + u, K - 1));
-        wave_dots<U>(h, W, v, a.H, lane, xk);
-#pragma unroll
-        for (int u = 0; u < U; ++u) x = lane == k + u ? xk[u] : x;
-      }
-    } else {
-      x = wave_dot(h, W + (int64_t)a.l.idx[r] * a.H, a.H, lane);
-    }
-    lm_loss_finish<DISTILL>(a, i, r, m, s, x);
+  if (i >= n) return;
+  const int64_t r = a.rows[i];
+  float m = kNegBig, s = 0.0f;
+  for (int e = lane; e < 2 * a.plan->fwd_runs; e += kWave) {
+    const float2 p = a.part[(int64_t)e * n + i];
+    lse_join(m, s, p.x, p.y, a.l.c);
   }
-  if (a.l.counter == nullptr) return;
-  __syncthreads();
-  total_by_last<256>(a.l);
+  wave_lse(m, s, a.l.c);
+  const bf16_t* h = a.hp + i * a.H;
+  const bf16_t* W = static_cast<const bf16_t*>(a.w);
+  float x = -INFINITY;
+  if (DISTILL) {
+    const int K = a.l.K, id = lane < K ? a.mid[r * K + lane] : -1;
+    constexpr int U = 4;
+    for (int k = 0; k < K; k += U) {
+      int v[U];
+      float xk[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) v[u] = lane_i(id, min(k + u, K - 1));
+      wave_dots<U>(h, W, v, a.H, lane, xk);
+#pragma unroll
+      for (int u = 0; u < U; ++u) x = lane == k + u ? xk[u] : x;
+    }
+  } else {
+    x = wave_dot(h, W + (int64_t)a.l.idx[r] * a.H, a.H, lane);
+  }
+  lm_loss_finish<DISTILL>(a, i, r, m, s, x);
 }
 
 // The same by a workgroup per row (lm_by_workgroup): few rows have two partial sums
