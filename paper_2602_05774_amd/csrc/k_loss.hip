@@ -21,6 +21,7 @@ namespace vsd {
 
 namespace {
 
+constexpr int kMembersFirstRows = 8192, kMembersFirstCols = 512 * 64 / 8 * 7;
 template <typename T, bool DISTILL, bool GRAD, int kThreads, int kNch, bool kMore>
 __device__ __forceinline__ void row_loss(const LossArgs& a) {
   constexpr int kWaves = kThreads / kWave, kStep = kThreads * 8;
@@ -68,13 +69,17 @@ __device__ __forceinline__ void row_loss(const LossArgs& a) {
     sp[lane] = e.p;
     if (lane == 0) sum_p = total;
   };
-  // The first wavefront's probabilities: while the row is on its way, but for rows of
-  // 512 threads x 8 before it is asked for (us, before / meanwhile: 16 384 x 32 000
-  // bf16 399 / 417, 4096 x 128 256 490 / 457, 9930 x 4673 68 / 66, 4000 x 9000
-  // float32 89 / 85).
-  constexpr bool kMembersFirst = DISTILL && kThreads == 512 && kNch == 8;
+  // The first wavefront's probabilities: while the row is on its way, but for many rows
+  // that fill at least 7/8 of 512 threads x 64 columns before it is asked for (us, before /
+  // meanwhile, bf16: 16 384 rows of 32 000, 4, 16 and 32 members, 390 / 410, 397 / 416 and
+  // 412 / 423; 16 384 of 28 672, 16, 355 / 372; 8192 of 32 768, 16, 217 / 227; 8192 of
+  // 29 500, 16, 201 / 204; but 4096 of 30 522, 16, 117 / 116; 96 of 32 000, 10, 20.2 / 19.4;
+  // 16 384 of 17 000 and 24 000, 32, 283 / 258 and 330 / 313; other threads and columns:
+  // 4096 of 128 256, 64, 499 / 471; 9930 of 4673, 46, 68 / 66; 4000 of 9000 float32, 90 / 85).
+  constexpr bool kMaybeFirst = DISTILL && kThreads == 512 && kNch == 8;
+  const bool members_first = kMaybeFirst && a.R >= kMembersFirstRows && a.V >= kMembersFirstCols;
   if (live) {
-    if constexpr (kMembersFirst) {
+    if (members_first) {
       members();
       __syncthreads();
     }
@@ -82,7 +87,7 @@ __device__ __forceinline__ void row_loss(const LossArgs& a) {
 #pragma unroll
       for (int j = 0; j < kNch; ++j) load_cols(row[j], X, first + j * kStep, a.V);
     }
-    if constexpr (!kMembersFirst) members();
+    if (!members_first) members();
     if constexpr (kNch > 0) {
 #pragma unroll
       for (int j = 0; j < kNch; ++j) {

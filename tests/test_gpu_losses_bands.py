@@ -87,6 +87,27 @@ def test_distillation_through_the_head(R, V, H, K, grad):
     _check_head(res, _host(h), _host(w), mem, weight, 0.9, 0.5, V)
 
 
+@pytest.mark.parametrize("R,V", ((8192, 28672), (8191, 30522), (8192, 30522), (8200, 28671)))
+def test_distillation_of_many_rows(R, V):
+    """Probabilities formed before the row is read and meanwhile, at both sides of the rule.  Every
+    row against the first of its kind, those against the oracle."""
+    kinds, K = 8, 13
+    _, few = _rows(kinds, V, "bf16", 66)
+    mem, (idx, val, z) = _members(kinds, V, K, 9, True, 1.25, dup=True)
+    reps = -(-R // kinds)
+    X = torch.full((R, (V + 7) // 8 * 8), math.nan, dtype=torch.bfloat16, device=DEV)[:, :V]
+    X.copy_(few.repeat(reps, 1)[:R])
+    many = [t.repeat(reps, *[1] * (t.dim() - 1))[:R].contiguous() for t in (idx, val, z)]
+    res = vsd.distill_loss(X, *many, temp_draft=0.8, temp_target=1.25, loss_scale=0.5, grad=True)
+    for r in range(0, R - R % kinds, 1024):
+        part = res.grad[r:min(R - R % kinds, r + 1024)]
+        assert torch.equal(part, res.grad[:kinds].repeat(len(part) // kinds, 1))
+    assert torch.equal(res.loss_row, res.loss_row[:kinds].repeat(reps)[:R])
+    ref = lo.losses(_host(few), *mem, None, 0.8, 0.5)
+    first = vsd.LossResult(res.loss_row[:kinds], res.lse[:kinds], torch.tensor(ref["total"]), res.grad[:kinds], res.device_error)
+    _check(first, _host(few), mem, None, 0.8, 0.5, "bf16")
+
+
 def test_as_many_rows_as_leave_the_wide_launches():
     """2^22 rows of more than 4096 columns: 256 threads a row that read it twice, here into the
     logits' own place.  Every row against the first of its kind, those against the oracle."""
