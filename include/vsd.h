@@ -240,7 +240,8 @@
  *   both summed in fp32 over g rounded to bf16, written, not accumulated into.
  *   The top logits: per row the k largest of the logits above -inf, the larger
  *   first, equal ones by the smaller index; slots past them hold -1 and -inf;
- *   lse[r] = log sum_v exp(y_v / temp_target) over all v columns.  With a map
+ *   lse[r] = log sum_v exp(y_v / temp_target) over all v columns (a NaN, which is
+ *   no entry, or +inf makes it NaN).  With a map
  *   d2t only the columns d2t[u] take part, each with the index u in [0,
  *   v_draft) (the lse stays that of all columns).
  *   loss_row, lse, top_idx ... hold R rows, contiguous; R < 2^24 (top logits:

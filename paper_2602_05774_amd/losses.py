@@ -269,7 +269,8 @@ def top_logits(Y, k, d2t=None, temp_target=1.0, workspace=None, device_error=Non
 
     d2t [v_draft] int32: only the columns d2t[u] take part, each with its draft
     index u (lse stays that of the whole row).  Equal logits: the smaller index
-    first; -inf logits are no entries.  Returns TopLogits."""
+    first; -inf and NaN logits are no entries (NaN and +inf make lse NaN).  Returns
+    TopLogits."""
     lib = _lib.load()
     if isinstance(Y, LmHead):
         raise ValueError("top_logits takes materialised logits")
