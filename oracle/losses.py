@@ -4,7 +4,7 @@
     distillation   l = sum_k p_k (log p_k - log q_{i_k})
     gradient       scale w / T (P q - sum_k p_k e_{i_k}),  q = softmax(x / T)
 
-members() gives every row's members; losses() the losses and the logits'
+label_members() and teacher_members() give every row's members; losses() the losses and the logits'
 gradient for them; head() the same through an LM head.
 """
 import numpy as np

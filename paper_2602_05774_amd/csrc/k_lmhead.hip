@@ -30,8 +30,6 @@
 #include "vsd_loss.hpp"
 #include "vsd_topk.hpp"
 
-
-
 namespace vsd {
 
 namespace {

@@ -7,8 +7,10 @@
 //
 // One workgroup per row.  With the gradient the row stays in registers (kNch
 // groups of eight columns per thread, all loads in flight at once) while its
-// log-sum-exp is formed, so the logits are read once and g is written once;
-// longer rows (kNch = 0) are read twice.  A row out of play is not read.
+// log-sum-exp is formed, so the logits are read once and g is written once; of
+// rows longer than 1024 threads hold the rest is read twice (kMore).  With kNch = 0
+// nothing is kept: the loss alone, and rows too many for wide workgroups, which are
+// read twice.  A row out of play is not read.
 //
 // Bound by those bytes: 20 480 rows of 32 000 (bf16, a quarter out of play) with
 // gradient in 440 us, 5.2 TB/s; 8192 of 128 256 in 786 us, 5.1 TB/s (a large copy:

@@ -484,8 +484,8 @@ vsd_status static_scratch(void** ptr) {
 }
 
 // ------------------------------------------------------------ base losses ---
-// A launch counts its work-items in 32 bits: 256 a row for the losses, 1024 for
-// the top logits.
+// Rows of a vsd_top_logits call: its documented limit (a launch counts its work-items,
+// 256 a row at most, in 32 bits).
 constexpr int64_t kMaxTopRows = (int64_t)1 << 22;
 constexpr int32_t kMaxVocab = (int32_t)1 << 30;  // column numbers of a sweep's last step stay within 32 bits
 

@@ -468,10 +468,11 @@ struct LossArgs {
 constexpr int64_t kTotalRows = 64;
 
 // Threads per row of the losses on materialised logits.  With the gradient a row
-// stays in registers: 32 columns a thread (float32: 16), 64 for 512 threads
-// (32 for 1024), and, what 1024 threads do not hold (131 072 columns, float32:
-// 65 536), the rest of it is read twice.  A launch counts its work-items in 32
-// bits: past 2^22 rows, 256 threads that read the row twice.
+// stays in registers, by its length: bf16 32 columns a thread of 64 to 512 threads,
+// then 64 of 512 and of 1024, then 128 of 1024; float32 32 of 64, 16 of 256 to 1024,
+// then 32 and 64 of 1024.  What 1024 threads do not hold (131 072 columns, float32:
+// 65 536) is read twice.  A launch counts its work-items in 32 bits: from 2^22 rows
+// on, rows of more than 4096 columns have 256 threads, which read them twice.
 // us of cross_entropy by threads x groups of eight columns:
 //   gradient, bf16    65 536 x 500      256 x 1  141     64 x 4    78
 //                     65 536 x 2000     256 x 1  194     64 x 4   118
@@ -607,11 +608,14 @@ __host__ __device__ constexpr bool lm_few_forward(int64_t R, int V, bool grad) {
 }
 // Rows joined by a workgroup each, not by a wavefront: few rows, and the
 // distillation's dot products (K members; 0: cross entropy) where the rows are no
-// more than two workgroups per CU or long and many.  The loss of R rows of 32 000 x H
-// by a wavefront and by a workgroup, us: R = 200, H = 2048, 16 and 64 members, 74.3
-// and 68.9, 95.7 and 75.8; 400, H = 256, 2 and 64, 38.0 and 39.7, 50.7 and 43.5; 700,
-// H = 2048, 2 and 64, 116 and 121, 145 and 143; 2000, H = 4096, 16 and 64, 481 and
-// 479, 615 and 585; 4000, H = 256, 64, 133 and 167; H = 2048, 64, 616 and 586.
+// more than two workgroups per CU or the products of a row are many.  The loss of R
+// rows of 32 000 x H with K members by a wavefront and by a workgroup, us: 400 rows,
+// H = 256, K = 2, 16 and 64, 38.5 / 39.1, 40.3 / 40.1, 51.3 / 44.5; H = 4096, K = 1 and
+// 16, 133.7 / 134.5, 144.2 / 138.1 (a member or two costs up to 1.2 us, many save up to
+// 11); 512 rows, H = 2048, K = 16, 92.0 / 89.0; beyond them K = 64 and H = 2048 of 1000,
+// 2000 and 9001 rows, 170 / 172, 324 / 315, 1364 / 1291; H = 4096, 315 / 310, 622 / 591,
+// 2650 / 2514; fewer products, 2000 rows, H = 1024, K = 64, 178 / 183; 9001, H = 2048,
+// K = 32, 1170 / 1157; 4000, H = 256, K = 64, 133 / 167.
 constexpr bool lm_by_workgroup(int64_t R, int V, int K, int H) {
   return lm_few(R, V) || (K > 0 && (R <= 2 * kLmCus || ((int64_t)K * H >= 1 << 17 && R < 1 << 20)));  // (32-bit launch)
 }

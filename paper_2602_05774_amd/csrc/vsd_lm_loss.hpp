@@ -1,8 +1,10 @@
 // The base losses through an LM head: logits x = h W^T formed tile by tile by
 // k_lmhead.hip's product loop (which includes this file after it) and consumed
-// in the accumulators.  Neither they (but for few rows) nor their gradient are kept: g is formed a
-// piece of the vocabulary at a time, in bf16 (the operand type of the two
-// products that read it), and both add up in fp32.
+// in the accumulators.  Neither they (but for few rows, and up to 8192 of a small
+// vocabulary: lm_few_keeps) nor their gradient are kept: g is formed a piece of the
+// vocabulary at a time, in bf16 (the operand type of the two products that read it:
+// against 64 bits bf16 gradients are off by 0.0022 of their size, 0.0017 with g in
+// fp32), and both add up in fp32.
 //
 //   rows     the rows that take part are listed and their hidden states copied
 //            to consecutive rows, followed by zero rows up to a multiple of 64:
