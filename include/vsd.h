@@ -24,6 +24,12 @@
  *   vsd_distill_loss      gradients: softmax cross entropy, and distillation
  *                         from a teacher's top logits, which
  *   vsd_top_logits        picks from the teacher's rows.
+ *   vsd_sample_rows       One token per row under the deployed rule: temperature,
+ *                         top-k, top-p, min-p, from given random numbers.
+ *   vsd_quantize_blocks,  A frozen head held in 8 bits: values with a scale for
+ *   vsd_block_product     each block of 128, and products of such matrices.
+ *   vsd_grad_norm,        The global norm of many gradients, and their scaling
+ *   vsd_clip_gradients    to a bound before an optimizer's step.
  *
  * Every call takes the logits either materialised ([R, ld] arrays) or, in
  * the fused LM-head variant (dims->hidden_dim > 0), as hidden states and an
@@ -248,6 +254,63 @@
  *   2^22), k <= VSD_MAX_TOP, temperatures in [1e-30, 1e30].  Calls that may
  *   overlap on the device need workspaces (and counters) of their own; a
  *   workspace may hold anything before a call.
+ *
+ * Draws under the deployed rule (vsd_sample_rows)
+ * -----------------------------------------------
+ *   Any R rows of v logits (vsd_rows, materialised), row r with its own number
+ *   u = u[r] in [0, 1) and settings T (temperature), k (top-k; 0: off), p
+ *   (top-p; 1: off), m (min-p; 0: off).  The row's entries are its logits above
+ *   -inf; with M the largest, w_v = exp((x_v - M) / T), 1 where x_v = M.  In
+ *   the order "larger logit, then smaller index":
+ *     top-k  keeps the first k entries (all, if there are fewer);
+ *     top-p  keeps of these the shortest prefix whose w sum to at least p times
+ *            the sum over all of them;
+ *     min-p  keeps of these the entries with w >= m.
+ *   With Z the sum of w over the kept entries, the token is the smallest index v
+ *   such that the kept entries up to v sum to more than u Z; log_prob[r] = log
+ *   (w_tok / Z), kept[r] their number.  T = 0 is greedy: the first entry in the
+ *   order (log_prob 0, kept 1; u, k, p and m play no part but must be valid).
+ *   Sums and comparisons are carried in 64 bits, so a token differs from that of
+ *   exact arithmetic only where a border lies within some 1e-14 of u or p.
+ *   A row without an entry has token -1, log_prob 0 and kept 0, one with a NaN
+ *   token -1, log_prob NaN and kept 0.  A row whose u or settings lie outside
+ *   their range (T = 0 or in [1e-30, 1e30], k >= 0, 0 < p <= 1, 0 <= m <= 1)
+ *   has token -1, log_prob 0 and kept 0 and reports VSD_DEVERR_SETTING_RANGE.
+ *
+ * Block matrices (vsd_quantize_blocks, vsd_block_product)
+ * -------------------------------------------------------
+ *   A block matrix [rows, cols] holds 8-bit values (OCP e4m3: 4 exponent and 3
+ *   mantissa bits, largest 448) with one fp32 scale for every `group` rows (1 or
+ *   128) x 128 columns:
+ *     x[i][j] = scales[j / 128][i / group] values[i][j].
+ *   Row i of the values starts at byte i*ld, ld a multiple of 128 >= cols; the
+ *   bytes past cols are zero.  scales[b] starts at element b*scale_ld, scale_ld
+ *   >= ceil(rows / group).
+ *   Quantising: scale = max(amax / 448, 2^-126), amax the block's largest
+ *   magnitude, and value = e4m3(x / scale): the fp32 quotient, to the nearest
+ *   value, ties to the even one.  A block with a NaN or an infinity has the
+ *   scale NaN.
+ *   Product: out[i][j] = sum_k a[i][k] b[j][k] over matrices with the same cols,
+ *   a with group 1, b with 1 or 128.  The products of a block's 8-bit values are
+ *   summed on the matrix cores, each such sum is multiplied by the product of
+ *   its two scales and added in fp32.  An fp32 result's sums are fp32 ones; a
+ *   bf16 result's come from the 8-bit matrix instructions, at twice the rate,
+ *   which cut each of eight products 2^13 below the largest's exponent (some
+ *   1e-5 of a sum of random terms; the result's rounding is 2^-8).  An output row depends on the
+ *   same row of a alone and an output column on the same row of b.  The three
+ *   products of a linear layer y = x w^T, with matrices quantised along the
+ *   dimension that is summed over: y from x and w; dx from dy and w^T; dw from
+ *   dy^T and x^T.
+ *
+ * Gradient norm and clipping (vsd_grad_norm, vsd_clip_gradients)
+ * --------------------------------------------------------------
+ *   norm = sqrt(sum over all tensors of the squares of their elements), summed
+ *   in 64 bits (no overflow, no underflow in fp32's range); scale = max_norm /
+ *   norm where norm > max_norm, else 1; every element becomes fp32(g) * scale,
+ *   rounded once to the output's type.  In place a scale of 1 writes nothing.
+ *   A norm that is not finite (a NaN or an infinity among the gradients) leaves
+ *   the tensors as they are (out of place: copies them) with scale NaN, by which
+ *   a trainer skips its step.  max_norm = +inf clips nothing.
  */
 #ifndef VSD_H
 #define VSD_H
@@ -279,9 +342,10 @@ enum {
   VSD_DEVERR_TOKEN_RANGE = 1, /* token outside [-1, v_draft) or -1 on a live slot */
   VSD_DEVERR_MAP_RANGE = 2,   /* d2t entry outside [0, v_target) */
   VSD_DEVERR_DEPTH_RANGE = 3, /* valid_depth entry outside [1, L] */
-  VSD_DEVERR_MAP_DUPLICATE = 4 /* two d2t entries name the same target token
+  VSD_DEVERR_MAP_DUPLICATE = 4, /* two d2t entries name the same target token
                                   (detected where the map is inverted: the
                                   fused LM head's draws, verification) */
+  VSD_DEVERR_SETTING_RANGE = 5 /* vsd_sample_rows: a row's u or setting out of range */
 };
 
 typedef enum vsd_dtype { VSD_F32 = 0, VSD_BF16 = 1 } vsd_dtype;
@@ -394,6 +458,38 @@ typedef struct vsd_loss_grad {
   void* grad_weight;     /* fused, optional: [v, H] */
   int32_t weight_dtype;  /* vsd_dtype of grad_weight */
 } vsd_loss_grad;
+
+/* The rule of vsd_sample_rows (see above): a setting for all rows, or, where the
+ * array is given, one per row ([R]). */
+typedef struct vsd_draw {
+  float temp;               /* 0: greedy */
+  int32_t top_k;            /* 0: off */
+  float top_p;              /* 1: off */
+  float min_p;              /* 0: off */
+  const float* row_temp;    /* optional */
+  const int32_t* row_top_k; /* optional */
+  const float* row_top_p;   /* optional */
+  const float* row_min_p;   /* optional */
+} vsd_draw;
+
+/* A block matrix (see above). */
+typedef struct vsd_blocks {
+  void* values;      /* [rows, ld] bytes, 16-byte aligned */
+  float* scales;     /* [ceil(cols / 128), scale_ld] */
+  int64_t rows;      /* 1 <= rows < 2^31 */
+  int64_t cols;      /* 1 <= cols < 2^31 */
+  int64_t ld;        /* a multiple of 128 >= cols */
+  int64_t scale_ld;  /* >= ceil(rows / group) */
+  int32_t group;     /* rows of a block: 1 or 128 */
+} vsd_blocks;
+
+/* One gradient: `rows` rows of `cols` elements, row r at element r*ld (a tensor
+ * that lies in one piece: one row). */
+typedef struct vsd_tensor {
+  void* data;        /* aligned to its element size */
+  int64_t rows, cols, ld;
+  int32_t dtype;     /* vsd_dtype */
+} vsd_tensor;
 
 /* E-step sampling (Alg. 1: z~ ~ q and z' ~ p; Alg. 2: z-bar greedy).
  * Writes tok_draft, tok_target, tok_greedy ([R] int32 each, draft-index
@@ -609,6 +705,43 @@ vsd_status vsd_top_logits(const vsd_rows* rows, const vsd_src* target, int32_t k
 /* Bytes of workspace the calls above need (host only). */
 vsd_status vsd_loss_workspace_bytes(const vsd_rows* rows, int32_t k, int32_t with_grad, size_t* bytes);
 vsd_status vsd_top_workspace_bytes(const vsd_rows* rows, int32_t with_map, size_t* bytes);
+
+/* One token per row (see "Draws under the deployed rule").  u [R]; tok [R];
+ * log_prob and kept [R] optional.  Materialised logits only; R < 2^22.
+ * `workspace` must hold vsd_draw_workspace_bytes() bytes (16-B aligned). */
+vsd_status vsd_sample_rows(const vsd_rows* rows, const vsd_src* target, const vsd_draw* draw, const float* u,
+                           int32_t* tok, float* log_prob, int32_t* kept, void* workspace, size_t workspace_bytes,
+                           int32_t* device_error, void* hip_stream);
+vsd_status vsd_draw_workspace_bytes(const vsd_rows* rows, size_t* bytes);
+
+/* Quantises x [rows, cols] (dtype, row stride ld >= cols elements, any alignment
+ * of its elements), or, with transpose, x^T: out->rows x out->cols is then cols x
+ * rows.  Writes all of out's rows up to ld (zeros past cols) and all scales. */
+vsd_status vsd_quantize_blocks(const void* x, int64_t rows, int64_t cols, int64_t ld, int32_t dtype, int32_t transpose,
+                               const vsd_blocks* out, void* hip_stream);
+
+/* out [a->rows, b->rows] (out_dtype, row stride out_ld elements, 16-byte aligned
+ * rows) = a b^T.  Columns past b->rows are not touched.  `workspace` must hold
+ * vsd_product_workspace_bytes(a, b) bytes (16-B aligned; it may be 0). */
+vsd_status vsd_block_product(const vsd_blocks* a, const vsd_blocks* b, void* out, int64_t out_ld, int32_t out_dtype,
+                             void* workspace, size_t workspace_bytes, void* hip_stream);
+vsd_status vsd_product_workspace_bytes(const vsd_blocks* a, const vsd_blocks* b, size_t* bytes);
+
+/* norm [1] of n >= 1 tensors (the array is host memory, read during the call;
+ * tensors without elements are allowed).  `workspace` must hold
+ * vsd_norm_workspace_bytes(n) bytes (16-B aligned). */
+vsd_status vsd_grad_norm(const vsd_tensor* grads, int32_t n, float* norm, void* workspace, size_t workspace_bytes,
+                         void* hip_stream);
+
+/* Scales n gradients to max_norm > 0: norm_out [1] (optional) and scale [1]
+ * (optional).  norm [1], if given, is used in place of the tensors' own (that of
+ * more tensors, or of all ranks; it is read when the stream gets there).  out:
+ * NULL for in place, or n tensors of the same rows and cols, of either dtype, each
+ * the gradient's own memory or none that the call reads.  Workspace as above. */
+vsd_status vsd_clip_gradients(const vsd_tensor* grads, const vsd_tensor* out, int32_t n, float max_norm,
+                              const float* norm, float* norm_out, float* scale, void* workspace,
+                              size_t workspace_bytes, void* hip_stream);
+vsd_status vsd_norm_workspace_bytes(int32_t n, size_t* bytes);
 
 const char* vsd_status_string(vsd_status status); /* static string */
 const char* vsd_last_error(void);                 /* thread-local detail */

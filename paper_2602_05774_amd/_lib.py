@@ -16,7 +16,7 @@ STATUS_NAMES = {0: "VSD_OK", 1: "VSD_ERR_NULL_POINTER", 2: "VSD_ERR_INVALID_SHAP
                 3: "VSD_ERR_INVALID_VALUE", 4: "VSD_ERR_MISALIGNED", 5: "VSD_ERR_MAP_REQUIRED",
                 6: "VSD_ERR_UNSUPPORTED", 7: "VSD_ERR_WORKSPACE", 8: "VSD_ERR_HIP"}
 DEVERR_NAMES = {0: "none", 1: "token out of range", 2: "map entry out of range", 3: "depth out of range",
-                4: "duplicate map entry"}
+                4: "duplicate map entry", 5: "setting out of range"}
 
 VSD_F32, VSD_BF16 = 0, 1
 VSD_GRAD_BASIC, VSD_GRAD_ARW, VSD_GRAD_ARW_CAR = 0, 1, 2
@@ -68,6 +68,20 @@ class VsdLossGrad(ctypes.Structure):
                 ("weight_dtype", c_i32)]
 
 
+class VsdDraw(ctypes.Structure):
+    _fields_ = [("temp", c_f32), ("top_k", c_i32), ("top_p", c_f32), ("min_p", c_f32),
+                ("row_temp", c_vp), ("row_top_k", c_vp), ("row_top_p", c_vp), ("row_min_p", c_vp)]
+
+
+class VsdBlocks(ctypes.Structure):
+    _fields_ = [("values", c_vp), ("scales", c_vp), ("rows", c_i64), ("cols", c_i64), ("ld", c_i64),
+                ("scale_ld", c_i64), ("group", c_i32)]
+
+
+class VsdTensor(ctypes.Structure):
+    _fields_ = [("data", c_vp), ("rows", c_i64), ("cols", c_i64), ("ld", c_i64), ("dtype", c_i32)]
+
+
 VSD_MAX_TOP = 64
 
 _lib = None
@@ -77,6 +91,8 @@ EXPORTS = ("vsd_sample_paths", "vsd_score_paths", "vsd_sample_score_paths", "vsd
            "vsd_sample_step", "vsd_score_paths_ctx", "vsd_weighted_loss_bwd_ctx", "vsd_verify_paths",
            "vsd_cross_entropy", "vsd_distill_loss", "vsd_top_logits", "vsd_loss_workspace_bytes",
            "vsd_top_workspace_bytes",
+           "vsd_sample_rows", "vsd_draw_workspace_bytes", "vsd_quantize_blocks", "vsd_block_product",
+           "vsd_product_workspace_bytes", "vsd_grad_norm", "vsd_clip_gradients", "vsd_norm_workspace_bytes",
            "vsd_score_workspace_bytes", "vsd_score_workspace_best_bytes", "vsd_status_string", "vsd_last_error", "vsd_abi_version")
 
 
@@ -135,6 +151,20 @@ def load():
     lib.vsd_loss_workspace_bytes.restype = c_i32
     lib.vsd_top_workspace_bytes.argtypes = [P(VsdRows), c_i32, P(ctypes.c_size_t)]
     lib.vsd_top_workspace_bytes.restype = c_i32
+    lib.vsd_sample_rows.argtypes = [P(VsdRows), P(VsdSrc), P(VsdDraw), c_vp, c_vp, c_vp, c_vp, c_vp, ctypes.c_size_t,
+                                    c_vp, c_vp]
+    lib.vsd_draw_workspace_bytes.argtypes = [P(VsdRows), P(ctypes.c_size_t)]
+    lib.vsd_quantize_blocks.argtypes = [c_vp, c_i64, c_i64, c_i64, c_i32, c_i32, P(VsdBlocks), c_vp]
+    lib.vsd_block_product.argtypes = [P(VsdBlocks), P(VsdBlocks), c_vp, c_i64, c_i32, c_vp, ctypes.c_size_t, c_vp]
+    lib.vsd_product_workspace_bytes.argtypes = [P(VsdBlocks), P(VsdBlocks), P(ctypes.c_size_t)]
+    lib.vsd_grad_norm.argtypes = [P(VsdTensor), c_i32, c_vp, c_vp, ctypes.c_size_t, c_vp]
+    lib.vsd_clip_gradients.argtypes = [P(VsdTensor), P(VsdTensor), c_i32, c_f32, c_vp, c_vp, c_vp, c_vp,
+                                       ctypes.c_size_t, c_vp]
+    lib.vsd_norm_workspace_bytes.argtypes = [c_i32, P(ctypes.c_size_t)]
+    for call in (lib.vsd_sample_rows, lib.vsd_draw_workspace_bytes, lib.vsd_quantize_blocks, lib.vsd_block_product,
+                 lib.vsd_product_workspace_bytes, lib.vsd_grad_norm, lib.vsd_clip_gradients,
+                 lib.vsd_norm_workspace_bytes):
+        call.restype = c_i32
     lib.vsd_status_string.argtypes = [c_i32]
     lib.vsd_status_string.restype = ctypes.c_char_p
     lib.vsd_last_error.argtypes = []

@@ -1,0 +1,145 @@
+// Quantising to 8-bit values with a scale per block of 1 x 128 or 128 x 128, of a
+// matrix or of its transpose (vsd_quantize_blocks).
+//
+// A workgroup owns a tile of 128 x 128 elements: a thread holds 8 x 8 of them,
+// the magnitudes' maxima meet in LDS, and every quotient is one IEEE division.
+#include "vsd_device.hpp"
+#include "vsd_kernels.hpp"
+
+namespace vsd {
+
+namespace {
+
+constexpr int kThreads = 256;
+
+// Magnitudes as integers: the larger number is the larger integer, a NaN above
+// infinity, so a maximum keeps it.
+__device__ __forceinline__ uint32_t magnitude(float x) { return __float_as_uint(x) & 0x7FFFFFFFu; }
+
+__device__ __forceinline__ float scale_of(uint32_t amax) {
+  return amax >= 0x7F800000u ? __builtin_nanf("") : fmaxf(__uint_as_float(amax) / 448.0f, 1.17549435e-38f);
+}
+// What a block's elements are divided by: its scale, or 1 where that is NaN (its
+// values then mean nothing, but padding stays zero).
+__device__ __forceinline__ float divisor(float scale) { return scale == scale ? scale : 1.0f; }
+
+// Two values, rounded to the nearest, ties to even (v_cvt_pk_fp8_f32): |x / s| <=
+// 448 up to a rounding that the conversion takes back.
+__device__ __forceinline__ uint32_t pack4(float a, float b, float c, float d) {
+  int v = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+  v = __builtin_amdgcn_cvt_pk_fp8_f32(c, d, v, true);
+  return (uint32_t)v;
+}
+
+// TRANS: the result's rows are x's columns.
+template <typename T, int kGroup, bool TRANS>
+__global__ __launch_bounds__(kThreads) void k_quantize(QuantArgs a) {
+  __shared__ uint32_t part[16][128];
+  __shared__ __align__(16) uint32_t out[TRANS ? 128 * 33 : 1];
+  const int t = threadIdx.x, tr = t >> 4, tc = t & 15;
+  const int64_t row0 = (int64_t)(blockIdx.x / a.col_tiles) * 128, col0 = (int64_t)(blockIdx.x % a.col_tiles) * 128;
+  const T* X = static_cast<const T*>(a.x);
+  float x[8][8];  // rows row0 + tr * 8 + i, columns col0 + tc * 8 + k
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const int64_t r = row0 + tr * 8 + i, c = col0 + tc * 8;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) x[i][k] = r < a.rows && c + k < a.cols ? load1(X + r * a.ld + c + k) : 0.0f;
+  }
+  uint32_t amax[8];  // of a row (TRANS: of a column) of the thread's
+#pragma unroll
+  for (int i = 0; i < 8; ++i) amax[i] = 0;
+#pragma unroll
+  for (int i = 0; i < 8; ++i)
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      const int at = TRANS ? k : i;
+      amax[at] = max(amax[at], magnitude(x[i][k]));
+    }
+  const int mine = TRANS ? tc : tr, other = TRANS ? tr : tc;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) part[other][mine * 8 + i] = amax[i];
+  __syncthreads();
+  if (t < 128) {
+    uint32_t top = part[0][t];
+    for (int k = 1; k < 16; ++k) top = max(top, part[k][t]);
+    part[0][t] = top;
+  }
+  __syncthreads();
+  if (kGroup == 128) {
+    if (t < kWave) {
+      uint32_t top = max(part[0][t], part[0][t + 64]);
+#pragma unroll
+      for (int d = 1; d < kWave; d <<= 1) top = max(top, (uint32_t)__shfl_xor((int)top, d));
+      part[0][t] = part[0][t + 64] = top;
+    }
+    __syncthreads();
+  }
+  float s[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) s[i] = divisor(scale_of(part[0][mine * 8 + i]));
+  // the tile of the result: rows out_row0 .., block b of the columns
+  const int64_t out_row0 = TRANS ? col0 : row0, b = (TRANS ? row0 : col0) / 128;
+  const int64_t out_rows = TRANS ? a.cols : a.rows;
+  if (t < 128 && (kGroup == 1 ? out_row0 + t < out_rows : t == 0))
+    a.scales[b * a.scale_ld + out_row0 / kGroup + t] = scale_of(part[0][t]);
+  if (!TRANS) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int64_t r = row0 + tr * 8 + i;
+      float q[8];
+#pragma unroll
+      for (int k = 0; k < 8; ++k) q[k] = x[i][k] / s[i];
+      if (r < a.rows)
+        *reinterpret_cast<uint2*>(a.values + r * a.out_ld + col0 + tc * 8) =
+            make_uint2(pack4(q[0], q[1], q[2], q[3]), pack4(q[4], q[5], q[6], q[7]));
+    }
+    return;
+  }
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    float q[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) q[i] = x[i][k] / s[k];
+    uint32_t* const to = out + (tc * 8 + k) * 33 + tr * 2;
+    to[0] = pack4(q[0], q[1], q[2], q[3]);
+    to[1] = pack4(q[4], q[5], q[6], q[7]);
+  }
+  __syncthreads();
+  for (int i = t; i < 128 * 32; i += kThreads) {
+    const int c = i >> 5, w = i & 31;
+    if (col0 + c < a.cols)
+      *reinterpret_cast<uint32_t*>(a.values + (col0 + c) * a.out_ld + row0 + w * 4) = out[c * 33 + w];
+  }
+}
+
+// Zeros in whole blocks of padding columns (a stride past the last block).
+__global__ __launch_bounds__(kThreads) void k_quant_pad(uint8_t* values, int64_t rows, int64_t from, int64_t ld) {
+  const int64_t per = (ld - from) / 16, n = rows * per;
+  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < n; i += (int64_t)gridDim.x * kThreads)
+    *reinterpret_cast<uint4*>(values + i / per * ld + from + i % per * 16) = make_uint4(0, 0, 0, 0);
+}
+
+template <typename T>
+hipError_t launch_t(const QuantArgs& a, int group, bool trans, hipStream_t s) {
+  const dim3 grid((unsigned)a.tiles), block(kThreads);
+  if (group == 1 && !trans) hipLaunchKernelGGL((k_quantize<T, 1, false>), grid, block, 0, s, a);
+  if (group == 1 && trans) hipLaunchKernelGGL((k_quantize<T, 1, true>), grid, block, 0, s, a);
+  if (group != 1 && !trans) hipLaunchKernelGGL((k_quantize<T, 128, false>), grid, block, 0, s, a);
+  if (group != 1 && trans) hipLaunchKernelGGL((k_quantize<T, 128, true>), grid, block, 0, s, a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_quantize(const QuantArgs& a, bool bf16, int group, bool trans, hipStream_t s) {
+  const int64_t done = ((trans ? a.rows : a.cols) + 127) / 128 * 128;
+  if (done < a.out_ld) {
+    hipLaunchKernelGGL(k_quant_pad, dim3(1024), dim3(kThreads), 0, s, a.values, trans ? a.cols : a.rows, done, a.out_ld);
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  return bf16 ? launch_t<bf16_t>(a, group, trans, s) : launch_t<float>(a, group, trans, s);
+}
+
+}  // namespace vsd

@@ -693,6 +693,139 @@ TopLayout top_layout(const vsd_rows* rows) {
   return w;
 }
 
+// ------------------------------------------------ draws, block matrices, gradients ---
+bool usable_setting(const vsd_draw* d) {
+  return (d->row_temp != nullptr || d->temp == 0.0f || usable_temp(d->temp)) &&
+         (d->row_top_k != nullptr || d->top_k >= 0) &&
+         (d->row_top_p != nullptr || (d->top_p > 0.0f && d->top_p <= 1.0f)) &&
+         (d->row_min_p != nullptr || (d->min_p >= 0.0f && d->min_p <= 1.0f));
+}
+
+constexpr int64_t kMaxBlockDim = ((int64_t)1 << 31) - 1;
+constexpr int64_t kMaxWorkgroups = (int64_t)1 << 24;  // of 256 threads or fewer
+
+vsd_status check_blocks(const vsd_blocks* m, const char* name) {
+  if (m == nullptr) return fail(VSD_ERR_NULL_POINTER, "%s is NULL", name);
+  if (m->values == nullptr || m->scales == nullptr)
+    return fail(VSD_ERR_NULL_POINTER, "%s: values and scales are required", name);
+  if (m->rows < 1 || m->rows > kMaxBlockDim || m->cols < 1 || m->cols > kMaxBlockDim)
+    return fail(VSD_ERR_INVALID_SHAPE, "%s: rows=%lld, cols=%lld outside [1,2^31)", name, (long long)m->rows,
+                (long long)m->cols);
+  if (m->group != 1 && m->group != 128)
+    return fail(VSD_ERR_INVALID_VALUE, "%s: group=%d is neither 1 nor 128", name, m->group);
+  if (m->ld < m->cols || m->ld % 128 != 0)
+    return fail(VSD_ERR_INVALID_SHAPE, "%s: ld=%lld is not a multiple of 128 >= cols=%lld", name, (long long)m->ld,
+                (long long)m->cols);
+  if (m->scale_ld < (m->rows + m->group - 1) / m->group)
+    return fail(VSD_ERR_INVALID_SHAPE, "%s: scale_ld=%lld < %lld row groups", name, (long long)m->scale_ld,
+                (long long)((m->rows + m->group - 1) / m->group));
+  if (!aligned16(m->values)) return fail(VSD_ERR_MISALIGNED, "%s: values not 16-byte aligned", name);
+  if (reinterpret_cast<uintptr_t>(m->scales) % 4 != 0)
+    return fail(VSD_ERR_MISALIGNED, "%s: scales not 4-byte aligned", name);
+  return VSD_OK;
+}
+
+vsd_status check_product(const vsd_blocks* a, const vsd_blocks* b) {
+  vsd_status st = check_blocks(a, "a");
+  if (st != VSD_OK) return st;
+  if ((st = check_blocks(b, "b")) != VSD_OK) return st;
+  if (a->group != 1) return fail(VSD_ERR_UNSUPPORTED, "a: group=%d (the rows' factor has group 1)", a->group);
+  if (a->cols != b->cols)
+    return fail(VSD_ERR_INVALID_SHAPE, "a has %lld columns, b %lld", (long long)a->cols, (long long)b->cols);
+  const int64_t mt = (a->rows + 31) / 32, nt = (b->rows + 31) / 32;
+  if (mt > kMaxWorkgroups * 4 / nt)
+    return fail(VSD_ERR_INVALID_SHAPE, "%lld x %lld results are too many for one call", (long long)a->rows,
+                (long long)b->rows);
+  return VSD_OK;
+}
+
+vsd_status check_workspace(const void* workspace, size_t given, size_t need) {
+  if (need == 0) return VSD_OK;
+  if (workspace == nullptr || given < need)
+    return fail(VSD_ERR_WORKSPACE, "workspace of %zu bytes required, %zu given", need,
+                workspace == nullptr ? (size_t)0 : given);
+  if (!aligned16(workspace)) return fail(VSD_ERR_MISALIGNED, "workspace not 16-byte aligned");
+  return VSD_OK;
+}
+
+vsd_status check_tensor(const vsd_tensor& t, const char* name, int i) {
+  if (t.dtype != VSD_F32 && t.dtype != VSD_BF16) return fail(VSD_ERR_INVALID_VALUE, "%s[%d]: dtype=%d", name, i, t.dtype);
+  if (t.rows < 0 || t.cols < 0 || t.rows > ((int64_t)1 << 44) || t.cols > ((int64_t)1 << 44) ||
+      (t.rows > 1 && t.cols > 0 && (t.ld < t.cols || t.ld > ((int64_t)1 << 44) || t.rows > ((int64_t)1 << 44) / t.ld)))
+    return fail(VSD_ERR_INVALID_SHAPE, "%s[%d]: rows=%lld, cols=%lld, ld=%lld", name, i, (long long)t.rows,
+                (long long)t.cols, (long long)t.ld);
+  if (t.rows == 0 || t.cols == 0) return VSD_OK;
+  if (t.data == nullptr) return fail(VSD_ERR_NULL_POINTER, "%s[%d]: data is NULL", name, i);
+  if (reinterpret_cast<uintptr_t>(t.data) % (t.dtype == VSD_F32 ? 4 : 2) != 0)
+    return fail(VSD_ERR_MISALIGNED, "%s[%d]: not aligned to its elements", name, i);
+  return VSD_OK;
+}
+
+vsd_status check_tensors(const vsd_tensor* g, const vsd_tensor* out, int32_t n) {
+  if (g == nullptr) return fail(VSD_ERR_NULL_POINTER, "grads is NULL");
+  if (n < 1 || n > (1 << 20)) return fail(VSD_ERR_INVALID_SHAPE, "n=%d tensors outside [1,2^20]", n);
+  int64_t chunks = 0;
+  for (int i = 0; i < n; ++i) {
+    vsd_status st = check_tensor(g[i], "grads", i);
+    if (st != VSD_OK) return st;
+    chunks += (g[i].rows * g[i].cols + vsd::kGradChunk - 1) / vsd::kGradChunk;
+    if (chunks > ((int64_t)1 << 30)) return fail(VSD_ERR_INVALID_SHAPE, "the tensors hold too many elements");
+    if (out == nullptr) continue;
+    if ((st = check_tensor(out[i], "out", i)) != VSD_OK) return st;
+    if (out[i].rows != g[i].rows || out[i].cols != g[i].cols)
+      return fail(VSD_ERR_INVALID_SHAPE, "out[%d] is %lld x %lld, its gradient %lld x %lld", i, (long long)out[i].rows,
+                  (long long)out[i].cols, (long long)g[i].rows, (long long)g[i].cols);
+    if (out[i].data == g[i].data && (out[i].dtype != g[i].dtype || (g[i].rows > 1 && out[i].ld != g[i].ld)))
+      return fail(VSD_ERR_INVALID_VALUE, "out[%d] is its gradient's memory with another type or stride", i);
+  }
+  return VSD_OK;
+}
+
+int norm_launches(int32_t n) { return (n + vsd::kGradTable - 1) / vsd::kGradTable; }
+size_t norm_bytes(int32_t n) { return align_up((size_t)norm_launches(n) * vsd::kGradGroups * sizeof(double)); }
+
+// Calls launch(table) for the tensors, kGradTable of them at a time.
+template <class F>
+hipError_t grad_launches(const vsd_tensor* g, const vsd_tensor* out, int32_t n, F&& launch) {
+  for (int32_t at = 0; at < n; at += vsd::kGradTable) {
+    vsd::GradTable t{};
+    t.first = at == 0;
+    int64_t chunks = 0;
+    for (int32_t i = at; i < n && i < at + vsd::kGradTable; ++i) {
+      const vsd_tensor& o = out == nullptr ? g[i] : out[i];
+      const int64_t size = g[i].rows * g[i].cols;
+      if (size == 0) continue;
+      vsd::GradEntry& e = t.e[t.n++];
+      const bool flat = g[i].rows == 1 || (g[i].ld == g[i].cols && o.ld == o.cols);
+      e.p = g[i].data;
+      e.out = o.data;
+      e.rows = flat ? 1 : g[i].rows;
+      e.cols = flat ? size : g[i].cols;
+      e.ld = flat ? size : g[i].ld;
+      e.out_ld = flat ? size : o.ld;
+      e.first = (int32_t)chunks;
+      e.bf16 = g[i].dtype == VSD_BF16;
+      e.out_bf16 = o.dtype == VSD_BF16;
+      chunks += (size + vsd::kGradChunk - 1) / vsd::kGradChunk;
+    }
+    t.chunks = (int32_t)chunks;
+    t.groups = (int32_t)std::max<int64_t>(1, std::min<int64_t>(chunks, vsd::kGradGroups));
+    const hipError_t e = launch(t);
+    if (e != hipSuccess) return e;
+  }
+  return hipSuccess;
+}
+
+// The sums of squares of all tensors, `parts` of them, into the workspace.
+hipError_t grad_squares(const vsd_tensor* g, int32_t n, double* part, int& parts, hipStream_t s) {
+  parts = 0;
+  return grad_launches(g, nullptr, n, [&](const vsd::GradTable& t) {
+    const hipError_t e = vsd::launch_grad_squares(t, part + parts, s);
+    parts += t.groups;
+    return e;
+  });
+}
+
 }  // namespace
 
 extern "C" {
@@ -1287,6 +1420,172 @@ vsd_status vsd_top_workspace_bytes(const vsd_rows* rows, int32_t with_map, size_
   if (st != VSD_OK) return st;
   if (bytes == nullptr) return fail(VSD_ERR_NULL_POINTER, "bytes is NULL");
   *bytes = with_map != 0 ? top_layout(rows).total : 0;
+  return ok();
+}
+
+vsd_status vsd_sample_rows(const vsd_rows* rows, const vsd_src* target, const vsd_draw* draw, const float* u,
+                           int32_t* tok, float* log_prob, int32_t* kept, void* workspace, size_t workspace_bytes,
+                           int32_t* device_error, void* hip_stream) {
+  vsd_status st = check_rows_struct(rows);
+  if (st != VSD_OK) return st;
+  if (rows->hidden_dim > 0) return fail(VSD_ERR_UNSUPPORTED, "vsd_sample_rows takes materialised logits");
+  if (rows->R >= kMaxTopRows)
+    return fail(VSD_ERR_INVALID_SHAPE, "R=%lld must be < 2^22", (long long)rows->R);
+  if ((st = check_rows_src(rows, target, "target")) != VSD_OK) return st;
+  if (draw == nullptr || u == nullptr || tok == nullptr || device_error == nullptr)
+    return fail(VSD_ERR_NULL_POINTER, "draw, u, tok and device_error are required");
+  if (!usable_setting(draw))
+    return fail(VSD_ERR_INVALID_VALUE, "temp=%g (0 or [1e-30, 1e30]), top_k=%d (>= 0), top_p=%g ((0, 1]) or min_p=%g "
+                "([0, 1]) out of range", draw->temp, draw->top_k, draw->top_p, draw->min_p);
+  (void)workspace;
+  (void)workspace_bytes;
+  vsd::DrawArgs a{};
+  a.Y = target->logits;
+  a.R = rows->R;
+  a.ld = rows->ld;
+  a.V = rows->v;
+  a.top_k = draw->top_k;
+  a.temp = draw->temp;
+  a.top_p = draw->top_p;
+  a.min_p = draw->min_p;
+  a.row_temp = draw->row_temp;
+  a.row_top_k = draw->row_top_k;
+  a.row_top_p = draw->row_top_p;
+  a.row_min_p = draw->row_min_p;
+  a.u = u;
+  a.tok = tok;
+  a.log_prob = log_prob;
+  a.kept = kept;
+  a.err = device_error;
+  const hipError_t e = vsd::launch_draw(a, rows->dtype == VSD_BF16, static_cast<hipStream_t>(hip_stream));
+  if (e != hipSuccess) return hip_fail(e, "k_draw launch");
+  return ok();
+}
+
+vsd_status vsd_draw_workspace_bytes(const vsd_rows* rows, size_t* bytes) {
+  vsd_status st = check_rows_struct(rows);
+  if (st != VSD_OK) return st;
+  if (bytes == nullptr) return fail(VSD_ERR_NULL_POINTER, "bytes is NULL");
+  *bytes = 0;
+  return ok();
+}
+
+vsd_status vsd_quantize_blocks(const void* x, int64_t rows, int64_t cols, int64_t ld, int32_t dtype, int32_t transpose,
+                               const vsd_blocks* out, void* hip_stream) {
+  vsd_status st = check_blocks(out, "out");
+  if (st != VSD_OK) return st;
+  if (x == nullptr) return fail(VSD_ERR_NULL_POINTER, "x is NULL");
+  if (dtype != VSD_F32 && dtype != VSD_BF16) return fail(VSD_ERR_INVALID_VALUE, "dtype=%d", dtype);
+  if (rows < 1 || cols < 1 || rows != (transpose ? out->cols : out->rows) || cols != (transpose ? out->rows : out->cols))
+    return fail(VSD_ERR_INVALID_SHAPE, "x is %lld x %lld, out %lld x %lld%s", (long long)rows, (long long)cols,
+                (long long)out->rows, (long long)out->cols, transpose ? " (transposed)" : "");
+  if (rows > 1 && ld < cols) return fail(VSD_ERR_INVALID_SHAPE, "ld=%lld < cols=%lld", (long long)ld, (long long)cols);
+  if (reinterpret_cast<uintptr_t>(x) % (dtype == VSD_F32 ? 4 : 2) != 0)
+    return fail(VSD_ERR_MISALIGNED, "x is not aligned to its elements");
+  const int64_t rt = (rows + 127) / 128, ct = (cols + 127) / 128;
+  if (rt >= kMaxWorkgroups / ct)
+    return fail(VSD_ERR_INVALID_SHAPE, "%lld x %lld elements are too many for one call", (long long)rows, (long long)cols);
+  vsd::QuantArgs a{};
+  a.x = x;
+  a.rows = rows;
+  a.cols = cols;
+  a.ld = ld;
+  a.values = static_cast<uint8_t*>(out->values);
+  a.scales = out->scales;
+  a.out_ld = out->ld;
+  a.scale_ld = out->scale_ld;
+  a.tiles = rt * ct;
+  a.col_tiles = (int32_t)ct;
+  const hipError_t e = vsd::launch_quantize(a, dtype == VSD_BF16, out->group, transpose != 0,
+                                            static_cast<hipStream_t>(hip_stream));
+  if (e != hipSuccess) return hip_fail(e, "k_quantize launch");
+  return ok();
+}
+
+vsd_status vsd_block_product(const vsd_blocks* a, const vsd_blocks* b, void* out, int64_t out_ld, int32_t out_dtype,
+                             void* workspace, size_t workspace_bytes, void* hip_stream) {
+  vsd_status st = check_product(a, b);
+  if (st != VSD_OK) return st;
+  if (out == nullptr) return fail(VSD_ERR_NULL_POINTER, "out is NULL");
+  if (out_dtype != VSD_F32 && out_dtype != VSD_BF16) return fail(VSD_ERR_INVALID_VALUE, "out_dtype=%d", out_dtype);
+  if (out_ld < b->rows)
+    return fail(VSD_ERR_INVALID_SHAPE, "out_ld=%lld < %lld columns", (long long)out_ld, (long long)b->rows);
+  if (!aligned16(out) || out_ld * (out_dtype == VSD_F32 ? 4 : 2) % 16 != 0)
+    return fail(VSD_ERR_MISALIGNED, "out or its row stride is not a multiple of 16 bytes");
+  (void)workspace;
+  (void)workspace_bytes;
+  vsd::BlockArgs p{};
+  p.a = static_cast<const uint8_t*>(a->values);
+  p.b = static_cast<const uint8_t*>(b->values);
+  p.sa = a->scales;
+  p.sb = b->scales;
+  p.out = out;
+  p.M = a->rows;
+  p.N = b->rows;
+  p.blocks = (a->cols + 127) / 128;
+  p.lda = a->ld;
+  p.ldb = b->ld;
+  p.ldsa = a->scale_ld;
+  p.ldsb = b->scale_ld;
+  p.ldo = out_ld;
+  const hipError_t e = vsd::launch_block_product(p, b->group, out_dtype == VSD_BF16, static_cast<hipStream_t>(hip_stream));
+  if (e != hipSuccess) return hip_fail(e, "k_block_product launch");
+  return ok();
+}
+
+vsd_status vsd_product_workspace_bytes(const vsd_blocks* a, const vsd_blocks* b, size_t* bytes) {
+  vsd_status st = check_product(a, b);
+  if (st != VSD_OK) return st;
+  if (bytes == nullptr) return fail(VSD_ERR_NULL_POINTER, "bytes is NULL");
+  *bytes = 0;
+  return ok();
+}
+
+vsd_status vsd_grad_norm(const vsd_tensor* grads, int32_t n, float* norm, void* workspace, size_t workspace_bytes,
+                         void* hip_stream) {
+  vsd_status st = check_tensors(grads, nullptr, n);
+  if (st != VSD_OK) return st;
+  if (norm == nullptr) return fail(VSD_ERR_NULL_POINTER, "norm is NULL");
+  if ((st = check_workspace(workspace, workspace_bytes, norm_bytes(n))) != VSD_OK) return st;
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  int parts;
+  hipError_t e = grad_squares(grads, n, static_cast<double*>(workspace), parts, s);
+  if (e != hipSuccess) return hip_fail(e, "k_grad_squares launch");
+  e = vsd::launch_grad_norm(static_cast<const double*>(workspace), parts, norm, s);
+  if (e != hipSuccess) return hip_fail(e, "k_grad_norm launch");
+  return ok();
+}
+
+vsd_status vsd_clip_gradients(const vsd_tensor* grads, const vsd_tensor* out, int32_t n, float max_norm,
+                              const float* norm, float* norm_out, float* scale, void* workspace,
+                              size_t workspace_bytes, void* hip_stream) {
+  vsd_status st = check_tensors(grads, out, n);
+  if (st != VSD_OK) return st;
+  if (!(max_norm > 0.0f)) return fail(VSD_ERR_INVALID_VALUE, "max_norm=%g must be > 0", max_norm);
+  if (norm == nullptr && (st = check_workspace(workspace, workspace_bytes, norm_bytes(n))) != VSD_OK) return st;
+  if (norm != nullptr && norm == norm_out) return fail(VSD_ERR_INVALID_VALUE, "norm_out is the norm that is given");
+  if (norm != nullptr && norm == scale) return fail(VSD_ERR_INVALID_VALUE, "scale is the norm that is given");
+  hipStream_t s = static_cast<hipStream_t>(hip_stream);
+  vsd::GradScale g{};
+  g.max_norm = max_norm;
+  g.norm = norm;
+  g.norm_out = norm_out;
+  g.scale_out = scale;
+  hipError_t e;
+  if (norm == nullptr) {
+    g.part = static_cast<const double*>(workspace);
+    e = grad_squares(grads, n, static_cast<double*>(workspace), g.parts, s);
+    if (e != hipSuccess) return hip_fail(e, "k_grad_squares launch");
+  }
+  e = grad_launches(grads, out, n, [&](const vsd::GradTable& t) { return vsd::launch_grad_scale(t, g, s); });
+  if (e != hipSuccess) return hip_fail(e, "k_grad_scale launch");
+  return ok();
+}
+
+vsd_status vsd_norm_workspace_bytes(int32_t n, size_t* bytes) {
+  if (n < 1 || n > (1 << 20)) return fail(VSD_ERR_INVALID_SHAPE, "n=%d tensors outside [1,2^20]", n);
+  if (bytes == nullptr) return fail(VSD_ERR_NULL_POINTER, "bytes is NULL");
+  *bytes = norm_bytes(n);
   return ok();
 }
 

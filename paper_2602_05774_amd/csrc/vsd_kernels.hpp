@@ -647,6 +647,77 @@ hipError_t launch_row_total(const LossArgs& a, hipStream_t s);
 hipError_t launch_top_bits(const int32_t* inv, int V, uint8_t* mapped, hipStream_t s);
 hipError_t launch_top_logits(const TopArgs& a, bool bf16, hipStream_t s);
 
+// Draws under the deployed rule.
+struct DrawArgs {
+  const void* Y;               // [R, ld]
+  int64_t R, ld;
+  int32_t V, top_k;
+  float temp, top_p, min_p;
+  const float* row_temp;       // [R] or null, as the next three
+  const int32_t* row_top_k;
+  const float* row_top_p;
+  const float* row_min_p;
+  const float* u;              // [R]
+  int32_t* tok;                // [R]
+  float* log_prob;             // [R] or null
+  int32_t* kept;               // [R] or null
+  int32_t* err;
+};
+
+// x [rows, cols] to 8-bit values and scales (of x^T: values [cols, out_ld]).
+struct QuantArgs {
+  const void* x;
+  int64_t rows, cols, ld;
+  uint8_t* values;
+  float* scales;
+  int64_t out_ld, scale_ld;
+  int64_t tiles;               // of 128 x 128 elements of x
+  int32_t col_tiles;
+};
+
+// out [M, N] = a [M, K] b [N, K]^T of block matrices, K in `blocks` of 128.
+struct BlockArgs {
+  const uint8_t* a;
+  const uint8_t* b;
+  const float* sa;
+  const float* sb;
+  void* out;
+  int64_t M, N, blocks, lda, ldb, ldsa, ldsb, ldo;
+  int64_t mt;                  // row tiles
+};
+
+// Gradients of one launch: `rows` rows of `cols` elements each, in chunks of
+// kGradChunk elements that the launch's workgroups take in turn.
+constexpr int kGradTable = 48, kGradChunk = 16384, kGradGroups = 1024;
+struct GradEntry {
+  const void* p;
+  void* out;                   // (the sums of squares: unused)
+  int64_t rows, cols, ld, out_ld;
+  int32_t first;               // the tensor's first chunk
+  uint8_t bf16, out_bf16;
+};
+struct GradTable {
+  GradEntry e[kGradTable];
+  int32_t n, chunks, groups;
+  int32_t first;               // this launch writes the call's norm and scale
+};
+static_assert(sizeof(GradTable) <= 3584, "a kernel's arguments are 4 KB at most");
+struct GradScale {
+  const double* part;          // the launches' sums of squares ...
+  int32_t parts;
+  float max_norm;
+  const float* norm;           // ... or the norm itself
+  float* norm_out;
+  float* scale_out;
+};
+
+hipError_t launch_draw(const DrawArgs& a, bool bf16, hipStream_t s);
+hipError_t launch_quantize(const QuantArgs& a, bool bf16, int group, bool trans, hipStream_t s);
+hipError_t launch_block_product(BlockArgs a, int group, bool bf16, hipStream_t s);
+hipError_t launch_grad_squares(const GradTable& t, double* part, hipStream_t s);
+hipError_t launch_grad_norm(const double* part, int n, float* norm, hipStream_t s);
+hipError_t launch_grad_scale(const GradTable& t, const GradScale& g, hipStream_t s);
+
 hipError_t launch_sample(const SampleArgs& a, bool bf16, hipStream_t s);
 hipError_t launch_sample_step(const SampleStepArgs& a, bool bf16, hipStream_t s);
 hipError_t launch_verify(const VerifyArgs& a, bool bf16, hipStream_t s);

@@ -1,0 +1,156 @@
+"""The gradients' norm and clipping against float64."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2602_05774_amd as vsd
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda"
+
+
+def _grads(sizes, seed, kinds=(torch.bfloat16, torch.float32)):
+    g = torch.Generator(device=DEV)
+    g.manual_seed(seed)
+    return [(torch.randn(*s, generator=g, device=DEV) * 10.0 ** -(i % 5)).to(kinds[i % len(kinds)]) for i, s in enumerate(sizes)]
+
+
+def _norm(grads):
+    return math.sqrt(math.fsum(float((t.double().cpu() ** 2).sum()) for t in grads))
+
+
+def _check_clipped(out, src, scale):
+    """fp32(g) * scale: the scale's rounding, the product's, the output's."""
+    for o, s in zip(out, src):
+        want = s.double().cpu() * scale
+        half = 2.0 ** -8 if o.dtype == torch.bfloat16 else 0.0
+        tiny = 2.0 ** -149 if o.dtype == torch.float32 else 2.0 ** -133
+        assert ((o.double().cpu() - want).abs() <= want.abs() * (half * 1.01 + 3 * 2.0 ** -24) + tiny).all()
+
+
+SETS = {
+    "one element": [(1,)],
+    "odd": [(3,), (17, 5), (1,), (1000,), (16385,), (7, 11, 13)],
+    "empty ones": [(0,), (5,), (0, 4), (33,)],
+    "many": [(1 + 37 * i,) for i in range(130)],
+    "large": [(300, 4099), (1 << 20,), (5,)],
+}
+
+
+@pytest.mark.parametrize("name", SETS)
+@pytest.mark.parametrize("kinds", [(torch.bfloat16,), (torch.float32,), (torch.bfloat16, torch.float32)])
+def test_norm_and_clip(name, kinds):
+    grads = _grads(SETS[name], 1, kinds)
+    norm = _norm(grads)
+    assert abs(float(vsd.grad_norm(grads)) - norm) <= 2.0 ** -24 * norm + 1e-12 * norm
+    before = [t.clone() for t in grads]
+    r = vsd.clip_gradients(grads, 10 * norm)
+    assert float(r.scale) == 1.0 and float(r.norm) == float(vsd.grad_norm(before))
+    assert all(torch.equal(a, b) for a, b in zip(grads, before))
+    bound = float(np.float32(0.3 * norm))
+    out = [torch.full_like(t, 9.0) for t in grads]
+    r = vsd.clip_gradients(grads, bound, out=out)
+    assert abs(float(r.scale) - bound / norm) <= 2.0 ** -23 * bound / norm
+    assert all(torch.equal(a, b) for a, b in zip(grads, before)) and r.grads[0] is out[0]
+    _check_clipped(out, before, bound / norm)
+    r = vsd.clip_gradients(grads, bound)
+    assert all(torch.equal(a, b) for a, b in zip(grads, out)) and r.grads[0] is grads[0]
+
+
+def test_other_output_type_and_a_copy():
+    grads = _grads(SETS["odd"], 2)
+    norm = _norm(grads)
+    for bound in (0.5 * norm, 2 * norm):
+        out = [torch.empty(t.shape, dtype=torch.float32 if t.dtype == torch.bfloat16 else torch.bfloat16, device=DEV) for t in grads]
+        vsd.clip_gradients(grads, bound, out=out)
+        _check_clipped(out, grads, min(1.0, float(np.float32(bound)) / norm))
+
+
+def test_strided_and_unaligned():
+    buf = torch.randn(50, 77, device=DEV)
+    flat = torch.randn(5001, device=DEV).bfloat16()
+    grads = [buf[3:40, 5:60], flat[1:4000], buf[45:46, 1:70], flat[4001:]]
+    norm = _norm(grads)
+    assert abs(float(vsd.grad_norm(grads)) - norm) <= 2.0 ** -24 * norm + 1e-12 * norm
+    keep, kept = buf.clone(), flat.clone()
+    to = torch.full((60, 80), 5.0, device=DEV)
+    out = [to[1:38, 3:58], torch.empty(3999, device=DEV, dtype=torch.bfloat16), torch.empty(1, 69, device=DEV),
+           torch.empty(1000, device=DEV, dtype=torch.bfloat16)]
+    vsd.clip_gradients(grads, 0.1 * norm, out=out)
+    _check_clipped(out, grads, float(np.float32(0.1 * norm)) / norm)
+    out[0].fill_(5.0)
+    assert (to == 5.0).all()
+    dense = [torch.empty(g.shape, dtype=g.dtype, device=DEV) for g in grads]
+    vsd.clip_gradients(grads, 0.1 * norm, out=dense)
+    vsd.clip_gradients(grads, 0.1 * norm)
+    assert all(torch.equal(a, b) for a, b in zip(dense, grads))
+    outside = torch.ones_like(buf, dtype=torch.bool)
+    outside[3:40, 5:60] = False
+    outside[45, 1:70] = False
+    assert torch.equal(buf[outside], keep[outside]) and flat[0] == kept[0] and flat[4000] == kept[4000]
+
+
+@pytest.mark.parametrize("bad", (math.inf, -math.inf, math.nan))
+def test_a_norm_that_is_not_finite_changes_nothing(bad):
+    grads = _grads(SETS["odd"], 3)
+    grads[4][9000] = bad
+    before = [t.clone() for t in grads]
+    r = vsd.clip_gradients(grads, 1e-3)
+    assert math.isnan(float(r.scale)) and not math.isfinite(float(r.norm))
+    assert all(torch.equal(a.view(torch.uint8), b.view(torch.uint8)) for a, b in zip(grads, before))
+    out = [torch.empty_like(t) for t in grads]
+    vsd.clip_gradients(grads, 1e-3, out=out)
+    assert all(torch.equal(a.nan_to_num(77.0), b.nan_to_num(77.0)) for a, b in zip(out, before))
+
+
+def test_extreme_magnitudes():
+    big = torch.full((4096,), 3e38, device=DEV)
+    assert math.isinf(float(vsd.grad_norm([big]))) and float(vsd.clip_gradients([big], math.inf).scale) == 1.0
+    tiny = torch.full((1 << 14,), 1e-40, device=DEV)
+    # (1e-40 is a subnormal number with a rounding of its own)
+    want = float(tiny[0].double()) * 128
+    assert abs(float(vsd.grad_norm([tiny])) - want) <= 2.0 ** -149
+    r = vsd.clip_gradients([big[:1], tiny], 1.0)
+    assert abs(float(r.scale) * 3e38 - 1.0) < 1e-6 and (tiny == 0).all()
+    zero = [torch.zeros(100, device=DEV)]
+    assert float(vsd.clip_gradients(zero, 1.0).scale) == 1.0
+
+
+def test_a_given_norm():
+    """That of other ranks' shards: the squares' sum is formed outside."""
+    a, b = _grads([(1000,), (70, 70)], 4), _grads([(501,)], 5)
+    both = torch.stack([vsd.grad_norm(a), vsd.grad_norm(b)]).double().norm().float().view(1)
+    want = _norm(a + b)
+    out = [torch.empty_like(t) for t in a]
+    r = vsd.clip_gradients(a, 0.01, norm=both, out=out)
+    assert torch.equal(r.norm, both)
+    _check_clipped(out, a, float(np.float32(0.01)) / float(both))
+    assert abs(float(both) - want) <= 3 * 2.0 ** -24 * want
+
+
+def test_same_twice_and_in_a_graph():
+    grads = _grads(SETS["many"], 6)
+    ws = torch.empty(vsd.norm_workspace_bytes(130), dtype=torch.uint8, device=DEV)
+    first = float(vsd.grad_norm(grads))
+    assert all(float(vsd.grad_norm(grads, workspace=ws)) == first for _ in range(5))
+    out = [torch.empty_like(t) for t in grads]
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        vsd.clip_gradients(grads, 0.5 * first, out=out)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=stream):
+            r = vsd.clip_gradients(grads, 0.5 * first, out=out)
+    torch.cuda.synchronize()
+    for k in range(3):
+        for t in grads:
+            t.mul_(1.5)
+        graph.replay()
+        torch.cuda.synchronize()
+        mine = [t.clone() for t in out]
+        e = vsd.clip_gradients(grads, 0.5 * first, out=out)
+        torch.cuda.synchronize()
+        assert torch.equal(r.norm, e.norm) and torch.equal(r.scale, e.scale)
+        assert all(torch.equal(x, y) for x, y in zip(mine, out))
