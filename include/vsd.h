@@ -722,10 +722,10 @@ vsd_status vsd_quantize_blocks(const void* x, int64_t rows, int64_t cols, int64_
 
 /* out [a->rows, b->rows] (out_dtype, row stride out_ld elements, 16-byte aligned
  * rows) = a b^T.  Columns past b->rows are not touched.  `workspace` must hold
- * vsd_product_workspace_bytes(a, b) bytes (16-B aligned; it may be 0). */
+ * vsd_product_workspace_bytes() bytes for them (16-B aligned; it may be 0). */
 vsd_status vsd_block_product(const vsd_blocks* a, const vsd_blocks* b, void* out, int64_t out_ld, int32_t out_dtype,
                              void* workspace, size_t workspace_bytes, void* hip_stream);
-vsd_status vsd_product_workspace_bytes(const vsd_blocks* a, const vsd_blocks* b, size_t* bytes);
+vsd_status vsd_product_workspace_bytes(const vsd_blocks* a, const vsd_blocks* b, int32_t out_dtype, size_t* bytes);
 
 /* norm [1] of n >= 1 tensors (the array is host memory, read during the call;
  * tensors without elements are allowed).  `workspace` must hold

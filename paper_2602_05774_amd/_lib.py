@@ -156,7 +156,7 @@ def load():
     lib.vsd_draw_workspace_bytes.argtypes = [P(VsdRows), P(ctypes.c_size_t)]
     lib.vsd_quantize_blocks.argtypes = [c_vp, c_i64, c_i64, c_i64, c_i32, c_i32, P(VsdBlocks), c_vp]
     lib.vsd_block_product.argtypes = [P(VsdBlocks), P(VsdBlocks), c_vp, c_i64, c_i32, c_vp, ctypes.c_size_t, c_vp]
-    lib.vsd_product_workspace_bytes.argtypes = [P(VsdBlocks), P(VsdBlocks), P(ctypes.c_size_t)]
+    lib.vsd_product_workspace_bytes.argtypes = [P(VsdBlocks), P(VsdBlocks), c_i32, P(ctypes.c_size_t)]
     lib.vsd_grad_norm.argtypes = [P(VsdTensor), c_i32, c_vp, c_vp, ctypes.c_size_t, c_vp]
     lib.vsd_clip_gradients.argtypes = [P(VsdTensor), P(VsdTensor), c_i32, c_f32, c_vp, c_vp, c_vp, c_vp,
                                        ctypes.c_size_t, c_vp]

@@ -82,14 +82,14 @@ def quantize_blocks(x, group=1, transpose=False, out=None):
     return out
 
 
-def product_workspace_bytes(a, b):
-    """Workspace bytes of block_product(a, b)."""
-    return _product_bytes(_blocks("a", a)[1], _blocks("b", b)[1])
+def product_workspace_bytes(a, b, dtype=torch.bfloat16):
+    """Workspace bytes of block_product(a, b, dtype)."""
+    return _product_bytes(_blocks("a", a)[1], _blocks("b", b)[1], VSD_BF16 if dtype == torch.bfloat16 else VSD_F32)
 
 
-def _product_bytes(a, b):
+def _product_bytes(a, b, kind):
     n = ctypes.c_size_t(0)
-    _lib.check(_lib.load().vsd_product_workspace_bytes(ctypes.byref(a), ctypes.byref(b), ctypes.byref(n)))
+    _lib.check(_lib.load().vsd_product_workspace_bytes(ctypes.byref(a), ctypes.byref(b), kind, ctypes.byref(n)))
     return n.value
 
 
@@ -118,9 +118,9 @@ def block_product(a, b, dtype=torch.bfloat16, out=None, workspace=None):
         elif (not isinstance(out, torch.Tensor) or tuple(out.shape) != (M, N) or out.device != dev
                 or out.dtype not in (torch.bfloat16, torch.float32) or (out.stride(1) != 1 and N != 1)):
             raise ValueError(f"out must be a bfloat16 or float32 tensor [{M}, {N}] on {dev} with unit column stride")
-        need = _product_bytes(A, Bm)
+        kind = VSD_BF16 if out.dtype == torch.bfloat16 else VSD_F32
+        need = _product_bytes(A, Bm, kind)
         ws = _workspace(need, workspace, dev)
         _lib.check(lib.vsd_block_product(ctypes.byref(A), ctypes.byref(Bm), out.data_ptr(), _row_stride(out),
-                                         VSD_BF16 if out.dtype == torch.bfloat16 else VSD_F32, _ptr(ws), need,
-                                         _stream(dev)))
+                                         kind, _ptr(ws), need, _stream(dev)))
     return out

@@ -9,28 +9,15 @@
 // results come from these instructions and fp32 results from the bf16 ones, which
 // sum in fp32, at half the rate: an e4m3 value is a bf16 value exactly.
 //
-// A wavefront owns a 32 x 32 tile and walks the blocks: each block's product is
-// formed on the matrix cores from zero and added, times its scales, in fp32.
-#include "vsd_device.hpp"
-#include "vsd_kernels.hpp"
+// Many rows: 256 x 256 tiles (vsd_block_tiles.hpp), the sum in ranges where there are
+// few tiles.
+// Few rows: a wavefront owns a 32 x 32 tile and walks the blocks: each block's product
+// is formed on the matrix cores from zero and added, times its scales, in fp32.
+#include "vsd_block_tiles.hpp"
 
 namespace vsd {
 
 namespace {
-
-typedef __attribute__((ext_vector_type(8))) int i32x8;
-typedef __attribute__((ext_vector_type(16))) float f32x16;
-typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
-typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
-
-// Eight of the type's values (two words) in bf16.
-__device__ __forceinline__ bf16x8 widen(int lo, int hi) {
-  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, false);
-  const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, true);
-  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, false);
-  const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, true);
-  return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
-}
 
 // sum_k a[m][k] b[n][k] over 64 values of k; lane l holds 32 of row l % 32 of both
 // operands, the same ones of each (the order of a sum's terms is free), and
@@ -87,8 +74,79 @@ __global__ __launch_bounds__(kWave) void k_block_product(BlockArgs a) {
   }
 }
 
+// The sum over the ranges, in their order.
 template <typename O>
-hipError_t launch_t(const BlockArgs& a, int group, hipStream_t s) {
+__global__ __launch_bounds__(256) void k_block_join(const float* part, int ranges, int64_t M, int64_t N, int64_t ldp, O* out,
+                                                    int64_t ldo) {
+  const int64_t per = ldp / 8, n = M * per;
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
+    const int64_t m = i / per, c = (i - m * per) * 8;
+    float x[8], y[8];
+    load8(part + m * ldp + c, x);
+    for (int r = 1; r < ranges; ++r) {
+      load8(part + (r * M + m) * ldp + c, y);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) x[k] += y[k];
+    }
+    O* const to = out + m * ldo + c;
+    if (c + 8 <= N) {
+      store8(to, x);
+    } else {
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if (c + k < N) store1(to + k, x[k]);
+    }
+  }
+}
+
+template <bool F8, typename O>
+void launch_tiles(const BlockTileArgs& t, int group, int ranges, hipStream_t s) {
+  const dim3 grid((unsigned)(t.mt * t.runs), (unsigned)ranges), block(block_tiles::kThreads);
+  if (group == 1)
+    hipLaunchKernelGGL((block_tiles::k_block_tiles<F8, 1, O>), grid, block, 0, s, t);
+  else
+    hipLaunchKernelGGL((block_tiles::k_block_tiles<F8, 128, O>), grid, block, 0, s, t);
+}
+
+template <typename O>
+hipError_t launch_by_tiles(const BlockArgs& a, const BlockPlan& p, int group, char* ws, hipStream_t s) {
+  constexpr bool kF32 = sizeof(O) == 4;
+  BlockTileArgs t{};
+  t.a = a.a;
+  t.b = a.b;
+  t.sa = a.sa;
+  t.sb = a.sb;
+  t.M = a.M;
+  t.N = a.N;
+  t.lda = a.lda;
+  t.ldb = a.ldb;
+  t.ldsa = a.ldsa;
+  t.ldsb = a.ldsb;
+  t.mt = (int32_t)((a.M + 255) / 256);
+  t.nt = (int32_t)((a.N + 255) / 256);
+  t.run = p.run;
+  t.runs = p.runs;
+  t.stages = (int32_t)a.blocks;
+  t.per = p.per;
+  if (p.ranges == 1) {
+    t.out = a.out;
+    t.ldo = a.ldo;
+    launch_tiles<!kF32, O>(t, group, 1, s);
+    return hipGetLastError();
+  }
+  t.out = ws;
+  t.ldo = (a.N + 7) / 8 * 8;
+  t.range_stride = a.M * t.ldo;
+  launch_tiles<!kF32, float>(t, group, p.ranges, s);
+  const int64_t n = (a.M * t.ldo / 8 + 255) / 256;
+  hipLaunchKernelGGL((k_block_join<O>), dim3((unsigned)(n < 4096 ? n : 4096)), dim3(256), 0, s,
+                     reinterpret_cast<const float*>(ws), p.ranges, a.M, a.N, t.ldo, static_cast<O*>(a.out), a.ldo);
+  return hipGetLastError();
+}
+
+template <typename O>
+hipError_t launch_t(const BlockArgs& a, const BlockPlan& p, int group, char* ws, hipStream_t s) {
+  if (p.tiles) return launch_by_tiles<O>(a, p, group, ws, s);
   const dim3 grid((unsigned)(a.mt * ((a.N + 31) / 32)));
   if (group == 1)
     hipLaunchKernelGGL((k_block_product<O, 1>), grid, dim3(kWave), 0, s, a);
@@ -99,9 +157,10 @@ hipError_t launch_t(const BlockArgs& a, int group, hipStream_t s) {
 
 }  // namespace
 
-hipError_t launch_block_product(BlockArgs a, int group, bool bf16, hipStream_t s) {
+hipError_t launch_block_product(BlockArgs a, const BlockPlan& p, int group, bool bf16, void* workspace, hipStream_t s) {
   a.mt = (a.M + 31) / 32;
-  return bf16 ? launch_t<bf16_t>(a, group, s) : launch_t<float>(a, group, s);
+  char* const ws = static_cast<char*>(workspace);
+  return bf16 ? launch_t<bf16_t>(a, p, group, ws, s) : launch_t<float>(a, p, group, ws, s);
 }
 
 }  // namespace vsd

@@ -733,10 +733,14 @@ vsd_status check_product(const vsd_blocks* a, const vsd_blocks* b) {
   if (a->cols != b->cols)
     return fail(VSD_ERR_INVALID_SHAPE, "a has %lld columns, b %lld", (long long)a->cols, (long long)b->cols);
   const int64_t mt = (a->rows + 31) / 32, nt = (b->rows + 31) / 32;
-  if (mt > kMaxWorkgroups * 4 / nt)
+  if (mt >= kMaxWorkgroups * 4 / nt)
     return fail(VSD_ERR_INVALID_SHAPE, "%lld x %lld results are too many for one call", (long long)a->rows,
                 (long long)b->rows);
   return VSD_OK;
+}
+
+vsd::BlockPlan product_plan(const vsd_blocks* a, const vsd_blocks* b, int32_t out_dtype) {
+  return vsd::block_plan(a->rows, b->rows, (a->cols + 127) / 128, a->ld, b->ld, out_dtype == VSD_F32);
 }
 
 vsd_status check_workspace(const void* workspace, size_t given, size_t need) {
@@ -1512,8 +1516,8 @@ vsd_status vsd_block_product(const vsd_blocks* a, const vsd_blocks* b, void* out
     return fail(VSD_ERR_INVALID_SHAPE, "out_ld=%lld < %lld columns", (long long)out_ld, (long long)b->rows);
   if (!aligned16(out) || out_ld * (out_dtype == VSD_F32 ? 4 : 2) % 16 != 0)
     return fail(VSD_ERR_MISALIGNED, "out or its row stride is not a multiple of 16 bytes");
-  (void)workspace;
-  (void)workspace_bytes;
+  const vsd::BlockPlan plan = product_plan(a, b, out_dtype);
+  if ((st = check_workspace(workspace, workspace_bytes, (size_t)plan.total)) != VSD_OK) return st;
   vsd::BlockArgs p{};
   p.a = static_cast<const uint8_t*>(a->values);
   p.b = static_cast<const uint8_t*>(b->values);
@@ -1528,16 +1532,18 @@ vsd_status vsd_block_product(const vsd_blocks* a, const vsd_blocks* b, void* out
   p.ldsa = a->scale_ld;
   p.ldsb = b->scale_ld;
   p.ldo = out_ld;
-  const hipError_t e = vsd::launch_block_product(p, b->group, out_dtype == VSD_BF16, static_cast<hipStream_t>(hip_stream));
+  const hipError_t e = vsd::launch_block_product(p, plan, b->group, out_dtype == VSD_BF16, workspace,
+                                                 static_cast<hipStream_t>(hip_stream));
   if (e != hipSuccess) return hip_fail(e, "k_block_product launch");
   return ok();
 }
 
-vsd_status vsd_product_workspace_bytes(const vsd_blocks* a, const vsd_blocks* b, size_t* bytes) {
+vsd_status vsd_product_workspace_bytes(const vsd_blocks* a, const vsd_blocks* b, int32_t out_dtype, size_t* bytes) {
   vsd_status st = check_product(a, b);
   if (st != VSD_OK) return st;
+  if (out_dtype != VSD_F32 && out_dtype != VSD_BF16) return fail(VSD_ERR_INVALID_VALUE, "out_dtype=%d", out_dtype);
   if (bytes == nullptr) return fail(VSD_ERR_NULL_POINTER, "bytes is NULL");
-  *bytes = 0;
+  *bytes = (size_t)product_plan(a, b, out_dtype).total;
   return ok();
 }
 

@@ -1,0 +1,339 @@
+// Products of block matrices by 256 x 256 tiles (see k_block.hip), many rows.
+//
+// Operands: U rows (of b: the result's columns) and V rows (of a: its rows), 128
+// bytes of each a stage: a block.  The schedule is that of the LM head's product loop: eight
+// wavefronts in two groups that run half a phase apart, one reading fragments and
+// issuing loads while the other multiplies; four phases a stage, one quadrant of
+// the tile each, every phase refilling the half operand whose last reader is past
+// (48 KB in flight, never drained); 16-byte chunks of a row swizzled over the banks.
+// What is added to it: a quadrant's product starts from zero and is joined to the
+// tile's fp32 sums, times its scales, in the group's next reading phase, where the
+// vector units would idle; the scales ride through LDS, loaded two stages ahead
+// with the operands.
+//   phase  reads   refills             multiplies   joins       waits for
+//   1      U0(t)   U1(t+1)             U0 V0        U1 V1(t-1)
+//   2      V1(t)   V0(t+2)             U0 V1        U0 V0
+//   3      U1(t)   U0(t+2)             U1 V0        U0 V1       V0(t+1)
+//   4      V0(t+1) V1(t+2), scales     U1 V1        U1 V0       all of t+1
+#pragma once
+
+#include "vsd_device.hpp"
+#include "vsd_kernels.hpp"
+
+namespace vsd {
+
+typedef __attribute__((ext_vector_type(4))) int i32x4;
+typedef __attribute__((ext_vector_type(8))) int i32x8;
+typedef __attribute__((ext_vector_type(16))) float f32x16;
+typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
+typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
+
+// Eight e4m3 values (two words) in bf16.
+__device__ __forceinline__ bf16x8 widen(int lo, int hi) {
+  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, false);
+  const bf16x2 b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(lo, 1.0f, true);
+  const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, false);
+  const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(hi, 1.0f, true);
+  return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
+
+namespace block_tiles {
+namespace {
+
+constexpr int kTile = 256, kThreads = 512, kRow = 128;  // bytes of a row a stage
+constexpr int kHalf = 128 * kRow, kBuf = 4 * kHalf;     // half an operand's stage; U0 U1 V0 V1
+constexpr int kScales = 2 * kBuf, kSlots = 4, kSlot = 2 * kTile * 4;  // V's 256 scales, U's 256
+constexpr int kLds = kScales + kSlots * kSlot;
+constexpr int kXcds = 8, kGroupRows = 4;
+static_assert(kLds <= 160 * 1024, "the stages and the scales fit the LDS");
+
+typedef __attribute__((address_space(3))) void lds_void;
+
+__device__ __forceinline__ int swz_u(int r) { return ((r >> 1) & 3) | (((r >> 5) & 1) << 2); }
+__device__ __forceinline__ int swz_v(int r) { return (r >> 1) & 7; }
+
+__device__ __forceinline__ void phase_barrier() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("" ::: "memory");
+}
+template <int N>
+__device__ __forceinline__ void wait_loads() {  // s_waitcnt: vmcnt bits 3:0 and 15:14, expcnt 6:4, lgkmcnt 11:8
+  __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4) | (15 << 8));
+  asm volatile("" ::: "memory");
+}
+__device__ __forceinline__ void wait_lds() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(15 | (3 << 14) | (7 << 4));
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+
+// Workgroup -> (row tile, run of column tiles): the workgroups of one XCD (ids are
+// dealt round-robin) walk groups of kGroupRows row tiles.
+__device__ __forceinline__ void tile_of(int pid, int nrt, int ncol, int& rt, int& col) {
+  const int total = nrt * ncol, xcd = pid % kXcds, local = pid / kXcds;
+  const int per = total / kXcds, extra = total % kXcds;
+  const int id = xcd * per + min(xcd, extra) + local;
+  const int g = id / (kGroupRows * ncol), in = id % (kGroupRows * ncol);
+  const int first = g * kGroupRows, rows = min(nrt - first, kGroupRows);
+  rt = first + in % rows;
+  col = in / rows;
+}
+
+// F8: 8-bit matrix instructions; else the values go through bf16 ones, converted
+// between the products.
+template <bool F8, int kGroup, typename O>
+__device__ __forceinline__ void tiles(const BlockTileArgs& a, uint8_t* lds) {
+  const int lane = threadIdx.x & 63, w = wave_id(), wr = w >> 2, wc = w & 3;
+  int rt, run;
+  tile_of(blockIdx.x, a.mt, a.runs, rt, run);
+  const int t_begin = run * a.run, t_end = min(t_begin + a.run, a.nt);
+  const int k_begin = (int)blockIdx.y * a.per, k_end = min(k_begin + a.per, a.stages);  // stages of this range
+  const int64_t m0 = (int64_t)rt * kTile;
+  auto rows = [&](const uint8_t* base, int64_t ld, int64_t n) {
+    return row_rsrc(base, (uint32_t)min(n, (int64_t)kTile) * (uint32_t)ld);
+  };
+  auto u_tile = [&](int t) { return rows(a.b + (int64_t)t * kTile * a.ldb, a.ldb, a.N - (int64_t)t * kTile); };
+  const __amdgpu_buffer_rsrc_t rv = rows(a.a + m0 * a.lda, a.lda, a.M - m0);
+  // where the wavefront's first load of a half starts for this lane (bytes); the
+  // second, 8 rows on, has the same swizzle (U), or the chunks' upper bit turned (V)
+  const int r0 = w * 16 + (lane >> 3);
+  const int ou = (int)(r0 * a.ldb + (((lane & 7) ^ swz_u(r0)) << 4));
+  const int ov = (int)(r0 * a.lda + (((lane & 7) ^ swz_v(r0)) << 4));
+  const int ldu = (int)a.ldb, ldv = (int)a.lda;
+  // a cursor: the tile and the stage; past the last one it repeats
+  struct Cursor {
+    __amdgpu_buffer_rsrc_t u;
+    int t, k;
+  };
+  auto advance = [&](Cursor& c) {
+    int t = c.t, k = c.k + 1;
+    if (k == k_end) {
+      if (t + 1 < t_end) {
+        c.u = u_tile(++t);
+        k = k_begin;
+      } else {
+        --k;
+      }
+    }
+    c.t = __builtin_amdgcn_readfirstlane(t);
+    c.k = __builtin_amdgcn_readfirstlane(k);
+  };
+  uint8_t* const mine = lds + w * 16 * kRow;
+  auto load_u = [&](int h, const Cursor& c, int buf) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(c.u, (lds_void*)(mine + buf * kBuf + h * kHalf + j * 8 * kRow), 16,
+                                               ou + (h * 128 + j * 8) * ldu, c.k * kRow, 0, 0);
+  };
+  auto load_v = [&](int h, const Cursor& c, int buf) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rv, (lds_void*)(mine + buf * kBuf + (2 + h) * kHalf + j * 8 * kRow), 16,
+                                               (ov ^ (j << 6)) + (h * 128 + j * 8) * ldv, c.k * kRow, 0, 0);
+  };
+  // one load a wavefront: 64 of V's scales (wavefronts 0 .. 3) or of U's
+  const bool of_v = w < 4;
+  const float* const scales = of_v ? a.sa + m0 : a.sb;
+  const int64_t scale_ld = of_v ? a.ldsa : a.ldsb, scale_n = of_v ? a.M - m0 : (a.N + kGroup - 1) / kGroup;
+  const int scale_tile = of_v ? 0 : kTile / kGroup;  // U's scales of a tile
+  const int scale_at = ((w & 3) * 64 + lane) / (of_v ? 1 : kGroup) * 4;
+  auto load_scales = [&](const Cursor& c, int slot) {
+    const int64_t j = c.k, first = (int64_t)c.t * scale_tile;
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(
+        row_rsrc(scales + j * scale_ld + first, (uint32_t)min(scale_n - first, (int64_t)kTile) * 4u),
+        (lds_void*)(lds + kScales + slot * kSlot + w * 256), 4, scale_at, 0, 0, 0);
+  };
+
+  // a lane's fragment addresses in the first quarter of a stage; quarter ks: ^ ks << 5
+  uint32_t fu_at, fv_at;
+  {
+    const int m = lane & 31, b = (m >> 2) & 1;
+    const int ru = 32 * b + 4 * (m >> 3) + (m & 3);
+    fu_at = (wr * 64 + ru) * kRow + (((lane >> 5) ^ swz_u(ru)) << 4);
+    fv_at = 2 * kHalf + (wc * 32 + m) * kRow + (((lane >> 5) ^ swz_v(m)) << 4);
+  }
+  f32x16 acc[2][2][2], tmp[2];
+  i32x4 fu[2][4], fv0[4], fv1[4];
+  auto frag = [&](uint32_t off) { return *reinterpret_cast<const i32x4*>(lds + off); };
+  auto read_u = [&](int buf, int half) {
+    const uint32_t at = fu_at + buf * kBuf;
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) fu[i][ks] = frag((at ^ (ks << 5)) + half * kHalf + i * 16 * kRow);
+  };
+  auto read_v = [&](i32x4 (&f)[4], int buf, int half) {
+    const uint32_t at = fv_at + buf * kBuf;
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) f[ks] = frag((at ^ (ks << 5)) + half * kHalf);
+  };
+  auto mult = [&](i32x4 (&v)[4]) {
+    __builtin_amdgcn_s_setprio(1);
+    if constexpr (F8) {
+#pragma unroll
+      for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const i32x8 x = __builtin_shufflevector(fu[i][2 * ks], fu[i][2 * ks + 1], 0, 1, 2, 3, 4, 5, 6, 7);
+          const i32x8 y = __builtin_shufflevector(v[2 * ks], v[2 * ks + 1], 0, 1, 2, 3, 4, 5, 6, 7);
+          tmp[i] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, y, ks == 0 ? f32x16{} : tmp[i], 0, 0, 0, 0, 0, 0);
+        }
+    } else {
+      // (the values' bf16 forms are made anew for every quadrant: kept, they would not fit)
+#pragma unroll
+      for (int ks = 0; ks < 4; ++ks) asm volatile("" : "+v"(fu[0][ks]), "+v"(fu[1][ks]), "+v"(v[ks]));
+#pragma unroll
+      for (int ks = 0; ks < 8; ++ks) {
+        const bf16x8 y = widen(v[ks >> 1][(ks & 1) * 2], v[ks >> 1][(ks & 1) * 2 + 1]);
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          tmp[i] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+              widen(fu[i][ks >> 1][(ks & 1) * 2], fu[i][ks >> 1][(ks & 1) * 2 + 1]), y, ks == 0 ? f32x16{} : tmp[i], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);  // (not all conversions first: they would fill the registers)
+      }
+    }
+    asm volatile("" : "+v"(tmp[0]), "+v"(tmp[1]));
+    __builtin_amdgcn_s_setprio(0);
+  };
+  // c += tmp times the scales of U half h (registers) and V half g (lanes)
+  auto join = [&](int h, int g, int slot) {
+    const float* const S = reinterpret_cast<const float*>(lds + kScales + slot * kSlot);
+    const float sv = S[g * 128 + wc * 32 + (lane & 31)];
+    if constexpr (kGroup == 128) {
+      const float s = sv * S[kTile + h * 128];
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) acc[h][g][i][e] = fmaf(tmp[i][e], s, acc[h][g][i][e]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const float4 u = *reinterpret_cast<const float4*>(S + kTile + h * 128 + wr * 64 + 32 * (lane >> 5) + 16 * i + 4 * q);
+          const float us[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            acc[h][g][i][4 * q + e] = fmaf(tmp[i][4 * q + e] * us[e], sv, acc[h][g][i][4 * q + e]);
+          if (q == 1) __builtin_amdgcn_sched_barrier(0);
+        }
+    }
+    asm volatile("" : "+v"(acc[h][g][0]), "+v"(acc[h][g][1]));  // (the sums stay in this phase and in their registers)
+  };
+  // the tile's results: 32 consecutive columns a lane in each half of the columns
+  O* const out = static_cast<O*>(a.out) + (int64_t)blockIdx.y * a.range_stride;
+  auto store = [&](int t) {
+    int l = lane;
+    asm volatile("" : "+v"(l));  // (its addresses are formed here, not kept across the loop)
+    const int64_t n = (int64_t)t * kTile + wr * 64 + 32 * (l >> 5);
+#pragma unroll
+    for (int g = 0; g < 2; ++g) {
+      const int64_t m = m0 + g * 128 + wc * 32 + (l & 31);
+      if (m >= a.M) continue;
+      O* const to = out + m * a.ldo + n;
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          float x[8];
+#pragma unroll
+          for (int e = 0; e < 8; ++e) x[e] = acc[h][g][c >> 1][(c & 1) * 8 + e];
+          const int at = h * 128 + c * 8;
+          if (n + at + 8 <= a.N) {
+            store8(to + at, x);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              if (n + at + e < a.N) store1(to + at + e, x[e]);
+          }
+        }
+    }
+  };
+
+  Cursor c1{u_tile(t_begin), t_begin, k_begin}, c2;
+  load_scales(c1, 0);
+  load_v(0, c1, 0);
+  load_u(0, c1, 0);
+  load_v(1, c1, 0);
+  load_u(1, c1, 0);
+  advance(c1);
+  c2 = c1;
+  advance(c2);
+  load_v(0, c1, 1);
+  load_u(0, c1, 1);
+  load_v(1, c1, 1);
+  load_scales(c1, 1);
+  wait_loads<7>();
+  phase_barrier();
+  if (wr == 1) phase_barrier();  // from here on this group runs half a phase behind
+  read_v(fv0, 0, 0);
+  wait_lds();
+  auto clear = [&]() {
+#pragma unroll
+    for (int q = 0; q < 8; ++q) acc[q >> 2][(q >> 1) & 1][q & 1] = f32x16{};
+  };
+  clear();
+  int p = 0, slot = 0;
+  for (int t = t_begin, k = k_begin; t < t_end; p ^= 1, slot = (slot + 1) & (kSlots - 1)) {
+    load_u(1, c1, p ^ 1);
+    read_u(p, 0);
+    if (k > k_begin) join(1, 1, (slot + kSlots - 1) & (kSlots - 1));
+    phase_barrier();
+    wait_lds();
+    mult(fv0);
+    phase_barrier();
+
+    load_v(0, c2, p);
+    read_v(fv1, p, 1);
+    join(0, 0, slot);
+    phase_barrier();
+    wait_lds();
+    mult(fv1);
+    phase_barrier();
+
+    load_u(0, c2, p);
+    read_u(p, 1);
+    join(0, 1, slot);
+    wait_loads<11>();
+    phase_barrier();
+    wait_lds();
+    mult(fv0);
+    phase_barrier();
+
+    load_v(1, c2, p);
+    load_scales(c2, (slot + 2) & (kSlots - 1));
+    read_v(fv0, p ^ 1, 0);
+    join(1, 0, slot);
+    wait_loads<7>();
+    phase_barrier();
+    wait_lds();
+    mult(fv1);
+    c1 = c2;
+    advance(c2);
+    if (wr == 0) phase_barrier();
+    if (++k == k_end) {  // both groups finish a tile between the same two barriers
+      join(1, 1, slot);
+      store(t);
+      clear();
+      ++t;
+      k = k_begin;
+    }
+    if (wr == 1) phase_barrier();
+  }
+  if (wr == 0) phase_barrier();
+  wait_loads<0>();  // the repeated loads have landed before the LDS is given up
+}
+
+template <bool F8, int kGroup, typename O>
+__global__ __launch_bounds__(kThreads) void k_block_tiles(BlockTileArgs a) {
+  __shared__ __align__(16) uint8_t lds[kLds];
+  tiles<F8, kGroup, O>(a, lds);
+}
+
+}  // namespace
+}  // namespace block_tiles
+}  // namespace vsd

@@ -686,6 +686,60 @@ struct BlockArgs {
   int64_t mt;                  // row tiles
 };
 
+// The same by 256 x 256 tiles: a workgroup takes `run` column tiles of a row tile,
+// and of the sum the stages (128 bytes of a row each) of range blockIdx.y.
+struct BlockTileArgs {
+  const uint8_t* a;
+  const uint8_t* b;
+  const float* sa;
+  const float* sb;
+  void* out;
+  int64_t M, N, lda, ldb, ldsa, ldsb, ldo;  // lda, ldb: bytes
+  int64_t range_stride;        // elements of the result between two ranges
+  int32_t mt, nt, run, runs;   // tiles; tiles of a run, runs
+  int32_t stages, per;         // stages, of a range
+};
+
+// How a product is computed: by single wavefronts, or by tiles (the workgroups' runs,
+// the sum's ranges), with these regions of the workspace.
+constexpr int64_t kBlockFewRows = 64;       // rows of a that wavefronts take
+constexpr int64_t kBlockMaxLd = 1 << 22;    // bytes of a row: 256 of them within 32-bit offsets
+constexpr int kBlockCus = 256, kBlockMaxRanges = 16;
+struct BlockPlan {
+  bool tiles;
+  int32_t run, runs, ranges, per;  // as in BlockTileArgs
+  int64_t total;                   // bytes of the ranges' sums (the workspace)
+};
+inline BlockPlan block_plan(int64_t M, int64_t N, int64_t blocks, int64_t lda, int64_t ldb, bool f32) {
+  BlockPlan p{};
+  const int64_t mt = (M + 255) / 256, nt = (N + 255) / 256, stages = blocks;
+  if (M <= kBlockFewRows || (lda > ldb ? lda : ldb) > kBlockMaxLd || mt * nt >= 1 << 22) return p;
+  p.tiles = true;
+  // time in us: a block takes about one (fp32 results two), a run three to start, a
+  // tile two to be stored; ranges' sums are written and read at some 4 MB a us
+  const int64_t each = f32 ? 2 : 1;
+  double best = 0.0;
+  for (int64_t ranges = 1; ranges <= kBlockMaxRanges; ++ranges) {
+    const int64_t per = (stages + ranges - 1) / ranges;
+    if (ranges > 1 && (per < 4 || (ranges - 1) * per >= stages || mt * nt * ranges > 2 * kBlockCus)) continue;
+    for (int64_t run = 1; run <= nt; ++run) {
+      const int64_t runs = (nt + run - 1) / run, groups = mt * runs * ranges;
+      if (run > 1 && (ranges > 1 || runs == (nt + run - 2) / (run - 1))) continue;
+      const double time = (double)((groups + kBlockCus - 1) / kBlockCus) * (double)(run * (per * each + 2) + 3) +
+                          (ranges > 1 ? 5.0 + 2e-6 * (double)(ranges * M * N) : 0.0);
+      if (best == 0.0 || time < best) {
+        best = time;
+        p.run = (int32_t)run;
+        p.runs = (int32_t)runs;
+        p.ranges = (int32_t)ranges;
+        p.per = (int32_t)per;
+      }
+    }
+  }
+  if (p.ranges > 1) p.total = (int64_t)p.ranges * M * ((N + 7) / 8 * 8) * 4;
+  return p;
+}
+
 // Gradients of one launch: `rows` rows of `cols` elements each, in chunks of
 // kGradChunk elements that the launch's workgroups take in turn.
 constexpr int kGradTable = 48, kGradChunk = 16384, kGradGroups = 1024;
@@ -713,7 +767,7 @@ struct GradScale {
 
 hipError_t launch_draw(const DrawArgs& a, bool bf16, hipStream_t s);
 hipError_t launch_quantize(const QuantArgs& a, bool bf16, int group, bool trans, hipStream_t s);
-hipError_t launch_block_product(BlockArgs a, int group, bool bf16, hipStream_t s);
+hipError_t launch_block_product(BlockArgs a, const BlockPlan& p, int group, bool bf16, void* workspace, hipStream_t s);
 hipError_t launch_grad_squares(const GradTable& t, double* part, hipStream_t s);
 hipError_t launch_grad_norm(const double* part, int n, float* norm, hipStream_t s);
 hipError_t launch_grad_scale(const GradTable& t, const GradScale& g, hipStream_t s);
