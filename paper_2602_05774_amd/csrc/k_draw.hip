@@ -1,11 +1,22 @@
 // One token per row under the deployed rule: temperature, top-k, top-p, min-p and
 // a given random number (vsd_sample_rows).
 //
-// One workgroup per row, sweeping it several times: the largest entry; the sum of
-// the weights, which sets their integer scale; for top-k and top-p the entry where
-// the count or the mass reaches its target, 8 bits of its value a sweep from
-// histograms of integers in LDS, and among equal entries by index; the kept
-// entries' mass; and the index where the mass up to it passes u Z.
+// The sweep (k_draw_sweep) reads the row once, a wavefront per span of 2048 columns:
+// the largest logit of every 128 columns and, where the rule needs it, the span's sum
+// of weights in double precision.  k_draw_finish, a workgroup per row, ends most rows
+// from these records and a few reads more:
+//  * greedy: the first group that holds the maximum;
+//  * no filter: the span in which the cumulative sum passes u Z, read again;
+//  * filters: a bound below which no kept entry lies (the K-th largest of the groups'
+//    maxima; the largest value such that the maxima from it on already weigh p Z;
+//    min-p's own), the groups that reach it read again, their entries listed in LDS
+//    in index order, and the borders of top-k and top-p found bit by bit.
+// Rows whose lists do not fit (flat ones, k in the thousands) are left to k_draw_row.
+// k_draw_row: one workgroup per row, sweeping it several times: the largest entry; the
+// sum of the weights, which sets their integer scale; for top-k and top-p the entry
+// where the count or the mass reaches its target, 8 bits of its value a sweep from
+// histograms of integers in LDS, and among equal entries by index; the kept entries'
+// mass; and the index where the mass up to it passes u Z.
 #include "vsd_draw64.hpp"
 #include "vsd_loss.hpp"
 
@@ -181,10 +192,8 @@ struct RowDraw {
 };
 
 template <typename T, int kThreads>
-__global__ __launch_bounds__(kThreads) void k_draw_row(DrawArgs a) {
+__device__ __forceinline__ void draw_row(const DrawArgs& a, int64_t r, typename RowDraw<T, kThreads>::Shared& sh) {
   using Row = RowDraw<T, kThreads>;
-  __shared__ typename Row::Shared sh;
-  const int64_t r = blockIdx.x;
   const DrawSettings d = draw_settings(a, r);
   if (!draw_valid(d)) {
     if (threadIdx.x == 0) {
@@ -271,19 +280,548 @@ __global__ __launch_bounds__(kThreads) void k_draw_row(DrawArgs a) {
   }
 }
 
+// Every row, or (todo) those that were left.
+template <typename T, int kThreads>
+__global__ __launch_bounds__(kThreads) void k_draw_row(DrawArgs a) {
+  __shared__ typename RowDraw<T, kThreads>::Shared sh;
+  const int64_t n = a.todo == nullptr ? a.R : *a.ntodo;
+  for (int64_t i = blockIdx.x; i < n; i += gridDim.x) {
+    draw_row<T, kThreads>(a, a.todo == nullptr ? i : a.todo[i], sh);
+    __syncthreads();
+  }
+}
+
+// ------------------------------------------------------------------ sweep ---
+__device__ __forceinline__ float min3f(float a, float b, float c) {
+  float r;
+  asm("v_min3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
+__device__ __forceinline__ float min8(const float (&v)[8]) {
+  return min3f(min3f(v[0], v[1], v[2]), min3f(v[3], v[4], v[5]), min3f(v[6], v[7], v[7]));
+}
+template <int CTRL>
+__device__ __forceinline__ double dpp_d(double v) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  const uint64_t lo = (uint32_t)dpp_i<CTRL>((int)(uint32_t)u), hi = (uint32_t)dpp_i<CTRL>((int)(u >> 32));
+  return __builtin_bit_cast(double, hi << 32 | lo);
+}
+__device__ __forceinline__ double lane_d(double v, int l) {
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  const uint64_t lo = (uint32_t)lane_i((int)(uint32_t)u, l), hi = (uint32_t)lane_i((int)(u >> 32), l);
+  return __builtin_bit_cast(double, hi << 32 | lo);
+}
+__device__ __forceinline__ double wave_sum_d(double v) {
+  v += dpp_d<kDppQuad1>(v);
+  v += dpp_d<kDppQuad2>(v);
+  v += dpp_d<kDppHalfMirror>(v);
+  v += dpp_d<kDppMirror>(v);
+  return (lane_d(v, 0) + lane_d(v, 16)) + (lane_d(v, 32) + lane_d(v, 48));
+}
+__device__ __forceinline__ float row16_max(float v) {
+  v = fmaxf(v, dpp_f<kDppQuad1>(v));
+  v = fmaxf(v, dpp_f<kDppQuad2>(v));
+  v = fmaxf(v, dpp_f<kDppHalfMirror>(v));
+  return fmaxf(v, dpp_f<kDppMirror>(v));
+}
+
+// Whether the rule needs the sum over all of the row's weights: the whole softmax, or
+// top-p of it.  (With top-k the sum is over the kept entries, which are listed.)
+__device__ __forceinline__ bool needs_sum(const DrawSettings& d) {
+  return d.temp > 0.0f && d.top_k == 0 && (d.top_p < 1.0f || d.min_p == 0.0f);
+}
+
+constexpr int kLoads = kDrawSpan / 512;  // of 8 columns a lane
+
 template <typename T>
-hipError_t launch_t(const DrawArgs& a, hipStream_t s) {
-  const dim3 grid((unsigned)a.R);
+__global__ __launch_bounds__(256) void k_draw_sweep(DrawArgs a) {
+  const int lane = threadIdx.x & 63, tasks = (a.S + a.per - 1) / a.per;
+  const int64_t task = (int64_t)blockIdx.x * 4 + wave_id();
+  const int64_t r = task / tasks;
+  if (task == 0 && lane == 0) *a.ntodo = 0;
+  if (r >= a.R) return;
+  const int first = (int)(task - r * tasks) * a.per, last = min(first + a.per, a.S);
+  const DrawSettings d = draw_settings(a, r);
+  const bool sums = needs_sum(d);
+  const double c = sums ? 1.4426950408889634074 / (double)d.temp : 0.0;
+  const T* Y = static_cast<const T*>(a.Y) + r * a.ld;
+  auto load = [&](Raw8<T> (&q)[kLoads], int span) {
+    const int base = span * kDrawSpan + lane * 8;
+    if (span * kDrawSpan + kDrawSpan <= a.V) {
+#pragma unroll
+      for (int u = 0; u < kLoads; ++u) q[u].load(Y + base + u * 512);
+    } else {
+#pragma unroll
+      for (int u = 0; u < kLoads; ++u) load_cols(q[u], Y, base + u * 512, a.V);
+    }
+  };
+  auto take = [&](const Raw8<T> (&q)[kLoads], int span) {
+    float top = -INFINITY, low = INFINITY, gm = -INFINITY;
+    bool nan = false;
+#pragma unroll
+    for (int u = 0; u < kLoads; ++u) {
+      float x[8];
+      q[u].get(x);
+      const float t = max8(x);
+      top = fmaxf(top, t);
+      low = fminf(low, min8(x));
+#pragma unroll
+      for (int k = 0; k < 8; k += 2) nan |= __builtin_isunordered(x[k], x[k + 1]);
+      const float g = row16_max(t);
+      if ((lane & 15) == u) gm = g;
+    }
+    const float m = wave_max(top);
+    int count = kDrawSpan;
+    if (__any(low == -INFINITY)) {
+      count = 0;
+#pragma unroll
+      for (int u = 0; u < kLoads; ++u) {
+        float x[8];
+        q[u].get(x);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) count += __builtin_popcountll(__ballot(x[k] > -INFINITY));
+      }
+    }
+    if (__any(nan)) count = -1;
+    double s = 0.0;
+    if (sums && m > -INFINITY) {
+      const double md = m;
+#pragma unroll
+      for (int u = 0; u < kLoads; ++u) {
+        float x[8];
+        q[u].get(x);
+        if (m < INFINITY) {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) s += exp2_64(((double)x[k] - md) * c);
+        } else {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) s += x[k] == m ? 1.0 : 0.0;
+        }
+      }
+      s = wave_sum_d(s);
+    }
+    const int64_t at = r * a.S + span;
+    if ((lane & 15) < kLoads) a.group_max[at * 16 + (lane & 15) * 4 + (lane >> 4)] = gm;
+    if (lane == 0) {
+      a.span_max[at] = m;
+      a.span_count[at] = count;
+      a.span_sum[at] = s;
+    }
+  };
+  static_assert(kDrawSpan / kDrawGroup == 16 && kLoads * 4 == 16, "sixteen groups of a span");
+  Raw8<T> q[2][kLoads];
+  load(q[0], first);
+  for (int s = first; s < last; s += 2) {
+    if (s + 1 < last) load(q[1], s + 1);
+    take(q[0], s);
+    if (s + 1 == last) break;
+    if (s + 2 < last) load(q[0], s + 2);
+    take(q[1], s + 1);
+  }
+}
+
+// ----------------------------------------------------------------- finish ---
+constexpr int kFinish = 256, kFinishWaves = kFinish / kWave;
+constexpr int kCap = 1024, kMine = kCap / kFinish;            // listed entries, of a thread
+constexpr int kGroups = kDrawSpans * 16, kMyGroups = kGroups / kFinish;
+constexpr double kListScale = 4503599627370496.0;             // 2^52: a list's weights sum to at most 2^62
+static_assert(kCap <= 1024 && kMyGroups == 8, "");
+
+struct FinishShared {
+  float x[kCap];
+  int32_t col[kCap];
+  int32_t groups[kGroups];
+  uint64_t red[2][kFinishWaves];
+  int64_t pick;
+  double pickd;
+};
+
+template <int CTRL>
+__device__ __forceinline__ uint64_t dpp_u64(uint64_t u) {
+  const uint64_t lo = (uint32_t)dpp_i<CTRL>((int)(uint32_t)u), hi = (uint32_t)dpp_i<CTRL>((int)(u >> 32));
+  return hi << 32 | lo;
+}
+__device__ __forceinline__ uint64_t lane_u64(uint64_t u, int l) {
+  return (uint64_t)(uint32_t)lane_i((int)(u >> 32), l) << 32 | (uint32_t)lane_i((int)(uint32_t)u, l);
+}
+__device__ __forceinline__ uint64_t wave_sum_u64(uint64_t v) {
+  v += dpp_u64<kDppQuad1>(v);
+  v += dpp_u64<kDppQuad2>(v);
+  v += dpp_u64<kDppHalfMirror>(v);
+  v += dpp_u64<kDppMirror>(v);
+  return (lane_u64(v, 0) + lane_u64(v, 16)) + (lane_u64(v, 32) + lane_u64(v, 48));
+}
+
+// Sums and scans over the workgroup; `turn` alternates between two sets of words, so
+// that one barrier a sum is enough.
+struct Block {
+  FinishShared& sh;
+  int turn;
+  __device__ __forceinline__ uint64_t sum(uint64_t v) {
+    v = wave_sum_u64(v);
+    turn ^= 1;
+    if ((threadIdx.x & 63) == 0) sh.red[turn][wave_id()] = v;
+    __syncthreads();
+    const uint64_t* r = sh.red[turn];
+    return (r[0] + r[1]) + (r[2] + r[3]);
+  }
+  template <typename N>
+  __device__ __forceinline__ N before(N v, N& all) {  // the sum over the threads before this one
+    static_assert(sizeof(N) == 8, "");
+    N upto = v;
+#pragma unroll
+    for (int d = 1; d < kWave; d <<= 1) {
+      const N o = __shfl_up(upto, d);
+      if ((int)(threadIdx.x & 63) >= d) upto += o;
+    }
+    turn ^= 1;
+    N* const r = reinterpret_cast<N*>(sh.red[turn]);
+    if ((threadIdx.x & 63) == 63) r[wave_id()] = upto;
+    __syncthreads();
+    N first = 0;
+    all = 0;
+#pragma unroll
+    for (int k = 0; k < kFinishWaves; ++k) {
+      if (k < wave_id()) first += r[k];
+      all += r[k];
+    }
+    // (upto - v would lose what v is small against)
+    const N prev = __shfl_up(upto, 1);
+    return first + ((threadIdx.x & 63) == 0 ? N(0) : prev);
+  }
+  __device__ __forceinline__ uint64_t least(uint64_t v) {
+#pragma unroll
+    for (int d = 1; d < kWave; d <<= 1) {
+      const uint64_t o = __shfl_xor(v, d);
+      v = o < v ? o : v;
+    }
+    turn ^= 1;
+    if ((threadIdx.x & 63) == 0) sh.red[turn][wave_id()] = v;
+    __syncthreads();
+    uint64_t t = sh.red[turn][0];
+#pragma unroll
+    for (int k = 1; k < kFinishWaves; ++k) t = sh.red[turn][k] < t ? sh.red[turn][k] : t;
+    return t;
+  }
+  // The largest key such that measure(key), the sum over entries of at least that key,
+  // reaches target (that of key 0 does); keys below 2^bits.
+  template <class M>
+  __device__ __forceinline__ uint32_t largest(int bits, uint64_t target, M&& measure) {
+    uint32_t key = 0;
+    for (int b = bits - 1; b >= 0; --b) {
+      const uint32_t t = key | 1u << b;
+      if (sum(measure(t)) >= target) key = t;
+    }
+    return key;
+  }
+};
+
+template <typename T>
+__global__ __launch_bounds__(kFinish) void k_draw_finish(DrawArgs a) {
+  constexpr int kBits = sizeof(T) == 2 ? 16 : 32, kDown = 32 - kBits;
+  __shared__ FinishShared sh;
+  Block blk{sh, 0};
+  const int t = threadIdx.x;
+  const int64_t r = blockIdx.x;
+  const T* Y = static_cast<const T*>(a.Y) + r * a.ld;
+  const DrawSettings d = draw_settings(a, r);
+  if (!draw_valid(d)) {
+    if (t == 0) {
+      report_error(a.err, VSD_DEVERR_SETTING_RANGE);
+      draw_result(a, r, -1, 0.0f, 0);
+    }
+    return;
+  }
+  auto key_of = [](float x) { return draw_order(x) >> kDown; };
+  auto value_of = [](uint32_t k) {
+    return draw_value(kDown == 0 || k >= 0x8000u ? k << kDown : k << kDown | 0xFFFFu);
+  };
+  const int G = a.S * 16;
+  float g[kMyGroups];  // the largest logits of groups 8 t .. 8 t + 7
+  if (t * kMyGroups < G) {
+    load8(a.group_max + r * G + t * kMyGroups, g);
+  } else {
+#pragma unroll
+    for (int k = 0; k < kMyGroups; ++k) g[k] = -INFINITY;
+  }
+  const bool span = t < a.S;
+  const float span_max = span ? a.span_max[r * a.S + t] : -INFINITY;
+  const int span_count = span ? a.span_count[r * a.S + t] : 0;
+  const uint64_t counts = blk.sum(span_count < 0 ? 1ull << 40 : (uint64_t)span_count);
+  const int n = (int)counts;
+  if (counts == 0 || counts >> 40 != 0) {
+    if (t == 0) draw_result(a, r, -1, counts == 0 ? 0.0f : __builtin_nanf(""), 0);
+    return;
+  }
+  const float m = value_of(~(uint32_t)blk.least(~key_of(span_max) & (0xFFFFFFFFu >> kDown)) & (0xFFFFFFFFu >> kDown));
+  if (d.temp == 0.0f) {
+    uint64_t at = ~0ull;
+#pragma unroll
+    for (int k = kMyGroups - 1; k >= 0; --k)
+      if (g[k] == m) at = (uint64_t)(t * kMyGroups + k);
+    at = blk.least(at);
+    uint64_t col = ~0ull;
+    if (t < kDrawGroup / 8) {
+      Raw8<T> q;
+      float x[8];
+      const int base = (int)at * kDrawGroup + t * 8;
+      load_cols(q, Y, base, a.V);
+      q.get(x);
+#pragma unroll
+      for (int k = 7; k >= 0; --k)
+        if (x[k] == m) col = (uint64_t)(base + k);
+    }
+    col = blk.least(col);
+    if (t == 0) draw_result(a, r, (int32_t)col, 0.0f, 1);
+    return;
+  }
+  const double c = 1.4426950408889634074 / (double)d.temp, temp = d.temp;
+  auto log_weight = [&](float x) { return x == m ? 0.0 : ((double)x - (double)m) / temp; };
+  const bool by_k = d.top_k > 0 && d.top_k < n, by_p = d.top_p < 1.0f, by_m = d.min_p > 0.0f;
+  double z = 0.0;  // the sum of all weights, where it is needed
+  if (!by_k) {
+    const double mine = span && span_max > -INFINITY && d.top_k == 0
+                            ? a.span_sum[r * a.S + t] * draw_weight(span_max, m, c) : 0.0;
+    const double before = blk.before(mine, z);
+    if (!by_p && !by_m && d.top_k == 0) {
+      // the whole softmax: the span, then the column
+      const double target = (double)d.u * z;
+      const uint64_t at = blk.least(span && before + mine > target ? (uint64_t)t : ~0ull);
+      if ((uint64_t)t == at) sh.pickd = target - before;
+      __syncthreads();
+      const int base = (int)at * kDrawSpan + t * 8;
+      Raw8<T> q;
+      float x[8];
+      load_cols(q, Y, base, a.V);
+      q.get(x);
+      double w = 0.0;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) w += x[k] > -INFINITY ? draw_weight(x[k], m, c) : 0.0;
+      double all;
+      double run = blk.before(w, all);
+      const double want = fmin(sh.pickd, all * (1.0 - 1e-15));  // (the span's sum may round otherwise)
+      uint64_t col = ~0ull;
+#pragma unroll
+      for (int k = 0; k < 8; ++k) {
+        run += x[k] > -INFINITY ? draw_weight(x[k], m, c) : 0.0;
+        if (col == ~0ull && run > want) col = (uint64_t)(base + k);
+      }
+      col = blk.least(col);
+      if (t == 0) {
+        const float xt = load1(Y + col);
+        draw_result(a, r, (int32_t)col, (float)(log_weight(xt) - log(z)), n);
+      }
+      return;
+    }
+  }
+  // the bound of the list
+  auto leave = [&]() {
+    if (t == 0) a.todo[atomicAdd(a.ntodo, 1)] = (int32_t)r;
+  };
+  float least = -INFINITY;
+  bool min_bound = false;  // everything that min-p keeps is listed, maybe not all that top-p keeps
+  if (n > kCap) {
+    if (by_k) {
+      if (d.top_k > kCap || d.top_k > G) return leave();
+      const uint32_t key = blk.largest(kBits, d.top_k, [&](uint32_t b) {
+        uint64_t count = 0;
+#pragma unroll
+        for (int k = 0; k < kMyGroups; ++k) count += key_of(g[k]) >= b ? 1 : 0;
+        return count;
+      });
+      least = value_of(key);
+    } else if (by_p) {
+      // (d.top_k > 0 here: at least n, so the sum was not formed)
+      if (d.top_k > 0 || (double)d.top_p * z > 1000.0) return leave();
+      uint64_t w[kMyGroups];
+#pragma unroll
+      for (int k = 0; k < kMyGroups; ++k) w[k] = g[k] > -INFINITY ? (uint64_t)(draw_weight(g[k], m, c) * kListScale) : 0;
+      const uint64_t target = (uint64_t)((double)d.top_p * z * (kListScale * (1.0 + 1e-9)));
+      uint64_t all = 0;
+#pragma unroll
+      for (int k = 0; k < kMyGroups; ++k) all += w[k];
+      if (blk.sum(all) < target) {
+        if (!by_m) return leave();
+      } else {
+        const uint32_t key = blk.largest(kBits, target, [&](uint32_t b) {
+          uint64_t mass = 0;
+#pragma unroll
+          for (int k = 0; k < kMyGroups; ++k) mass += key_of(g[k]) >= b ? w[k] : 0;
+          return mass;
+        });
+        least = value_of(key);
+      }
+    } else if (!by_m) {
+      return leave();  // (top-k of at least n entries and nothing else)
+    }
+    if (by_m && !(by_k && by_p)) {
+      // w >= min_p: x >= m + T log(min_p), less what the roundings may be off by
+      const double at = (double)m + temp * log((double)d.min_p);
+      const float bound = (float)(at - 1e-6 * (fabs((double)m) + fabs(at)) - 1e-30);
+      if (m < INFINITY && bound > least) {
+        least = bound;
+        min_bound = true;
+      }
+    }
+  }
+  // the groups that reach it, and their entries, both in index order
+  int ngroups;
+  {
+    uint64_t mine = 0, all;
+#pragma unroll
+    for (int k = 0; k < kMyGroups; ++k) mine += g[k] >= least && g[k] > -INFINITY ? 1 : 0;
+    int at = (int)blk.before(mine, all);
+    ngroups = (int)all;
+#pragma unroll
+    for (int k = 0; k < kMyGroups; ++k)
+      if (g[k] >= least && g[k] > -INFINITY) sh.groups[at++] = t * kMyGroups + k;
+    __syncthreads();
+  }
+  constexpr int kSets = 4, kSet = kFinish / 16;  // a set: 16 groups, a thread eight columns
+  int listed = 0;
+  for (int first = 0; first < ngroups; first += kSets * kSet) {
+    Raw8<T> q[kSets];
+    int base[kSets];
+    uint64_t counts4 = 0;  // 16 bits a set
+#pragma unroll
+    for (int s = 0; s < kSets; ++s) {
+      const int i = first + s * kSet + (t >> 4);
+      base[s] = i < ngroups ? sh.groups[i] * kDrawGroup + (t & 15) * 8 : a.V;
+      load_cols(q[s], Y, base[s], a.V);
+    }
+#pragma unroll
+    for (int s = 0; s < kSets; ++s) {
+      float x[8];
+      q[s].get(x);
+#pragma unroll
+      for (int k = 0; k < 8; ++k) counts4 += x[k] >= least && x[k] > -INFINITY ? 1ull << (16 * s) : 0ull;
+    }
+    uint64_t all;
+    const uint64_t before = blk.before(counts4, all);
+#pragma unroll
+    for (int s = 0; s < kSets; ++s) {
+      int at = listed + (int)((before >> (16 * s)) & 0xFFFFu);
+      float x[8];
+      q[s].get(x);
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if (x[k] >= least && x[k] > -INFINITY) {
+          if (at < kCap) {
+            sh.x[at] = x[k];
+            sh.col[at] = base[s] + k;
+          }
+          ++at;
+        }
+      listed += (int)((all >> (16 * s)) & 0xFFFFu);
+    }
+    if (listed > kCap) return leave();
+  }
+  __syncthreads();
+  // a thread's entries: kMine t .. kMine t + kMine - 1 of the list
+  float x[kMine];
+  uint32_t key[kMine];
+  uint64_t w[kMine];
+  bool in[kMine], enough[kMine];
+#pragma unroll
+  for (int k = 0; k < kMine; ++k) {
+    const int i = t * kMine + k;
+    in[k] = i < listed;
+    x[k] = in[k] ? sh.x[i] : -INFINITY;
+    key[k] = key_of(x[k]);
+    const double v = in[k] ? draw_weight(x[k], m, c) : 0.0;
+    w[k] = (uint64_t)(v * kListScale + 0.5);
+    enough[k] = v >= (double)d.min_p;
+  }
+  // keeps of the entries in play those larger than `at`, and the first `ties` equal to it
+  auto cut = [&](uint32_t at, uint64_t ties) {
+    uint64_t mine = 0, all;
+#pragma unroll
+    for (int k = 0; k < kMine; ++k) mine += in[k] && key[k] == at ? 1 : 0;
+    uint64_t before = blk.before(mine, all);
+#pragma unroll
+    for (int k = 0; k < kMine; ++k) {
+      if (!in[k]) continue;
+      if (key[k] == at)
+        in[k] = before++ < ties;
+      else
+        in[k] = key[k] > at;
+    }
+  };
+  auto over = [&](auto&& f) {
+    uint64_t s = 0;
+#pragma unroll
+    for (int k = 0; k < kMine; ++k) s += in[k] ? f(k) : 0ull;
+    return s;
+  };
+  if (by_k) {
+    const uint32_t at = blk.largest(kBits, d.top_k, [&](uint32_t b) { return over([&](int k) { return key[k] >= b ? 1ull : 0ull; }); });
+    cut(at, d.top_k - blk.sum(over([&](int k) { return key[k] > at ? 1ull : 0ull; })));
+  }
+  if (by_p) {
+    const uint64_t all = blk.sum(over([&](int k) { return w[k]; }));
+    const double whole = by_k || n <= kCap ? (double)all : z * kListScale;
+    const double goal = __builtin_ceil((double)d.top_p * whole);
+    if (goal <= (double)all) {
+      const uint64_t target = (uint64_t)goal;
+      const uint32_t at = blk.largest(kBits, target, [&](uint32_t b) { return over([&](int k) { return key[k] >= b ? w[k] : 0ull; }); });
+      const uint64_t above = blk.sum(over([&](int k) { return key[k] > at ? w[k] : 0ull; }));
+      const uint64_t each = (uint64_t)(draw_weight(value_of(at), m, c) * kListScale + 0.5);
+      cut(at, (target - above + each - 1) / each);
+    } else if (!min_bound) {
+      return leave();
+    }
+  }
+#pragma unroll
+  for (int k = 0; k < kMine; ++k) in[k] = in[k] && enough[k];
+  const uint64_t kept = blk.sum(over([](int) { return 1ull; }));
+  uint64_t mass;
+  const uint64_t sum = over([&](int k) { return w[k]; });
+  const uint64_t before = blk.before(sum, mass);
+  const uint64_t target = (uint64_t)((double)d.u * (double)mass);
+  if (before <= target && target < before + sum) {
+    uint64_t run = before;
+    bool found = false;
+#pragma unroll
+    for (int k = 0; k < kMine; ++k) {
+      if (!in[k] || found) continue;
+      run += w[k];
+      if (run > target) {
+        found = true;
+        draw_result(a, r, sh.col[t * kMine + k], (float)(log_weight(x[k]) - log((double)mass / kListScale)), (int32_t)kept);
+      }
+    }
+  }
+}
+
+template <typename T, int kThreads>
+void launch_rows(const DrawArgs& a, int64_t groups, hipStream_t s) {
+  hipLaunchKernelGGL((k_draw_row<T, kThreads>), dim3((unsigned)groups), dim3(kThreads), 0, s, a);
+}
+
+template <typename T>
+hipError_t launch_t(DrawArgs a, hipStream_t s) {
+  if (a.todo != nullptr) {
+    const int64_t waves = a.R * ((a.S + a.per - 1) / a.per);
+    hipLaunchKernelGGL((k_draw_sweep<T>), dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((k_draw_finish<T>), dim3((unsigned)a.R), dim3(kFinish), 0, s, a);
+    if (a.V <= kCap) return hipGetLastError();  // (every list fits)
+  }
+  const int64_t groups = a.todo != nullptr && a.R > 512 ? 512 : a.R;
   if (a.V <= 4096)
-    hipLaunchKernelGGL((k_draw_row<T, 256>), grid, dim3(256), 0, s, a);
+    launch_rows<T, 256>(a, groups, s);
   else
-    hipLaunchKernelGGL((k_draw_row<T, 1024>), grid, dim3(1024), 0, s, a);
+    launch_rows<T, 1024>(a, groups, s);
   return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_draw(const DrawArgs& a, bool bf16, hipStream_t s) {
+hipError_t launch_draw(DrawArgs a, bool bf16, hipStream_t s) {
+  if (a.todo != nullptr) {
+    // spans a wavefront sweeps: one until the chip is full several times over
+    a.per = 1;
+    while (a.per < 8 && a.R * ((a.S + a.per - 1) / a.per) > 65536) a.per *= 2;
+  }
   return bf16 ? launch_t<bf16_t>(a, s) : launch_t<float>(a, s);
 }
 

@@ -1441,9 +1441,19 @@ vsd_status vsd_sample_rows(const vsd_rows* rows, const vsd_src* target, const vs
   if (!usable_setting(draw))
     return fail(VSD_ERR_INVALID_VALUE, "temp=%g (0 or [1e-30, 1e30]), top_k=%d (>= 0), top_p=%g ((0, 1]) or min_p=%g "
                 "([0, 1]) out of range", draw->temp, draw->top_k, draw->top_p, draw->min_p);
-  (void)workspace;
-  (void)workspace_bytes;
+  const vsd::DrawLayout w = vsd::draw_layout(rows->R, rows->v);
+  if ((st = check_workspace(workspace, workspace_bytes, (size_t)w.total)) != VSD_OK) return st;
   vsd::DrawArgs a{};
+  if (w.S > 0) {
+    char* const ws = static_cast<char*>(workspace);
+    a.S = w.S;
+    a.group_max = reinterpret_cast<float*>(ws + w.group_max);
+    a.span_sum = reinterpret_cast<double*>(ws + w.span_sum);
+    a.span_max = reinterpret_cast<float*>(ws + w.span_max);
+    a.span_count = reinterpret_cast<int32_t*>(ws + w.span_count);
+    a.ntodo = reinterpret_cast<int32_t*>(ws + w.todo);
+    a.todo = a.ntodo + 1;
+  }
   a.Y = target->logits;
   a.R = rows->R;
   a.ld = rows->ld;
@@ -1470,7 +1480,7 @@ vsd_status vsd_draw_workspace_bytes(const vsd_rows* rows, size_t* bytes) {
   vsd_status st = check_rows_struct(rows);
   if (st != VSD_OK) return st;
   if (bytes == nullptr) return fail(VSD_ERR_NULL_POINTER, "bytes is NULL");
-  *bytes = 0;
+  *bytes = (size_t)vsd::draw_layout(rows->R, rows->v).total;
   return ok();
 }
 

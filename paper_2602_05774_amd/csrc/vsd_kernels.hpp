@@ -662,7 +662,38 @@ struct DrawArgs {
   float* log_prob;             // [R] or null
   int32_t* kept;               // [R] or null
   int32_t* err;
+  // the sweep's records, per row: S spans of kDrawSpan columns, 16 groups of a span
+  int32_t S;
+  int32_t per;                 // spans a wavefront sweeps
+  float* group_max;            // [R, 16 S]
+  double* span_sum;            // [R, S] weights relative to the span's largest logit
+  float* span_max;             // [R, S]
+  int32_t* span_count;         // [R, S] entries; -1: a NaN among them
+  int32_t* todo;               // rows left to k_draw_row, ntodo[0] of them
+  int32_t* ntodo;
 };
+constexpr int kDrawSpan = 2048, kDrawGroup = 128, kDrawSpans = 128;  // (the most spans that the records are for)
+struct DrawLayout {
+  int32_t S;                   // 0: no records
+  int64_t group_max, span_sum, span_max, span_count, todo, total;  // offsets
+};
+inline DrawLayout draw_layout(int64_t R, int32_t V) {
+  DrawLayout w{};
+  const int64_t S = ((int64_t)V + kDrawSpan - 1) / kDrawSpan;
+  if (S > kDrawSpans) return w;
+  w.S = (int32_t)S;
+  auto take = [&](int64_t bytes) {
+    const int64_t at = w.total;
+    w.total += (bytes + 255) / 256 * 256;
+    return at;
+  };
+  w.group_max = take(R * S * 16 * 4);
+  w.span_sum = take(R * S * 8);
+  w.span_max = take(R * S * 4);
+  w.span_count = take(R * S * 4);
+  w.todo = take((R + 1) * 4);
+  return w;
+}
 
 // x [rows, cols] to 8-bit values and scales (of x^T: values [cols, out_ld]).
 struct QuantArgs {
@@ -765,7 +796,7 @@ struct GradScale {
   float* scale_out;
 };
 
-hipError_t launch_draw(const DrawArgs& a, bool bf16, hipStream_t s);
+hipError_t launch_draw(DrawArgs a, bool bf16, hipStream_t s);
 hipError_t launch_quantize(const QuantArgs& a, bool bf16, int group, bool trans, hipStream_t s);
 hipError_t launch_block_product(BlockArgs a, const BlockPlan& p, int group, bool bf16, void* workspace, hipStream_t s);
 hipError_t launch_grad_squares(const GradTable& t, double* part, hipStream_t s);
