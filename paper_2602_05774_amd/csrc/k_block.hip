@@ -11,7 +11,8 @@
 //
 // Many rows: 256 x 256 tiles (vsd_block_tiles.hpp), the sum in ranges where there are
 // few tiles.
-// Few rows: a wavefront owns a 32 x 32 tile and walks the blocks: each block's product
+// Few rows: a stream of b (k_block_few).  Rows too long for the tiles' offsets: a
+// wavefront per 32 x 32 tile that walks the blocks.  In all of them a block's product
 // is formed on the matrix cores from zero and added, times its scales, in fp32.
 #include "vsd_block_tiles.hpp"
 
@@ -74,6 +75,78 @@ __global__ __launch_bounds__(kWave) void k_block_product(BlockArgs a) {
   }
 }
 
+// Few rows (kTiles x 32 at most): a stream of b.  A workgroup owns 32 of b's rows; its
+// wavefronts take the blocks of its range in turn, the next block's loads in flight
+// (64 bytes of a row a lane, whole cache lines), and their sums meet in LDS in the
+// wavefronts' order.
+template <typename O, bool EXACT, int kGroup, int kTiles, int kWaves>
+__global__ __launch_bounds__(kWaves * kWave) void k_block_few(BlockArgs a) {
+  __shared__ float sums[kWaves - 1][kTiles * 16][kWave];
+  const int lane = threadIdx.x & 63, wave = wave_id();
+  const int64_t n0 = (int64_t)blockIdx.x * 32, n = min(n0 + (lane & 31), a.N - 1);
+  const int64_t begin = (int64_t)blockIdx.y * a.per, end = min(begin + a.per, a.blocks);
+  const uint8_t* const pb = a.b + n * a.ldb + (lane >> 5) * 32;
+  const float* const sb = a.sb + n / kGroup;
+  const uint8_t* pa[kTiles];
+#pragma unroll
+  for (int t = 0; t < kTiles; ++t) pa[t] = a.a + min((int64_t)(t * 32 + (lane & 31)), a.M - 1) * a.lda + (lane >> 5) * 32;
+  struct Step {
+    i32x8 b[2], a[kTiles][2];
+    float sb;
+  };
+  auto load = [&](int64_t j) {
+    Step s;
+    s.b[0] = load32(pb + j * 128);
+    s.b[1] = load32(pb + j * 128 + 64);
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) {
+      s.a[t][0] = load32(pa[t] + j * 128);
+      s.a[t][1] = load32(pa[t] + j * 128 + 64);
+    }
+    s.sb = sb[j * a.ldsb];
+    return s;
+  };
+  f32x16 acc[kTiles] = {};
+  int64_t j = begin + wave;
+  Step next;
+  if (j < end) next = load(j);
+  for (; j < end; j += kWaves) {
+    const Step s = next;
+    next = load(min(j + kWaves, end - 1));
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t) {
+      // (a lane's results: column l % 32, rows 8 (e / 4) + 4 (l / 32) + e % 4 of a tile)
+      f32x16 c = block_step<EXACT>(s.a[t][0], s.b[0], f32x16{});
+      c = block_step<EXACT>(s.a[t][1], s.b[1], c);
+      const float* const sa = a.sa + j * a.ldsa;
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const int64_t row = t * 32 + 8 * (e >> 2) + 4 * (lane >> 5) + (e & 3);
+        acc[t][e] = fmaf(c[e], sa[min(row, a.M - 1)] * s.sb, acc[t][e]);
+      }
+    }
+  }
+  if (wave > 0) {
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) sums[wave - 1][t * 16 + e][lane] = acc[t][e];
+  }
+  __syncthreads();
+  if (wave > 0 || n0 + (lane & 31) >= a.N) return;
+  O* const out = static_cast<O*>(a.out) + (int64_t)blockIdx.y * a.range_stride;
+#pragma unroll
+  for (int t = 0; t < kTiles; ++t)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const int64_t row = t * 32 + 8 * (e >> 2) + 4 * (lane >> 5) + (e & 3);
+      float v = acc[t][e];
+#pragma unroll
+      for (int w = 0; w < kWaves - 1; ++w) v += sums[w][t * 16 + e][lane];
+      if (row < a.M) store1(out + row * a.ldo + n, v);
+    }
+}
+
 // The sum over the ranges, in their order.
 template <typename O>
 __global__ __launch_bounds__(256) void k_block_join(const float* part, int ranges, int64_t M, int64_t N, int64_t ldp, O* out,
@@ -97,6 +170,50 @@ __global__ __launch_bounds__(256) void k_block_join(const float* part, int range
         if (c + k < N) store1(to + k, x[k]);
     }
   }
+}
+
+// The ranges' sums (in the workspace) to the result.
+template <typename O>
+void launch_join(const BlockArgs& a, int ranges, int64_t ldp, const char* ws, hipStream_t s) {
+  const int64_t n = (a.M * ldp / 8 + 255) / 256;
+  hipLaunchKernelGGL((k_block_join<O>), dim3((unsigned)(n < 4096 ? n : 4096)), dim3(256), 0, s,
+                     reinterpret_cast<const float*>(ws), ranges, a.M, a.N, ldp, static_cast<O*>(a.out), a.ldo);
+}
+
+template <typename O, bool EXACT, int kGroup>
+void launch_few_t(const BlockArgs& a, const BlockPlan& p, hipStream_t s) {
+  const dim3 grid((unsigned)((a.N + 31) / 32), (unsigned)p.ranges);
+  if (a.M <= 32 && p.waves == 4)
+    hipLaunchKernelGGL((k_block_few<O, EXACT, kGroup, 1, 4>), grid, dim3(256), 0, s, a);
+  else if (a.M <= 32)
+    hipLaunchKernelGGL((k_block_few<O, EXACT, kGroup, 1, 8>), grid, dim3(512), 0, s, a);
+  else if (p.waves == 4)
+    hipLaunchKernelGGL((k_block_few<O, EXACT, kGroup, 2, 4>), grid, dim3(256), 0, s, a);
+  else
+    hipLaunchKernelGGL((k_block_few<O, EXACT, kGroup, 2, 8>), grid, dim3(512), 0, s, a);
+}
+
+template <typename O>
+hipError_t launch_few(BlockArgs a, const BlockPlan& p, int group, char* ws, hipStream_t s) {
+  constexpr bool kExact = sizeof(O) == 4;
+  a.per = p.per;
+  if (p.ranges == 1) {
+    if (group == 1)
+      launch_few_t<O, kExact, 1>(a, p, s);
+    else
+      launch_few_t<O, kExact, 128>(a, p, s);
+    return hipGetLastError();
+  }
+  BlockArgs r = a;
+  r.out = ws;
+  r.ldo = (a.N + 7) / 8 * 8;
+  r.range_stride = a.M * r.ldo;
+  if (group == 1)
+    launch_few_t<float, kExact, 1>(r, p, s);
+  else
+    launch_few_t<float, kExact, 128>(r, p, s);
+  launch_join<O>(a, p.ranges, r.ldo, ws, s);
+  return hipGetLastError();
 }
 
 template <bool F8, typename O>
@@ -138,15 +255,14 @@ hipError_t launch_by_tiles(const BlockArgs& a, const BlockPlan& p, int group, ch
   t.ldo = (a.N + 7) / 8 * 8;
   t.range_stride = a.M * t.ldo;
   launch_tiles<!kF32, float>(t, group, p.ranges, s);
-  const int64_t n = (a.M * t.ldo / 8 + 255) / 256;
-  hipLaunchKernelGGL((k_block_join<O>), dim3((unsigned)(n < 4096 ? n : 4096)), dim3(256), 0, s,
-                     reinterpret_cast<const float*>(ws), p.ranges, a.M, a.N, t.ldo, static_cast<O*>(a.out), a.ldo);
+  launch_join<O>(a, p.ranges, t.ldo, ws, s);
   return hipGetLastError();
 }
 
 template <typename O>
 hipError_t launch_t(const BlockArgs& a, const BlockPlan& p, int group, char* ws, hipStream_t s) {
   if (p.tiles) return launch_by_tiles<O>(a, p, group, ws, s);
+  if (a.M <= kBlockFewRows) return launch_few<O>(a, p, group, ws, s);
   const dim3 grid((unsigned)(a.mt * ((a.N + 31) / 32)));
   if (group == 1)
     hipLaunchKernelGGL((k_block_product<O, 1>), grid, dim3(kWave), 0, s, a);

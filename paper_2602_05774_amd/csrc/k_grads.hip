@@ -16,11 +16,6 @@ namespace {
 
 constexpr int kThreads = 256;
 
-template <typename T>
-__device__ __forceinline__ float element(const void* p, int64_t i) {
-  return load1(static_cast<const T*>(p) + i);
-}
-
 // f(chunk, tensor) for this workgroup's chunks of the table
 template <class F>
 __device__ __forceinline__ void chunks(const GradTable& t, F&& f) {
@@ -31,14 +26,36 @@ __device__ __forceinline__ void chunks(const GradTable& t, F&& f) {
   }
 }
 
-// f(index into the source, index into the output) for a thread's elements of a chunk
-template <class F>
-__device__ __forceinline__ void elements(const GradEntry& e, int chunk, F&& f) {
-  const int64_t n = e.rows * e.cols, lo = (int64_t)chunk * kGradChunk, hi = min(lo + kGradChunk, n);
-  for (int64_t i = lo + threadIdx.x; i < hi; i += kThreads) {
-    const int64_t r = e.rows == 1 ? 0 : i / e.cols, c = i - r * e.cols;
-    f(r * e.ld + c, r * e.out_ld + c);
+// Elements by address: their number up to the next multiple of 16 bytes.
+__device__ __forceinline__ int to_aligned(const void* p, int es) {
+  return (int)((16 - (reinterpret_cast<uintptr_t>(p) & 15u)) & 15u) / es;
+}
+
+// A chunk of a tensor: one(i, o) for single elements (offsets into the source and
+// the output), eight(i, o) for eight from a 16-byte boundary of both.
+template <class One, class Eight>
+__device__ __forceinline__ void elements(const GradEntry& e, int chunk, One&& one, Eight&& eight) {
+  const int64_t n = e.rows * e.cols, lo = (int64_t)chunk * kGradChunk;
+  const int len = (int)min((int64_t)kGradChunk, n - lo), t = threadIdx.x;
+  if (e.rows > 1) {
+    for (int i = t; i < len; i += kThreads) {
+      const int64_t r = (lo + i) / e.cols, c = lo + i - r * e.cols;
+      one(r * e.ld + c, r * e.out_ld + c);
+    }
+    return;
   }
+  const int es = e.bf16 ? 2 : 4, out_es = e.out_bf16 ? 2 : 4;
+  const int head = min(len, to_aligned(static_cast<const char*>(e.p) + lo * es, es));
+  const bool both = ((reinterpret_cast<uintptr_t>(e.out) + (lo + head) * out_es) & 15u) == 0;
+  const int body = both ? (len - head) / 8 : 0, tail = head + body * 8;
+  if (t < head) one(lo + t, lo + t);
+  if (body == kGradChunk / 8) {  // (the usual chunk: all its loads may be in flight)
+#pragma unroll
+    for (int k = 0; k < kGradChunk / 8 / kThreads; ++k) eight(lo + (k * kThreads + t) * 8, lo + (k * kThreads + t) * 8);
+    return;
+  }
+  for (int i = t; i < body; i += kThreads) eight(lo + head + i * 8, lo + head + i * 8);
+  for (int i = tail + t; i < len; i += kThreads) one(lo + i, lo + i);
 }
 
 __device__ __forceinline__ double block_sum(double v, double* red) {
@@ -50,17 +67,34 @@ __device__ __forceinline__ double block_sum(double v, double* red) {
   return (red[0] + red[1]) + (red[2] + red[3]);
 }
 
+template <typename T>
+__device__ __forceinline__ void squares(const GradEntry& e, int chunk, double (&s)[4]) {
+  const T* p = static_cast<const T*>(e.p);
+  elements(
+      e, chunk,
+      [&](int64_t i, int64_t) {
+        const double x = load1(p + i);
+        s[0] = __builtin_fma(x, x, s[0]);
+      },
+      [&](int64_t i, int64_t) {
+        float x[8];
+        load8(p + i, x);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) s[k & 3] = __builtin_fma((double)x[k], (double)x[k], s[k & 3]);
+      });
+}
+
 __global__ __launch_bounds__(kThreads) void k_grad_squares(GradTable t, double* part) {
   __shared__ double red[kThreads / kWave];
-  double s = 0.0;
+  double s[4] = {0.0, 0.0, 0.0, 0.0};
   chunks(t, [&](int chunk, const GradEntry& e) {
-    elements(e, chunk, [&](int64_t i, int64_t) {
-      const double x = e.bf16 ? element<bf16_t>(e.p, i) : element<float>(e.p, i);
-      s = __builtin_fma(x, x, s);
-    });
+    if (e.bf16)
+      squares<bf16_t>(e, chunk, s);
+    else
+      squares<float>(e, chunk, s);
   });
-  s = block_sum(s, red);
-  if (threadIdx.x == 0) part[blockIdx.x] = s;
+  const double all = block_sum((s[0] + s[1]) + (s[2] + s[3]), red);
+  if (threadIdx.x == 0) part[blockIdx.x] = all;
 }
 
 __device__ __forceinline__ double norm_of(const double* part, int n, double* red) {
@@ -75,6 +109,21 @@ __global__ __launch_bounds__(kThreads) void k_grad_norm(const double* part, int 
   if (threadIdx.x == 0) *norm = (float)v;
 }
 
+template <typename T, typename O>
+__device__ __forceinline__ void scaled(const GradEntry& e, int chunk, float scale) {
+  const T* p = static_cast<const T*>(e.p);
+  O* const out = static_cast<O*>(e.out);
+  elements(
+      e, chunk, [&](int64_t i, int64_t o) { store1(out + o, load1(p + i) * scale); },
+      [&](int64_t i, int64_t o) {
+        float x[8];
+        load8(p + i, x);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) x[k] *= scale;
+        store8(out + o, x);
+      });
+}
+
 __global__ __launch_bounds__(kThreads) void k_grad_scale(GradTable t, GradScale g) {
   __shared__ double red[kThreads / kWave];
   const double norm = g.norm != nullptr ? (double)*g.norm : norm_of(g.part, g.parts, red);
@@ -86,13 +135,14 @@ __global__ __launch_bounds__(kThreads) void k_grad_scale(GradTable t, GradScale 
   }
   chunks(t, [&](int chunk, const GradEntry& e) {
     if (scale == 1.0f && e.out == e.p) return;
-    elements(e, chunk, [&](int64_t i, int64_t o) {
-      const float x = (e.bf16 ? element<bf16_t>(e.p, i) : element<float>(e.p, i)) * scale;
-      if (e.out_bf16)
-        store1(static_cast<bf16_t*>(e.out) + o, x);
-      else
-        store1(static_cast<float*>(e.out) + o, x);
-    });
+    if (e.bf16 && e.out_bf16)
+      scaled<bf16_t, bf16_t>(e, chunk, scale);
+    else if (e.bf16)
+      scaled<bf16_t, float>(e, chunk, scale);
+    else if (e.out_bf16)
+      scaled<float, bf16_t>(e, chunk, scale);
+    else
+      scaled<float, float>(e, chunk, scale);
   });
 }
 

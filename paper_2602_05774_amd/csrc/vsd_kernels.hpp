@@ -715,6 +715,7 @@ struct BlockArgs {
   void* out;
   int64_t M, N, blocks, lda, ldb, ldsa, ldsb, ldo;
   int64_t mt;                  // row tiles
+  int64_t per, range_stride;   // few rows: blocks of range blockIdx.y, elements between two ranges' results
 };
 
 // The same by 256 x 256 tiles: a workgroup takes `run` column tiles of a row tile,
@@ -738,13 +739,26 @@ constexpr int64_t kBlockMaxLd = 1 << 22;    // bytes of a row: 256 of them withi
 constexpr int kBlockCus = 256, kBlockMaxRanges = 16;
 struct BlockPlan {
   bool tiles;
-  int32_t run, runs, ranges, per;  // as in BlockTileArgs
+  int32_t run, runs;               // as in BlockTileArgs
+  int32_t ranges, per;             // ranges of the sum, blocks of one
+  int32_t waves;                   // few rows: wavefronts that share a workgroup's range
   int64_t total;                   // bytes of the ranges' sums (the workspace)
 };
 inline BlockPlan block_plan(int64_t M, int64_t N, int64_t blocks, int64_t lda, int64_t ldb, bool f32) {
   BlockPlan p{};
   const int64_t mt = (M + 255) / 256, nt = (N + 255) / 256, stages = blocks;
-  if (M <= kBlockFewRows || (lda > ldb ? lda : ldb) > kBlockMaxLd || mt * nt >= 1 << 22) return p;
+  if (M <= kBlockFewRows) {
+    // a workgroup per 32 columns; its wavefronts, and where those workgroups do not
+    // fill the chip ranges too, share the blocks, four at least each
+    const int64_t cols = (N + 31) / 32;
+    p.waves = cols >= 2 * kBlockCus || blocks < 32 ? 4 : 8;
+    p.ranges = 1;
+    while (p.ranges < kBlockMaxRanges && cols * p.ranges < kBlockCus && blocks >= 8 * p.waves * p.ranges) p.ranges *= 2;
+    p.per = (int32_t)((blocks + p.ranges - 1) / p.ranges);
+    if (p.ranges > 1) p.total = (int64_t)p.ranges * M * ((N + 7) / 8 * 8) * 4;
+    return p;
+  }
+  if ((lda > ldb ? lda : ldb) > kBlockMaxLd || mt * nt >= 1 << 22) return p;
   p.tiles = true;
   // time in us: a block takes about one (fp32 results two), a run three to start, a
   // tile two to be stored; ranges' sums are written and read at some 4 MB a us
@@ -773,7 +787,7 @@ inline BlockPlan block_plan(int64_t M, int64_t N, int64_t blocks, int64_t lda, i
 
 // Gradients of one launch: `rows` rows of `cols` elements each, in chunks of
 // kGradChunk elements that the launch's workgroups take in turn.
-constexpr int kGradTable = 48, kGradChunk = 16384, kGradGroups = 1024;
+constexpr int kGradTable = 64, kGradChunk = 8192, kGradGroups = 2048;
 struct GradEntry {
   const void* p;
   void* out;                   // (the sums of squares: unused)
@@ -786,7 +800,7 @@ struct GradTable {
   int32_t n, chunks, groups;
   int32_t first;               // this launch writes the call's norm and scale
 };
-static_assert(sizeof(GradTable) <= 3584, "a kernel's arguments are 4 KB at most");
+static_assert(sizeof(GradTable) <= 3840, "a kernel's arguments are 4 KB at most");
 struct GradScale {
   const double* part;          // the launches' sums of squares ...
   int32_t parts;
