@@ -78,7 +78,7 @@ class VsdBlocks(ctypes.Structure):
                 ("scale_ld", c_i64), ("group", c_i32)]
 
 
-class VsdTensor(ctypes.Structure):
+class VsdTensor(ctypes.Structure):  # (vsd_grad_norm and vsd_clip_gradients take arrays of it, as addresses)
     _fields_ = [("data", c_vp), ("rows", c_i64), ("cols", c_i64), ("ld", c_i64), ("dtype", c_i32)]
 
 
@@ -157,8 +157,8 @@ def load():
     lib.vsd_quantize_blocks.argtypes = [c_vp, c_i64, c_i64, c_i64, c_i32, c_i32, P(VsdBlocks), c_vp]
     lib.vsd_block_product.argtypes = [P(VsdBlocks), P(VsdBlocks), c_vp, c_i64, c_i32, c_vp, ctypes.c_size_t, c_vp]
     lib.vsd_product_workspace_bytes.argtypes = [P(VsdBlocks), P(VsdBlocks), c_i32, P(ctypes.c_size_t)]
-    lib.vsd_grad_norm.argtypes = [P(VsdTensor), c_i32, c_vp, c_vp, ctypes.c_size_t, c_vp]
-    lib.vsd_clip_gradients.argtypes = [P(VsdTensor), P(VsdTensor), c_i32, c_f32, c_vp, c_vp, c_vp, c_vp,
+    lib.vsd_grad_norm.argtypes = [c_vp, c_i32, c_vp, c_vp, ctypes.c_size_t, c_vp]
+    lib.vsd_clip_gradients.argtypes = [c_vp, c_vp, c_i32, c_f32, c_vp, c_vp, c_vp, c_vp,
                                        ctypes.c_size_t, c_vp]
     lib.vsd_norm_workspace_bytes.argtypes = [c_i32, P(ctypes.c_size_t)]
     for call in (lib.vsd_sample_rows, lib.vsd_draw_workspace_bytes, lib.vsd_quantize_blocks, lib.vsd_block_product,

@@ -16,13 +16,16 @@ namespace {
 
 constexpr int kThreads = 256;
 
-// f(chunk, tensor) for this workgroup's chunks of the table
+// f(chunk, tensor) for this workgroup's chunks of the table; lane k looks at tensor k
+// (a search of the arguments would wait for one load after another).
 template <class F>
 __device__ __forceinline__ void chunks(const GradTable& t, F&& f) {
-  int k = 0;
+  static_assert(kGradTable <= kWave, "a lane per tensor");
+  const int lane = threadIdx.x & 63;
+  const int first = lane < kGradTable ? t.first[lane] : 0x7FFFFFFF;
   for (int c = blockIdx.x; c < t.chunks; c += gridDim.x) {
-    while (k + 1 < t.n && t.e[k + 1].first <= c) ++k;
-    f(c - t.e[k].first, t.e[k]);
+    const int k = __builtin_popcountll(__ballot(first <= c)) - 1;
+    f(c - lane_i(first, k), t.e[k]);
   }
 }
 
@@ -129,7 +132,7 @@ __global__ __launch_bounds__(kThreads) void k_grad_scale(GradTable t, GradScale 
   const double norm = g.norm != nullptr ? (double)*g.norm : norm_of(g.part, g.parts, red);
   const bool finite = norm <= 1.7976931348623157e308;
   const float scale = !finite ? 1.0f : norm > (double)g.max_norm ? (float)((double)g.max_norm / norm) : 1.0f;
-  if (blockIdx.x == 0 && threadIdx.x == 0 && t.first) {
+  if (blockIdx.x == 0 && threadIdx.x == 0 && t.reports) {
     if (g.norm_out != nullptr) *g.norm_out = (float)norm;
     if (g.scale_out != nullptr) *g.scale_out = finite ? scale : __builtin_nanf("");
   }

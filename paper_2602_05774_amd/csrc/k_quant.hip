@@ -31,8 +31,9 @@ __device__ __forceinline__ uint32_t pack4(float a, float b, float c, float d) {
   return (uint32_t)v;
 }
 
-// TRANS: the result's rows are x's columns.
-template <typename T, int kGroup, bool TRANS>
+// TRANS: the result's rows are x's columns.  ALIGNED: x's rows start at multiples of
+// 16 bytes.
+template <typename T, int kGroup, bool TRANS, bool ALIGNED>
 __global__ __launch_bounds__(kThreads) void k_quantize(QuantArgs a) {
   __shared__ uint32_t part[16][128];
   __shared__ __align__(16) uint32_t out[TRANS ? 128 * 33 : 1];
@@ -43,8 +44,12 @@ __global__ __launch_bounds__(kThreads) void k_quantize(QuantArgs a) {
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const int64_t r = row0 + tr * 8 + i, c = col0 + tc * 8;
+    if (ALIGNED && r < a.rows && c + 8 <= a.cols) {
+      load8(X + r * a.ld + c, x[i]);
+    } else {
 #pragma unroll
-    for (int k = 0; k < 8; ++k) x[i][k] = r < a.rows && c + k < a.cols ? load1(X + r * a.ld + c + k) : 0.0f;
+      for (int k = 0; k < 8; ++k) x[i][k] = r < a.rows && c + k < a.cols ? load1(X + r * a.ld + c + k) : 0.0f;
+    }
   }
   uint32_t amax[8];  // of a row (TRANS: of a column) of the thread's
 #pragma unroll
@@ -106,10 +111,12 @@ __global__ __launch_bounds__(kThreads) void k_quantize(QuantArgs a) {
     to[1] = pack4(q[4], q[5], q[6], q[7]);
   }
   __syncthreads();
-  for (int i = t; i < 128 * 32; i += kThreads) {
-    const int c = i >> 5, w = i & 31;
+#pragma unroll
+  for (int i = t; i < 128 * 8; i += kThreads) {
+    const int c = i >> 3, w = (i & 7) * 4;
+    const uint32_t* const from = out + c * 33 + w;
     if (col0 + c < a.cols)
-      *reinterpret_cast<uint32_t*>(a.values + (col0 + c) * a.out_ld + row0 + w * 4) = out[c * 33 + w];
+      *reinterpret_cast<uint4*>(a.values + (col0 + c) * a.out_ld + row0 + w * 4) = make_uint4(from[0], from[1], from[2], from[3]);
   }
 }
 
@@ -120,13 +127,13 @@ __global__ __launch_bounds__(kThreads) void k_quant_pad(uint8_t* values, int64_t
     *reinterpret_cast<uint4*>(values + i / per * ld + from + i % per * 16) = make_uint4(0, 0, 0, 0);
 }
 
-template <typename T>
+template <typename T, bool ALIGNED>
 hipError_t launch_t(const QuantArgs& a, int group, bool trans, hipStream_t s) {
   const dim3 grid((unsigned)a.tiles), block(kThreads);
-  if (group == 1 && !trans) hipLaunchKernelGGL((k_quantize<T, 1, false>), grid, block, 0, s, a);
-  if (group == 1 && trans) hipLaunchKernelGGL((k_quantize<T, 1, true>), grid, block, 0, s, a);
-  if (group != 1 && !trans) hipLaunchKernelGGL((k_quantize<T, 128, false>), grid, block, 0, s, a);
-  if (group != 1 && trans) hipLaunchKernelGGL((k_quantize<T, 128, true>), grid, block, 0, s, a);
+  if (group == 1 && !trans) hipLaunchKernelGGL((k_quantize<T, 1, false, ALIGNED>), grid, block, 0, s, a);
+  if (group == 1 && trans) hipLaunchKernelGGL((k_quantize<T, 1, true, ALIGNED>), grid, block, 0, s, a);
+  if (group != 1 && !trans) hipLaunchKernelGGL((k_quantize<T, 128, false, ALIGNED>), grid, block, 0, s, a);
+  if (group != 1 && trans) hipLaunchKernelGGL((k_quantize<T, 128, true, ALIGNED>), grid, block, 0, s, a);
   return hipGetLastError();
 }
 
@@ -139,7 +146,9 @@ hipError_t launch_quantize(const QuantArgs& a, bool bf16, int group, bool trans,
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  return bf16 ? launch_t<bf16_t>(a, group, trans, s) : launch_t<float>(a, group, trans, s);
+  const bool aligned = (reinterpret_cast<uintptr_t>(a.x) | (uint64_t)(a.ld * (bf16 ? 2 : 4))) % 16 == 0;
+  if (aligned) return bf16 ? launch_t<bf16_t, true>(a, group, trans, s) : launch_t<float, true>(a, group, trans, s);
+  return bf16 ? launch_t<bf16_t, false>(a, group, trans, s) : launch_t<float, false>(a, group, trans, s);
 }
 
 }  // namespace vsd

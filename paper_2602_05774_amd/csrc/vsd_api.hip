@@ -793,12 +793,14 @@ template <class F>
 hipError_t grad_launches(const vsd_tensor* g, const vsd_tensor* out, int32_t n, F&& launch) {
   for (int32_t at = 0; at < n; at += vsd::kGradTable) {
     vsd::GradTable t{};
-    t.first = at == 0;
+    t.reports = at == 0;
+    for (int32_t& first : t.first) first = 0x7FFFFFFF;
     int64_t chunks = 0;
     for (int32_t i = at; i < n && i < at + vsd::kGradTable; ++i) {
       const vsd_tensor& o = out == nullptr ? g[i] : out[i];
       const int64_t size = g[i].rows * g[i].cols;
       if (size == 0) continue;
+      t.first[t.n] = (int32_t)chunks;
       vsd::GradEntry& e = t.e[t.n++];
       const bool flat = g[i].rows == 1 || (g[i].ld == g[i].cols && o.ld == o.cols);
       e.p = g[i].data;
@@ -807,7 +809,6 @@ hipError_t grad_launches(const vsd_tensor* g, const vsd_tensor* out, int32_t n, 
       e.cols = flat ? size : g[i].cols;
       e.ld = flat ? size : g[i].ld;
       e.out_ld = flat ? size : o.ld;
-      e.first = (int32_t)chunks;
       e.bf16 = g[i].dtype == VSD_BF16;
       e.out_bf16 = o.dtype == VSD_BF16;
       chunks += (size + vsd::kGradChunk - 1) / vsd::kGradChunk;

@@ -787,18 +787,18 @@ inline BlockPlan block_plan(int64_t M, int64_t N, int64_t blocks, int64_t lda, i
 
 // Gradients of one launch: `rows` rows of `cols` elements each, in chunks of
 // kGradChunk elements that the launch's workgroups take in turn.
-constexpr int kGradTable = 64, kGradChunk = 8192, kGradGroups = 2048;
+constexpr int kGradTable = 56, kGradChunk = 8192, kGradGroups = 2048;
 struct GradEntry {
   const void* p;
   void* out;                   // (the sums of squares: unused)
   int64_t rows, cols, ld, out_ld;
-  int32_t first;               // the tensor's first chunk
-  uint8_t bf16, out_bf16;
+  int32_t bf16, out_bf16;
 };
 struct GradTable {
   GradEntry e[kGradTable];
+  int32_t first[kGradTable];   // each tensor's first chunk (past the last tensor: none has it)
   int32_t n, chunks, groups;
-  int32_t first;               // this launch writes the call's norm and scale
+  int32_t reports;             // this launch writes the call's norm and scale
 };
 static_assert(sizeof(GradTable) <= 3840, "a kernel's arguments are 4 KB at most");
 struct GradScale {
