@@ -47,6 +47,21 @@ __device__ __forceinline__ i32x8 load32(const uint8_t* p) {
   return i32x8{u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
 }
 
+// One block of a 16 x 16 tile, lane l holding 32 bytes of row l % 16 of both operands:
+// the result's column l % 16, rows 4 (l / 16) .. + 3.
+template <bool EXACT>
+__device__ __forceinline__ f32x4 block16(const i32x8& a, const i32x8& b) {
+  f32x4 c{};
+  if constexpr (EXACT) {
+#pragma unroll
+    for (int k = 0; k < 8; k += 2)
+      c = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(a[k], a[k + 1]), widen(b[k], b[k + 1]), c, 0, 0, 0);
+  } else {
+    c = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 0, 0, 0, 0);
+  }
+  return c;
+}
+
 template <typename O, int kGroup>
 __global__ __launch_bounds__(kWave) void k_block_product(BlockArgs a) {
   const int lane = threadIdx.x;
@@ -75,87 +90,89 @@ __global__ __launch_bounds__(kWave) void k_block_product(BlockArgs a) {
   }
 }
 
-// Few rows (kTiles x 32 at most): a stream of b.  A workgroup owns 32 of b's rows; its
-// wavefronts take the blocks of its range in turn, the next block's loads in flight
-// (64 bytes of a row a lane, whole cache lines), and their sums meet in LDS in the
-// wavefronts' order.  b's rows are the products' rows (registers) and a's their
-// columns (lanes), so that a's scales are one load a block and b's, of 128 rows, one
-// for all: with the factors the other way round each block took 16 loads of a's
-// scales and one token (32 000 x 4096) 35 us, 48 rows (32 003 x 2048, fp32) 32.
+// Few rows (16 kTiles at most): a stream of b.  A workgroup owns 32 of b's rows, as two
+// tiles of 16; its wavefronts take the blocks of its range in turn, the next block of b
+// in flight, and their sums meet in LDS in the wavefronts' order.  Four lanes read 64
+// consecutive bytes of a row (a value's place in the sum is free, so the lanes of a
+// row take neighbouring 16-byte chunks): with the 32 x 32 instructions and 16 bytes of
+// 64 rows a load, addresses bounded it (us, that / this: @FEW@).
+// b's rows are the products' rows (registers) and a's their columns (lanes), so that
+// a's scales are one load a block and b's, of 128 rows, one for all.
 template <typename O, bool EXACT, int kGroup, int kTiles, int kWaves>
 __global__ __launch_bounds__(kWaves * kWave) void k_block_few(BlockArgs a) {
-  __shared__ float sums[kWaves - 1][kTiles * 16][kWave];
-  const int lane = threadIdx.x & 63, wave = wave_id(), half = lane >> 5;
+  __shared__ float sums[kWaves - 1][kTiles * 8][kWave];
+  const int lane = threadIdx.x & 63, wave = wave_id(), quarter = lane >> 4;
   const int64_t n0 = (int64_t)blockIdx.x * 32;
   const int64_t begin = (int64_t)blockIdx.y * a.per, end = min(begin + a.per, a.blocks);
-  const uint8_t* const pb = a.b + min(n0 + (lane & 31), a.N - 1) * a.ldb + half * 32;
+  const uint8_t* pb[2];
   const uint8_t* pa[kTiles];
   const float* sa[kTiles];
 #pragma unroll
+  for (int u = 0; u < 2; ++u) pb[u] = a.b + min(n0 + u * 16 + (lane & 15), a.N - 1) * a.ldb + quarter * 16;
+#pragma unroll
   for (int t = 0; t < kTiles; ++t) {
-    const int64_t m = min((int64_t)(t * 32 + (lane & 31)), a.M - 1);
-    pa[t] = a.a + m * a.lda + half * 32;
+    const int64_t m = min((int64_t)(t * 16 + (lane & 15)), a.M - 1);
+    pa[t] = a.a + m * a.lda + quarter * 16;
     sa[t] = a.sa + m;
   }
-  // rows 8 q + 4 half .. + 3 of the tile are registers 4 q .. 4 q + 3
-  constexpr int kSb = kGroup == 1 ? 16 : 1;
-  struct Step {
-    i32x8 b[2], a[kTiles][2];
-    float sa[kTiles], sb[kSb];
+  auto load = [&](const uint8_t* p) {
+    const int4 x = *reinterpret_cast<const int4*>(p), y = *reinterpret_cast<const int4*>(p + 64);
+    return i32x8{x.x, x.y, x.z, x.w, y.x, y.y, y.z, y.w};
   };
-  auto load = [&](int64_t j) {
-    Step s;
-    s.b[0] = load32(pb + j * 128);
-    s.b[1] = load32(pb + j * 128 + 64);
-#pragma unroll
-    for (int t = 0; t < kTiles; ++t) {
-      s.a[t][0] = load32(pa[t] + j * 128);
-      s.a[t][1] = load32(pa[t] + j * 128 + 64);
-      s.sa[t] = sa[t][j * a.ldsa];
-    }
-    const float* const sb = a.sb + j * a.ldsb;
-    if constexpr (kGroup == 1) {
-#pragma unroll
-      for (int e = 0; e < 16; ++e) s.sb[e] = sb[min(n0 + 8 * (e >> 2) + 4 * half + (e & 3), a.N - 1)];
-    } else {
-      s.sb[0] = sb[n0 / kGroup];
-    }
-    return s;
-  };
-  f32x16 acc[kTiles] = {};
+  f32x4 acc[kTiles][2] = {};
+  i32x8 next[2] = {};
   int64_t j = begin + wave;
-  Step next;
-  if (j < end) next = load(j);
+  if (j < end) {
+    next[0] = load(pb[0] + j * 128);
+    next[1] = load(pb[1] + j * 128);
+  }
   for (; j < end; j += kWaves) {
-    const Step s = next;
-    next = load(min(j + kWaves, end - 1));
+    const i32x8 b[2] = {next[0], next[1]};
+    const int64_t ahead = min(j + kWaves, end - 1) * 128;
+    next[0] = load(pb[0] + ahead);
+    next[1] = load(pb[1] + ahead);
+    const float* const sbj = a.sb + j * a.ldsb;
+    float sb[2][4];
+#pragma unroll
+    for (int u = 0; u < 2; ++u)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if (kGroup == 1)
+          sb[u][e] = sbj[min(n0 + u * 16 + quarter * 4 + e, a.N - 1)];
+        else
+          sb[u][e] = sbj[n0 / kGroup];
+      }
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
-      f32x16 c = block_step<EXACT>(s.b[0], s.a[t][0], f32x16{});
-      c = block_step<EXACT>(s.b[1], s.a[t][1], c);
+      const i32x8 x = load(pa[t] + j * 128);
+      const float s = sa[t][j * a.ldsa];
 #pragma unroll
-      for (int e = 0; e < 16; ++e) acc[t][e] = fmaf(c[e], s.sa[t] * s.sb[kGroup == 1 ? e : 0], acc[t][e]);
+      for (int u = 0; u < 2; ++u) {
+        const f32x4 c = block16<EXACT>(b[u], x);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[t][u][e] = fmaf(c[e], s * sb[u][e], acc[t][u][e]);
+      }
     }
   }
   if (wave > 0) {
 #pragma unroll
     for (int t = 0; t < kTiles; ++t)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) sums[wave - 1][t * 16 + e][lane] = acc[t][e];
+      for (int e = 0; e < 8; ++e) sums[wave - 1][t * 8 + e][lane] = acc[t][e >> 2][e & 3];
   }
   __syncthreads();
   if (wave > 0) return;
   O* const out = static_cast<O*>(a.out) + (int64_t)blockIdx.y * a.range_stride;
 #pragma unroll
   for (int t = 0; t < kTiles; ++t) {
-    const int64_t m = t * 32 + (lane & 31);
+    const int64_t m = t * 16 + (lane & 15);
     if (m >= a.M) return;
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      float v = acc[t][e];
+    for (int e = 0; e < 8; ++e) {
+      float v = acc[t][e >> 2][e & 3];
 #pragma unroll
-      for (int w = 0; w < kWaves - 1; ++w) v += sums[w][t * 16 + e][lane];
-      const int64_t n = n0 + 8 * (e >> 2) + 4 * half + (e & 3);
+      for (int w = 0; w < kWaves - 1; ++w) v += sums[w][t * 8 + e][lane];
+      const int64_t n = n0 + (e >> 2) * 16 + quarter * 4 + (e & 3);
       if (n < a.N) store1(out + m * a.ldo + n, v);
     }
   }
@@ -194,17 +211,23 @@ void launch_join(const BlockArgs& a, int ranges, int64_t ldp, const char* ws, hi
                      reinterpret_cast<const float*>(ws), ranges, a.M, a.N, ldp, static_cast<O*>(a.out), a.ldo);
 }
 
+template <typename O, bool EXACT, int kGroup, int kTiles>
+void launch_few_m(const BlockArgs& a, const BlockPlan& p, hipStream_t s) {
+  const dim3 grid((unsigned)((a.N + 31) / 32), (unsigned)p.ranges);
+  if (p.waves == 4)
+    hipLaunchKernelGGL((k_block_few<O, EXACT, kGroup, kTiles, 4>), grid, dim3(256), 0, s, a);
+  else
+    hipLaunchKernelGGL((k_block_few<O, EXACT, kGroup, kTiles, 8>), grid, dim3(512), 0, s, a);
+}
+
 template <typename O, bool EXACT, int kGroup>
 void launch_few_t(const BlockArgs& a, const BlockPlan& p, hipStream_t s) {
-  const dim3 grid((unsigned)((a.N + 31) / 32), (unsigned)p.ranges);
-  if (a.M <= 32 && p.waves == 4)
-    hipLaunchKernelGGL((k_block_few<O, EXACT, kGroup, 1, 4>), grid, dim3(256), 0, s, a);
+  if (a.M <= 16)
+    launch_few_m<O, EXACT, kGroup, 1>(a, p, s);
   else if (a.M <= 32)
-    hipLaunchKernelGGL((k_block_few<O, EXACT, kGroup, 1, 8>), grid, dim3(512), 0, s, a);
-  else if (p.waves == 4)
-    hipLaunchKernelGGL((k_block_few<O, EXACT, kGroup, 2, 4>), grid, dim3(256), 0, s, a);
+    launch_few_m<O, EXACT, kGroup, 2>(a, p, s);
   else
-    hipLaunchKernelGGL((k_block_few<O, EXACT, kGroup, 2, 8>), grid, dim3(512), 0, s, a);
+    launch_few_m<O, EXACT, kGroup, 4>(a, p, s);
 }
 
 template <typename O>

@@ -24,6 +24,7 @@ namespace vsd {
 
 typedef __attribute__((ext_vector_type(4))) int i32x4;
 typedef __attribute__((ext_vector_type(8))) int i32x8;
+typedef __attribute__((ext_vector_type(4))) float f32x4;
 typedef __attribute__((ext_vector_type(16))) float f32x16;
 typedef __attribute__((ext_vector_type(2))) __bf16 bf16x2;
 typedef __attribute__((ext_vector_type(8))) __bf16 bf16x8;
@@ -81,6 +82,16 @@ __device__ __forceinline__ void tile_of(int pid, int nrt, int ncol, int& rt, int
   const int first = g * kGroupRows, rows = min(nrt - first, kGroupRows);
   rt = first + in % rows;
   col = in / rows;
+}
+
+template <int N>
+struct Index {
+  static constexpr int value = N;
+};
+template <class F>
+__device__ __forceinline__ void each16(F&& f) {
+  f(Index<0>{}), f(Index<1>{}), f(Index<2>{}), f(Index<3>{}), f(Index<4>{}), f(Index<5>{}), f(Index<6>{}), f(Index<7>{});
+  f(Index<8>{}), f(Index<9>{}), f(Index<10>{}), f(Index<11>{}), f(Index<12>{}), f(Index<13>{}), f(Index<14>{}), f(Index<15>{});
 }
 
 // F8: 8-bit matrix instructions; else the values go through bf16 ones, converted
@@ -210,17 +221,18 @@ __device__ __forceinline__ void tiles(const BlockTileArgs& a, uint8_t* lds) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) acc[h][g][i][e] = fmaf(tmp[i][e], s, acc[h][g][i][e]);
     } else {
+      // a lane's registers are 16 consecutive U rows: their scales lie in the 16 lanes of
+      // its DPP row, and the multiplication takes lane e's
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const float4 u = *reinterpret_cast<const float4*>(S + kTile + h * 128 + wr * 64 + 32 * (lane >> 5) + 16 * i + 4 * q);
-          const float us[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            acc[h][g][i][4 * q + e] = fmaf(tmp[i][4 * q + e] * us[e], sv, acc[h][g][i][4 * q + e]);
-          if (q == 1) __builtin_amdgcn_sched_barrier(0);
-        }
+      for (int i = 0; i < 2; ++i) {
+        const float u = S[kTile + h * 128 + wr * 64 + 32 * (lane >> 5) + 16 * i + (lane & 15)];
+        auto one = [&](auto e) {
+          constexpr int kE = decltype(e)::value;
+          const float ue = dpp_f<0x150 + kE>(u);  // row_newbcast
+          acc[h][g][i][kE] = fmaf(tmp[i][kE] * ue, sv, acc[h][g][i][kE]);
+        };
+        each16(one);
+      }
     }
     asm volatile("" : "+v"(acc[h][g][0]), "+v"(acc[h][g][1]));  // (the sums stay in this phase and in their registers)
   };
