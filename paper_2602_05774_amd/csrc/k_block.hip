@@ -128,9 +128,6 @@ __global__ __launch_bounds__(kWaves * kWave) void k_block_few(BlockArgs a) {
   }
   for (; j < end; j += kWaves) {
     const i32x8 b[2] = {next[0], next[1]};
-    const int64_t ahead = min(j + kWaves, end - 1) * 128;
-    next[0] = load(pb[0] + ahead);
-    next[1] = load(pb[1] + ahead);
     const float* const sbj = a.sb + j * a.ldsb;
     float sb[2][4];
 #pragma unroll
@@ -142,17 +139,27 @@ __global__ __launch_bounds__(kWaves * kWave) void k_block_few(BlockArgs a) {
         else
           sb[u][e] = sbj[n0 / kGroup];
       }
+    i32x8 x[kTiles];
+    float s[kTiles];
 #pragma unroll
     for (int t = 0; t < kTiles; ++t) {
-      const i32x8 x = load(pa[t] + j * 128);
-      const float s = sa[t][j * a.ldsa];
+      x[t] = load(pa[t] + j * 128);
+      s[t] = sa[t][j * a.ldsa];
+    }
+    // (loads return in order: b's next block, from HBM, is asked for after a's, from L2)
+    __builtin_amdgcn_sched_barrier(0);
+    const int64_t ahead = min(j + kWaves, end - 1) * 128;
+    next[0] = load(pb[0] + ahead);
+    next[1] = load(pb[1] + ahead);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int t = 0; t < kTiles; ++t)
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
-        const f32x4 c = block16<EXACT>(b[u], x);
+        const f32x4 c = block16<EXACT>(b[u], x[t]);
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc[t][u][e] = fmaf(c[e], s * sb[u][e], acc[t][u][e]);
+        for (int e = 0; e < 4; ++e) acc[t][u][e] = fmaf(c[e], s[t] * sb[u][e], acc[t][u][e]);
       }
-    }
   }
   if (wave > 0) {
 #pragma unroll
@@ -226,6 +233,8 @@ void launch_few_t(const BlockArgs& a, const BlockPlan& p, hipStream_t s) {
     launch_few_m<O, EXACT, kGroup, 1>(a, p, s);
   else if (a.M <= 32)
     launch_few_m<O, EXACT, kGroup, 2>(a, p, s);
+  else if (a.M <= 48)
+    launch_few_m<O, EXACT, kGroup, 3>(a, p, s);
   else
     launch_few_m<O, EXACT, kGroup, 4>(a, p, s);
 }
@@ -299,7 +308,7 @@ hipError_t launch_by_tiles(const BlockArgs& a, const BlockPlan& p, int group, ch
 template <typename O>
 hipError_t launch_t(const BlockArgs& a, const BlockPlan& p, int group, char* ws, hipStream_t s) {
   if (p.tiles) return launch_by_tiles<O>(a, p, group, ws, s);
-  if (a.M <= kBlockFewRows) return launch_few<O>(a, p, group, ws, s);
+  if (p.few) return launch_few<O>(a, p, group, ws, s);
   const dim3 grid((unsigned)(a.mt * ((a.N + 31) / 32)));
   if (group == 1)
     hipLaunchKernelGGL((k_block_product<O, 1>), grid, dim3(kWave), 0, s, a);

@@ -732,54 +732,61 @@ struct BlockTileArgs {
   int32_t stages, per;         // stages, of a range
 };
 
-// How a product is computed: by single wavefronts, or by tiles (the workgroups' runs,
-// the sum's ranges), with these regions of the workspace.
-constexpr int64_t kBlockFewRows = 64;       // rows of a that wavefronts take
+// How a product is computed: a's few rows against a stream of b, by tiles, or (rows too
+// long for the tiles' 32-bit offsets) by single wavefronts.
+constexpr int64_t kBlockFewRows = 64;       // the most rows that the stream is written for
 constexpr int64_t kBlockMaxLd = 1 << 22;    // bytes of a row: 256 of them within 32-bit offsets
 constexpr int kBlockCus = 256, kBlockMaxRanges = 16;
 struct BlockPlan {
-  bool tiles;
+  bool few, tiles;
   int32_t run, runs;               // as in BlockTileArgs
   int32_t ranges, per;             // ranges of the sum, blocks of one
-  int32_t waves;                   // few rows: wavefronts that share a workgroup's range
+  int32_t waves;                   // few: wavefronts that share a workgroup's range
   int64_t total;                   // bytes of the ranges' sums (the workspace)
 };
 inline BlockPlan block_plan(int64_t M, int64_t N, int64_t blocks, int64_t lda, int64_t ldb, bool f32) {
   BlockPlan p{};
-  const int64_t mt = (M + 255) / 256, nt = (N + 255) / 256, stages = blocks;
-  if (M <= kBlockFewRows) {
+  const int64_t mt = (M + 255) / 256, nt = (N + 255) / 256;
+  // by tiles, in us: a block of a tile takes about two (fp32 results four), a run four
+  // to start, a tile three to be stored; the ranges' sums are written and read at some
+  // 4 MB a us.  (Measured against it: 48 x 128 256 x 4096 126 / 138, 48 x 32 003 x 2048
+  // 32 / 34, to fp32 45 / 50.)
+  double best = 0.0;
+  if ((lda > ldb ? lda : ldb) <= kBlockMaxLd && mt * nt < 1 << 22) {
+    p.tiles = true;
+    const int64_t each = f32 ? 4 : 2;
+    for (int64_t ranges = 1; ranges <= kBlockMaxRanges; ++ranges) {
+      const int64_t per = (blocks + ranges - 1) / ranges;
+      if (ranges > 1 && (per < 4 || (ranges - 1) * per >= blocks || mt * nt * ranges > 2 * kBlockCus)) continue;
+      for (int64_t run = 1; run <= nt; ++run) {
+        const int64_t runs = (nt + run - 1) / run, groups = mt * runs * ranges;
+        if (run > 1 && (ranges > 1 || runs == (nt + run - 2) / (run - 1))) continue;
+        const double time = (double)((groups + kBlockCus - 1) / kBlockCus) * (double)(run * (per * each + 3) + 4) +
+                            (ranges > 1 ? 5.0 + 2e-6 * (double)(ranges * M * N) : 0.0);
+        if (best == 0.0 || time < best) {
+          best = time;
+          p.run = (int32_t)run;
+          p.runs = (int32_t)runs;
+          p.ranges = (int32_t)ranges;
+          p.per = (int32_t)per;
+        }
+      }
+    }
+  }
+  // as a stream: b at 5.6 MB a us, and every 16 rows of a a quarter of that again
+  // (measured / this: 1 x 128 256 x 4096 94 / 124, 48 x 128 256 x 4096 171 / 171, 48 x 32 003
+  // x 2048 26 / 27)
+  const double stream = 6.0 + 1e-6 * (double)(N * blocks * 128) * (0.18 + 0.045 * (double)((M + 15) / 16));
+  if (M <= kBlockFewRows && (!p.tiles || M <= 16 || stream < best)) {
     // a workgroup per 32 columns; its wavefronts, and where those workgroups do not
     // fill the chip ranges too, share the blocks, four at least each
     const int64_t cols = (N + 31) / 32;
+    p = BlockPlan{};
+    p.few = true;
     p.waves = cols >= 2 * kBlockCus || blocks < 32 ? 4 : 8;
     p.ranges = 1;
     while (p.ranges < kBlockMaxRanges && cols * p.ranges < kBlockCus && blocks >= 8 * p.waves * p.ranges) p.ranges *= 2;
     p.per = (int32_t)((blocks + p.ranges - 1) / p.ranges);
-    if (p.ranges > 1) p.total = (int64_t)p.ranges * M * ((N + 7) / 8 * 8) * 4;
-    return p;
-  }
-  if ((lda > ldb ? lda : ldb) > kBlockMaxLd || mt * nt >= 1 << 22) return p;
-  p.tiles = true;
-  // time in us: a block takes about one (fp32 results two), a run three to start, a
-  // tile two to be stored; ranges' sums are written and read at some 4 MB a us
-  const int64_t each = f32 ? 2 : 1;
-  double best = 0.0;
-  for (int64_t ranges = 1; ranges <= kBlockMaxRanges; ++ranges) {
-    const int64_t per = (stages + ranges - 1) / ranges;
-    if (ranges > 1 && (per < 4 || (ranges - 1) * per >= stages || mt * nt * ranges > 2 * kBlockCus)) continue;
-    for (int64_t run = 1; run <= nt; ++run) {
-      const int64_t runs = (nt + run - 1) / run, groups = mt * runs * ranges;
-      if (run > 1 && (ranges > 1 || runs == (nt + run - 2) / (run - 1))) continue;
-      const double time = (double)((groups + kBlockCus - 1) / kBlockCus) * (double)(run * (per * each + 2) + 3) +
-                          (ranges > 1 ? 5.0 + 2e-6 * (double)(ranges * M * N) : 0.0);
-      if (best == 0.0 || time < best) {
-        best = time;
-        p.run = (int32_t)run;
-        p.runs = (int32_t)runs;
-        p.ranges = (int32_t)ranges;
-        p.per = (int32_t)per;
-      }
-    }
   }
   if (p.ranges > 1) p.total = (int64_t)p.ranges * M * ((N + 7) / 8 * 8) * 4;
   return p;
