@@ -7,14 +7,14 @@
 // the tile each, every phase refilling the half operand whose last reader is past
 // (48 KB in flight, never drained); 16-byte chunks of a row swizzled over the banks.
 // What is added to it: a quadrant's product starts from zero and is joined to the
-// tile's fp32 sums, times its scales, in the group's next reading phase, where the
-// vector units would idle; the scales ride through LDS, loaded two stages ahead
-// with the operands.
-//   phase  reads   refills             multiplies   joins       waits for
-//   1      U0(t)   U1(t+1)             U0 V0        U1 V1(t-1)
-//   2      V1(t)   V0(t+2)             U0 V1        U0 V0
-//   3      U1(t)   U0(t+2)             U1 V0        U0 V1       V0(t+1)
-//   4      V0(t+1) V1(t+2), scales     U1 V1        U1 V0       all of t+1
+// tile's fp32 sums, times its scales, by the vector units while the matrix cores form
+// the other half of the phase's products; the scales ride through LDS, loaded two
+// stages ahead with the operands.
+//   phase  reads   refills             multiplies   waits for
+//   1      U0(t)   U1(t+1)             U0 V0
+//   2      V1(t)   V0(t+2)             U0 V1
+//   3      U1(t)   U0(t+2)             U1 V0        V0(t+1)
+//   4      V0(t+1) V1(t+2), scales     U1 V1        all of t+1
 #pragma once
 
 #include "vsd_device.hpp"
@@ -182,17 +182,62 @@ __device__ __forceinline__ void tiles(const BlockTileArgs& a, uint8_t* lds) {
 #pragma unroll
     for (int ks = 0; ks < 4; ++ks) f[ks] = frag((at ^ (ks << 5)) + half * kHalf);
   };
-  auto mult = [&](i32x4 (&v)[4]) {
+  // The scales of U half h and V half g: read ahead of the phase's fragments (LDS
+  // returns in order), so that the join does not wait for those.
+  struct Scales {
+    float v, u[kGroup == 1 ? 2 : 1];
+  };
+  auto scales_of = [&](int h, int g, int slot) {
+    const float* const S = reinterpret_cast<const float*>(lds + kScales + slot * kSlot);
+    Scales s;
+    s.v = S[g * 128 + wc * 32 + (lane & 31)];
+    if constexpr (kGroup == 1) {
+      // a lane's registers are 16 consecutive U rows: their scales lie in the 16 lanes of
+      // its DPP row, and the join takes lane e's
+#pragma unroll
+      for (int i = 0; i < 2; ++i) s.u[i] = S[kTile + h * 128 + wr * 64 + 32 * (lane >> 5) + 16 * i + (lane & 15)];
+    } else {
+      s.u[0] = S[kTile + h * 128];
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    return s;
+  };
+  // acc += tmp[i] times the scales of U (registers) and V (lanes)
+  auto join = [&](int h, int g, int i, const Scales& s) {
+    if constexpr (kGroup == 128) {
+      const float both = s.v * s.u[0];
+#pragma unroll
+      for (int e = 0; e < 16; ++e) acc[h][g][i][e] = fmaf(tmp[i][e], both, acc[h][g][i][e]);
+    } else {
+      each16([&](auto e) {
+        constexpr int kE = decltype(e)::value;
+        const float ue = dpp_f<0x150 + kE>(s.u[i]);  // row_newbcast
+        acc[h][g][i][kE] = fmaf(tmp[i][kE] * ue, s.v, acc[h][g][i][kE]);
+      });
+    }
+    asm volatile("" : "+v"(acc[h][g][i]));  // (the sums stay in this phase and in their registers)
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  // A phase's products, of U half h and V half g.  8-bit: while the matrix cores form one
+  // half of them, the vector units join the other: tmp[1] of the quadrant before
+  // (`pending`: there is one), then this one's tmp[0].
+  auto mult = [&](i32x4 (&v)[4], int h, int g, const Scales& s, int h1, int g1, const Scales& s1, bool pending) {
     __builtin_amdgcn_s_setprio(1);
     if constexpr (F8) {
+      auto half = [&](int i) {
 #pragma unroll
-      for (int ks = 0; ks < 2; ++ks)
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
+        for (int ks = 0; ks < 2; ++ks) {
           const i32x8 x = __builtin_shufflevector(fu[i][2 * ks], fu[i][2 * ks + 1], 0, 1, 2, 3, 4, 5, 6, 7);
           const i32x8 y = __builtin_shufflevector(v[2 * ks], v[2 * ks + 1], 0, 1, 2, 3, 4, 5, 6, 7);
           tmp[i] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, y, ks == 0 ? f32x16{} : tmp[i], 0, 0, 0, 0, 0, 0);
         }
+        asm volatile("" : "+v"(tmp[i]));
+        __builtin_amdgcn_sched_barrier(0);
+      };
+      half(0);
+      if (pending) join(h1, g1, 1, s1);
+      half(1);
+      join(h, g, 0, s);
     } else {
       // (the values' bf16 forms are made anew for every quadrant: kept, they would not fit)
 #pragma unroll
@@ -206,35 +251,18 @@ __device__ __forceinline__ void tiles(const BlockTileArgs& a, uint8_t* lds) {
               widen(fu[i][ks >> 1][(ks & 1) * 2], fu[i][ks >> 1][(ks & 1) * 2 + 1]), y, ks == 0 ? f32x16{} : tmp[i], 0, 0, 0);
         __builtin_amdgcn_sched_barrier(0);  // (not all conversions first: they would fill the registers)
       }
+      asm volatile("" : "+v"(tmp[0]), "+v"(tmp[1]));
     }
-    asm volatile("" : "+v"(tmp[0]), "+v"(tmp[1]));
     __builtin_amdgcn_s_setprio(0);
   };
-  // c += tmp times the scales of U half h (registers) and V half g (lanes)
-  auto join = [&](int h, int g, int slot) {
-    const float* const S = reinterpret_cast<const float*>(lds + kScales + slot * kSlot);
-    const float sv = S[g * 128 + wc * 32 + (lane & 31)];
-    if constexpr (kGroup == 128) {
-      const float s = sv * S[kTile + h * 128];
-#pragma unroll
-      for (int i = 0; i < 2; ++i)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) acc[h][g][i][e] = fmaf(tmp[i][e], s, acc[h][g][i][e]);
-    } else {
-      // a lane's registers are 16 consecutive U rows: their scales lie in the 16 lanes of
-      // its DPP row, and the multiplication takes lane e's
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        const float u = S[kTile + h * 128 + wr * 64 + 32 * (lane >> 5) + 16 * i + (lane & 15)];
-        auto one = [&](auto e) {
-          constexpr int kE = decltype(e)::value;
-          const float ue = dpp_f<0x150 + kE>(u);  // row_newbcast
-          acc[h][g][i][kE] = fmaf(tmp[i][kE] * ue, sv, acc[h][g][i][kE]);
-        };
-        each16(one);
-      }
+  // fp32 results: the conversions fill the products' phases, so both halves are joined
+  // in the reading phase after them.
+  auto join_read = [&](int h, int g, const Scales& s) {
+    if constexpr (!F8) {
+      __builtin_amdgcn_sched_barrier(0);
+      join(h, g, 0, s);
+      join(h, g, 1, s);
     }
-    asm volatile("" : "+v"(acc[h][g][0]), "+v"(acc[h][g][1]));  // (the sums stay in this phase and in their registers)
   };
   // the tile's results: 32 consecutive columns a lane in each half of the columns
   O* const out = static_cast<O*>(a.out) + (int64_t)blockIdx.y * a.range_stride;
@@ -290,45 +318,68 @@ __device__ __forceinline__ void tiles(const BlockTileArgs& a, uint8_t* lds) {
   };
   clear();
   int p = 0, slot = 0;
+  Scales s[4];  // of the quadrants, in their order
+  // Stores are counted with the loads and end in their order, so a wait for loads that
+  // were issued after a tile's stores waits for the stores.  The next tile's U1 is
+  // therefore asked for before them, and its first stage's waits leave the stores of a
+  // whole tile (each wavefront's kStores) out: they have almost two stages to drain.
+  constexpr int kStores = sizeof(O) == 2 ? 16 : 32;
+  bool stored = false, whole = false;  // a tile was stored just now, all of it
   for (int t = t_begin, k = k_begin; t < t_end; p ^= 1, slot = (slot + 1) & (kSlots - 1)) {
-    load_u(1, c1, p ^ 1);
+    const bool pending = k > k_begin;
+    s[0] = scales_of(0, 0, slot);
+    if (!stored) load_u(1, c1, p ^ 1);
     read_u(p, 0);
-    if (k > k_begin) join(1, 1, (slot + kSlots - 1) & (kSlots - 1));
+    if (pending) join_read(1, 1, s[3]);
     phase_barrier();
     wait_lds();
-    mult(fv0);
+    mult(fv0, 0, 0, s[0], 1, 1, s[3], pending);
     phase_barrier();
 
+    s[1] = scales_of(0, 1, slot);
     load_v(0, c2, p);
     read_v(fv1, p, 1);
-    join(0, 0, slot);
+    join_read(0, 0, s[0]);
     phase_barrier();
     wait_lds();
-    mult(fv1);
+    mult(fv1, 0, 1, s[1], 0, 0, s[0], true);
     phase_barrier();
 
+    s[2] = scales_of(1, 0, slot);
     load_u(0, c2, p);
     read_u(p, 1);
-    join(0, 1, slot);
-    wait_loads<11>();
+    join_read(0, 1, s[1]);
+    if (whole)
+      wait_loads<11 + kStores>();
+    else
+      wait_loads<11>();
     phase_barrier();
     wait_lds();
-    mult(fv0);
+    mult(fv0, 1, 0, s[2], 0, 1, s[1], true);
     phase_barrier();
 
+    s[3] = scales_of(1, 1, slot);
     load_v(1, c2, p);
     load_scales(c2, (slot + 2) & (kSlots - 1));
     read_v(fv0, p ^ 1, 0);
-    join(1, 0, slot);
-    wait_loads<7>();
+    join_read(1, 0, s[2]);
+    if (whole)
+      wait_loads<7 + kStores>();
+    else
+      wait_loads<7>();
     phase_barrier();
     wait_lds();
-    mult(fv1);
+    mult(fv1, 1, 1, s[3], 1, 0, s[2], true);
     c1 = c2;
     advance(c2);
     if (wr == 0) phase_barrier();
+    stored = whole = false;
     if (++k == k_end) {  // both groups finish a tile between the same two barriers
-      join(1, 1, slot);
+      join_read(1, 1, s[3]);
+      if (F8) join(1, 1, 1, s[3]);
+      load_u(1, c1, p);
+      stored = true;
+      whole = m0 + kTile <= a.M && (int64_t)(t + 1) * kTile <= a.N;
       store(t);
       clear();
       ++t;

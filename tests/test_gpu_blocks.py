@@ -127,6 +127,22 @@ def test_product(M, N, K, group, kind):
     _check_product(out, a, b, kind)
 
 
+@pytest.mark.parametrize("M,N,K,group,kind", [(5000, 10300, 140, 128, "bf16"), (4100, 12000, 300, 1, "bf16"),
+                                              (5120, 10240, 256, 128, "f32"), (2600, 17000, 129, 1, "f32")])
+def test_product_of_many_tiles(M, N, K, group, kind):
+    """More tiles than workgroups fit: runs of them, whole and partial, one after another."""
+    a, b = _matrix(M, K, 1, 11), _matrix(N, K, group, 12)
+    out = vsd.block_product(a, b, dtype=torch.float32 if kind == "f32" else torch.bfloat16)
+    A, Bm = (torch.from_numpy(ob.dense(m.values.float().cpu().numpy(), m.scales.cpu().numpy(), K)).to(DEV) for m in (a, b))
+    nb = -(-K // 128)
+    for r in range(0, M, 512):  # the bar of _check_product, the cut of 8-bit products bounded by all of them
+        want, size = A[r:r + 512] @ Bm.t(), A[r:r + 512].abs() @ Bm.t().abs()
+        bar = (128 * 2.0 ** -23 + (nb + 40) * 2.0 ** -24) * size
+        if kind == "bf16":
+            bar += 2.0 ** -8 * 1.01 * want.abs() + 7 * 2.0 ** -13 * size
+        assert ((out[r:r + 512].double() - want).abs() <= bar).all(), r
+
+
 @pytest.mark.parametrize("group", (1, 128))
 def test_product_of_strided_matrices(group):
     """Padded values, ranges of wider scales, a result inside a wider buffer whose rest stays."""
