@@ -11,8 +11,9 @@
 //    maxima; the largest value such that the maxima from it on already weigh p Z;
 //    min-p's own), the groups that reach it read again, their entries listed in LDS
 //    in index order, and the borders of top-k and top-p found bit by bit.
-// Rows whose lists do not fit (flat ones, k in the thousands) are left to k_draw_row.
-// k_draw_row: one workgroup per row, sweeping it several times: the largest entry; the
+// k_draw_left takes the rows whose lists do not fit: flat ones by draw_flat, others (k in
+// the thousands, long runs of equal logits) by draw_row, which also takes rows of more
+// than 262 144 columns (k_draw_row): one workgroup per row, sweeping it several times: the largest entry; the
 // sum of the weights, which sets their integer scale; for top-k and top-p the entry
 // where the count or the mass reaches its target, 8 bits of its value a sweep from
 // histograms of integers in LDS, and among equal entries by index; the kept entries'
@@ -280,15 +281,10 @@ __device__ __forceinline__ void draw_row(const DrawArgs& a, int64_t r, typename 
   }
 }
 
-// Every row, or (todo) those that were left.
 template <typename T, int kThreads>
 __global__ __launch_bounds__(kThreads) void k_draw_row(DrawArgs a) {
   __shared__ typename RowDraw<T, kThreads>::Shared sh;
-  const int64_t n = a.todo == nullptr ? a.R : *a.ntodo;
-  for (int64_t i = blockIdx.x; i < n; i += gridDim.x) {
-    draw_row<T, kThreads>(a, a.todo == nullptr ? i : a.todo[i], sh);
-    __syncthreads();
-  }
+  draw_row<T, kThreads>(a, blockIdx.x, sh);
 }
 
 // ------------------------------------------------------------------ sweep ---
@@ -427,15 +423,6 @@ constexpr int kGroups = kDrawSpans * 16, kMyGroups = kGroups / kFinish;
 constexpr double kListScale = 4503599627370496.0;             // 2^52: a list's weights sum to at most 2^62
 static_assert(kCap <= 1024 && kMyGroups == 8, "");
 
-struct FinishShared {
-  float x[kCap];
-  int32_t col[kCap];
-  int32_t groups[kGroups];
-  uint64_t red[2][kFinishWaves];
-  int64_t pick;
-  double pickd;
-};
-
 template <int CTRL>
 __device__ __forceinline__ uint64_t dpp_u64(uint64_t u) {
   const uint64_t lo = (uint32_t)dpp_i<CTRL>((int)(uint32_t)u), hi = (uint32_t)dpp_i<CTRL>((int)(u >> 32));
@@ -452,18 +439,32 @@ __device__ __forceinline__ uint64_t wave_sum_u64(uint64_t v) {
   return (lane_u64(v, 0) + lane_u64(v, 16)) + (lane_u64(v, 32) + lane_u64(v, 48));
 }
 
-// Sums and scans over the workgroup; `turn` alternates between two sets of words, so
-// that one barrier a sum is enough.
+// Sums and scans over a workgroup of kW wavefronts; `turn` alternates between two sets
+// of words, so that one barrier a sum is enough.
+template <int kW>
 struct Block {
-  FinishShared& sh;
+  uint64_t (*red)[3][kW];
   int turn;
-  __device__ __forceinline__ uint64_t sum(uint64_t v) {
-    v = wave_sum_u64(v);
+  template <int N>
+  __device__ __forceinline__ void sums(uint64_t (&v)[N]) {
     turn ^= 1;
-    if ((threadIdx.x & 63) == 0) sh.red[turn][wave_id()] = v;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      v[i] = wave_sum_u64(v[i]);
+      if ((threadIdx.x & 63) == 0) red[turn][i][wave_id()] = v[i];
+    }
     __syncthreads();
-    const uint64_t* r = sh.red[turn];
-    return (r[0] + r[1]) + (r[2] + r[3]);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      v[i] = red[turn][i][0];
+#pragma unroll
+      for (int k = 1; k < kW; ++k) v[i] += red[turn][i][k];
+    }
+  }
+  __device__ __forceinline__ uint64_t sum(uint64_t v) {
+    uint64_t s[1] = {v};
+    sums(s);
+    return s[0];
   }
   template <typename N>
   __device__ __forceinline__ N before(N v, N& all) {  // the sum over the threads before this one
@@ -475,13 +476,13 @@ struct Block {
       if ((int)(threadIdx.x & 63) >= d) upto += o;
     }
     turn ^= 1;
-    N* const r = reinterpret_cast<N*>(sh.red[turn]);
+    N* const r = reinterpret_cast<N*>(red[turn][0]);
     if ((threadIdx.x & 63) == 63) r[wave_id()] = upto;
     __syncthreads();
     N first = 0;
     all = 0;
 #pragma unroll
-    for (int k = 0; k < kFinishWaves; ++k) {
+    for (int k = 0; k < kW; ++k) {
       if (k < wave_id()) first += r[k];
       all += r[k];
     }
@@ -496,31 +497,62 @@ struct Block {
       v = o < v ? o : v;
     }
     turn ^= 1;
-    if ((threadIdx.x & 63) == 0) sh.red[turn][wave_id()] = v;
+    if ((threadIdx.x & 63) == 0) red[turn][0][wave_id()] = v;
     __syncthreads();
-    uint64_t t = sh.red[turn][0];
+    uint64_t t = red[turn][0][0];
 #pragma unroll
-    for (int k = 1; k < kFinishWaves; ++k) t = sh.red[turn][k] < t ? sh.red[turn][k] : t;
+    for (int k = 1; k < kW; ++k) t = red[turn][0][k] < t ? red[turn][0][k] : t;
     return t;
   }
-  // The largest key such that measure(key), the sum over entries of at least that key,
-  // reaches target (that of key 0 does); keys below 2^bits.
+  // The smallest and the largest key (32 bits) of the threads' [lo, hi].
+  __device__ __forceinline__ void range(uint32_t& lo, uint32_t& hi) {
+    uint32_t nhi = ~hi;
+#pragma unroll
+    for (int d = 1; d < kWave; d <<= 1) {
+      lo = min(lo, (uint32_t)__shfl_xor((int)lo, d));
+      nhi = min(nhi, (uint32_t)__shfl_xor((int)nhi, d));
+    }
+    turn ^= 1;
+    if ((threadIdx.x & 63) == 0) red[turn][0][wave_id()] = (uint64_t)nhi << 32 | lo;
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < kW; ++k) {
+      lo = min(lo, (uint32_t)red[turn][0][k]);
+      nhi = min(nhi, (uint32_t)(red[turn][0][k] >> 32));
+    }
+    hi = ~nhi;
+  }
+  // The largest key in [lo, hi] such that measure(key), the sum over entries of at least
+  // that key, reaches target (that of lo does): two bits of it a round.
   template <class M>
-  __device__ __forceinline__ uint32_t largest(int bits, uint64_t target, M&& measure) {
-    uint32_t key = 0;
-    for (int b = bits - 1; b >= 0; --b) {
-      const uint32_t t = key | 1u << b;
-      if (sum(measure(t)) >= target) key = t;
+  __device__ __forceinline__ uint32_t largest(uint32_t lo, uint32_t hi, uint64_t target, M&& measure) {
+    int bits = lo == hi ? 0 : 32 - __builtin_clz(lo ^ hi);
+    uint32_t key = bits == 32 ? 0u : hi >> bits << bits;
+    while (bits > 0) {
+      bits = bits > 2 ? bits - 2 : 0;
+      uint64_t s[3];
+#pragma unroll
+      for (int i = 0; i < 3; ++i) s[i] = measure(key | (uint32_t)(i + 1) << bits);
+      sums(s);
+      key |= (uint32_t)(s[2] >= target ? 3 : s[1] >= target ? 2 : s[0] >= target ? 1 : 0) << bits;
     }
     return key;
   }
 };
 
+struct FinishShared {
+  float x[kCap];
+  int32_t col[kCap];
+  int32_t groups[kGroups];
+  uint64_t red[2][3][kFinishWaves];
+  double pickd;
+};
+
 template <typename T>
 __global__ __launch_bounds__(kFinish) void k_draw_finish(DrawArgs a) {
-  constexpr int kBits = sizeof(T) == 2 ? 16 : 32, kDown = 32 - kBits;
+  constexpr int kDown = sizeof(T) == 2 ? 16 : 0;  // (bf16: 16 bits of order)
   __shared__ FinishShared sh;
-  Block blk{sh, 0};
+  Block<kFinishWaves> blk{sh.red, 0};
   const int t = threadIdx.x;
   const int64_t r = blockIdx.x;
   const T* Y = static_cast<const T*>(a.Y) + r * a.ld;
@@ -553,7 +585,16 @@ __global__ __launch_bounds__(kFinish) void k_draw_finish(DrawArgs a) {
     if (t == 0) draw_result(a, r, -1, counts == 0 ? 0.0f : __builtin_nanf(""), 0);
     return;
   }
-  const float m = value_of(~(uint32_t)blk.least(~key_of(span_max) & (0xFFFFFFFFu >> kDown)) & (0xFFFFFFFFu >> kDown));
+  // the range of the groups' maxima (of groups that have an entry)
+  uint32_t low = 0xFFFFFFFFu, high = 0;
+#pragma unroll
+  for (int k = 0; k < kMyGroups; ++k)
+    if (g[k] > -INFINITY) {
+      low = min(low, key_of(g[k]));
+      high = max(high, key_of(g[k]));
+    }
+  blk.range(low, high);
+  const float m = value_of(high);
   if (d.temp == 0.0f) {
     uint64_t at = ~0ull;
 #pragma unroll
@@ -622,14 +663,14 @@ __global__ __launch_bounds__(kFinish) void k_draw_finish(DrawArgs a) {
   bool min_bound = false;  // everything that min-p keeps is listed, maybe not all that top-p keeps
   if (n > kCap) {
     if (by_k) {
-      if (d.top_k > kCap || d.top_k > G) return leave();
-      const uint32_t key = blk.largest(kBits, d.top_k, [&](uint32_t b) {
-        uint64_t count = 0;
+      auto count = [&](uint32_t b) {
+        uint64_t c = 0;
 #pragma unroll
-        for (int k = 0; k < kMyGroups; ++k) count += key_of(g[k]) >= b ? 1 : 0;
-        return count;
-      });
-      least = value_of(key);
+        for (int k = 0; k < kMyGroups; ++k) c += g[k] > -INFINITY && key_of(g[k]) >= b ? 1 : 0;
+        return c;
+      };
+      if (d.top_k > kCap || blk.sum(count(0)) < (uint64_t)d.top_k) return leave();
+      least = value_of(blk.largest(low, high, d.top_k, count));
     } else if (by_p) {
       // (d.top_k > 0 here: at least n, so the sum was not formed)
       if (d.top_k > 0 || (double)d.top_p * z > 1000.0) return leave();
@@ -643,13 +684,12 @@ __global__ __launch_bounds__(kFinish) void k_draw_finish(DrawArgs a) {
       if (blk.sum(all) < target) {
         if (!by_m) return leave();
       } else {
-        const uint32_t key = blk.largest(kBits, target, [&](uint32_t b) {
+        least = value_of(blk.largest(low, high, target, [&](uint32_t b) {
           uint64_t mass = 0;
 #pragma unroll
           for (int k = 0; k < kMyGroups; ++k) mass += key_of(g[k]) >= b ? w[k] : 0;
           return mass;
-        });
-        least = value_of(key);
+        }));
       }
     } else if (!by_m) {
       return leave();  // (top-k of at least n entries and nothing else)
@@ -747,14 +787,25 @@ __global__ __launch_bounds__(kFinish) void k_draw_finish(DrawArgs a) {
         in[k] = key[k] > at;
     }
   };
+  // (the list's keys: from the bound's, or the smallest listed, to the maximum's)
+  uint32_t kmin = 0xFFFFFFFFu, kmax = 0;
+  if (by_k || by_p) {
+#pragma unroll
+    for (int k = 0; k < kMine; ++k)
+      if (in[k]) {
+        kmin = min(kmin, key[k]);
+        kmax = max(kmax, key[k]);
+      }
+    blk.range(kmin, kmax);
+  }
   auto over = [&](auto&& f) {
     uint64_t s = 0;
 #pragma unroll
     for (int k = 0; k < kMine; ++k) s += in[k] ? f(k) : 0ull;
     return s;
   };
-  if (by_k) {
-    const uint32_t at = blk.largest(kBits, d.top_k, [&](uint32_t b) { return over([&](int k) { return key[k] >= b ? 1ull : 0ull; }); });
+  if (by_k && listed > d.top_k) {
+    const uint32_t at = blk.largest(kmin, kmax, d.top_k, [&](uint32_t b) { return over([&](int k) { return key[k] >= b ? 1ull : 0ull; }); });
     cut(at, d.top_k - blk.sum(over([&](int k) { return key[k] > at ? 1ull : 0ull; })));
   }
   if (by_p) {
@@ -763,7 +814,7 @@ __global__ __launch_bounds__(kFinish) void k_draw_finish(DrawArgs a) {
     const double goal = __builtin_ceil((double)d.top_p * whole);
     if (goal <= (double)all) {
       const uint64_t target = (uint64_t)goal;
-      const uint32_t at = blk.largest(kBits, target, [&](uint32_t b) { return over([&](int k) { return key[k] >= b ? w[k] : 0ull; }); });
+      const uint32_t at = blk.largest(kmin, kmax, target, [&](uint32_t b) { return over([&](int k) { return key[k] >= b ? w[k] : 0ull; }); });
       const uint64_t above = blk.sum(over([&](int k) { return key[k] > at ? w[k] : 0ull; }));
       const uint64_t each = (uint64_t)(draw_weight(value_of(at), m, c) * kListScale + 0.5);
       cut(at, (target - above + each - 1) / each);
@@ -793,24 +844,287 @@ __global__ __launch_bounds__(kFinish) void k_draw_finish(DrawArgs a) {
   }
 }
 
-template <typename T, int kThreads>
-void launch_rows(const DrawArgs& a, int64_t groups, hipStream_t s) {
-  hipLaunchKernelGGL((k_draw_row<T, kThreads>), dim3((unsigned)groups), dim3(kThreads), 0, s, a);
+// ------------------------------------------------------------- flat rows ---
+// A row whose kept entries do not fit a list, bounded by top-p or min-p of the whole
+// softmax: two sweeps by a workgroup of 1024 threads.  The first (top-p) sums fp32
+// weights in 2048 bins of equal width between the largest logit and one below which
+// less than 1 - p of the mass can lie; within 1e-4 of p Z, far more than fp32 sums are
+// off, they tell the bins that hold the border.  The second forms the weights in 64
+// bits: of the entries above those bins per 512 columns, and the entries in them go to
+// a list, where the border is found as in k_draw_finish.
+constexpr int kFlat = 1024, kFlatWaves = kFlat / kWave, kBins = 2048, kFlatCap = 2048;
+constexpr int kFlatMine = kFlatCap / kFlat, kPieces = kDrawSpans * kDrawSpan / 512;
+struct FlatShared {
+  union {
+    float bins[kBins];
+    struct {
+      float x[kFlatCap];
+      int32_t col[kFlatCap];
+    } list;
+  };
+  uint64_t pieces[kPieces];  // kept mass of every 512 columns
+  uint64_t red[2][3][kFlatWaves];
+  uint64_t target;
+  int32_t n, at;
+};
+
+// False: left to draw_row.
+template <typename T>
+__device__ __forceinline__ bool draw_flat(const DrawArgs& a, int64_t r, FlatShared& sh) {
+  constexpr int kDown = sizeof(T) == 2 ? 16 : 0;
+  const DrawSettings d = draw_settings(a, r);
+  if (d.top_k > 0) return false;
+  Block<kFlatWaves> blk{sh.red, 0};
+  const int t = threadIdx.x, lane = t & 63, wave = wave_id(), V = a.V;
+  const T* Y = static_cast<const T*>(a.Y) + r * a.ld;
+  auto key_of = [](float x) { return draw_order(x) >> kDown; };
+  const bool span = t < a.S;
+  const float span_max = span ? a.span_max[r * a.S + t] : -INFINITY;
+  uint32_t lo = draw_order(span_max), hi = lo;
+  if (!span) lo = 0xFFFFFFFFu, hi = 0;
+  blk.range(lo, hi);
+  const float m = draw_value(hi);
+  const double c = 1.4426950408889634074 / (double)d.temp, temp = d.temp;
+  const uint64_t n = blk.sum(span ? (uint64_t)a.span_count[r * a.S + t] : 0);
+  const bool by_p = d.top_p < 1.0f;
+  double z = (double)n;
+  if (by_p) (void)blk.before(span && span_max > -INFINITY ? a.span_sum[r * a.S + t] * draw_weight(span_max, m, c) : 0.0, z);
+  const int e = 62 - (ilogb(z) + 1);
+  const double scale = __builtin_ldexp(1.0, e), min_p = d.min_p;
+  const double goal = __builtin_ceil((double)d.top_p * z * scale);
+
+  float inv = 0.0f;  // bins: (m - x) inv
+  const float c32 = (float)c;
+  auto bin_of = [&](float x) { return min((uint32_t)((m - x) * inv), (uint32_t)(kBins - 1)); };
+  int first = kBins, last = -1;  // the bins with the border
+  for (int i = t; i < kPieces; i += kFlat) sh.pieces[i] = 0;
+  if (t == 0) sh.n = 0;
+  if (by_p) {
+    const double depth = -temp * log((1.0 - (double)d.top_p) * z / (double)n);
+    inv = (float)fmin((kBins - 1) / depth, 3e38);
+    for (int i = t; i < kBins; i += kFlat) sh.bins[i] = 0.0f;
+    __syncthreads();
+    for (int base = t * 8; base < V; base += kFlat * 8) {
+      Raw8<T> q;
+      float x[8];
+      load_cols(q, Y, base, V);
+      q.get(x);
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if (x[k] > -INFINITY)
+          atomicAdd(&sh.bins[bin_of(x[k])], x[k] == m ? 1.0f : __builtin_amdgcn_exp2f((x[k] - m) * c32));
+    }
+    __syncthreads();
+    // (two bins a thread)
+    const double mine[2] = {(double)sh.bins[2 * t], (double)sh.bins[2 * t + 1]};
+    double all;
+    double run = blk.before(mine[0] + mine[1], all);
+    const double want = (double)d.top_p * z;
+    uint64_t b1 = ~0ull, b2 = ~0ull;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      run += mine[i];
+      if (b1 == ~0ull && run >= want * (1.0 - 1e-4)) b1 = (uint64_t)(2 * t + i);
+      if (b2 == ~0ull && run >= want * (1.0 + 1e-4)) b2 = (uint64_t)(2 * t + i);
+    }
+    b1 = blk.least(b1);
+    b2 = blk.least(b2);
+    if (b2 >= kBins - 1) return false;
+    first = (int)b1;
+    last = (int)b2;
+  }
+  // min-p: entries far below the bound are not weighed
+  const float bound = min_p > 0.0 && m < INFINITY
+                          ? (float)((double)m + temp * log(min_p) -
+                                    1e-6 * (fabs((double)m) + fabs((double)m + temp * log(min_p))) - 1e-30)
+                          : -INFINITY;
+  auto weigh = [&](float x, double& w) {
+    w = draw_weight(x, m, c);
+    return (uint64_t)(w * scale + 0.5);
+  };
+  __syncthreads();
+  uint64_t above = 0, count = 0;
+  const int pieces = (V + 511) / 512;
+  for (int p = wave; p < pieces; p += kFlatWaves) {
+    Raw8<T> q;
+    float x[8];
+    const int base = p * 512 + lane * 8;
+    load_cols(q, Y, base, V);
+    q.get(x);
+    uint64_t mass = 0;
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      if (!(x[k] > -INFINITY)) continue;
+      if (by_p) {
+        const int b = (int)bin_of(x[k]);
+        if (b > last) continue;
+        if (b >= first) {
+          const int at = atomicAdd(&sh.n, 1);
+          if (at < kFlatCap) {
+            sh.list.x[at] = x[k];
+            sh.list.col[at] = base + k;
+          }
+          continue;
+        }
+      } else if (x[k] < bound) {
+        continue;
+      }
+      double w;
+      const uint64_t W = weigh(x[k], w);
+      above += W;
+      if (w >= min_p) {
+        mass += W;
+        ++count;
+      }
+    }
+    mass = wave_sum_u64(mass);
+    if (lane == 0) sh.pieces[p] = mass;
+  }
+  __syncthreads();
+  const int listed = sh.n;
+  if (listed > kFlatCap) return false;
+  uint32_t least = 0;  // the smallest kept key of the list, and the last column with it
+  int limit = 0x7FFFFFFF;
+  if (by_p) {
+    above = blk.sum(above);
+    float x[kFlatMine];
+    uint32_t key[kFlatMine];
+    int col[kFlatMine];
+    uint64_t w[kFlatMine], listed_mass = 0;
+    bool enough[kFlatMine], in[kFlatMine];
+    uint32_t kmin = 0xFFFFFFFFu, kmax = 0;
+#pragma unroll
+    for (int k = 0; k < kFlatMine; ++k) {
+      const int i = t * kFlatMine + k;
+      in[k] = i < listed;
+      x[k] = in[k] ? sh.list.x[i] : -INFINITY;
+      col[k] = in[k] ? sh.list.col[i] : 0;
+      key[k] = key_of(x[k]);
+      double v = 0.0;
+      w[k] = in[k] ? weigh(x[k], v) : 0;
+      enough[k] = v >= min_p;
+      listed_mass += w[k];
+      if (in[k]) {
+        kmin = min(kmin, key[k]);
+        kmax = max(kmax, key[k]);
+      }
+    }
+    blk.range(kmin, kmax);
+    listed_mass = blk.sum(listed_mass);
+    const uint64_t target = (uint64_t)goal;
+    if (above >= target || above + listed_mass < target) return false;  // (the border is elsewhere)
+    const uint64_t need = target - above;
+    auto over = [&](auto&& f) {
+      uint64_t s = 0;
+#pragma unroll
+      for (int k = 0; k < kFlatMine; ++k) s += in[k] ? f(k) : 0ull;
+      return s;
+    };
+    least = blk.largest(kmin, kmax, need, [&](uint32_t b) { return over([&](int k) { return key[k] >= b ? w[k] : 0ull; }); });
+    uint64_t s[2] = {over([&](int k) { return key[k] > least ? w[k] : 0ull; }), over([&](int k) { return key[k] == least ? w[k] : 0ull; })};
+    blk.sums(s);
+    double v;
+    const uint64_t each = weigh(draw_value(kDown == 0 || least >= 0x8000u ? least << kDown : least << kDown | 0xFFFFu), v);
+    const uint64_t ties = (need - s[0] + each - 1) / each;
+    if (ties * each < s[1]) {
+      // the columns of the first `ties` of them: as the largest of reversed columns
+      const uint32_t top = (uint32_t)V;
+      limit = (int)(top - blk.largest(0, top, ties, [&](uint32_t b) {
+                      return over([&](int k) { return key[k] == least && top - (uint32_t)col[k] >= b ? 1ull : 0ull; });
+                    }));
+    }
+#pragma unroll
+    for (int k = 0; k < kFlatMine; ++k)
+      if (in[k] && enough[k] && (key[k] > least || (key[k] == least && col[k] <= limit))) {
+        atomicAdd(reinterpret_cast<unsigned long long*>(&sh.pieces[col[k] >> 9]), (unsigned long long)w[k]);
+        ++count;
+      }
+    __syncthreads();
+  }
+  count = blk.sum(count);
+  const uint64_t mine = t < pieces ? sh.pieces[t] : 0;
+  uint64_t mass;
+  const uint64_t before = blk.before(mine, mass);
+  const uint64_t target = (uint64_t)((double)d.u * (double)mass);
+  if (before <= target && target < before + mine) {
+    sh.at = t;
+    sh.target = target - before;
+  }
+  __syncthreads();
+  if (wave > 0) return true;
+  Raw8<T> q;
+  float x[8];
+  const int base = sh.at * 512 + lane * 8;
+  load_cols(q, Y, base, V);
+  q.get(x);
+  uint64_t w[8], sum = 0;
+#pragma unroll
+  for (int k = 0; k < 8; ++k) {
+    w[k] = 0;
+    if (!(x[k] > -INFINITY)) continue;
+    if (by_p) {
+      const int b = (int)bin_of(x[k]);
+      const uint32_t key = key_of(x[k]);
+      if (b > last || (b >= first && !(key > least || (key == least && base + k <= limit)))) continue;
+    } else if (x[k] < bound) {
+      continue;
+    }
+    double v;
+    const uint64_t W = weigh(x[k], v);
+    if (v >= min_p) sum += w[k] = W;
+  }
+  uint64_t run = sum;
+#pragma unroll
+  for (int s = 1; s < kWave; s <<= 1) {
+    const uint64_t o = __shfl_up(run, s);
+    if (lane >= s) run += o;
+  }
+  run -= sum;
+  const uint64_t want = sh.target;
+  bool found = false;
+  if (run <= want && want < run + sum) {
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      run += w[k];
+      if (!found && run > want) {
+        found = true;
+        const double lw = x[k] == m ? 0.0 : ((double)x[k] - (double)m) / temp;
+        draw_result(a, r, base + k, (float)(lw - log((double)mass * __builtin_ldexp(1.0, -e))), (int32_t)count);
+      }
+    }
+  }
+  return true;
+}
+
+// The rows that were left.
+template <typename T>
+__global__ __launch_bounds__(kFlat) void k_draw_left(DrawArgs a) {
+  __shared__ union {
+    FlatShared flat;
+    typename RowDraw<T, kFlat>::Shared row;
+  } sh;
+  const int64_t n = *a.ntodo;
+  for (int64_t i = blockIdx.x; i < n; i += gridDim.x) {
+    const int64_t r = a.todo[i];
+    if (!draw_flat<T>(a, r, sh.flat)) {
+      __syncthreads();
+      draw_row<T, kFlat>(a, r, sh.row);
+    }
+    __syncthreads();
+  }
 }
 
 template <typename T>
 hipError_t launch_t(DrawArgs a, hipStream_t s) {
-  if (a.todo != nullptr) {
-    const int64_t waves = a.R * ((a.S + a.per - 1) / a.per);
-    hipLaunchKernelGGL((k_draw_sweep<T>), dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, s, a);
-    hipLaunchKernelGGL((k_draw_finish<T>), dim3((unsigned)a.R), dim3(kFinish), 0, s, a);
-    if (a.V <= kCap) return hipGetLastError();  // (every list fits)
+  if (a.todo == nullptr) {  // (more columns than the records are for)
+    hipLaunchKernelGGL((k_draw_row<T, kFlat>), dim3((unsigned)a.R), dim3(kFlat), 0, s, a);
+    return hipGetLastError();
   }
-  const int64_t groups = a.todo != nullptr && a.R > 512 ? 512 : a.R;
-  if (a.V <= 4096)
-    launch_rows<T, 256>(a, groups, s);
-  else
-    launch_rows<T, 1024>(a, groups, s);
+  const int64_t waves = a.R * ((a.S + a.per - 1) / a.per);
+  hipLaunchKernelGGL((k_draw_sweep<T>), dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, s, a);
+  hipLaunchKernelGGL((k_draw_finish<T>), dim3((unsigned)a.R), dim3(kFinish), 0, s, a);
+  if (a.V > kCap)  // (else every list fits)
+    hipLaunchKernelGGL((k_draw_left<T>), dim3((unsigned)(a.R < 512 ? a.R : 512)), dim3(kFlat), 0, s, a);
   return hipGetLastError();
 }
 
