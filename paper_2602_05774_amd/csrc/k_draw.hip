@@ -3,7 +3,7 @@
 //
 // The sweep (k_draw_sweep) reads the row once, a wavefront per span of 2048 columns:
 // the largest logit of every 128 columns and, where the rule needs it, the span's sum
-// of weights in double precision.  k_draw_finish, a workgroup per row, ends most rows
+// of weights in double precision.  k_draw_finish, a wavefront per row, ends most rows
 // from these records and a few reads more:
 //  * greedy: the first group that holds the maximum;
 //  * no filter: the span in which the cumulative sum passes u Z, read again;
@@ -418,10 +418,10 @@ __global__ __launch_bounds__(256) void k_draw_sweep(DrawArgs a) {
 
 // ----------------------------------------------------------------- finish ---
 constexpr int kFinish = 256, kFinishWaves = kFinish / kWave;
-constexpr int kCap = 1024, kMine = kCap / kFinish;            // listed entries, of a thread
-constexpr int kGroups = kDrawSpans * 16, kMyGroups = kGroups / kFinish;
-constexpr double kListScale = 4503599627370496.0;             // 2^52: a list's weights sum to at most 2^62
-static_assert(kCap <= 1024 && kMyGroups == 8, "");
+constexpr int kCap = 512;                             // listed entries
+constexpr int kGroups = kDrawSpans * 16;
+constexpr double kListScale = 4503599627370496.0;     // 2^52: a list's weights sum to at most 2^61
+static_assert(kCap <= 1024 && kGroups <= 65536 && kDrawSpans == 2 * kWave, "");
 
 template <int CTRL>
 __device__ __forceinline__ uint64_t dpp_u64(uint64_t u) {
@@ -540,25 +540,68 @@ struct Block {
   }
 };
 
+// A row's list: entries in index order.
 struct FinishShared {
-  float x[kCap];
-  int32_t col[kCap];
-  int32_t groups[kGroups];
-  uint64_t red[2][3][kFinishWaves];
-  double pickd;
+  uint64_t w[kCap];       // integer weights
+  uint32_t key[kCap];     // order of the logit
+  int32_t col[kCap];      // column; kDropped: min-p drops it
+  uint16_t groups[kGroups];
 };
+constexpr int32_t kDropped = (int32_t)0x80000000u;
 
-template <typename T>
+// Over a wavefront: sums of three, scans, keys.
+__device__ __forceinline__ uint32_t wave_least(uint32_t v) {
+#pragma unroll
+  for (int d = 1; d < kWave; d <<= 1) v = min(v, (uint32_t)__shfl_xor((int)v, d));
+  return v;
+}
+template <typename N>
+__device__ __forceinline__ N wave_before(N v, N& all) {
+  N upto = v;
+#pragma unroll
+  for (int d = 1; d < kWave; d <<= 1) {
+    const N o = __shfl_up(upto, d);
+    if ((int)(threadIdx.x & 63) >= d) upto += o;
+  }
+  all = __shfl(upto, kWave - 1);
+  const N prev = __shfl_up(upto, 1);  // (upto - v would lose what v is small against)
+  return (threadIdx.x & 63) == 0 ? N(0) : prev;
+}
+// The largest key in [lo, hi] such that the sum over entries of at least that key
+// reaches target (that of lo does), two bits of it a round; measure(keys, sums): a
+// lane's sums for three keys.
+template <class M>
+__device__ __forceinline__ uint32_t wave_largest(uint32_t lo, uint32_t hi, uint64_t target, M&& measure) {
+  int bits = lo == hi ? 0 : 32 - __builtin_clz(lo ^ hi);
+  uint32_t key = bits == 32 ? 0u : hi >> bits << bits;
+#pragma unroll 1
+  while (bits > 0) {
+    bits = bits > 2 ? bits - 2 : 0;
+    const uint32_t t[3] = {key | 1u << bits, key | 2u << bits, key | 3u << bits};
+    uint64_t s[3] = {0, 0, 0};
+    measure(t, s);
+#pragma unroll
+    for (int i = 0; i < 3; ++i) s[i] = wave_sum_u64(s[i]);
+    key |= (uint32_t)(s[2] >= target ? 3 : s[1] >= target ? 2 : s[0] >= target ? 1 : 0) << bits;
+  }
+  return key;
+}
+
+// One row by one wavefront (no barrier: what bounds it is how long the chain of its
+// instructions takes); kPer groups a lane.  A workgroup of four wavefronts a row, its
+// sums through LDS, took 24 us for 8 rows of 128 256 and 119 for 4096: @FINISH@.
+template <typename T, int kPer>
 __global__ __launch_bounds__(kFinish) void k_draw_finish(DrawArgs a) {
   constexpr int kDown = sizeof(T) == 2 ? 16 : 0;  // (bf16: 16 bits of order)
-  __shared__ FinishShared sh;
-  Block<kFinishWaves> blk{sh.red, 0};
-  const int t = threadIdx.x;
-  const int64_t r = blockIdx.x;
+  __shared__ FinishShared all_rows[kFinishWaves];
+  const int lane = threadIdx.x & 63;
+  const int64_t r = (int64_t)blockIdx.x * kFinishWaves + wave_id();
+  if (r >= a.R) return;
+  FinishShared& sh = all_rows[wave_id()];
   const T* Y = static_cast<const T*>(a.Y) + r * a.ld;
   const DrawSettings d = draw_settings(a, r);
   if (!draw_valid(d)) {
-    if (t == 0) {
+    if (lane == 0) {
       report_error(a.err, VSD_DEVERR_SETTING_RANGE);
       draw_result(a, r, -1, 0.0f, 0);
     }
@@ -568,127 +611,176 @@ __global__ __launch_bounds__(kFinish) void k_draw_finish(DrawArgs a) {
   auto value_of = [](uint32_t k) {
     return draw_value(kDown == 0 || k >= 0x8000u ? k << kDown : k << kDown | 0xFFFFu);
   };
+  // LDS written by some lanes is read by others of the wavefront
+  auto settle = []() {
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+  };
   const int G = a.S * 16;
-  float g[kMyGroups];  // the largest logits of groups 8 t .. 8 t + 7
-  if (t * kMyGroups < G) {
-    load8(a.group_max + r * G + t * kMyGroups, g);
-  } else {
-#pragma unroll
-    for (int k = 0; k < kMyGroups; ++k) g[k] = -INFINITY;
-  }
-  const bool span = t < a.S;
-  const float span_max = span ? a.span_max[r * a.S + t] : -INFINITY;
-  const int span_count = span ? a.span_count[r * a.S + t] : 0;
-  const uint64_t counts = blk.sum(span_count < 0 ? 1ull << 40 : (uint64_t)span_count);
-  const int n = (int)counts;
-  if (counts == 0 || counts >> 40 != 0) {
-    if (t == 0) draw_result(a, r, -1, counts == 0 ? 0.0f : __builtin_nanf(""), 0);
-    return;
-  }
-  // the range of the groups' maxima (of groups that have an entry)
+  // lane l: groups kPer l .. (keys; 0: no entry), spans 2 l and 2 l + 1
+  uint32_t g[kPer];
   uint32_t low = 0xFFFFFFFFu, high = 0;
 #pragma unroll
-  for (int k = 0; k < kMyGroups; ++k)
-    if (g[k] > -INFINITY) {
-      low = min(low, key_of(g[k]));
-      high = max(high, key_of(g[k]));
+  for (int k = 0; k < kPer; k += 4) {
+    const int at = lane * kPer + k;
+    float4 v = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY);
+    if (at < G) v = *reinterpret_cast<const float4*>(a.group_max + r * G + at);
+    const float x[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      g[k + i] = x[i] > -INFINITY ? key_of(x[i]) : 0u;
+      low = min(low, g[k + i] - 1u);  // (none: the largest)
+      high = max(high, g[k + i]);
     }
-  blk.range(low, high);
+  }
+  float span_max[2];
+  uint64_t counts = 0;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int s = 2 * lane + i;
+    span_max[i] = s < a.S ? a.span_max[r * a.S + s] : -INFINITY;
+    const int count = s < a.S ? a.span_count[r * a.S + s] : 0;
+    counts += count < 0 ? 1ull << 40 : (uint64_t)count;
+  }
+  counts = wave_sum_u64(counts);
+  const int n = (int)counts;
+  if (counts == 0 || counts >> 40 != 0) {
+    if (lane == 0) draw_result(a, r, -1, counts == 0 ? 0.0f : __builtin_nanf(""), 0);
+    return;
+  }
+  low = wave_least(low) + 1u;
+  high = ~wave_least(~high);
   const float m = value_of(high);
   if (d.temp == 0.0f) {
-    uint64_t at = ~0ull;
+    uint32_t at = 0xFFFFFFFFu;
 #pragma unroll
-    for (int k = kMyGroups - 1; k >= 0; --k)
-      if (g[k] == m) at = (uint64_t)(t * kMyGroups + k);
-    at = blk.least(at);
-    uint64_t col = ~0ull;
-    if (t < kDrawGroup / 8) {
+    for (int k = kPer - 1; k >= 0; --k)
+      if (g[k] == high) at = (uint32_t)(lane * kPer + k);
+    at = wave_least(at);
+    uint32_t col = 0xFFFFFFFFu;
+    if (lane < kDrawGroup / 8) {
       Raw8<T> q;
       float x[8];
-      const int base = (int)at * kDrawGroup + t * 8;
+      const int base = (int)at * kDrawGroup + lane * 8;
       load_cols(q, Y, base, a.V);
       q.get(x);
 #pragma unroll
       for (int k = 7; k >= 0; --k)
-        if (x[k] == m) col = (uint64_t)(base + k);
+        if (x[k] == m) col = (uint32_t)(base + k);
     }
-    col = blk.least(col);
-    if (t == 0) draw_result(a, r, (int32_t)col, 0.0f, 1);
+    col = wave_least(col);
+    if (lane == 0) draw_result(a, r, (int32_t)col, 0.0f, 1);
     return;
   }
   const double c = 1.4426950408889634074 / (double)d.temp, temp = d.temp;
   auto log_weight = [&](float x) { return x == m ? 0.0 : ((double)x - (double)m) / temp; };
   const bool by_k = d.top_k > 0 && d.top_k < n, by_p = d.top_p < 1.0f, by_m = d.min_p > 0.0f;
   double z = 0.0;  // the sum of all weights, where it is needed
-  if (!by_k) {
-    const double mine = span && span_max > -INFINITY && d.top_k == 0
-                            ? a.span_sum[r * a.S + t] * draw_weight(span_max, m, c) : 0.0;
-    const double before = blk.before(mine, z);
-    if (!by_p && !by_m && d.top_k == 0) {
-      // the whole softmax: the span, then the column
+  if (needs_sum(d)) {
+    double mine[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      mine[i] = span_max[i] > -INFINITY ? a.span_sum[r * a.S + 2 * lane + i] * draw_weight(span_max[i], m, c) : 0.0;
+    const double before = wave_before(mine[0] + mine[1], z);
+    if (!by_p && !by_m) {
+      // the whole softmax: the span, then its four rounds of 512 columns, then the column
       const double target = (double)d.u * z;
-      const uint64_t at = blk.least(span && before + mine > target ? (uint64_t)t : ~0ull);
-      if ((uint64_t)t == at) sh.pickd = target - before;
-      __syncthreads();
-      const int base = (int)at * kDrawSpan + t * 8;
-      Raw8<T> q;
-      float x[8];
-      load_cols(q, Y, base, a.V);
-      q.get(x);
-      double w = 0.0;
+      const uint32_t at = wave_least(before + mine[0] > target ? 2 * lane
+                                     : before + (mine[0] + mine[1]) > target ? 2 * lane + 1 : 0xFFFFFFFFu);
+      double want = target - before - ((at & 1u) != 0u ? mine[0] : 0.0);
+      want = lane_d(want, (int)(at >> 1));
+      double passed = 0.0;
+      int tok = -1, positive = -1;  // (positive: the last column of any weight, should roundings pass the span)
+#pragma unroll 1
+      for (int u = 0; u < kLoads && tok < 0; ++u) {
+        const int base = (int)at * kDrawSpan + u * 512 + lane * 8;
+        Raw8<T> q;
+        float x[8];
+        load_cols(q, Y, base, a.V);
+        q.get(x);
+        double w[8], sum = 0.0, all;
 #pragma unroll
-      for (int k = 0; k < 8; ++k) w += x[k] > -INFINITY ? draw_weight(x[k], m, c) : 0.0;
-      double all;
-      double run = blk.before(w, all);
-      const double want = fmin(sh.pickd, all * (1.0 - 1e-15));  // (the span's sum may round otherwise)
-      uint64_t col = ~0ull;
+        for (int k = 0; k < 8; ++k) sum += w[k] = x[k] > -INFINITY ? draw_weight(x[k], m, c) : 0.0;
+        double run = passed + wave_before(sum, all);
+        uint32_t col = 0xFFFFFFFFu, some = 0;
 #pragma unroll
-      for (int k = 0; k < 8; ++k) {
-        run += x[k] > -INFINITY ? draw_weight(x[k], m, c) : 0.0;
-        if (col == ~0ull && run > want) col = (uint64_t)(base + k);
+        for (int k = 0; k < 8; ++k) {
+          run += w[k];
+          if (w[k] > 0.0) {
+            some = (uint32_t)(base + k) + 1u;
+            if (col == 0xFFFFFFFFu && run > want) col = (uint32_t)(base + k);
+          }
+        }
+        tok = (int)wave_least(col);
+        some = ~wave_least(~some);
+        if (some > 0) positive = (int)some - 1;
+        passed += all;
       }
-      col = blk.least(col);
-      if (t == 0) {
-        const float xt = load1(Y + col);
-        draw_result(a, r, (int32_t)col, (float)(log_weight(xt) - log(z)), n);
+      if (tok < 0) tok = positive;
+      if (lane == 0) {
+        const float xt = load1(Y + tok);
+        draw_result(a, r, tok, (float)(log_weight(xt) - log(z)), n);
       }
       return;
     }
   }
   // the bound of the list
   auto leave = [&]() {
-    if (t == 0) a.todo[atomicAdd(a.ntodo, 1)] = (int32_t)r;
+    if (lane == 0) a.todo[atomicAdd(a.ntodo, 1)] = (int32_t)r;
   };
   float least = -INFINITY;
   bool min_bound = false;  // everything that min-p keeps is listed, maybe not all that top-p keeps
   if (n > kCap) {
     if (by_k) {
-      auto count = [&](uint32_t b) {
-        uint64_t c = 0;
+      if (d.top_k > kCap) return leave();
+      uint64_t have = 0;
 #pragma unroll
-        for (int k = 0; k < kMyGroups; ++k) c += g[k] > -INFINITY && key_of(g[k]) >= b ? 1 : 0;
-        return c;
-      };
-      if (d.top_k > kCap || blk.sum(count(0)) < (uint64_t)d.top_k) return leave();
-      least = value_of(blk.largest(low, high, d.top_k, count));
+      for (int k = 0; k < kPer; ++k) have += g[k] > 0u ? 1 : 0;
+      if (wave_sum_u64(have) < (uint64_t)d.top_k) return leave();
+      // (three counts of 21 bits in the first sum)
+      uint32_t key = low == high ? high : 0u;
+      if (low != high) {
+        int bits = 32 - __builtin_clz(low ^ high);
+        key = bits == 32 ? 0u : high >> bits << bits;
+#pragma unroll 1
+        while (bits > 0) {
+          bits = bits > 2 ? bits - 2 : 0;
+          uint64_t s = 0;
+#pragma unroll
+          for (int k = 0; k < kPer; ++k) {
+            const uint32_t over = g[k] >= key ? min((g[k] - key) >> bits, 3u) : 0u;  // of the three keys, how many it reaches
+            s += over == 3u ? 1ull << 42 | 1ull << 21 | 1ull : over == 2u ? 1ull << 21 | 1ull : over == 1u ? 1ull : 0ull;
+          }
+          s = wave_sum_u64(s);
+          const uint32_t want = (uint32_t)d.top_k;
+          key |= (uint32_t)((s >> 42) >= want ? 3 : ((s >> 21) & 0x1FFFFFu) >= want ? 2 : (s & 0x1FFFFFu) >= want ? 1 : 0) << bits;
+        }
+      }
+      least = value_of(key);
     } else if (by_p) {
-      // (d.top_k > 0 here: at least n, so the sum was not formed)
-      if (d.top_k > 0 || (double)d.top_p * z > 1000.0) return leave();
-      uint64_t w[kMyGroups];
-#pragma unroll
-      for (int k = 0; k < kMyGroups; ++k) w[k] = g[k] > -INFINITY ? (uint64_t)(draw_weight(g[k], m, c) * kListScale) : 0;
-      const uint64_t target = (uint64_t)((double)d.top_p * z * (kListScale * (1.0 + 1e-9)));
+      // (with d.top_k > 0, at least n, the sum was not formed)
+      if (d.top_k > 0) return leave();
+      // fp32 weights of the maxima, a little too small: enough for a bound
+      uint32_t w[kPer];
       uint64_t all = 0;
+      const float c32 = (float)c;
 #pragma unroll
-      for (int k = 0; k < kMyGroups; ++k) all += w[k];
-      if (blk.sum(all) < target) {
+      for (int k = 0; k < kPer; ++k) {
+        const float x = value_of(g[k]);
+        w[k] = g[k] > 0u ? (uint32_t)((x == m ? 1.0f : __builtin_amdgcn_exp2f((x - m) * c32)) * 0.9999f * 1073741824.0f) : 0u;
+        all += w[k];
+      }
+      all = wave_sum_u64(all);
+      const double goal = (double)d.top_p * z * 1073741824.0 + 1.0;
+      if ((double)all < goal) {
         if (!by_m) return leave();
       } else {
-        least = value_of(blk.largest(low, high, target, [&](uint32_t b) {
-          uint64_t mass = 0;
+        least = value_of(wave_largest(low, high, (uint64_t)goal, [&](const uint32_t (&t)[3], uint64_t (&s)[3]) {
 #pragma unroll
-          for (int k = 0; k < kMyGroups; ++k) mass += key_of(g[k]) >= b ? w[k] : 0;
-          return mass;
+          for (int k = 0; k < kPer; ++k)
+#pragma unroll
+            for (int i = 0; i < 3; ++i) s[i] += g[k] >= t[i] ? w[k] : 0u;
         }));
       }
     } else if (!by_m) {
@@ -705,142 +797,168 @@ __global__ __launch_bounds__(kFinish) void k_draw_finish(DrawArgs a) {
     }
   }
   // the groups that reach it, and their entries, both in index order
+  const uint32_t least_key = least > -INFINITY ? key_of(least) : 1u;
   int ngroups;
   {
     uint64_t mine = 0, all;
 #pragma unroll
-    for (int k = 0; k < kMyGroups; ++k) mine += g[k] >= least && g[k] > -INFINITY ? 1 : 0;
-    int at = (int)blk.before(mine, all);
+    for (int k = 0; k < kPer; ++k) mine += g[k] >= least_key ? 1 : 0;
+    int at = (int)wave_before(mine, all);
     ngroups = (int)all;
 #pragma unroll
-    for (int k = 0; k < kMyGroups; ++k)
-      if (g[k] >= least && g[k] > -INFINITY) sh.groups[at++] = t * kMyGroups + k;
-    __syncthreads();
+    for (int k = 0; k < kPer; ++k)
+      if (g[k] >= least_key) sh.groups[at++] = (uint16_t)(lane * kPer + k);
+    settle();
   }
-  constexpr int kSets = 4, kSet = kFinish / 16;  // a set: 16 groups, a thread eight columns
+  constexpr int kSets = 4, kSet = kWave / 16;  // a set: 4 groups, a lane eight columns
   int listed = 0;
+#pragma unroll 1
   for (int first = 0; first < ngroups; first += kSets * kSet) {
     Raw8<T> q[kSets];
     int base[kSets];
     uint64_t counts4 = 0;  // 16 bits a set
 #pragma unroll
     for (int s = 0; s < kSets; ++s) {
-      const int i = first + s * kSet + (t >> 4);
-      base[s] = i < ngroups ? sh.groups[i] * kDrawGroup + (t & 15) * 8 : a.V;
+      const int i = first + s * kSet + (lane >> 4);
+      base[s] = i < ngroups ? (int)sh.groups[i] * kDrawGroup + (lane & 15) * 8 : a.V;
       load_cols(q[s], Y, base[s], a.V);
     }
+    uint32_t reach = 0;  // a bit per entry
 #pragma unroll
     for (int s = 0; s < kSets; ++s) {
       float x[8];
       q[s].get(x);
 #pragma unroll
-      for (int k = 0; k < 8; ++k) counts4 += x[k] >= least && x[k] > -INFINITY ? 1ull << (16 * s) : 0ull;
+      for (int k = 0; k < 8; ++k) reach |= x[k] >= least && x[k] > -INFINITY ? 1u << (8 * s + k) : 0u;
+      counts4 |= (uint64_t)__builtin_popcount(reach >> (8 * s) & 0xFFu) << (16 * s);
     }
     uint64_t all;
-    const uint64_t before = blk.before(counts4, all);
+    const uint64_t before = wave_before(counts4, all);
 #pragma unroll
     for (int s = 0; s < kSets; ++s) {
       int at = listed + (int)((before >> (16 * s)) & 0xFFFFu);
       float x[8];
       q[s].get(x);
+      if ((reach >> (8 * s) & 0xFFu) != 0u) {
 #pragma unroll
-      for (int k = 0; k < 8; ++k)
-        if (x[k] >= least && x[k] > -INFINITY) {
-          if (at < kCap) {
-            sh.x[at] = x[k];
-            sh.col[at] = base[s] + k;
+        for (int k = 0; k < 8; ++k)
+          if ((reach >> (8 * s + k) & 1u) != 0u) {
+            if (at < kCap) {
+              sh.key[at] = key_of(x[k]);
+              sh.col[at] = base[s] + k;
+            }
+            ++at;
           }
-          ++at;
-        }
+      }
       listed += (int)((all >> (16 * s)) & 0xFFFFu);
     }
     if (listed > kCap) return leave();
   }
-  __syncthreads();
-  // a thread's entries: kMine t .. kMine t + kMine - 1 of the list
-  float x[kMine];
-  uint32_t key[kMine];
-  uint64_t w[kMine];
-  bool in[kMine], enough[kMine];
-#pragma unroll
-  for (int k = 0; k < kMine; ++k) {
-    const int i = t * kMine + k;
-    in[k] = i < listed;
-    x[k] = in[k] ? sh.x[i] : -INFINITY;
-    key[k] = key_of(x[k]);
-    const double v = in[k] ? draw_weight(x[k], m, c) : 0.0;
-    w[k] = (uint64_t)(v * kListScale + 0.5);
-    enough[k] = v >= (double)d.min_p;
+  settle();
+  uint32_t kmin = 0xFFFFFFFFu, kmax = 0;
+#pragma unroll 1
+  for (int i = lane; i < listed; i += kWave) {
+    const uint32_t key = sh.key[i];
+    const double v = draw_weight(value_of(key), m, c);
+    sh.w[i] = (uint64_t)(v * kListScale + 0.5);
+    if (v < (double)d.min_p) sh.col[i] |= kDropped;
+    kmin = min(kmin, key);
+    kmax = max(kmax, key);
   }
-  // keeps of the entries in play those larger than `at`, and the first `ties` equal to it
-  auto cut = [&](uint32_t at, uint64_t ties) {
-    uint64_t mine = 0, all;
-#pragma unroll
-    for (int k = 0; k < kMine; ++k) mine += in[k] && key[k] == at ? 1 : 0;
-    uint64_t before = blk.before(mine, all);
-#pragma unroll
-    for (int k = 0; k < kMine; ++k) {
-      if (!in[k]) continue;
-      if (key[k] == at)
-        in[k] = before++ < ties;
-      else
-        in[k] = key[k] > at;
+  settle();
+  kmin = wave_least(kmin);
+  kmax = ~wave_least(~kmax);
+  // the entries in play: of a key above `border`, or of that key the first `ties`
+  uint32_t border = 0;
+  uint64_t ties = ~0ull;
+  // sums over the entries in play of at least three keys
+  auto in_play = [&](auto&& f) {  // f(entry), in index order by lanes
+    if (ties == ~0ull) {
+#pragma unroll 1
+      for (int i = lane; i < listed; i += kWave)
+        if (sh.key[i] >= border) f(i);
+      return;
+    }
+    uint64_t seen = 0;  // entries of the border's key before this round of 64
+#pragma unroll 1
+    for (int first = 0; first < listed; first += kWave) {
+      const int i = first + lane;
+      const uint32_t key = i < listed ? sh.key[i] : 0u;
+      const uint64_t equal = __ballot(i < listed && key == border);
+      const uint64_t rank = seen + (uint64_t)__builtin_popcountll(equal & ((1ull << lane) - 1));
+      if (i < listed && (key > border || (key == border && rank < ties))) f(i);
+      seen += (uint64_t)__builtin_popcountll(equal);
     }
   };
-  // (the list's keys: from the bound's, or the smallest listed, to the maximum's)
-  uint32_t kmin = 0xFFFFFFFFu, kmax = 0;
-  if (by_k || by_p) {
-#pragma unroll
-    for (int k = 0; k < kMine; ++k)
-      if (in[k]) {
-        kmin = min(kmin, key[k]);
-        kmax = max(kmax, key[k]);
-      }
-    blk.range(kmin, kmax);
-  }
-  auto over = [&](auto&& f) {
-    uint64_t s = 0;
-#pragma unroll
-    for (int k = 0; k < kMine; ++k) s += in[k] ? f(k) : 0ull;
-    return s;
-  };
   if (by_k && listed > d.top_k) {
-    const uint32_t at = blk.largest(kmin, kmax, d.top_k, [&](uint32_t b) { return over([&](int k) { return key[k] >= b ? 1ull : 0ull; }); });
-    cut(at, d.top_k - blk.sum(over([&](int k) { return key[k] > at ? 1ull : 0ull; })));
+    const uint32_t at = wave_largest(kmin, kmax, d.top_k, [&](const uint32_t (&t)[3], uint64_t (&s)[3]) {
+#pragma unroll 1
+      for (int i = lane; i < listed; i += kWave) {
+        const uint32_t key = sh.key[i];
+#pragma unroll
+        for (int j = 0; j < 3; ++j) s[j] += key >= t[j] ? 1 : 0;
+      }
+    });
+    uint64_t above = 0;
+#pragma unroll 1
+    for (int i = lane; i < listed; i += kWave) above += sh.key[i] > at ? 1 : 0;
+    border = at;
+    ties = d.top_k - wave_sum_u64(above);
   }
   if (by_p) {
-    const uint64_t all = blk.sum(over([&](int k) { return w[k]; }));
+    uint64_t all = 0;
+    in_play([&](int i) { all += sh.w[i]; });
+    all = wave_sum_u64(all);
     const double whole = by_k || n <= kCap ? (double)all : z * kListScale;
     const double goal = __builtin_ceil((double)d.top_p * whole);
     if (goal <= (double)all) {
       const uint64_t target = (uint64_t)goal;
-      const uint32_t at = blk.largest(kmin, kmax, target, [&](uint32_t b) { return over([&](int k) { return key[k] >= b ? w[k] : 0ull; }); });
-      const uint64_t above = blk.sum(over([&](int k) { return key[k] > at ? w[k] : 0ull; }));
+      const uint32_t at = wave_largest(max(kmin, border), kmax, target, [&](const uint32_t (&t)[3], uint64_t (&s)[3]) {
+        in_play([&](int i) {
+          const uint32_t key = sh.key[i];
+          const uint64_t w = sh.w[i];
+#pragma unroll
+          for (int j = 0; j < 3; ++j) s[j] += key >= t[j] ? w : 0;
+        });
+      });
+      uint64_t above = 0;
+      in_play([&](int i) { above += sh.key[i] > at ? sh.w[i] : 0; });
+      above = wave_sum_u64(above);
       const uint64_t each = (uint64_t)(draw_weight(value_of(at), m, c) * kListScale + 0.5);
-      cut(at, (target - above + each - 1) / each);
+      const uint64_t need = (target - above + each - 1) / each;
+      ties = at == border && ties < need ? ties : need;
+      border = at;
     } else if (!min_bound) {
       return leave();
     }
   }
-#pragma unroll
-  for (int k = 0; k < kMine; ++k) in[k] = in[k] && enough[k];
-  const uint64_t kept = blk.sum(over([](int) { return 1ull; }));
-  uint64_t mass;
-  const uint64_t sum = over([&](int k) { return w[k]; });
-  const uint64_t before = blk.before(sum, mass);
-  const uint64_t target = (uint64_t)((double)d.u * (double)mass);
-  if (before <= target && target < before + sum) {
-    uint64_t run = before;
-    bool found = false;
-#pragma unroll
-    for (int k = 0; k < kMine; ++k) {
-      if (!in[k] || found) continue;
-      run += w[k];
-      if (run > target) {
-        found = true;
-        draw_result(a, r, sh.col[t * kMine + k], (float)(log_weight(x[k]) - log((double)mass / kListScale)), (int32_t)kept);
-      }
+  // the kept entries' mass, and the one in which it passes u of it
+  uint64_t mass = 0, kept = 0;
+  in_play([&](int i) {
+    if (sh.col[i] >= 0) {
+      mass += sh.w[i];
+      ++kept;
     }
+  });
+  mass = wave_sum_u64(mass);
+  kept = wave_sum_u64(kept);
+  const uint64_t target = (uint64_t)((double)d.u * (double)mass);
+  uint64_t passed = 0, seen = 0;
+#pragma unroll 1
+  for (int first = 0; first < listed; first += kWave) {
+    const int i = first + lane;
+    const uint32_t key = i < listed ? sh.key[i] : 0u;
+    const uint64_t equal = __ballot(i < listed && key == border);
+    const uint64_t rank = seen + (uint64_t)__builtin_popcountll(equal & ((1ull << lane) - 1));
+    const bool in = i < listed && sh.col[i] >= 0 && (key > border || (key == border && rank < ties));
+    seen += (uint64_t)__builtin_popcountll(equal);
+    const uint64_t w = in ? sh.w[i] : 0;
+    uint64_t all;
+    const uint64_t before = passed + wave_before(w, all);
+    if (before <= target && target < before + w)
+      draw_result(a, r, sh.col[i], (float)(log_weight(value_of(key)) - log((double)mass / kListScale)), (int32_t)kept);
+    passed += all;
+    if (passed > target) break;
   }
 }
 
@@ -895,7 +1013,9 @@ __device__ __forceinline__ bool draw_flat(const DrawArgs& a, int64_t r, FlatShar
 
   float inv = 0.0f;  // bins: (m - x) inv
   const float c32 = (float)c;
-  auto bin_of = [&](float x) { return min((uint32_t)((m - x) * inv), (uint32_t)(kBins - 1)); };
+  auto bin_of = [&](float x) {  // (the largest's difference to itself is 0 also where it is infinite)
+    return x == m ? 0u : (uint32_t)fminf((m - x) * inv, (float)(kBins - 1));
+  };
   int first = kBins, last = -1;  // the bins with the border
   for (int i = t; i < kPieces; i += kFlat) sh.pieces[i] = 0;
   if (t == 0) sh.n = 0;
@@ -910,9 +1030,10 @@ __device__ __forceinline__ bool draw_flat(const DrawArgs& a, int64_t r, FlatShar
       load_cols(q, Y, base, V);
       q.get(x);
 #pragma unroll
-      for (int k = 0; k < 8; ++k)
-        if (x[k] > -INFINITY)
-          atomicAdd(&sh.bins[bin_of(x[k])], x[k] == m ? 1.0f : __builtin_amdgcn_exp2f((x[k] - m) * c32));
+      for (int k = 0; k < 8; ++k) {
+        const uint32_t b = bin_of(x[k]);  // (the last one holds all the rest: not needed, and one address for most lanes)
+        if (b < kBins - 1) atomicAdd(&sh.bins[b], x[k] == m ? 1.0f : __builtin_amdgcn_exp2f((x[k] - m) * c32));
+      }
     }
     __syncthreads();
     // (two bins a thread)
@@ -1122,7 +1243,13 @@ hipError_t launch_t(DrawArgs a, hipStream_t s) {
   }
   const int64_t waves = a.R * ((a.S + a.per - 1) / a.per);
   hipLaunchKernelGGL((k_draw_sweep<T>), dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, s, a);
-  hipLaunchKernelGGL((k_draw_finish<T>), dim3((unsigned)a.R), dim3(kFinish), 0, s, a);
+  const dim3 rows((unsigned)((a.R + kFinishWaves - 1) / kFinishWaves));
+  if (a.S <= 16)
+    hipLaunchKernelGGL((k_draw_finish<T, 4>), rows, dim3(kFinish), 0, s, a);
+  else if (a.S <= 64)
+    hipLaunchKernelGGL((k_draw_finish<T, 16>), rows, dim3(kFinish), 0, s, a);
+  else
+    hipLaunchKernelGGL((k_draw_finish<T, 32>), rows, dim3(kFinish), 0, s, a);
   if (a.V > kCap)  // (else every list fits)
     hipLaunchKernelGGL((k_draw_left<T>), dim3((unsigned)(a.R < 512 ? a.R : 512)), dim3(kFlat), 0, s, a);
   return hipGetLastError();
