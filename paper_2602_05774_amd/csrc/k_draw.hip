@@ -540,49 +540,55 @@ struct Block {
   }
 };
 
-// A row's list: entries in index order.
+// A row's list: its columns in order, and the groups that they lie in.
 struct FinishShared {
-  uint64_t w[kCap];       // integer weights
-  uint32_t key[kCap];     // order of the logit
-  int32_t col[kCap];      // column; kDropped: min-p drops it
+  int32_t col[kCap];
   uint16_t groups[kGroups];
 };
-constexpr int32_t kDropped = (int32_t)0x80000000u;
 
-// Over a wavefront: sums of three, scans, keys.
+// Over a wavefront, by DPP (an LDS permute's latency six times over is what a chain of
+// them would cost): the least, and sums of the lanes before (row_shr 1, 2, 4, 8, then the
+// last lanes of the rows before).
 __device__ __forceinline__ uint32_t wave_least(uint32_t v) {
-#pragma unroll
-  for (int d = 1; d < kWave; d <<= 1) v = min(v, (uint32_t)__shfl_xor((int)v, d));
-  return v;
+  v = min(v, (uint32_t)dpp_i<kDppQuad1>((int)v));
+  v = min(v, (uint32_t)dpp_i<kDppQuad2>((int)v));
+  v = min(v, (uint32_t)dpp_i<kDppHalfMirror>((int)v));
+  v = min(v, (uint32_t)dpp_i<kDppMirror>((int)v));
+  return min(min((uint32_t)lane_i((int)v, 0), (uint32_t)lane_i((int)v, 16)),
+             min((uint32_t)lane_i((int)v, 32), (uint32_t)lane_i((int)v, 48)));
+}
+template <int CTRL, int ROWS>
+__device__ __forceinline__ uint64_t dpp_zero(uint64_t u) {  // 0 where no lane is named
+  const uint64_t lo = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(uint32_t)u, CTRL, ROWS, 0xF, false);
+  const uint64_t hi = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)(u >> 32), CTRL, ROWS, 0xF, false);
+  return hi << 32 | lo;
+}
+template <int CTRL, int ROWS, typename N>
+__device__ __forceinline__ N dpp_add(N v) {
+  return v + __builtin_bit_cast(N, dpp_zero<CTRL, ROWS>(__builtin_bit_cast(uint64_t, v)));
 }
 template <typename N>
 __device__ __forceinline__ N wave_before(N v, N& all) {
-  N upto = v;
-#pragma unroll
-  for (int d = 1; d < kWave; d <<= 1) {
-    const N o = __shfl_up(upto, d);
-    if ((int)(threadIdx.x & 63) >= d) upto += o;
-  }
-  all = __shfl(upto, kWave - 1);
-  const N prev = __shfl_up(upto, 1);  // (upto - v would lose what v is small against)
-  return (threadIdx.x & 63) == 0 ? N(0) : prev;
+  static_assert(sizeof(N) == 8, "");
+  v = dpp_add<0x111, 0xF>(v);
+  v = dpp_add<0x112, 0xF>(v);
+  v = dpp_add<0x114, 0xF>(v);
+  v = dpp_add<0x118, 0xF>(v);
+  v = dpp_add<0x142, 0xA>(v);  // row_bcast15 to rows 1 and 3
+  v = dpp_add<0x143, 0xC>(v);  // row_bcast31 to rows 2 and 3
+  const uint64_t u = __builtin_bit_cast(uint64_t, v);
+  all = __builtin_bit_cast(N, lane_u64(u, 63));
+  return __builtin_bit_cast(N, dpp_zero<0x138, 0xF>(u));  // wave_shr 1
 }
-// The largest key in [lo, hi] such that the sum over entries of at least that key
-// reaches target (that of lo does), two bits of it a round; measure(keys, sums): a
-// lane's sums for three keys.
-template <class M>
-__device__ __forceinline__ uint32_t wave_largest(uint32_t lo, uint32_t hi, uint64_t target, M&& measure) {
+// The largest key in [lo, hi] that reaches(key) (lo's does), bit by bit.
+template <class F>
+__device__ __forceinline__ uint32_t wave_largest(uint32_t lo, uint32_t hi, F&& reaches) {
   int bits = lo == hi ? 0 : 32 - __builtin_clz(lo ^ hi);
   uint32_t key = bits == 32 ? 0u : hi >> bits << bits;
 #pragma unroll 1
-  while (bits > 0) {
-    bits = bits > 2 ? bits - 2 : 0;
-    const uint32_t t[3] = {key | 1u << bits, key | 2u << bits, key | 3u << bits};
-    uint64_t s[3] = {0, 0, 0};
-    measure(t, s);
-#pragma unroll
-    for (int i = 0; i < 3; ++i) s[i] = wave_sum_u64(s[i]);
-    key |= (uint32_t)(s[2] >= target ? 3 : s[1] >= target ? 2 : s[0] >= target ? 1 : 0) << bits;
+  while (--bits >= 0) {
+    const uint32_t t = key | 1u << bits;
+    if (reaches(t)) key = t;
   }
   return key;
 }
@@ -734,29 +740,14 @@ __global__ __launch_bounds__(kFinish) void k_draw_finish(DrawArgs a) {
   if (n > kCap) {
     if (by_k) {
       if (d.top_k > kCap) return leave();
-      uint64_t have = 0;
+      auto count = [&](uint32_t at) {
+        int s = 0;
 #pragma unroll
-      for (int k = 0; k < kPer; ++k) have += g[k] > 0u ? 1 : 0;
-      if (wave_sum_u64(have) < (uint64_t)d.top_k) return leave();
-      // (three counts of 21 bits in the first sum)
-      uint32_t key = low == high ? high : 0u;
-      if (low != high) {
-        int bits = 32 - __builtin_clz(low ^ high);
-        key = bits == 32 ? 0u : high >> bits << bits;
-#pragma unroll 1
-        while (bits > 0) {
-          bits = bits > 2 ? bits - 2 : 0;
-          uint64_t s = 0;
-#pragma unroll
-          for (int k = 0; k < kPer; ++k) {
-            const uint32_t over = g[k] >= key ? min((g[k] - key) >> bits, 3u) : 0u;  // of the three keys, how many it reaches
-            s += over == 3u ? 1ull << 42 | 1ull << 21 | 1ull : over == 2u ? 1ull << 21 | 1ull : over == 1u ? 1ull : 0ull;
-          }
-          s = wave_sum_u64(s);
-          const uint32_t want = (uint32_t)d.top_k;
-          key |= (uint32_t)((s >> 42) >= want ? 3 : ((s >> 21) & 0x1FFFFFu) >= want ? 2 : (s & 0x1FFFFFu) >= want ? 1 : 0) << bits;
-        }
-      }
+        for (int k = 0; k < kPer; ++k) s += __builtin_popcountll(__ballot(g[k] >= at));
+        return s;
+      };
+      if (count(1u) < d.top_k) return leave();
+      const uint32_t key = wave_largest(low, high, [&](uint32_t at) { return count(at) >= d.top_k; });
       least = value_of(key);
     } else if (by_p) {
       // (with d.top_k > 0, at least n, the sum was not formed)
@@ -776,11 +767,12 @@ __global__ __launch_bounds__(kFinish) void k_draw_finish(DrawArgs a) {
       if ((double)all < goal) {
         if (!by_m) return leave();
       } else {
-        least = value_of(wave_largest(low, high, (uint64_t)goal, [&](const uint32_t (&t)[3], uint64_t (&s)[3]) {
+        const uint64_t target = (uint64_t)goal;
+        least = value_of(wave_largest(low, high, [&](uint32_t at) {
+          uint64_t s = 0;
 #pragma unroll
-          for (int k = 0; k < kPer; ++k)
-#pragma unroll
-            for (int i = 0; i < 3; ++i) s[i] += g[k] >= t[i] ? w[k] : 0u;
+          for (int k = 0; k < kPer; ++k) s += g[k] >= at ? w[k] : 0u;
+          return wave_sum_u64(s) >= target;
         }));
       }
     } else if (!by_m) {
@@ -810,155 +802,134 @@ __global__ __launch_bounds__(kFinish) void k_draw_finish(DrawArgs a) {
       if (g[k] >= least_key) sh.groups[at++] = (uint16_t)(lane * kPer + k);
     settle();
   }
-  constexpr int kSets = 4, kSet = kWave / 16;  // a set: 4 groups, a lane eight columns
+  constexpr int kSets = 8, kSet = kWave / 16;  // a set: 4 groups, a lane eight columns
   int listed = 0;
 #pragma unroll 1
   for (int first = 0; first < ngroups; first += kSets * kSet) {
     Raw8<T> q[kSets];
     int base[kSets];
-    uint64_t counts4 = 0;  // 16 bits a set
 #pragma unroll
     for (int s = 0; s < kSets; ++s) {
       const int i = first + s * kSet + (lane >> 4);
       base[s] = i < ngroups ? (int)sh.groups[i] * kDrawGroup + (lane & 15) * 8 : a.V;
       load_cols(q[s], Y, base[s], a.V);
     }
-    uint32_t reach = 0;  // a bit per entry
+    uint64_t reach = 0, counts[2] = {0, 0}, all[2], before[2];  // a bit per entry; 16 bits a set
 #pragma unroll
     for (int s = 0; s < kSets; ++s) {
       float x[8];
       q[s].get(x);
+      uint32_t bits = 0;
 #pragma unroll
-      for (int k = 0; k < 8; ++k) reach |= x[k] >= least && x[k] > -INFINITY ? 1u << (8 * s + k) : 0u;
-      counts4 |= (uint64_t)__builtin_popcount(reach >> (8 * s) & 0xFFu) << (16 * s);
+      for (int k = 0; k < 8; ++k) bits |= x[k] >= least && x[k] > -INFINITY ? 1u << k : 0u;
+      reach |= (uint64_t)bits << (8 * s);
+      counts[s >> 2] |= (uint64_t)__builtin_popcount(bits) << (16 * (s & 3));
     }
-    uint64_t all;
-    const uint64_t before = wave_before(counts4, all);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) before[i] = wave_before(counts[i], all[i]);
 #pragma unroll
     for (int s = 0; s < kSets; ++s) {
-      int at = listed + (int)((before >> (16 * s)) & 0xFFFFu);
-      float x[8];
-      q[s].get(x);
-      if ((reach >> (8 * s) & 0xFFu) != 0u) {
-#pragma unroll
-        for (int k = 0; k < 8; ++k)
-          if ((reach >> (8 * s + k) & 1u) != 0u) {
-            if (at < kCap) {
-              sh.key[at] = key_of(x[k]);
-              sh.col[at] = base[s] + k;
-            }
-            ++at;
-          }
+      int at = listed + (int)((before[s >> 2] >> (16 * (s & 3))) & 0xFFFFu);
+      uint32_t bits = (uint32_t)(reach >> (8 * s)) & 0xFFu;
+      while (bits != 0u) {
+        if (at < kCap) sh.col[at] = base[s] + __builtin_ctz(bits);
+        ++at;
+        bits &= bits - 1u;
       }
-      listed += (int)((all >> (16 * s)) & 0xFFFFu);
+      listed += (int)((all[s >> 2] >> (16 * (s & 3))) & 0xFFFFu);
     }
     if (listed > kCap) return leave();
   }
   settle();
-  uint32_t kmin = 0xFFFFFFFFu, kmax = 0;
-#pragma unroll 1
-  for (int i = lane; i < listed; i += kWave) {
-    const uint32_t key = sh.key[i];
-    const double v = draw_weight(value_of(key), m, c);
-    sh.w[i] = (uint64_t)(v * kListScale + 0.5);
-    if (v < (double)d.min_p) sh.col[i] |= kDropped;
-    kmin = min(kmin, key);
-    kmax = max(kmax, key);
+  // entry 64 j + lane of the list: column, key, weight; `in`: in play, a bit each
+  constexpr int kMine = kCap / kWave;
+  int32_t col[kMine];
+  uint32_t key[kMine], in = 0, enough = 0;
+  uint64_t w[kMine];
+#pragma unroll
+  for (int j = 0; j < kMine; ++j) {
+    const int i = j * kWave + lane;
+    key[j] = 0;
+    w[j] = 0;
+    if (j * kWave >= listed) continue;  // (of the whole wavefront, here and below)
+    if (i < listed) {
+      col[j] = sh.col[i];
+      key[j] = key_of(load1(Y + col[j]));
+      in |= 1u << j;
+    }
   }
-  settle();
+  uint32_t kmin = 0xFFFFFFFFu, kmax = 0;
+#pragma unroll
+  for (int j = 0; j < kMine; ++j) {
+    if (j * kWave >= listed) continue;
+    if ((in >> j & 1u) == 0u) continue;
+    const double v = draw_weight(value_of(key[j]), m, c);
+    w[j] = (uint64_t)(v * kListScale + 0.5);
+    enough |= v >= (double)d.min_p ? 1u << j : 0u;
+    kmin = min(kmin, key[j]);
+    kmax = max(kmax, key[j]);
+  }
   kmin = wave_least(kmin);
   kmax = ~wave_least(~kmax);
-  // the entries in play: of a key above `border`, or of that key the first `ties`
-  uint32_t border = 0;
-  uint64_t ties = ~0ull;
-  // sums over the entries in play of at least three keys
-  auto in_play = [&](auto&& f) {  // f(entry), in index order by lanes
-    if (ties == ~0ull) {
-#pragma unroll 1
-      for (int i = lane; i < listed; i += kWave)
-        if (sh.key[i] >= border) f(i);
-      return;
-    }
-    uint64_t seen = 0;  // entries of the border's key before this round of 64
-#pragma unroll 1
-    for (int first = 0; first < listed; first += kWave) {
-      const int i = first + lane;
-      const uint32_t key = i < listed ? sh.key[i] : 0u;
-      const uint64_t equal = __ballot(i < listed && key == border);
-      const uint64_t rank = seen + (uint64_t)__builtin_popcountll(equal & ((1ull << lane) - 1));
-      if (i < listed && (key > border || (key == border && rank < ties))) f(i);
-      seen += (uint64_t)__builtin_popcountll(equal);
+  auto mass_of = [&](uint32_t at) {  // of the entries in play of at least that key
+    uint64_t s = 0;
+#pragma unroll
+    for (int j = 0; j < kMine; ++j)
+      if (j * kWave < listed) s += (in >> j & 1u) != 0u && key[j] >= at ? w[j] : 0;
+    return wave_sum_u64(s);
+  };
+  auto count_of = [&](uint32_t at) {
+    int s = 0;
+#pragma unroll
+    for (int j = 0; j < kMine; ++j)
+      if (j * kWave < listed) s += __builtin_popcountll(__ballot((in >> j & 1u) != 0u && key[j] >= at));
+    return s;
+  };
+  // keeps of the entries in play those above `at`, and the first `ties` of that key
+  auto cut = [&](uint32_t at, uint64_t ties) {
+    uint64_t seen = 0;
+#pragma unroll
+    for (int j = 0; j < kMine; ++j) {
+      if (j * kWave >= listed) continue;
+      const bool mine = (in >> j & 1u) != 0u, equal = mine && key[j] == at;
+      const uint64_t who = __ballot(equal);
+      const uint64_t rank = seen + (uint64_t)__builtin_popcountll(who & ((1ull << lane) - 1));
+      if (mine && !(key[j] > at || (equal && rank < ties))) in &= ~(1u << j);
+      seen += (uint64_t)__builtin_popcountll(who);
     }
   };
   if (by_k && listed > d.top_k) {
-    const uint32_t at = wave_largest(kmin, kmax, d.top_k, [&](const uint32_t (&t)[3], uint64_t (&s)[3]) {
-#pragma unroll 1
-      for (int i = lane; i < listed; i += kWave) {
-        const uint32_t key = sh.key[i];
-#pragma unroll
-        for (int j = 0; j < 3; ++j) s[j] += key >= t[j] ? 1 : 0;
-      }
-    });
-    uint64_t above = 0;
-#pragma unroll 1
-    for (int i = lane; i < listed; i += kWave) above += sh.key[i] > at ? 1 : 0;
-    border = at;
-    ties = d.top_k - wave_sum_u64(above);
+    const uint32_t at = wave_largest(kmin, kmax, [&](uint32_t b) { return count_of(b) >= d.top_k; });
+    cut(at, (uint64_t)(d.top_k - count_of(at + 1u)));
   }
   if (by_p) {
-    uint64_t all = 0;
-    in_play([&](int i) { all += sh.w[i]; });
-    all = wave_sum_u64(all);
+    const uint64_t all = mass_of(0u);
     const double whole = by_k || n <= kCap ? (double)all : z * kListScale;
     const double goal = __builtin_ceil((double)d.top_p * whole);
     if (goal <= (double)all) {
       const uint64_t target = (uint64_t)goal;
-      const uint32_t at = wave_largest(max(kmin, border), kmax, target, [&](const uint32_t (&t)[3], uint64_t (&s)[3]) {
-        in_play([&](int i) {
-          const uint32_t key = sh.key[i];
-          const uint64_t w = sh.w[i];
-#pragma unroll
-          for (int j = 0; j < 3; ++j) s[j] += key >= t[j] ? w : 0;
-        });
-      });
-      uint64_t above = 0;
-      in_play([&](int i) { above += sh.key[i] > at ? sh.w[i] : 0; });
-      above = wave_sum_u64(above);
+      const uint32_t at = wave_largest(kmin, kmax, [&](uint32_t b) { return mass_of(b) >= target; });
       const uint64_t each = (uint64_t)(draw_weight(value_of(at), m, c) * kListScale + 0.5);
-      const uint64_t need = (target - above + each - 1) / each;
-      ties = at == border && ties < need ? ties : need;
-      border = at;
+      cut(at, (target - mass_of(at + 1u) + each - 1) / each);
     } else if (!min_bound) {
       return leave();
     }
   }
-  // the kept entries' mass, and the one in which it passes u of it
-  uint64_t mass = 0, kept = 0;
-  in_play([&](int i) {
-    if (sh.col[i] >= 0) {
-      mass += sh.w[i];
-      ++kept;
-    }
-  });
-  mass = wave_sum_u64(mass);
-  kept = wave_sum_u64(kept);
+  in &= enough;
+  const int kept = count_of(0u);
+  const uint64_t mass = mass_of(0u);
+  // the entry in which the mass passes u of it
   const uint64_t target = (uint64_t)((double)d.u * (double)mass);
-  uint64_t passed = 0, seen = 0;
-#pragma unroll 1
-  for (int first = 0; first < listed; first += kWave) {
-    const int i = first + lane;
-    const uint32_t key = i < listed ? sh.key[i] : 0u;
-    const uint64_t equal = __ballot(i < listed && key == border);
-    const uint64_t rank = seen + (uint64_t)__builtin_popcountll(equal & ((1ull << lane) - 1));
-    const bool in = i < listed && sh.col[i] >= 0 && (key > border || (key == border && rank < ties));
-    seen += (uint64_t)__builtin_popcountll(equal);
-    const uint64_t w = in ? sh.w[i] : 0;
+  uint64_t passed = 0;
+#pragma unroll
+  for (int j = 0; j < kMine; ++j) {
+    if (j * kWave >= listed) continue;
+    const uint64_t mine = (in >> j & 1u) != 0u ? w[j] : 0;
     uint64_t all;
-    const uint64_t before = passed + wave_before(w, all);
-    if (before <= target && target < before + w)
-      draw_result(a, r, sh.col[i], (float)(log_weight(value_of(key)) - log((double)mass / kListScale)), (int32_t)kept);
+    const uint64_t before = passed + wave_before(mine, all);
+    if (before <= target && target < before + mine)
+      draw_result(a, r, col[j], (float)(log_weight(value_of(key[j])) - log((double)mass / kListScale)), kept);
     passed += all;
-    if (passed > target) break;
   }
 }
 
