@@ -439,113 +439,6 @@ __device__ __forceinline__ uint64_t wave_sum_u64(uint64_t v) {
   return (lane_u64(v, 0) + lane_u64(v, 16)) + (lane_u64(v, 32) + lane_u64(v, 48));
 }
 
-// Sums and scans over a workgroup of kW wavefronts; `turn` alternates between two sets
-// of words, so that one barrier a sum is enough.
-template <int kW>
-struct Block {
-  uint64_t (*red)[3][kW];
-  int turn;
-  template <int N>
-  __device__ __forceinline__ void sums(uint64_t (&v)[N]) {
-    turn ^= 1;
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      v[i] = wave_sum_u64(v[i]);
-      if ((threadIdx.x & 63) == 0) red[turn][i][wave_id()] = v[i];
-    }
-    __syncthreads();
-#pragma unroll
-    for (int i = 0; i < N; ++i) {
-      v[i] = red[turn][i][0];
-#pragma unroll
-      for (int k = 1; k < kW; ++k) v[i] += red[turn][i][k];
-    }
-  }
-  __device__ __forceinline__ uint64_t sum(uint64_t v) {
-    uint64_t s[1] = {v};
-    sums(s);
-    return s[0];
-  }
-  template <typename N>
-  __device__ __forceinline__ N before(N v, N& all) {  // the sum over the threads before this one
-    static_assert(sizeof(N) == 8, "");
-    N upto = v;
-#pragma unroll
-    for (int d = 1; d < kWave; d <<= 1) {
-      const N o = __shfl_up(upto, d);
-      if ((int)(threadIdx.x & 63) >= d) upto += o;
-    }
-    turn ^= 1;
-    N* const r = reinterpret_cast<N*>(red[turn][0]);
-    if ((threadIdx.x & 63) == 63) r[wave_id()] = upto;
-    __syncthreads();
-    N first = 0;
-    all = 0;
-#pragma unroll
-    for (int k = 0; k < kW; ++k) {
-      if (k < wave_id()) first += r[k];
-      all += r[k];
-    }
-    // (upto - v would lose what v is small against)
-    const N prev = __shfl_up(upto, 1);
-    return first + ((threadIdx.x & 63) == 0 ? N(0) : prev);
-  }
-  __device__ __forceinline__ uint64_t least(uint64_t v) {
-#pragma unroll
-    for (int d = 1; d < kWave; d <<= 1) {
-      const uint64_t o = __shfl_xor(v, d);
-      v = o < v ? o : v;
-    }
-    turn ^= 1;
-    if ((threadIdx.x & 63) == 0) red[turn][0][wave_id()] = v;
-    __syncthreads();
-    uint64_t t = red[turn][0][0];
-#pragma unroll
-    for (int k = 1; k < kW; ++k) t = red[turn][0][k] < t ? red[turn][0][k] : t;
-    return t;
-  }
-  // The smallest and the largest key (32 bits) of the threads' [lo, hi].
-  __device__ __forceinline__ void range(uint32_t& lo, uint32_t& hi) {
-    uint32_t nhi = ~hi;
-#pragma unroll
-    for (int d = 1; d < kWave; d <<= 1) {
-      lo = min(lo, (uint32_t)__shfl_xor((int)lo, d));
-      nhi = min(nhi, (uint32_t)__shfl_xor((int)nhi, d));
-    }
-    turn ^= 1;
-    if ((threadIdx.x & 63) == 0) red[turn][0][wave_id()] = (uint64_t)nhi << 32 | lo;
-    __syncthreads();
-#pragma unroll
-    for (int k = 0; k < kW; ++k) {
-      lo = min(lo, (uint32_t)red[turn][0][k]);
-      nhi = min(nhi, (uint32_t)(red[turn][0][k] >> 32));
-    }
-    hi = ~nhi;
-  }
-  // The largest key in [lo, hi] such that measure(key), the sum over entries of at least
-  // that key, reaches target (that of lo does): two bits of it a round.
-  template <class M>
-  __device__ __forceinline__ uint32_t largest(uint32_t lo, uint32_t hi, uint64_t target, M&& measure) {
-    int bits = lo == hi ? 0 : 32 - __builtin_clz(lo ^ hi);
-    uint32_t key = bits == 32 ? 0u : hi >> bits << bits;
-    while (bits > 0) {
-      bits = bits > 2 ? bits - 2 : 0;
-      uint64_t s[3];
-#pragma unroll
-      for (int i = 0; i < 3; ++i) s[i] = measure(key | (uint32_t)(i + 1) << bits);
-      sums(s);
-      key |= (uint32_t)(s[2] >= target ? 3 : s[1] >= target ? 2 : s[0] >= target ? 1 : 0) << bits;
-    }
-    return key;
-  }
-};
-
-// A row's list: its columns in order, and the groups that they lie in.
-struct FinishShared {
-  int32_t col[kCap];
-  uint16_t groups[kGroups];
-};
-
 // Over a wavefront, by DPP (an LDS permute's latency six times over is what a chain of
 // them would cost): the least, and sums of the lanes before (row_shr 1, 2, 4, 8, then the
 // last lanes of the rows before).
@@ -580,6 +473,84 @@ __device__ __forceinline__ N wave_before(N v, N& all) {
   all = __builtin_bit_cast(N, lane_u64(u, 63));
   return __builtin_bit_cast(N, dpp_zero<0x138, 0xF>(u));  // wave_shr 1
 }
+// Sums and scans over a workgroup of kW wavefronts; `turn` alternates between two sets
+// of words, so that one barrier a sum is enough.
+template <int kW>
+struct Block {
+  uint64_t (*red)[3][kW];
+  int turn;
+  template <int N>
+  __device__ __forceinline__ void sums(uint64_t (&v)[N]) {
+    turn ^= 1;
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      v[i] = wave_sum_u64(v[i]);
+      if ((threadIdx.x & 63) == 0) red[turn][i][wave_id()] = v[i];
+    }
+    __syncthreads();
+    // (a lane per wavefront: every wavefront reading all words held up the LDS)
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int i = 0; i < N; ++i) v[i] = wave_sum_u64(lane < kW ? red[turn][i][lane] : 0ull);
+  }
+  __device__ __forceinline__ uint64_t sum(uint64_t v) {
+    uint64_t s[1] = {v};
+    sums(s);
+    return s[0];
+  }
+  template <typename N>
+  __device__ __forceinline__ N before(N v, N& all) {  // the sum over the threads before this one
+    N mine;
+    const N prev = wave_before(v, mine);
+    const int lane = threadIdx.x & 63;
+    turn ^= 1;
+    N* const r = reinterpret_cast<N*>(red[turn][0]);
+    if (lane == 0) r[wave_id()] = mine;
+    __syncthreads();
+    const N first = wave_before(lane < kW ? r[lane] : N(0), all);
+    return __builtin_bit_cast(N, lane_u64(__builtin_bit_cast(uint64_t, first), wave_id())) + prev;
+  }
+  __device__ __forceinline__ uint32_t least(uint32_t v) {
+    uint32_t lo = v, hi = 0;
+    range(lo, hi);
+    return lo;
+  }
+  // The smallest and the largest key (32 bits) of the threads' [lo, hi].
+  __device__ __forceinline__ void range(uint32_t& lo, uint32_t& hi) {
+    lo = wave_least(lo);
+    uint32_t nhi = wave_least(~hi);
+    const int lane = threadIdx.x & 63;
+    turn ^= 1;
+    if (lane == 0) red[turn][0][wave_id()] = (uint64_t)nhi << 32 | lo;
+    __syncthreads();
+    const uint64_t u = lane < kW ? red[turn][0][lane] : ~0ull;
+    lo = wave_least((uint32_t)u);
+    hi = ~wave_least((uint32_t)(u >> 32));
+  }
+  // The largest key in [lo, hi] such that measure(key), the sum over entries of at least
+  // that key, reaches target (that of lo does): two bits of it a round.
+  template <class M>
+  __device__ __forceinline__ uint32_t largest(uint32_t lo, uint32_t hi, uint64_t target, M&& measure) {
+    int bits = lo == hi ? 0 : 32 - __builtin_clz(lo ^ hi);
+    uint32_t key = bits == 32 ? 0u : hi >> bits << bits;
+    while (bits > 0) {
+      bits = bits > 2 ? bits - 2 : 0;
+      uint64_t s[3];
+#pragma unroll
+      for (int i = 0; i < 3; ++i) s[i] = measure(key | (uint32_t)(i + 1) << bits);
+      sums(s);
+      key |= (uint32_t)(s[2] >= target ? 3 : s[1] >= target ? 2 : s[0] >= target ? 1 : 0) << bits;
+    }
+    return key;
+  }
+};
+
+// A row's list: its columns in order, and the groups that they lie in.
+struct FinishShared {
+  int32_t col[kCap];
+  uint16_t groups[kGroups];
+};
+
 // The largest key in [lo, hi] that reaches(key) (lo's does), bit by bit.
 template <class F>
 __device__ __forceinline__ uint32_t wave_largest(uint32_t lo, uint32_t hi, F&& reaches) {
@@ -936,7 +907,7 @@ __global__ __launch_bounds__(kFinish) void k_draw_finish(DrawArgs a) {
 // ------------------------------------------------------------- flat rows ---
 // A row whose kept entries do not fit a list, bounded by top-p or min-p of the whole
 // softmax: two sweeps by a workgroup of 1024 threads.  The first (top-p) sums fp32
-// weights in 2048 bins of equal width between the largest logit and one below which
+// weights, as integers, in 2048 bins of equal width between the largest logit and one below which
 // less than 1 - p of the mass can lie; within 1e-4 of p Z, far more than fp32 sums are
 // off, they tell the bins that hold the border.  The second forms the weights in 64
 // bits: of the entries above those bins per 512 columns, and the entries in them go to
@@ -945,7 +916,7 @@ constexpr int kFlat = 1024, kFlatWaves = kFlat / kWave, kBins = 2048, kFlatCap =
 constexpr int kFlatMine = kFlatCap / kFlat, kPieces = kDrawSpans * kDrawSpan / 512;
 struct FlatShared {
   union {
-    float bins[kBins];
+    uint32_t bins[kBins];
     struct {
       float x[kFlatCap];
       int32_t col[kFlatCap];
@@ -993,17 +964,21 @@ __device__ __forceinline__ bool draw_flat(const DrawArgs& a, int64_t r, FlatShar
   if (by_p) {
     const double depth = -temp * log((1.0 - (double)d.top_p) * z / (double)n);
     inv = (float)fmin((kBins - 1) / depth, 3e38);
-    for (int i = t; i < kBins; i += kFlat) sh.bins[i] = 0.0f;
+    const float bin_scale = __builtin_ldexpf(1.0f, 30 - (ilogb(z) + 1));  // (all weights together: below 2^31)
+    for (int i = t; i < kBins; i += kFlat) sh.bins[i] = 0u;
     __syncthreads();
+    Raw8<T> q;
+    load_cols(q, Y, t * 8, V);
+#pragma unroll 1
     for (int base = t * 8; base < V; base += kFlat * 8) {
-      Raw8<T> q;
       float x[8];
-      load_cols(q, Y, base, V);
       q.get(x);
+      load_cols(q, Y, min(base + kFlat * 8, V), V);
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
         const uint32_t b = bin_of(x[k]);  // (the last one holds all the rest: not needed, and one address for most lanes)
-        if (b < kBins - 1) atomicAdd(&sh.bins[b], x[k] == m ? 1.0f : __builtin_amdgcn_exp2f((x[k] - m) * c32));
+        const float w = x[k] == m ? 1.0f : __builtin_amdgcn_exp2f((x[k] - m) * c32);
+        if (b < kBins - 1) atomicAdd(&sh.bins[b], (uint32_t)fmaf(w, bin_scale, 0.5f));
       }
     }
     __syncthreads();
@@ -1011,13 +986,13 @@ __device__ __forceinline__ bool draw_flat(const DrawArgs& a, int64_t r, FlatShar
     const double mine[2] = {(double)sh.bins[2 * t], (double)sh.bins[2 * t + 1]};
     double all;
     double run = blk.before(mine[0] + mine[1], all);
-    const double want = (double)d.top_p * z;
-    uint64_t b1 = ~0ull, b2 = ~0ull;
+    const double want = (double)d.top_p * z * (double)bin_scale;
+    uint32_t b1 = 0xFFFFFFFFu, b2 = 0xFFFFFFFFu;
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       run += mine[i];
-      if (b1 == ~0ull && run >= want * (1.0 - 1e-4)) b1 = (uint64_t)(2 * t + i);
-      if (b2 == ~0ull && run >= want * (1.0 + 1e-4)) b2 = (uint64_t)(2 * t + i);
+      if (b1 == 0xFFFFFFFFu && run >= want * (1.0 - 1e-4)) b1 = (uint32_t)(2 * t + i);
+      if (b2 == 0xFFFFFFFFu && run >= want * (1.0 + 1e-4)) b2 = (uint32_t)(2 * t + i);
     }
     b1 = blk.least(b1);
     b2 = blk.least(b2);
@@ -1037,37 +1012,52 @@ __device__ __forceinline__ bool draw_flat(const DrawArgs& a, int64_t r, FlatShar
   __syncthreads();
   uint64_t above = 0, count = 0;
   const int pieces = (V + 511) / 512;
+  Raw8<T> q;
+  load_cols(q, Y, wave * 512 + lane * 8, V);
+#pragma unroll 1
   for (int p = wave; p < pieces; p += kFlatWaves) {
-    Raw8<T> q;
     float x[8];
-    const int base = p * 512 + lane * 8;
-    load_cols(q, Y, base, V);
     q.get(x);
+    const int base = p * 512 + lane * 8;
+    load_cols(q, Y, min(base + kFlatWaves * 512, V), V);
+    uint32_t over = 0, at_border = 0;  // entries above the border's bins, and in them
+#pragma unroll
+    for (int k = 0; k < 8; ++k) {
+      bool is_over = x[k] > -INFINITY && x[k] >= bound, is_at = false;
+      if (by_p) {
+        const int b = (int)bin_of(x[k]);
+        is_at = x[k] > -INFINITY && b >= first && b <= last;
+        is_over = x[k] > -INFINITY && b < first;
+      }
+      over |= is_over ? 1u << k : 0u;
+      at_border |= is_at ? 1u << k : 0u;
+    }
     uint64_t mass = 0;
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
-      if (!(x[k] > -INFINITY)) continue;
-      if (by_p) {
-        const int b = (int)bin_of(x[k]);
-        if (b > last) continue;
-        if (b >= first) {
-          const int at = atomicAdd(&sh.n, 1);
+      if (!__any((over >> k & 1u) != 0u)) continue;
+      double w;
+      const uint64_t W = (over >> k & 1u) != 0u ? weigh(x[k], w) : 0;
+      above += W;
+      const bool keeps = (over >> k & 1u) != 0u && w >= min_p;
+      mass += keeps ? W : 0;
+      count += keeps ? 1 : 0;
+    }
+    if (__any(at_border != 0u)) {
+      uint64_t all;
+      int at = (int)wave_before((uint64_t)__builtin_popcount(at_border), all);
+      int from = 0;
+      if (lane == 0) from = atomicAdd(&sh.n, (int)all);
+      at += __builtin_amdgcn_readfirstlane(from);
+#pragma unroll
+      for (int k = 0; k < 8; ++k)
+        if ((at_border >> k & 1u) != 0u) {
           if (at < kFlatCap) {
             sh.list.x[at] = x[k];
             sh.list.col[at] = base + k;
           }
-          continue;
+          ++at;
         }
-      } else if (x[k] < bound) {
-        continue;
-      }
-      double w;
-      const uint64_t W = weigh(x[k], w);
-      above += W;
-      if (w >= min_p) {
-        mass += W;
-        ++count;
-      }
     }
     mass = wave_sum_u64(mass);
     if (lane == 0) sh.pieces[p] = mass;
@@ -1144,7 +1134,6 @@ __device__ __forceinline__ bool draw_flat(const DrawArgs& a, int64_t r, FlatShar
   }
   __syncthreads();
   if (wave > 0) return true;
-  Raw8<T> q;
   float x[8];
   const int base = sh.at * 512 + lane * 8;
   load_cols(q, Y, base, V);
