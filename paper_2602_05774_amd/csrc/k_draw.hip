@@ -382,18 +382,21 @@ __global__ __launch_bounds__(256) void k_draw_sweep(DrawArgs a) {
     double s = 0.0;
     if (sums && m > -INFINITY) {
       const double md = m;
+      auto sum = [&](auto&& weight) {
 #pragma unroll
-      for (int u = 0; u < kLoads; ++u) {
-        float x[8];
-        q[u].get(x);
-        if (m < INFINITY) {
+        for (int u = 0; u < kLoads; ++u) {
+          float x[8];
+          q[u].get(x);
 #pragma unroll
-          for (int k = 0; k < 8; ++k) s += exp2_64(((double)x[k] - md) * c);
-        } else {
-#pragma unroll
-          for (int k = 0; k < 8; ++k) s += x[k] == m ? 1.0 : 0.0;
+          for (int k = 0; k < 8; ++k) s += weight(x[k]);
         }
-      }
+      };
+      if (m == INFINITY)
+        sum([&](float x) { return x == m ? 1.0 : 0.0; });
+      else if (__all(((double)low - md) * c > -1000.0))
+        sum([&](float x) { return exp2_64_near(((double)x - md) * c); });
+      else
+        sum([&](float x) { return exp2_64(((double)x - md) * c); });
       s = wave_sum_d(s);
     }
     const int64_t at = r * a.S + span;
