@@ -736,8 +736,10 @@ vsd_status vsd_grad_norm(const vsd_tensor* grads, int32_t n, float* norm, void* 
 /* Scales n gradients to max_norm > 0: norm_out [1] (optional) and scale [1]
  * (optional).  norm [1], if given, is used in place of the tensors' own (that of
  * more tensors, or of all ranks; it is read when the stream gets there).  out:
- * NULL for in place, or n tensors of the same rows and cols, of either dtype, each
- * the gradient's own memory or none that the call reads.  Workspace as above. */
+ * NULL for in place, or n tensors of the same rows and cols, of either dtype.  What
+ * is written may not overlap what another tensor reads or writes (a gradient named
+ * twice, say: VSD_ERR_INVALID_VALUE; vsd_grad_norm counts it twice).  Workspace as
+ * above. */
 vsd_status vsd_clip_gradients(const vsd_tensor* grads, const vsd_tensor* out, int32_t n, float max_norm,
                               const float* norm, float* norm_out, float* scale, void* workspace,
                               size_t workspace_bytes, void* hip_stream);

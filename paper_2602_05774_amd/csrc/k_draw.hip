@@ -383,13 +383,15 @@ __global__ __launch_bounds__(256) void k_draw_sweep(DrawArgs a) {
     if (sums && m > -INFINITY) {
       const double md = m;
       auto sum = [&](auto&& weight) {
+        double s2[2] = {0.0, 0.0};
 #pragma unroll
         for (int u = 0; u < kLoads; ++u) {
           float x[8];
           q[u].get(x);
 #pragma unroll
-          for (int k = 0; k < 8; ++k) s += weight(x[k]);
+          for (int k = 0; k < 8; ++k) s2[k & 1] += weight(x[k]);
         }
+        s = s2[0] + s2[1];
       };
       if (m == INFINITY)
         sum([&](float x) { return x == m ? 1.0 : 0.0; });
@@ -1224,7 +1226,7 @@ hipError_t launch_draw(DrawArgs a, bool bf16, hipStream_t s) {
   if (a.todo != nullptr) {
     // spans a wavefront sweeps: one until the chip is full several times over
     a.per = 1;
-    while (a.per < 8 && a.R * ((a.S + a.per - 1) / a.per) > 65536) a.per *= 2;
+    while (a.per < 16 && a.R * ((a.S + a.per - 1) / a.per) > 32768) a.per *= 2;
   }
   return bf16 ? launch_t<bf16_t>(a, s) : launch_t<float>(a, s);
 }

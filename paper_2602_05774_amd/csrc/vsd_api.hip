@@ -5,7 +5,9 @@
 #include <cstdarg>
 #include <cstdio>
 #include <mutex>
+#include <new>
 #include <string>
+#include <vector>
 
 #include "vsd_device.hpp"
 #include "vsd_kernels.hpp"
@@ -782,6 +784,48 @@ vsd_status check_tensors(const vsd_tensor* g, const vsd_tensor* out, int32_t n) 
     if (out[i].data == g[i].data && (out[i].dtype != g[i].dtype || (g[i].rows > 1 && out[i].ld != g[i].ld)))
       return fail(VSD_ERR_INVALID_VALUE, "out[%d] is its gradient's memory with another type or stride", i);
   }
+  return VSD_OK;
+}
+
+// Whether two tensors share bytes: none where their ranges are apart, or where both are
+// columns of rows of one stride and the columns are apart.
+struct Extent {
+  uintptr_t at, end, row, width;  // bytes; row: the stride, 0 where the tensor lies in one piece
+  int32_t i;
+  bool written;
+};
+Extent extent_of(const vsd_tensor& t, int32_t i, bool written) {
+  const int64_t es = t.dtype == VSD_F32 ? 4 : 2;
+  const uintptr_t at = reinterpret_cast<uintptr_t>(t.data);
+  const bool strided = t.rows > 1 && t.ld != t.cols;
+  const int64_t last = strided ? (t.rows - 1) * t.ld + t.cols : t.rows * t.cols;
+  return Extent{at, at + (uintptr_t)(last * es), strided ? (uintptr_t)(t.ld * es) : 0, (uintptr_t)(t.cols * es), i, written};
+}
+bool share_bytes(const Extent& a, const Extent& b) {  // a.at <= b.at < a.end
+  if (a.row == 0 || a.row != b.row) return true;
+  const uintptr_t d = (b.at - a.at) % a.row;
+  return d < a.width || d + b.width > a.row;
+}
+
+// The workgroups scale the tensors in any order: what one writes, no other may read or write.
+vsd_status check_apart(const vsd_tensor* g, const vsd_tensor* out, int32_t n) {
+  std::vector<Extent> e;
+  try {
+    e.reserve((size_t)n * 2);
+  } catch (const std::bad_alloc&) {  // (no exception leaves a C entry)
+    return fail(VSD_ERR_WORKSPACE, "no host memory to look through %d tensors", n);
+  }
+  for (int32_t i = 0; i < n; ++i) {
+    if (g[i].rows == 0 || g[i].cols == 0) continue;
+    const bool in_place = out == nullptr || out[i].data == g[i].data;
+    e.push_back(extent_of(g[i], i, in_place));
+    if (!in_place) e.push_back(extent_of(out[i], i, true));
+  }
+  std::sort(e.begin(), e.end(), [](const Extent& a, const Extent& b) { return a.at < b.at; });
+  for (size_t a = 0; a < e.size(); ++a)
+    for (size_t b = a + 1; b < e.size() && e[b].at < e[a].end; ++b)
+      if ((e[a].written || e[b].written) && share_bytes(e[a], e[b]))
+        return fail(VSD_ERR_INVALID_VALUE, "tensors %d and %d overlap, and one of them is written", e[a].i, e[b].i);
   return VSD_OK;
 }
 
@@ -1579,6 +1623,7 @@ vsd_status vsd_clip_gradients(const vsd_tensor* grads, const vsd_tensor* out, in
   vsd_status st = check_tensors(grads, out, n);
   if (st != VSD_OK) return st;
   if (!(max_norm > 0.0f)) return fail(VSD_ERR_INVALID_VALUE, "max_norm=%g must be > 0", max_norm);
+  if ((st = check_apart(grads, out, n)) != VSD_OK) return st;
   if (norm == nullptr && (st = check_workspace(workspace, workspace_bytes, norm_bytes(n))) != VSD_OK) return st;
   if (norm != nullptr && norm == norm_out) return fail(VSD_ERR_INVALID_VALUE, "norm_out is the norm that is given");
   if (norm != nullptr && norm == scale) return fail(VSD_ERR_INVALID_VALUE, "scale is the norm that is given");

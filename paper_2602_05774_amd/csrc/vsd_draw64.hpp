@@ -45,7 +45,8 @@ __device__ __forceinline__ double exp2_64_near(double t) {
   p = __builtin_fma(p, f, 0x1.62e42fef89d1ep-1);
   p = __builtin_fma(p, f, 1.0);
   const uint64_t u = __builtin_bit_cast(uint64_t, p);
-  const uint32_t hi = (uint32_t)(u >> 32) + ((uint32_t)__builtin_bit_cast(uint64_t, r) << 20);
+  uint32_t hi;  // (written in C++ the shift and the addition become four 64-bit operations)
+  asm("v_lshl_add_u32 %0, %1, 20, %2" : "=v"(hi) : "v"((uint32_t)__builtin_bit_cast(uint64_t, r)), "v"((uint32_t)(u >> 32)));
   return __builtin_bit_cast(double, (uint64_t)hi << 32 | (uint32_t)u);
 }
 

@@ -137,6 +137,53 @@ def test_flat_rows():
         _check(vsd.sample_rows(X, u, *s), X, u, s)
 
 
+@pytest.mark.parametrize("settings", [(1.0, 0, 1.0, 0.0), (0.8, 0, 0.3, 0.0), (1.0, 700, 1.0, 0.0), (0.7, 300, 0.9, 0.0),
+                                      (1.2, 0, 1.0, 0.01), (1.0, 0, 0.5, 0.05), (0.0, 0, 1.0, 0.0)])
+@pytest.mark.parametrize("V,kind", [(513, "f32"), (2048, "bf16"), (20000, "f32"), (65537, "bf16"), (262144, "bf16"),
+                                    (262147, "bf16"), (300001, "f32")])
+def test_lists_and_flat_rows_in_every_band(V, kind, settings):
+    """Lists that fit and that do not, with the records' largest vocabulary and past it."""
+    buf, X = _rows(5, V, kind, V)
+    X[1] *= 0.1                # flat
+    X[2] = X[2].round()        # long runs of equal logits
+    X[3, V // 3] = 40.0        # one entry has it all
+    X[4, ::2] = -INF
+    u = _u(5, V + 1)
+    _check(vsd.sample_rows(X, u, *settings), X, u, settings)
+
+
+@pytest.mark.parametrize("kind", ("f32", "bf16"))
+def test_borders_among_equal_logits_of_whole_rows(kind):
+    """Equal weights sum exactly: p Z of V equal logits is the border itself."""
+    for V in (500, 1000, 40000, 131072):
+        _, X = _rows(3, V, kind, 1)
+        X.fill_(2.5)
+        X[1, ::2] = -INF
+        u = _u(3, 2)
+        for p in (0.5, 0.25, 0.125):
+            _check(vsd.sample_rows(X, u, 0.7, 0, p, 0.0), X, u, (0.7, 0, p, 0.0))
+
+
+def test_two_calls_at_once():
+    """On two streams, each with its own workspace: the results of one after the other."""
+    sets = []
+    for seed, R, V in ((21, 600, 33000), (22, 300, 65000)):
+        _, X = _rows(R, V, "bf16", seed)
+        X[::7] *= 0.2
+        u = _u(R, seed)
+        sets.append((X, u, (0.9, 0, 0.9, 0.0), vsd.sample_rows(X, u, 0.9, 0, 0.9, 0.0)))
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in sets]
+    for _ in range(3):
+        got = []
+        for s, (X, u, st, _) in zip(streams, sets):
+            with torch.cuda.stream(s):
+                got.append(vsd.sample_rows(X, u, *st))
+        torch.cuda.synchronize()
+        for r, (_, _, _, want) in zip(got, sets):
+            assert all(torch.equal(a, b) for a, b in zip(r[:3], want[:3]))
+
+
 def test_a_row_alone_and_among_others():
     """The same results whatever the number of rows, their stride and the call."""
     buf, X = _rows(700, 3001, "bf16", 10)

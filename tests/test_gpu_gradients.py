@@ -105,6 +105,22 @@ def test_a_norm_that_is_not_finite_changes_nothing(bad):
     assert all(torch.equal(a.nan_to_num(77.0), b.nan_to_num(77.0)) for a, b in zip(out, before))
 
 
+def test_a_gradient_named_twice():
+    t = torch.randn(1000, device=DEV)
+    assert abs(float(vsd.grad_norm([t, t])) - math.sqrt(2) * _norm([t])) <= 1e-6 * _norm([t])
+    keep = t.clone()
+    with pytest.raises(vsd.VsdError, match="overlap"):
+        vsd.clip_gradients([t, t], 0.1)
+    with pytest.raises(vsd.VsdError, match="overlap"):
+        vsd.clip_gradients([t[:600], t[500:]], 0.1)
+    assert torch.equal(t, keep)
+    vsd.clip_gradients([t[:500], t[500:]], 0.1)
+    assert abs(_norm([t]) - 0.1) < 1e-6
+    out = [torch.empty_like(t), torch.empty_like(t)]
+    vsd.clip_gradients([t, t], 0.05, out=out)       # read twice, written apart
+    assert torch.equal(out[0], out[1])
+
+
 def test_extreme_magnitudes():
     big = torch.full((4096,), 3e38, device=DEV)
     assert math.isinf(float(vsd.grad_norm([big]))) and float(vsd.clip_gradients([big], math.inf).scale) == 1.0
