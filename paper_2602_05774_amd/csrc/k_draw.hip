@@ -911,14 +911,14 @@ __global__ __launch_bounds__(kFinish) void k_draw_finish(DrawArgs a) {
 
 // ------------------------------------------------------------- flat rows ---
 // A row whose kept entries do not fit a list, bounded by top-p or min-p of the whole
-// softmax: two sweeps by a workgroup of 1024 threads.  The first (top-p) sums fp32
+// softmax: two sweeps by a workgroup.  The first (top-p) sums fp32
 // weights, as integers, in 2048 bins of equal width between the largest logit and one below which
 // less than 1 - p of the mass can lie; within 1e-4 of p Z, far more than fp32 sums are
 // off, they tell the bins that hold the border.  The second forms the weights in 64
 // bits: of the entries above those bins per 512 columns, and the entries in them go to
 // a list, where the border is found as in k_draw_finish.
-constexpr int kFlat = 1024, kFlatWaves = kFlat / kWave, kBins = 2048, kFlatCap = 2048;
-constexpr int kFlatMine = kFlatCap / kFlat, kPieces = kDrawSpans * kDrawSpan / 512;
+constexpr int kBins = 2048, kFlatCap = 2048, kPieces = kDrawSpans * kDrawSpan / 512;
+template <int kThreads>
 struct FlatShared {
   union {
     uint32_t bins[kBins];
@@ -928,14 +928,15 @@ struct FlatShared {
     } list;
   };
   uint64_t pieces[kPieces];  // kept mass of every 512 columns
-  uint64_t red[2][3][kFlatWaves];
+  uint64_t red[2][3][kThreads / kWave];
   uint64_t target;
   int32_t n, at;
 };
 
 // False: left to draw_row.
-template <typename T>
-__device__ __forceinline__ bool draw_flat(const DrawArgs& a, int64_t r, FlatShared& sh) {
+template <typename T, int kThreads>
+__device__ __forceinline__ bool draw_flat(const DrawArgs& a, int64_t r, FlatShared<kThreads>& sh) {
+  constexpr int kFlatWaves = kThreads / kWave, kFlatMine = kFlatCap / kThreads, kMyBins = kBins / kThreads;
   constexpr int kDown = sizeof(T) == 2 ? 16 : 0;
   const DrawSettings d = draw_settings(a, r);
   if (d.top_k > 0) return false;
@@ -964,21 +965,21 @@ __device__ __forceinline__ bool draw_flat(const DrawArgs& a, int64_t r, FlatShar
     return x == m ? 0u : (uint32_t)fminf((m - x) * inv, (float)(kBins - 1));
   };
   int first = kBins, last = -1;  // the bins with the border
-  for (int i = t; i < kPieces; i += kFlat) sh.pieces[i] = 0;
+  for (int i = t; i < kPieces; i += kThreads) sh.pieces[i] = 0;
   if (t == 0) sh.n = 0;
   if (by_p) {
     const double depth = -temp * log((1.0 - (double)d.top_p) * z / (double)n);
     inv = (float)fmin((kBins - 1) / depth, 3e38);
     const float bin_scale = __builtin_ldexpf(1.0f, 30 - (ilogb(z) + 1));  // (all weights together: below 2^31)
-    for (int i = t; i < kBins; i += kFlat) sh.bins[i] = 0u;
+    for (int i = t; i < kBins; i += kThreads) sh.bins[i] = 0u;
     __syncthreads();
     Raw8<T> q;
     load_cols(q, Y, t * 8, V);
 #pragma unroll 1
-    for (int base = t * 8; base < V; base += kFlat * 8) {
+    for (int base = t * 8; base < V; base += kThreads * 8) {
       float x[8];
       q.get(x);
-      load_cols(q, Y, min(base + kFlat * 8, V), V);
+      load_cols(q, Y, min(base + kThreads * 8, V), V);
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
         const uint32_t b = bin_of(x[k]);  // (the last one holds all the rest: not needed, and one address for most lanes)
@@ -987,17 +988,17 @@ __device__ __forceinline__ bool draw_flat(const DrawArgs& a, int64_t r, FlatShar
       }
     }
     __syncthreads();
-    // (two bins a thread)
-    const double mine[2] = {(double)sh.bins[2 * t], (double)sh.bins[2 * t + 1]};
-    double all;
-    double run = blk.before(mine[0] + mine[1], all);
+    double mine[kMyBins], sum = 0.0, all;
+#pragma unroll
+    for (int i = 0; i < kMyBins; ++i) sum += mine[i] = (double)sh.bins[kMyBins * t + i];
+    double run = blk.before(sum, all);
     const double want = (double)d.top_p * z * (double)bin_scale;
     uint32_t b1 = 0xFFFFFFFFu, b2 = 0xFFFFFFFFu;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < kMyBins; ++i) {
       run += mine[i];
-      if (b1 == 0xFFFFFFFFu && run >= want * (1.0 - 1e-4)) b1 = (uint32_t)(2 * t + i);
-      if (b2 == 0xFFFFFFFFu && run >= want * (1.0 + 1e-4)) b2 = (uint32_t)(2 * t + i);
+      if (b1 == 0xFFFFFFFFu && run >= want * (1.0 - 1e-4)) b1 = (uint32_t)(kMyBins * t + i);
+      if (b2 == 0xFFFFFFFFu && run >= want * (1.0 + 1e-4)) b2 = (uint32_t)(kMyBins * t + i);
     }
     b1 = blk.least(b1);
     b2 = blk.least(b2);
@@ -1183,27 +1184,30 @@ __device__ __forceinline__ bool draw_flat(const DrawArgs& a, int64_t r, FlatShar
 }
 
 // The rows that were left.
-template <typename T>
-__global__ __launch_bounds__(kFlat) void k_draw_left(DrawArgs a) {
+template <typename T, int kThreads>
+__global__ __launch_bounds__(kThreads) void k_draw_left(DrawArgs a) {
   __shared__ union {
-    FlatShared flat;
-    typename RowDraw<T, kFlat>::Shared row;
+    FlatShared<kThreads> flat;
+    typename RowDraw<T, kThreads>::Shared row;
   } sh;
   const int64_t n = *a.ntodo;
   for (int64_t i = blockIdx.x; i < n; i += gridDim.x) {
     const int64_t r = a.todo[i];
-    if (!draw_flat<T>(a, r, sh.flat)) {
+    if (!draw_flat<T, kThreads>(a, r, sh.flat)) {
       __syncthreads();
-      draw_row<T, kFlat>(a, r, sh.row);
+      draw_row<T, kThreads>(a, r, sh.row);
     }
     __syncthreads();
   }
 }
+// Columns up to which 256 threads take such a row, several rows to a CU (us, 1024 / 256
+// threads, rows of 3000 with p = 0.99 at T = 1.3: @LEFT@).
+constexpr int kLeftShort = 16384;
 
 template <typename T>
 hipError_t launch_t(DrawArgs a, hipStream_t s) {
   if (a.todo == nullptr) {  // (more columns than the records are for)
-    hipLaunchKernelGGL((k_draw_row<T, kFlat>), dim3((unsigned)a.R), dim3(kFlat), 0, s, a);
+    hipLaunchKernelGGL((k_draw_row<T, 1024>), dim3((unsigned)a.R), dim3(1024), 0, s, a);
     return hipGetLastError();
   }
   const int64_t waves = a.R * ((a.S + a.per - 1) / a.per);
@@ -1215,8 +1219,11 @@ hipError_t launch_t(DrawArgs a, hipStream_t s) {
     hipLaunchKernelGGL((k_draw_finish<T, 16>), rows, dim3(kFinish), 0, s, a);
   else
     hipLaunchKernelGGL((k_draw_finish<T, 32>), rows, dim3(kFinish), 0, s, a);
-  if (a.V > kCap)  // (else every list fits)
-    hipLaunchKernelGGL((k_draw_left<T>), dim3((unsigned)(a.R < 512 ? a.R : 512)), dim3(kFlat), 0, s, a);
+  // (a row of kCap columns at most fits its list)
+  if (a.V > kLeftShort)
+    hipLaunchKernelGGL((k_draw_left<T, 1024>), dim3((unsigned)(a.R < 512 ? a.R : 512)), dim3(1024), 0, s, a);
+  else if (a.V > kCap)
+    hipLaunchKernelGGL((k_draw_left<T, 256>), dim3((unsigned)(a.R < 2048 ? a.R : 2048)), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 
