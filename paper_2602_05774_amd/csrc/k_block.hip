@@ -95,7 +95,9 @@ __global__ __launch_bounds__(kWave) void k_block_product(BlockArgs a) {
 // in flight, and their sums meet in LDS in the wavefronts' order.  Four lanes read 64
 // consecutive bytes of a row (a value's place in the sum is free, so the lanes of a
 // row take neighbouring 16-byte chunks): with the 32 x 32 instructions and 16 bytes of
-// 64 rows a load, addresses bounded it (us, that / this: @FEW@).
+// 64 rows a load the chunks of a line were fetched by four loads.  Loads return in
+// order, so a's (from L2) are asked for before b's next block (from HBM): the other way
+// round 48 rows of 32 003 x 2048 took 36 us instead of 29.
 // b's rows are the products' rows (registers) and a's their columns (lanes), so that
 // a's scales are one load a block and b's, of 128 rows, one for all.
 template <typename O, bool EXACT, int kGroup, int kTiles, int kWaves>
@@ -146,7 +148,6 @@ __global__ __launch_bounds__(kWaves * kWave) void k_block_few(BlockArgs a) {
       x[t] = load(pa[t] + j * 128);
       s[t] = sa[t][j * a.ldsa];
     }
-    // (loads return in order: b's next block, from HBM, is asked for after a's, from L2)
     __builtin_amdgcn_sched_barrier(0);
     const int64_t ahead = min(j + kWaves, end - 1) * 128;
     next[0] = load(pb[0] + ahead);

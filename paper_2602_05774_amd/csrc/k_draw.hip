@@ -11,8 +11,8 @@
 //    maxima; the largest value such that the maxima from it on already weigh p Z;
 //    min-p's own), the groups that reach it read again, their entries listed in LDS
 //    in index order, and the borders of top-k and top-p found bit by bit.
-// k_draw_left takes the rows whose lists do not fit: flat ones by draw_flat, others (k in
-// the thousands, long runs of equal logits) by draw_row, which also takes rows of more
+// k_draw_left takes the rows whose lists do not fit: flat ones by draw_flat, others (k
+// above 2048, long runs of equal logits) by draw_row, which also takes rows of more
 // than 262 144 columns (k_draw_row): one workgroup per row, sweeping it several times: the largest entry; the
 // sum of the weights, which sets their integer scale; for top-k and top-p the entry
 // where the count or the mass reaches its target, 8 bits of its value a sweep from
@@ -423,10 +423,13 @@ __global__ __launch_bounds__(256) void k_draw_sweep(DrawArgs a) {
 
 // ----------------------------------------------------------------- finish ---
 constexpr int kFinish = 256, kFinishWaves = kFinish / kWave;
-constexpr int kCap = 512;                             // listed entries
+// Listed entries.  Rows of 513 to 1024 columns, whose few groups bound little, are listed
+// whole (us, 512 / 1024: 8192 rows of 1000 at T = 1.3, p = 0.99 548 / 137; 65 536 of 500
+// 698 / 835).
+constexpr int kCap = 512, kCapShort = 1024;
 constexpr int kGroups = kDrawSpans * 16;
 constexpr double kListScale = 4503599627370496.0;     // 2^52: a list's weights sum to at most 2^61
-static_assert(kCap <= 1024 && kGroups <= 65536 && kDrawSpans == 2 * kWave, "");
+static_assert(kCapShort <= 1024 && kGroups <= 65536 && kDrawSpans == 2 * kWave, "");
 
 template <int CTRL>
 __device__ __forceinline__ uint64_t dpp_u64(uint64_t u) {
@@ -551,6 +554,7 @@ struct Block {
 };
 
 // A row's list: its columns in order, and the groups that they lie in.
+template <int kCap>
 struct FinishShared {
   int32_t col[kCap];
   uint16_t groups[kGroups];
@@ -571,15 +575,16 @@ __device__ __forceinline__ uint32_t wave_largest(uint32_t lo, uint32_t hi, F&& r
 
 // One row by one wavefront (no barrier: what bounds it is how long the chain of its
 // instructions takes); kPer groups a lane.  A workgroup of four wavefronts a row, its
-// sums through LDS, took 24 us for 8 rows of 128 256 and 119 for 4096: @FINISH@.
-template <typename T, int kPer>
+// sums through LDS, took 24 us for 8 rows of 128 256 (k = 50, p = 0.9) and 119 for 4096 (p =
+// 0.95); this 19 and 73.
+template <typename T, int kPer, int kCap>
 __global__ __launch_bounds__(kFinish) void k_draw_finish(DrawArgs a) {
   constexpr int kDown = sizeof(T) == 2 ? 16 : 0;  // (bf16: 16 bits of order)
-  __shared__ FinishShared all_rows[kFinishWaves];
+  __shared__ FinishShared<kCap> all_rows[kFinishWaves];
   const int lane = threadIdx.x & 63;
   const int64_t r = (int64_t)blockIdx.x * kFinishWaves + wave_id();
   if (r >= a.R) return;
-  FinishShared& sh = all_rows[wave_id()];
+  FinishShared<kCap>& sh = all_rows[wave_id()];
   const T* Y = static_cast<const T*>(a.Y) + r * a.ld;
   const DrawSettings d = draw_settings(a, r);
   if (!draw_valid(d)) {
@@ -910,11 +915,11 @@ __global__ __launch_bounds__(kFinish) void k_draw_finish(DrawArgs a) {
 }
 
 // ------------------------------------------------------------- flat rows ---
-// A row whose kept entries do not fit a list, bounded by top-p or min-p of the whole
-// softmax: two sweeps by a workgroup.  The first (top-p) sums fp32
+// A row whose kept entries do not fit a wavefront's list: two sweeps by a workgroup.  The first (top-p) sums fp32
 // weights, as integers, in 2048 bins of equal width between the largest logit and one below which
 // less than 1 - p of the mass can lie; within 1e-4 of p Z, far more than fp32 sums are
-// off, they tell the bins that hold the border.  The second forms the weights in 64
+// off, they tell the bins that hold the border.  (Top-k up to 2048: counts, and the
+// bins of the first k entries.)  The second forms the weights in 64
 // bits: of the entries above those bins per 512 columns, and the entries in them go to
 // a list, where the border is found as in k_draw_finish.
 constexpr int kBins = 2048, kFlatCap = 2048, kPieces = kDrawSpans * kDrawSpan / 512;
@@ -939,7 +944,6 @@ __device__ __forceinline__ bool draw_flat(const DrawArgs& a, int64_t r, FlatShar
   constexpr int kFlatWaves = kThreads / kWave, kFlatMine = kFlatCap / kThreads, kMyBins = kBins / kThreads;
   constexpr int kDown = sizeof(T) == 2 ? 16 : 0;
   const DrawSettings d = draw_settings(a, r);
-  if (d.top_k > 0) return false;
   Block<kFlatWaves> blk{sh.red, 0};
   const int t = threadIdx.x, lane = t & 63, wave = wave_id(), V = a.V;
   const T* Y = static_cast<const T*>(a.Y) + r * a.ld;
@@ -952,9 +956,10 @@ __device__ __forceinline__ bool draw_flat(const DrawArgs& a, int64_t r, FlatShar
   const float m = draw_value(hi);
   const double c = 1.4426950408889634074 / (double)d.temp, temp = d.temp;
   const uint64_t n = blk.sum(span ? (uint64_t)a.span_count[r * a.S + t] : 0);
-  const bool by_p = d.top_p < 1.0f;
-  double z = (double)n;
-  if (by_p) (void)blk.before(span && span_max > -INFINITY ? a.span_sum[r * a.S + t] * draw_weight(span_max, m, c) : 0.0, z);
+  const bool by_p = d.top_p < 1.0f, by_k = d.top_k > 0;
+  if (by_k && ((uint64_t)d.top_k >= n || d.top_k > kFlatCap)) return false;
+  double z = by_k ? (double)kFlatCap : (double)n;  // (at least the mass of what may be kept: sets the integers' scale)
+  if (by_p && !by_k) (void)blk.before(span && span_max > -INFINITY ? a.span_sum[r * a.S + t] * draw_weight(span_max, m, c) : 0.0, z);
   const int e = 62 - (ilogb(z) + 1);
   const double scale = __builtin_ldexp(1.0, e), min_p = d.min_p;
   const double goal = __builtin_ceil((double)d.top_p * z * scale);
@@ -964,13 +969,27 @@ __device__ __forceinline__ bool draw_flat(const DrawArgs& a, int64_t r, FlatShar
   auto bin_of = [&](float x) {  // (the largest's difference to itself is 0 also where it is infinite)
     return x == m ? 0u : (uint32_t)fminf((m - x) * inv, (float)(kBins - 1));
   };
-  int first = kBins, last = -1;  // the bins with the border
+  int first = kBins, last = -1;  // the bins whose entries are listed
   for (int i = t; i < kPieces; i += kThreads) sh.pieces[i] = 0;
   if (t == 0) sh.n = 0;
-  if (by_p) {
-    const double depth = -temp * log((1.0 - (double)d.top_p) * z / (double)n);
+  if (by_p || by_k) {
+    // depth: top-p, as above; top-k, to as far below the least of the groups' maxima as
+    // that lies below the largest logit (a border further down is draw_row's)
+    double depth;
+    if (by_k) {
+      float low = INFINITY;
+      for (int i = t; i < a.S * 16; i += kThreads) {
+        const float g = a.group_max[r * a.S * 16 + i];
+        if (g > -INFINITY) low = fminf(low, g);
+      }
+      uint32_t low_key = draw_order(low), high_key = 0;
+      blk.range(low_key, high_key);
+      depth = fmax(2.0 * ((double)m - (double)draw_value(low_key)), 1e-30);
+    } else {
+      depth = -temp * log((1.0 - (double)d.top_p) * z / (double)n);
+    }
     inv = (float)fmin((kBins - 1) / depth, 3e38);
-    const float bin_scale = __builtin_ldexpf(1.0f, 30 - (ilogb(z) + 1));  // (all weights together: below 2^31)
+    const float bin_scale = by_k ? 1.0f : __builtin_ldexpf(1.0f, 30 - (ilogb(z) + 1));  // (weights together: below 2^31)
     for (int i = t; i < kBins; i += kThreads) sh.bins[i] = 0u;
     __syncthreads();
     Raw8<T> q;
@@ -983,7 +1002,7 @@ __device__ __forceinline__ bool draw_flat(const DrawArgs& a, int64_t r, FlatShar
 #pragma unroll
       for (int k = 0; k < 8; ++k) {
         const uint32_t b = bin_of(x[k]);  // (the last one holds all the rest: not needed, and one address for most lanes)
-        const float w = x[k] == m ? 1.0f : __builtin_amdgcn_exp2f((x[k] - m) * c32);
+        const float w = by_k || x[k] == m ? 1.0f : __builtin_amdgcn_exp2f((x[k] - m) * c32);
         if (b < kBins - 1) atomicAdd(&sh.bins[b], (uint32_t)fmaf(w, bin_scale, 0.5f));
       }
     }
@@ -992,18 +1011,19 @@ __device__ __forceinline__ bool draw_flat(const DrawArgs& a, int64_t r, FlatShar
 #pragma unroll
     for (int i = 0; i < kMyBins; ++i) sum += mine[i] = (double)sh.bins[kMyBins * t + i];
     double run = blk.before(sum, all);
-    const double want = (double)d.top_p * z * (double)bin_scale;
+    // (top-k: every entry from the largest to the bin that completes the k)
+    const double want = by_k ? (double)d.top_k : (double)d.top_p * z * (double)bin_scale;
     uint32_t b1 = 0xFFFFFFFFu, b2 = 0xFFFFFFFFu;
 #pragma unroll
     for (int i = 0; i < kMyBins; ++i) {
       run += mine[i];
-      if (b1 == 0xFFFFFFFFu && run >= want * (1.0 - 1e-4)) b1 = (uint32_t)(kMyBins * t + i);
-      if (b2 == 0xFFFFFFFFu && run >= want * (1.0 + 1e-4)) b2 = (uint32_t)(kMyBins * t + i);
+      if (b1 == 0xFFFFFFFFu && run >= want * (by_k ? 1.0 : 1.0 - 1e-4)) b1 = (uint32_t)(kMyBins * t + i);
+      if (b2 == 0xFFFFFFFFu && run >= want * (by_k ? 1.0 : 1.0 + 1e-4)) b2 = (uint32_t)(kMyBins * t + i);
     }
     b1 = blk.least(b1);
     b2 = blk.least(b2);
     if (b2 >= kBins - 1) return false;
-    first = (int)b1;
+    first = by_k ? 0 : (int)b1;
     last = (int)b2;
   }
   // min-p: entries far below the bound are not weighed
@@ -1030,7 +1050,7 @@ __device__ __forceinline__ bool draw_flat(const DrawArgs& a, int64_t r, FlatShar
 #pragma unroll
     for (int k = 0; k < 8; ++k) {
       bool is_over = x[k] > -INFINITY && x[k] >= bound, is_at = false;
-      if (by_p) {
+      if (by_p || by_k) {
         const int b = (int)bin_of(x[k]);
         is_at = x[k] > -INFINITY && b >= first && b <= last;
         is_over = x[k] > -INFINITY && b < first;
@@ -1073,12 +1093,12 @@ __device__ __forceinline__ bool draw_flat(const DrawArgs& a, int64_t r, FlatShar
   if (listed > kFlatCap) return false;
   uint32_t least = 0;  // the smallest kept key of the list, and the last column with it
   int limit = 0x7FFFFFFF;
-  if (by_p) {
+  if (by_p || by_k) {
     above = blk.sum(above);
     float x[kFlatMine];
     uint32_t key[kFlatMine];
     int col[kFlatMine];
-    uint64_t w[kFlatMine], listed_mass = 0;
+    uint64_t w[kFlatMine];
     bool enough[kFlatMine], in[kFlatMine];
     uint32_t kmin = 0xFFFFFFFFu, kmax = 0;
 #pragma unroll
@@ -1091,39 +1111,56 @@ __device__ __forceinline__ bool draw_flat(const DrawArgs& a, int64_t r, FlatShar
       double v = 0.0;
       w[k] = in[k] ? weigh(x[k], v) : 0;
       enough[k] = v >= min_p;
-      listed_mass += w[k];
       if (in[k]) {
         kmin = min(kmin, key[k]);
         kmax = max(kmax, key[k]);
       }
     }
     blk.range(kmin, kmax);
-    listed_mass = blk.sum(listed_mass);
-    const uint64_t target = (uint64_t)goal;
-    if (above >= target || above + listed_mass < target) return false;  // (the border is elsewhere)
-    const uint64_t need = target - above;
-    auto over = [&](auto&& f) {
+    auto over = [&](auto&& g) {
       uint64_t s = 0;
 #pragma unroll
-      for (int k = 0; k < kFlatMine; ++k) s += in[k] ? f(k) : 0ull;
+      for (int k = 0; k < kFlatMine; ++k) s += in[k] ? g(k) : 0ull;
       return s;
     };
-    least = blk.largest(kmin, kmax, need, [&](uint32_t b) { return over([&](int k) { return key[k] >= b ? w[k] : 0ull; }); });
-    uint64_t s[2] = {over([&](int k) { return key[k] > least ? w[k] : 0ull; }), over([&](int k) { return key[k] == least ? w[k] : 0ull; })};
-    blk.sums(s);
-    double v;
-    const uint64_t each = weigh(draw_value(kDown == 0 || least >= 0x8000u ? least << kDown : least << kDown | 0xFFFFu), v);
-    const uint64_t ties = (need - s[0] + each - 1) / each;
-    if (ties * each < s[1]) {
-      // the columns of the first `ties` of them: as the largest of reversed columns
-      const uint32_t top = (uint32_t)V;
-      limit = (int)(top - blk.largest(0, top, ties, [&](uint32_t b) {
-                      return over([&](int k) { return key[k] == least && top - (uint32_t)col[k] >= b ? 1ull : 0ull; });
-                    }));
+    // keeps the entries above `least` and the first `ties` of that key (of `have`)
+    auto cut = [&](uint64_t ties, uint64_t have) {
+      limit = 0x7FFFFFFF;
+      if (ties < have) {  // their columns: the largest of reversed ones
+        const uint32_t top = (uint32_t)V;
+        limit = (int)(top - blk.largest(0, top, ties, [&](uint32_t b) {
+                        return over([&](int k) { return key[k] == least && top - (uint32_t)col[k] >= b ? 1ull : 0ull; });
+                      }));
+      }
+#pragma unroll
+      for (int k = 0; k < kFlatMine; ++k) in[k] = in[k] && (key[k] > least || (key[k] == least && col[k] <= limit));
+    };
+    if (by_k) {
+      auto count_of = [&](uint32_t b) { return over([&](int k) { return key[k] >= b ? 1ull : 0ull; }); };
+      least = blk.largest(kmin, kmax, d.top_k, count_of);
+      uint64_t s[2] = {count_of(least + 1u), count_of(least)};
+      blk.sums(s);
+      cut((uint64_t)d.top_k - s[0], s[1] - s[0]);
+    }
+    if (by_p) {
+      const uint64_t listed_mass = blk.sum(over([&](int k) { return w[k]; }));
+      const uint64_t target = (uint64_t)(by_k ? __builtin_ceil((double)d.top_p * (double)listed_mass) : goal);
+      if (above >= target || above + listed_mass < target) return false;  // (the border is elsewhere)
+      const uint64_t need = target - above;
+      auto mass_of = [&](uint32_t b) { return over([&](int k) { return key[k] >= b ? w[k] : 0ull; }); };
+      const uint32_t before = least;
+      const int limit_before = limit;
+      least = blk.largest(kmin, kmax, need, mass_of);
+      uint64_t s[2] = {mass_of(least + 1u), mass_of(least)};
+      blk.sums(s);
+      double v;
+      const uint64_t each = weigh(draw_value(kDown == 0 || least >= 0x8000u ? least << kDown : least << kDown | 0xFFFFu), v);
+      cut((need - s[0] + each - 1) / each, (s[1] - s[0]) / each);
+      if (least == before) limit = min(limit, limit_before);
     }
 #pragma unroll
     for (int k = 0; k < kFlatMine; ++k)
-      if (in[k] && enough[k] && (key[k] > least || (key[k] == least && col[k] <= limit))) {
+      if (in[k] && enough[k]) {
         atomicAdd(reinterpret_cast<unsigned long long*>(&sh.pieces[col[k] >> 9]), (unsigned long long)w[k]);
         ++count;
       }
@@ -1149,7 +1186,7 @@ __device__ __forceinline__ bool draw_flat(const DrawArgs& a, int64_t r, FlatShar
   for (int k = 0; k < 8; ++k) {
     w[k] = 0;
     if (!(x[k] > -INFINITY)) continue;
-    if (by_p) {
+    if (by_p || by_k) {
       const int b = (int)bin_of(x[k]);
       const uint32_t key = key_of(x[k]);
       if (b > last || (b >= first && !(key > least || (key == least && base + k <= limit)))) continue;
@@ -1201,7 +1238,7 @@ __global__ __launch_bounds__(kThreads) void k_draw_left(DrawArgs a) {
   }
 }
 // Columns up to which 256 threads take such a row, several rows to a CU (us, 1024 / 256
-// threads, rows of 3000 with p = 0.99 at T = 1.3: @LEFT@).
+// threads, p = 0.99 at T = 1.3: 8192 rows of 3000 1070 / 571, 4000 of 12 000 640 / 383).
 constexpr int kLeftShort = 16384;
 
 template <typename T>
@@ -1213,16 +1250,18 @@ hipError_t launch_t(DrawArgs a, hipStream_t s) {
   const int64_t waves = a.R * ((a.S + a.per - 1) / a.per);
   hipLaunchKernelGGL((k_draw_sweep<T>), dim3((unsigned)((waves + 3) / 4)), dim3(256), 0, s, a);
   const dim3 rows((unsigned)((a.R + kFinishWaves - 1) / kFinishWaves));
-  if (a.S <= 16)
-    hipLaunchKernelGGL((k_draw_finish<T, 4>), rows, dim3(kFinish), 0, s, a);
+  if (a.V > kCap && a.V <= kCapShort)
+    hipLaunchKernelGGL((k_draw_finish<T, 4, kCapShort>), rows, dim3(kFinish), 0, s, a);
+  else if (a.S <= 16)
+    hipLaunchKernelGGL((k_draw_finish<T, 4, kCap>), rows, dim3(kFinish), 0, s, a);
   else if (a.S <= 64)
-    hipLaunchKernelGGL((k_draw_finish<T, 16>), rows, dim3(kFinish), 0, s, a);
+    hipLaunchKernelGGL((k_draw_finish<T, 16, kCap>), rows, dim3(kFinish), 0, s, a);
   else
-    hipLaunchKernelGGL((k_draw_finish<T, 32>), rows, dim3(kFinish), 0, s, a);
-  // (a row of kCap columns at most fits its list)
+    hipLaunchKernelGGL((k_draw_finish<T, 32, kCap>), rows, dim3(kFinish), 0, s, a);
+  // (a row of kCapShort columns at most fits its list)
   if (a.V > kLeftShort)
     hipLaunchKernelGGL((k_draw_left<T, 1024>), dim3((unsigned)(a.R < 512 ? a.R : 512)), dim3(1024), 0, s, a);
-  else if (a.V > kCap)
+  else if (a.V > kCapShort)
     hipLaunchKernelGGL((k_draw_left<T, 256>), dim3((unsigned)(a.R < 2048 ? a.R : 2048)), dim3(256), 0, s, a);
   return hipGetLastError();
 }
