@@ -284,8 +284,9 @@
  *   128) x 128 columns:
  *     x[i][j] = scales[j / 128][i / group] values[i][j].
  *   Row i of the values starts at byte i*ld, ld a multiple of 128 >= cols; the
- *   bytes past cols are zero.  scales[b] starts at element b*scale_ld, scale_ld
- *   >= ceil(rows / group).
+ *   bytes from cols to the end of its last block are zero, those behind it (other
+ *   data's, where ld is larger) are neither read nor written.  scales[b] starts at
+ *   element b*scale_ld, scale_ld >= ceil(rows / group).
  *   Quantising: scale = max(amax / 448, 2^-126), amax the block's largest
  *   magnitude, and value = e4m3(x / scale): the fp32 quotient, to the nearest
  *   value, ties to the even one.  A block with a NaN or an infinity has the
@@ -716,7 +717,7 @@ vsd_status vsd_draw_workspace_bytes(const vsd_rows* rows, size_t* bytes);
 
 /* Quantises x [rows, cols] (dtype, row stride ld >= cols elements, any alignment
  * of its elements), or, with transpose, x^T: out->rows x out->cols is then cols x
- * rows.  Writes all of out's rows up to ld (zeros past cols) and all scales. */
+ * rows.  Writes all of out's blocks (zeros past cols) and all scales. */
 vsd_status vsd_quantize_blocks(const void* x, int64_t rows, int64_t cols, int64_t ld, int32_t dtype, int32_t transpose,
                                const vsd_blocks* out, void* hip_stream);
 

@@ -21,7 +21,7 @@ BLOCK = 128
 class BlockMatrix(NamedTuple):
     """A matrix [rows, cols] of 8-bit values with a scale for every block of 1 or 128
     rows x 128 columns."""
-    values: torch.Tensor  # [rows, ld] float8_e4m3fn, ld a multiple of 128 >= cols, zeros past cols
+    values: torch.Tensor  # [rows, ld] float8_e4m3fn, ld a multiple of 128 >= cols, zeros past cols in the last block
     scales: torch.Tensor  # [ceil(cols / 128), rows] f32, or [ceil(cols / 128), ceil(rows / 128)]
     cols: int
 

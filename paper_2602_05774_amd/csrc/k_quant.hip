@@ -120,13 +120,6 @@ __global__ __launch_bounds__(kThreads) void k_quantize(QuantArgs a) {
   }
 }
 
-// Zeros in whole blocks of padding columns (a stride past the last block).
-__global__ __launch_bounds__(kThreads) void k_quant_pad(uint8_t* values, int64_t rows, int64_t from, int64_t ld) {
-  const int64_t per = (ld - from) / 16, n = rows * per;
-  for (int64_t i = (int64_t)blockIdx.x * kThreads + threadIdx.x; i < n; i += (int64_t)gridDim.x * kThreads)
-    *reinterpret_cast<uint4*>(values + i / per * ld + from + i % per * 16) = make_uint4(0, 0, 0, 0);
-}
-
 template <typename T, bool ALIGNED>
 hipError_t launch_t(const QuantArgs& a, int group, bool trans, hipStream_t s) {
   const dim3 grid((unsigned)a.tiles), block(kThreads);
@@ -140,12 +133,6 @@ hipError_t launch_t(const QuantArgs& a, int group, bool trans, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_quantize(const QuantArgs& a, bool bf16, int group, bool trans, hipStream_t s) {
-  const int64_t done = ((trans ? a.rows : a.cols) + 127) / 128 * 128;
-  if (done < a.out_ld) {
-    hipLaunchKernelGGL(k_quant_pad, dim3(1024), dim3(kThreads), 0, s, a.values, trans ? a.cols : a.rows, done, a.out_ld);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-  }
   const bool aligned = (reinterpret_cast<uintptr_t>(a.x) | (uint64_t)(a.ld * (bf16 ? 2 : 4))) % 16 == 0;
   if (aligned) return bf16 ? launch_t<bf16_t, true>(a, group, trans, s) : launch_t<float, true>(a, group, trans, s);
   return bf16 ? launch_t<bf16_t, false>(a, group, trans, s) : launch_t<float, false>(a, group, trans, s);

@@ -25,7 +25,7 @@ def _check_quant(q, x, group, trans):
     val, sc = ob.quantize(x.float().cpu().numpy(), group, trans)
     assert q.cols == val.shape[1] and tuple(q.scales.shape) == sc.shape
     assert np.array_equal(q.scales.cpu().numpy(), sc, equal_nan=True)
-    got = q.values.float().cpu().numpy()
+    got = q.values[:, :-(-q.cols // 128) * 128].float().cpu().numpy()  # whole blocks
     assert np.all(got[:, q.cols:] == 0) and not np.signbit(got[:, q.cols:]).any()
     finite = np.isfinite(ob.dense(np.ones_like(val), sc, q.cols))
     assert np.array_equal(got[:, :q.cols][finite], val[finite])
@@ -57,18 +57,34 @@ def test_quantize_extremes(group, trans):
 
 @pytest.mark.parametrize("trans", (False, True))
 def test_quantize_strides(trans):
-    """A range of a wider buffer, from an address of no alignment; a result with padding."""
+    """A range of a wider buffer, from an address of no alignment; a result inside wider
+    buffers whose rest stays (their last rows end with its last block)."""
     wide = _source(200, 517, "bf16", 2)
     x = wide[1:150, 3:400]
     rows, cols = x.shape[::-1] if trans else x.shape
     nb = -(-cols // 128)
     for group in (1, 128):
         _check_quant(vsd.quantize_blocks(x, group, trans), x, group, trans)
-        out = vsd.BlockMatrix(torch.full((rows + 2, nb * 128 + 384), 7.0, device=DEV).to(torch.float8_e4m3fn)[1:-1, :nb * 128 + 256],
-                              torch.full((nb, -(-rows // group) + 5), -1.0, device=DEV)[:, :-(-rows // group)], cols)
-        res = vsd.quantize_blocks(x, group, trans, out=out)
-        assert res is out
-        _check_quant(res, x, group, trans)
+        groups = -(-rows // group)
+        for at in (128, 384):  # the first blocks of wider rows, and the end of theirs
+            val = torch.full((rows + 2, nb * 128 + 384), 7.0, device=DEV).to(torch.float8_e4m3fn)
+            sc = torch.full((nb, groups + 5), -1.0, device=DEV)
+            out = vsd.BlockMatrix(val[1:-1, at:], sc[:, :groups], cols)
+            res = vsd.quantize_blocks(x, group, trans, out=out)
+            assert res is out
+            _check_quant(res, x, group, trans)
+            rest = torch.ones_like(val, dtype=torch.bool)
+            rest[1:-1, at:at + nb * 128] = False
+            assert (val.float()[rest] == 7).all() and (sc[:, groups:] == -1).all()
+
+
+def test_quantize_one_row_of_a_range():
+    """One row whose buffer is wider than its blocks, by less than one."""
+    x = _source(1, 100, "f32", 4)
+    val = torch.full((240,), 7.0, device=DEV).to(torch.float8_e4m3fn)
+    out = vsd.BlockMatrix(val[:200].view(1, 200), torch.empty(1, 1, device=DEV), 100)
+    _check_quant(vsd.quantize_blocks(x, out=out), x, 1, False)
+    assert (val[128:].float() == 7).all()
 
 
 def test_quantize_every_value():
