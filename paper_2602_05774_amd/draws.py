@@ -5,6 +5,7 @@ the current HIP stream of the tensors' device.
 """
 import ctypes
 import functools
+import operator
 from typing import NamedTuple
 
 import torch
@@ -64,10 +65,11 @@ def sample_rows(Y, u, temp_target=1.0, top_k=0, top_p=1.0, min_p=0.0, workspace=
     k, row_k = _setting("top_k", top_k, torch.int32, R, dev)
     p, row_p = _setting("top_p", top_p, torch.float32, R, dev)
     m, row_m = _setting("min_p", min_p, torch.float32, R, dev)
+    k = operator.index(k)
     if k < 0:
         raise ValueError(f"top_k={k} must be >= 0")
     # (more than a row has is all of them: larger numbers than 32 bits hold are too)
-    draw = _lib.VsdDraw(t, min(int(k), 0x7FFFFFFF), p, m, row_t, row_k, row_p, row_m)
+    draw = _lib.VsdDraw(t, min(k, 0x7FFFFFFF), p, m, row_t, row_k, row_p, row_m)
     with _device(dev):
         out = torch.empty(3 * R, dtype=torch.int32, device=dev)
         tok, lp, kept = torch.split_with_sizes(out, (R, R, R))

@@ -35,9 +35,9 @@ _KINDS = {torch.float32: _lib.VSD_F32, torch.bfloat16: _lib.VSD_BF16}
 
 def _fields(name, t, on):
     """VsdTensor's fields of a tensor that lies in one piece, or of [R, C] rows with a stride."""
-    kind = _KINDS.get(t.dtype)
+    kind = _KINDS.get(getattr(t, "dtype", None))
     if kind is None:
-        raise ValueError(f"{name} must be bfloat16 or float32 tensors, got {t.dtype}")
+        raise ValueError(f"{name} must be bfloat16 or float32 tensors, got {getattr(t, 'dtype', t)}")
     if t.get_device() != on:
         raise ValueError(f"{name} must be tensors on one device")
     if t.is_contiguous():
