@@ -428,7 +428,7 @@ constexpr int kFinish = 256, kFinishWaves = kFinish / kWave;
 // 698 / 835).
 constexpr int kCap = 512, kCapShort = 1024;
 constexpr int kGroups = kDrawSpans * 16;
-constexpr double kListScale = 4503599627370496.0;     // 2^52: a list's weights sum to at most 2^61
+constexpr double kListScale = 4503599627370496.0;     // 2^52: a list's weights sum to at most 2^62
 static_assert(kCapShort <= 1024 && kGroups <= 65536 && kDrawSpans == 2 * kWave, "");
 
 template <int CTRL>
@@ -576,7 +576,7 @@ __device__ __forceinline__ uint32_t wave_largest(uint32_t lo, uint32_t hi, F&& r
 // One row by one wavefront (no barrier: what bounds it is how long the chain of its
 // instructions takes); kPer groups a lane.  A workgroup of four wavefronts a row, its
 // sums through LDS, took 24 us for 8 rows of 128 256 (k = 50, p = 0.9) and 119 for 4096 (p =
-// 0.95); this 19 and 73.
+// 0.95); this 19 and 72.
 template <typename T, int kPer, int kCap>
 __global__ __launch_bounds__(kFinish) void k_draw_finish(DrawArgs a) {
   constexpr int kDown = sizeof(T) == 2 ? 16 : 0;  // (bf16: 16 bits of order)
@@ -986,7 +986,7 @@ __device__ __forceinline__ bool draw_flat(const DrawArgs& a, int64_t r, FlatShar
       blk.range(low_key, high_key);
       depth = fmax(2.0 * ((double)m - (double)draw_value(low_key)), 1e-30);
     } else {
-      depth = -temp * log((1.0 - (double)d.top_p) * z / (double)n);
+      depth = fmax(-temp * log((1.0 - (double)d.top_p) * z / (double)n), 1e-30);
     }
     inv = (float)fmin((kBins - 1) / depth, 3e38);
     const float bin_scale = by_k ? 1.0f : __builtin_ldexpf(1.0f, 30 - (ilogb(z) + 1));  // (weights together: below 2^31)
