@@ -7,6 +7,11 @@
 // squares are formed and summed in double precision: fp32 squares would overflow
 // from 1.8e19 on and lose elements below 1e-19 (double FMAs issue at the rate of
 // fp32 ones on this chip, far above what memory feeds).
+//
+// Bytes bound both: of 500 million bf16 elements in 150 tensors the squares run at 4.8
+// TB/s of reads, the scaling at 5.2 of both (us a launch of a third: 69, 129).  Not kept:
+// the scaling from the last chunk back, for what the caches still hold (150), chunks of
+// 16 384 elements and 4096 workgroups (no faster).
 #include "vsd_device.hpp"
 #include "vsd_kernels.hpp"
 
