@@ -34,11 +34,20 @@ __device__ __forceinline__ uint32_t pack4(float a, float b, float c, float d) {
   return (uint32_t)v;
 }
 
+// Eight values from an address of any alignment: the compiler's own wide loads, which
+// take one (rows of odd lengths by single elements: 6144 x 4099 bf16 42 us, so 23).
+template <typename T>
+__device__ __forceinline__ void load8_any(const T* p, float (&v)[8]) {
+  T q[8] __attribute__((aligned(16)));
+  __builtin_memcpy(q, p, sizeof(q));
+  load8(q, v);
+}
+
 // 16 rows x 4 blocks a workgroup (a block's 16 scales are one line), a lane 8 columns.
 // (us, by tiles of 128 x 128 / this: 1 x 4096 bf16 8.1 / 5.2, 6144 x 4096 23.3 / 21.4, 2000
 // x 33 000 54 / 45, 20 000 x 4096 fp32 79 / 70.)
 constexpr int kRowBlocks = 4;
-template <typename T, bool ALIGNED>
+template <typename T>
 __device__ __forceinline__ void row_blocks(const QuantArgs& a, int64_t r, int b0) {
   const int tc = threadIdx.x & 15;
   const T* X = static_cast<const T*>(a.x) + r * a.ld;
@@ -46,8 +55,8 @@ __device__ __forceinline__ void row_blocks(const QuantArgs& a, int64_t r, int b0
 #pragma unroll
   for (int b = 0; b < kRowBlocks; ++b) {
     const int64_t c = (int64_t)(b0 + b) * 128 + tc * 8;
-    if (ALIGNED && r < a.rows && c + 8 <= a.cols) {
-      load8(X + c, x[b]);
+    if (r < a.rows && c + 8 <= a.cols) {
+      load8_any(X + c, x[b]);
     } else {
 #pragma unroll
       for (int k = 0; k < 8; ++k) x[b][k] = r < a.rows && c + k < a.cols ? load1(X + c + k) : 0.0f;
@@ -72,19 +81,18 @@ __device__ __forceinline__ void row_blocks(const QuantArgs& a, int64_t r, int b0
         make_uint2(pack4(q[0], q[1], q[2], q[3]), pack4(q[4], q[5], q[6], q[7]));
   }
 }
-template <typename T, bool ALIGNED>
+template <typename T>
 __global__ __launch_bounds__(kThreads) void k_quantize_rows(QuantArgs a) {
   const int groups = (a.col_tiles + kRowBlocks - 1) / kRowBlocks;
   const int64_t n = (a.rows + 15) / 16 * groups;
   for (int64_t i = blockIdx.x; i < n; i += gridDim.x) {
     const int64_t q = i / groups;
-    row_blocks<T, ALIGNED>(a, q * 16 + (threadIdx.x >> 4), (int)(i - q * groups) * kRowBlocks);
+    row_blocks<T>(a, q * 16 + (threadIdx.x >> 4), (int)(i - q * groups) * kRowBlocks);
   }
 }
 
-// TRANS: the result's rows are x's columns.  ALIGNED: x's rows start at multiples of
-// 16 bytes.
-template <typename T, int kGroup, bool TRANS, bool ALIGNED>
+// TRANS: the result's rows are x's columns.
+template <typename T, int kGroup, bool TRANS>
 __global__ __launch_bounds__(kThreads) void k_quantize(QuantArgs a) {
   static_assert(kGroup == 128 || TRANS, "rows' blocks are k_quantize_rows's");
   __shared__ uint32_t part[16][128];
@@ -96,8 +104,8 @@ __global__ __launch_bounds__(kThreads) void k_quantize(QuantArgs a) {
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const int64_t r = row0 + tr * 8 + i, c = col0 + tc * 8;
-    if (ALIGNED && r < a.rows && c + 8 <= a.cols) {
-      load8(X + r * a.ld + c, x[i]);
+    if (r < a.rows && c + 8 <= a.cols) {
+      load8_any(X + r * a.ld + c, x[i]);
     } else {
 #pragma unroll
       for (int k = 0; k < 8; ++k) x[i][k] = r < a.rows && c + k < a.cols ? load1(X + r * a.ld + c + k) : 0.0f;
@@ -172,25 +180,23 @@ __global__ __launch_bounds__(kThreads) void k_quantize(QuantArgs a) {
   }
 }
 
-template <typename T, bool ALIGNED>
+template <typename T>
 hipError_t launch_t(const QuantArgs& a, int group, bool trans, hipStream_t s) {
   const dim3 grid((unsigned)a.tiles), block(kThreads);
   if (group == 1 && !trans) {
     const int64_t n = (a.rows + 15) / 16 * ((a.col_tiles + kRowBlocks - 1) / kRowBlocks);
-    hipLaunchKernelGGL((k_quantize_rows<T, ALIGNED>), dim3((unsigned)(n < 1 << 22 ? n : 1 << 22)), block, 0, s, a);
+    hipLaunchKernelGGL((k_quantize_rows<T>), dim3((unsigned)(n < 1 << 22 ? n : 1 << 22)), block, 0, s, a);
   }
-  if (group == 1 && trans) hipLaunchKernelGGL((k_quantize<T, 1, true, ALIGNED>), grid, block, 0, s, a);
-  if (group != 1 && !trans) hipLaunchKernelGGL((k_quantize<T, 128, false, ALIGNED>), grid, block, 0, s, a);
-  if (group != 1 && trans) hipLaunchKernelGGL((k_quantize<T, 128, true, ALIGNED>), grid, block, 0, s, a);
+  if (group == 1 && trans) hipLaunchKernelGGL((k_quantize<T, 1, true>), grid, block, 0, s, a);
+  if (group != 1 && !trans) hipLaunchKernelGGL((k_quantize<T, 128, false>), grid, block, 0, s, a);
+  if (group != 1 && trans) hipLaunchKernelGGL((k_quantize<T, 128, true>), grid, block, 0, s, a);
   return hipGetLastError();
 }
 
 }  // namespace
 
 hipError_t launch_quantize(const QuantArgs& a, bool bf16, int group, bool trans, hipStream_t s) {
-  const bool aligned = (reinterpret_cast<uintptr_t>(a.x) | (uint64_t)(a.ld * (bf16 ? 2 : 4))) % 16 == 0;
-  if (aligned) return bf16 ? launch_t<bf16_t, true>(a, group, trans, s) : launch_t<float, true>(a, group, trans, s);
-  return bf16 ? launch_t<bf16_t, false>(a, group, trans, s) : launch_t<float, false>(a, group, trans, s);
+  return bf16 ? launch_t<bf16_t>(a, group, trans, s) : launch_t<float>(a, group, trans, s);
 }
 
 }  // namespace vsd
