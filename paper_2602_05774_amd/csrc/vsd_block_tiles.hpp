@@ -10,9 +10,9 @@
 // tile's fp32 sums, times its scales, by the vector units while the matrix cores form
 // the other half of the phase's products; the scales ride through LDS, loaded two
 // stages ahead with the operands.
-// 6144 x 128 256 x 4096 to bf16: 3.12 ms, 2.07 PFLOP/s; a stage takes 3900 cycles, 2048 of
-// them matrix instructions (without the joins 2914 us, without loads 2795, without stores
-// 2894).  32 000 x 2048 x 9001 to fp32: 1.25 ms, 0.94 PFLOP/s, the VALU shared by the
+// 6144 x 128 256 x 4096 to bf16: 3.08 ms, 2.1 PFLOP/s; a stage takes 3900 cycles, 2048 of
+// them matrix instructions (of 3281 us an earlier form took 2914 without the joins, 2795
+// without loads, 2894 without stores).  32 000 x 2048 x 9001 to fp32: 1.25 ms, 0.94 PFLOP/s, the VALU shared by the
 // conversions to bf16 and the other group's joins.
 //   phase  reads   refills             multiplies   waits for
 //   1      U0(t)   U1(t+1)             U0 V0
@@ -86,6 +86,18 @@ __device__ __forceinline__ void tile_of(int pid, int nrt, int ncol, int& rt, int
   const int first = g * kGroupRows, rows = min(nrt - first, kGroupRows);
   rt = first + in % rows;
   col = in / rows;
+}
+
+// A lane's x of the other lane (by CTRL) and its y change places: where `odd`, x becomes
+// the other's y, else y the other's x.
+template <int CTRL>
+__device__ __forceinline__ void quad_swap(uint32_t (&x)[4], uint32_t (&y)[4], bool odd) {
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const uint32_t got = (uint32_t)dpp_i<CTRL>((int)(odd ? x[w] : y[w]));
+    x[w] = odd ? got : x[w];
+    y[w] = odd ? y[w] : got;
+  }
 }
 
 template <int N>
@@ -268,31 +280,58 @@ __device__ __forceinline__ void tiles(const BlockTileArgs& a, uint8_t* lds) {
       join(h, g, 1, s);
     }
   };
-  // the tile's results: 32 consecutive columns a lane in each half of the columns
+  // The tile's results: 32 consecutive columns a lane in each half of the columns.  Four
+  // lanes change pieces, so that they store 64 consecutive bytes of a row (us, each lane
+  // 16 bytes of its row / this: 16 384 x 5000 x 100 to fp32 167 / 107, to bf16 60 / 48,
+  // 16 384 x 16 384 x 64 to fp32 917 / 404, 6144 x 128 256 x 4096 to bf16 3130 / 3080).
   O* const out = static_cast<O*>(a.out) + (int64_t)blockIdx.y * a.range_stride;
   auto store = [&](int t) {
     int l = lane;
     asm volatile("" : "+v"(l));  // (its addresses are formed here, not kept across the loop)
     const int64_t n = (int64_t)t * kTile + wr * 64 + 32 * (l >> 5);
+    const int q = l & 3;
+    constexpr int kPer = 16 / (int)sizeof(O);  // results of a 16-byte piece
 #pragma unroll
     for (int g = 0; g < 2; ++g) {
-      const int64_t m = m0 + g * 128 + wc * 32 + (l & 31);
-      if (m >= a.M) continue;
-      O* const to = out + m * a.ldo + n;
+      const int64_t m = m0 + g * 128 + wc * 32 + (l & 28);
 #pragma unroll
       for (int h = 0; h < 2; ++h)
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          float x[8];
+        for (int c = 0; c < 32; c += 4 * kPer) {
+          uint32_t d[4][4];  // a row's pieces c .. c + 4 kPer; then: four rows, the lane's piece of each
 #pragma unroll
-          for (int e = 0; e < 8; ++e) x[e] = acc[h][g][c >> 1][(c & 1) * 8 + e];
-          const int at = h * 128 + c * 8;
-          if (n + at + 8 <= a.N) {
-            store8(to + at, x);
-          } else {
+          for (int k = 0; k < 4; ++k)
 #pragma unroll
-            for (int e = 0; e < 8; ++e)
-              if (n + at + e < a.N) store1(to + at + e, x[e]);
+            for (int w = 0; w < 4; ++w) {
+              if constexpr (sizeof(O) == 4) {
+                const int e = c + k * 4 + w;
+                d[k][w] = __float_as_uint(acc[h][g][e >> 4][e & 15]);
+              } else {
+                const int e = c + k * 8 + w * 2;
+                d[k][w] = pack_bf16x2(acc[h][g][e >> 4][e & 15], acc[h][g][e >> 4][(e & 15) + 1]);
+              }
+            }
+          quad_swap<kDppQuad1>(d[0], d[1], (q & 1) != 0);
+          quad_swap<kDppQuad1>(d[2], d[3], (q & 1) != 0);
+          quad_swap<kDppQuad2>(d[0], d[2], (q & 2) != 0);
+          quad_swap<kDppQuad2>(d[1], d[3], (q & 2) != 0);
+          const int64_t at = n + h * 128 + c + q * kPer;
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            if (m + k >= a.M) continue;
+            O* const to = out + (m + k) * a.ldo + at;
+            if (at + kPer <= a.N) {
+              *reinterpret_cast<uint4*>(to) = make_uint4(d[k][0], d[k][1], d[k][2], d[k][3]);
+            } else {
+#pragma unroll
+              for (int e = 0; e < kPer; ++e) {
+                if (at + e >= a.N) continue;
+                if constexpr (sizeof(O) == 4)
+                  to[e] = __uint_as_float(d[k][e]);
+                else
+                  to[e] = (O)(d[k][e >> 1] >> (16 * (e & 1)));
+              }
+            }
           }
         }
     }
