@@ -675,8 +675,8 @@ __global__ __launch_bounds__(kFinish) void k_draw_finish(DrawArgs a) {
     if (!by_p && !by_m) {
       // the whole softmax: the span, then its four rounds of 512 columns, then the column
       const double target = (double)d.u * z;
-      const uint32_t at = wave_least(before + mine[0] > target ? 2 * lane
-                                     : before + (mine[0] + mine[1]) > target ? 2 * lane + 1 : 0xFFFFFFFFu);
+      const int which = draw_span(before, mine[0], mine[1], target);
+      const uint32_t at = wave_least(which < 0 ? 0xFFFFFFFFu : (uint32_t)(2 * lane + which));
       double want = target - before - ((at & 1u) != 0u ? mine[0] : 0.0);
       want = lane_d(want, (int)(at >> 1));
       double passed = 0.0;

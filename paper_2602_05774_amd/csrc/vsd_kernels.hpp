@@ -695,6 +695,17 @@ inline DrawLayout draw_layout(int64_t R, int32_t V) {
   return w;
 }
 
+// Which of a lane's two spans, of weights first and second behind `before`, the row's
+// cumulative sum passes target in (-1: in neither).  The sum up to a lane and the scan's
+// `before` of the next add their terms in other orders, so target may lie between the
+// two: a span without weight is never taken.  Some lane's is for target <= (1 - 2^-24)
+// times the scan's total, as the sum behind the last span with weight is that up to a
+// few roundings.
+__host__ __device__ inline int draw_span(double before, double first, double second, double target) {
+  if (first > 0.0 && before + first > target) return 0;
+  return second > 0.0 && before + (first + second) > target ? 1 : -1;
+}
+
 // x [rows, cols] to 8-bit values and scales (of x^T: values [cols, out_ld]).
 struct QuantArgs {
   const void* x;
