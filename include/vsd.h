@@ -272,6 +272,8 @@
  *   order (log_prob 0, kept 1; u, k, p and m play no part but must be valid).
  *   Sums and comparisons are carried in 64 bits, so a token differs from that of
  *   exact arithmetic only where a border lies within some 1e-12 of u or p.
+ *   A weight that 64 bits hold as 0 (exp of -746 or less, any finite logit's where
+ *   M = +inf) is not drawn.
  *   A row without an entry has token -1, log_prob 0 and kept 0, one with a NaN
  *   token -1, log_prob NaN and kept 0.  A row whose u or settings lie outside
  *   their range (T = 0 or in [1e-30, 1e30], k >= 0, 0 < p <= 1, 0 <= m <= 1)

@@ -16,7 +16,7 @@ namespace vsd {
 // constant term 1 (equal logits' sums are exact) whose largest relative error there is
 // least, 1.5e-14.  (double FMAs issue at the rate of fp32 ones on this chip.)
 __device__ __forceinline__ double exp2_64(double t) {
-  t = __builtin_fmax(t, -1060.0);
+  t = __builtin_fmax(t, -1100.0);  // (2^-1100 is 0 here: u = 0 draws no finite logit of a row with +inf)
   const double n = __builtin_rint(t), f = t - n;
   double p = 0x1.b3de2fe9dfa6cp-24;
   p = __builtin_fma(p, f, 0x1.63e6965b042a6p-20);
