@@ -245,11 +245,21 @@ hipError_t launch_few(BlockArgs a, const BlockPlan& p, int group, char* ws, hipS
   constexpr bool kExact = sizeof(O) == 4;
   a.per = p.per;
   if (p.ranges == 1) {
-    if (group == 1)
-      launch_few_t<O, kExact, 1>(a, p, s);
-    else
-      launch_few_t<O, kExact, 128>(a, p, s);
-    return hipGetLastError();
+    static_assert(kBlockFewCols % 128 == 0, "a launch starts with a block of 128 of b's rows");
+    for (int64_t n0 = 0; n0 < a.N; n0 += kBlockFewCols) {
+      BlockArgs c = a;
+      c.b += n0 * a.ldb;
+      c.sb += n0 / group;
+      c.out = static_cast<O*>(a.out) + n0;
+      c.N = a.N - n0 < kBlockFewCols ? a.N - n0 : kBlockFewCols;
+      if (group == 1)
+        launch_few_t<O, kExact, 1>(c, p, s);
+      else
+        launch_few_t<O, kExact, 128>(c, p, s);
+      const hipError_t e = hipGetLastError();
+      if (e != hipSuccess) return e;
+    }
+    return hipSuccess;
   }
   BlockArgs r = a;
   r.out = ws;

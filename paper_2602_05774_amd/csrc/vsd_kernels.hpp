@@ -746,6 +746,7 @@ struct BlockTileArgs {
 // How a product is computed: a's few rows against a stream of b, by tiles, or (rows too
 // long for the tiles' 32-bit offsets) by single wavefronts.
 constexpr int64_t kBlockFewRows = 64;       // the most rows that the stream is written for
+constexpr int64_t kBlockFewCols = 1 << 28;  // columns of one launch of it: 2^31 work-items (fewer than 2^32 are allowed)
 constexpr int64_t kBlockMaxLd = 1 << 22;    // bytes of a row: 256 of them within 32-bit offsets
 constexpr int kBlockCus = 256, kBlockMaxRanges = 16;
 struct BlockPlan {
