@@ -7,6 +7,7 @@
 #include <mutex>
 #include <new>
 #include <string>
+#include <utility>
 #include <vector>
 
 #include "vsd_device.hpp"
@@ -787,10 +788,10 @@ vsd_status check_tensors(const vsd_tensor* g, const vsd_tensor* out, int32_t n) 
   return VSD_OK;
 }
 
-// Whether two tensors share bytes: none where their ranges are apart, or where both are
-// columns of rows of one stride and the columns are apart.
+// The bytes of a tensor: n pieces of `width` bytes, `step` apart.
 struct Extent {
-  uintptr_t at, end, row, width;  // bytes; row: the stride, 0 where the tensor lies in one piece
+  uintptr_t at, end;
+  int64_t n, step, width;
   int32_t i;
   bool written;
 };
@@ -798,13 +799,43 @@ Extent extent_of(const vsd_tensor& t, int32_t i, bool written) {
   const int64_t es = t.dtype == VSD_F32 ? 4 : 2;
   const uintptr_t at = reinterpret_cast<uintptr_t>(t.data);
   const bool strided = t.rows > 1 && t.ld != t.cols;
-  const int64_t last = strided ? (t.rows - 1) * t.ld + t.cols : t.rows * t.cols;
-  return Extent{at, at + (uintptr_t)(last * es), strided ? (uintptr_t)(t.ld * es) : 0, (uintptr_t)(t.cols * es), i, written};
+  Extent e{at, 0, strided ? t.rows : 1, strided ? t.ld * es : (int64_t)1 << 62, (strided ? t.cols : t.rows * t.cols) * es,
+           i, written};
+  e.end = at + (uintptr_t)((e.n - 1) * e.step + e.width);
+  return e;
 }
-bool share_bytes(const Extent& a, const Extent& b) {  // a.at <= b.at < a.end
-  if (a.row == 0 || a.row != b.row) return true;
-  const uintptr_t d = (b.at - a.at) % a.row;
-  return d < a.width || d + b.width > a.row;
+
+// The sum of floor((p i + c) / m) over 0 <= i < n, modulo 2^128: the whole parts of p / m
+// and c / m are summed apart; what is left are lattice points under a line of slope below
+// 1, counted by columns of the other axis, where p and m have changed places.
+typedef unsigned __int128 u128;
+u128 floor_sum(u128 n, u128 m, u128 p, u128 c) {
+  u128 sum = 0;
+  while (n > 0) {
+    sum += (p / m) * (n * (n - 1) / 2) + (c / m) * n;
+    p %= m;
+    c %= m;
+    const u128 top = p * n + c;  // (below 2^110: strides below 2^63, 2^44 rows at most)
+    n = top / m;
+    c = top % m;
+    std::swap(m, p);  // (p was 0: n is, too)
+  }
+  return sum;
+}
+
+// Whether two tensors share bytes.  Piece i of a begins s - (a.width - 1) behind b, and
+// touches a piece of b where s mod b.step < a.width + b.width - 1; s advances by a.step.
+bool share_bytes(const Extent& a, const Extent& b) {
+  const __int128 w = (__int128)a.width + b.width - 1, last = (__int128)(b.n - 1) * b.step + w - 1;
+  const __int128 s0 = (__int128)a.at - (__int128)b.at + a.width - 1;
+  if (s0 > last) return false;
+  const __int128 from = s0 < 0 ? (-s0 + a.step - 1) / a.step : 0;  // the pieces with 0 <= s <= last
+  const __int128 to = std::min<__int128>(a.n - 1, (last - s0) / a.step);
+  if (from > to) return false;
+  if (w >= b.step) return true;
+  const u128 n = (u128)(to - from + 1), m = (u128)b.step, p = (u128)a.step % m, c = (u128)(s0 + from * a.step) % m;
+  // s mod m < w as the difference of two whole quotients, summed
+  return n + floor_sum(n, m, p, c) != floor_sum(n, m, p, c + m - (u128)w);
 }
 
 // The workgroups scale the tensors in any order: what one writes, no other may read or write.
