@@ -741,8 +741,8 @@ vsd_status vsd_grad_norm(const vsd_tensor* grads, int32_t n, float* norm, void* 
  * more tensors, or of all ranks; it is read when the stream gets there).  out:
  * NULL for in place, or n tensors of the same rows and cols, of either dtype.  What
  * is written may not overlap what another tensor reads or writes (a gradient named
- * twice, say: VSD_ERR_INVALID_VALUE; vsd_grad_norm counts it twice).  Workspace as
- * above. */
+ * twice, say: VSD_ERR_INVALID_VALUE; vsd_grad_norm counts it twice), norm may not
+ * lie in what is written, norm_out and scale in no tensor.  Workspace as above. */
 vsd_status vsd_clip_gradients(const vsd_tensor* grads, const vsd_tensor* out, int32_t n, float max_norm,
                               const float* norm, float* norm_out, float* scale, void* workspace,
                               size_t workspace_bytes, void* hip_stream);

@@ -860,6 +860,31 @@ vsd_status check_apart(const vsd_tensor* g, const vsd_tensor* out, int32_t n) {
   return VSD_OK;
 }
 
+// The words of a call: the given norm, which every workgroup reads, lies in nothing that is
+// written, what is returned in no tensor.
+vsd_status check_words(const vsd_tensor* g, const vsd_tensor* out, int32_t n, const float* norm, const float* norm_out,
+                       const float* scale) {
+  const struct {
+    const float* at;
+    const char* name;
+    bool written;
+  } words[] = {{norm, "norm", false}, {norm_out, "norm_out", true}, {scale, "scale", true}};
+  for (const auto& w : words) {
+    if (w.at == nullptr) continue;
+    const vsd_tensor word{const_cast<float*>(w.at), 1, 1, 1, VSD_F32};
+    const Extent x = extent_of(word, 0, w.written);
+    auto meets = [&](const vsd_tensor& t, bool written) {
+      if (t.rows == 0 || t.cols == 0 || !(written || w.written)) return false;
+      const Extent e = extent_of(t, 0, written);
+      return x.at < e.end && e.at < x.end && share_bytes(x, e);
+    };
+    for (int32_t i = 0; i < n; ++i)
+      if (meets(g[i], out == nullptr || out[i].data == g[i].data) || (out != nullptr && meets(out[i], true)))
+        return fail(VSD_ERR_INVALID_VALUE, "%s lies in tensor %d", w.name, i);
+  }
+  return VSD_OK;
+}
+
 int norm_launches(int32_t n) { return (n + vsd::kGradTable - 1) / vsd::kGradTable; }
 size_t norm_bytes(int32_t n) { return align_up((size_t)norm_launches(n) * vsd::kGradGroups * sizeof(double)); }
 
@@ -1658,6 +1683,7 @@ vsd_status vsd_clip_gradients(const vsd_tensor* grads, const vsd_tensor* out, in
   if (norm == nullptr && (st = check_workspace(workspace, workspace_bytes, norm_bytes(n))) != VSD_OK) return st;
   if (norm != nullptr && norm == norm_out) return fail(VSD_ERR_INVALID_VALUE, "norm_out is the norm that is given");
   if (norm != nullptr && norm == scale) return fail(VSD_ERR_INVALID_VALUE, "scale is the norm that is given");
+  if ((st = check_words(grads, out, n, norm, norm_out, scale)) != VSD_OK) return st;
   hipStream_t s = static_cast<hipStream_t>(hip_stream);
   vsd::GradScale g{};
   g.max_norm = max_norm;

@@ -26,3 +26,16 @@ def test_pieces_beside_a_gradients_columns(kind):
     assert torch.equal(buf[rest], keep[rest])
     with pytest.raises(vsd.VsdError, match="overlap"):
         vsd.clip_gradients([buf[:, :40], buf[5, 39:60]], math.inf)
+
+
+def test_a_norm_of_the_tensors():
+    """Refused where it would be scaled while it is read; read from a gradient that stays."""
+    buf = torch.tensor([3.0, 4.0, 5.0, 0.0], device=DEV)
+    for grads in ([buf], [buf[:2], buf[2:]]):
+        with pytest.raises(vsd.VsdError, match="norm lies in tensor"):
+            vsd.clip_gradients(grads, 1.0, norm=buf[2:3])
+    out = torch.empty_like(buf)
+    r = vsd.clip_gradients([buf], 1.0, norm=buf[2:3], out=[out])
+    assert torch.equal(out, buf * r.scale) and float(r.norm) == 5.0
+    r = vsd.clip_gradients([buf[:2]], 1.0, norm=buf[2:3])
+    assert float(r.norm) == 5.0 and buf[2] == 5.0 and torch.equal(buf[:2], out[:2])

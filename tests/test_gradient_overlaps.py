@@ -1,5 +1,5 @@
 """Which tensors vsd_clip_gradients takes for overlapping, against the sets of their
-bytes; every call here lacks its workspace, so nothing is launched."""
+bytes; every call here is refused, for its workspace if for nothing else."""
 import ctypes
 import os
 import random
@@ -87,3 +87,20 @@ def test_pieces_in_the_gaps_of_rows(lib):
     hit = next(i for i in range(n) if (1009 * i - 1) % 1013 == 0)
     assert not _overlap(lib, [(A, hit, 1, 1009, 0), (A + 4, n, 1, 1013, 0)])
     assert _overlap(lib, [(A, hit + 1, 1, 1009, 0), (A + 4, n, 1, 1013, 0)])
+
+
+def test_words_in_tensors(lib):
+    """The given norm in what is written, what is returned in any tensor."""
+    rows, flat = (A, 10, 60, 100, 0), (A + 8000, 1, 100, 100, 1)
+    to = [(A + 10000, 10, 60, 60, 0), (A + 20000, 1, 100, 100, 1)]
+    ws = A + (1 << 20)
+
+    def refused(norm=None, norm_out=None, scale=None, out=None):
+        code = lib.vsd_clip_gradients(_table([rows, flat]), None if out is None else _table(out), 2, 1.0, norm, norm_out,
+                                      scale, ws, 1 << 30, None)
+        return code == 3 and " lies in tensor " in lib.vsd_last_error().decode()
+
+    inside = (A, A + 236, A + 400 * 9 + 8, A + 8000, A + 8198)
+    assert all(refused(norm=at) for at in inside) and all(refused(norm_out=at) for at in inside)
+    assert all(refused(scale=at) for at in inside) and all(refused(scale=at, out=to) for at in inside)
+    assert all(refused(norm=at, out=to) for at in (A + 10000, A + 12396, A + 20000))
