@@ -299,8 +299,13 @@
  *   its two scales and added in fp32.  An fp32 result's sums are fp32 ones; a
  *   bf16 result's come from the 8-bit matrix instructions, at twice the rate,
  *   which cut each of eight products 2^13 below the largest's exponent (some
- *   1e-5 of a sum of random terms; the result's rounding is 2^-8).  An output row depends on the
- *   same row of a alone and an output column on the same row of b.  The three
+ *   1e-5 of a sum of random terms; the result's rounding is 2^-8).  The product of
+ *   two scales is an fp32 number too: blocks whose largest magnitudes multiply to
+ *   2^145 or more, or to less than 2^-108, overflow (a sum of 0 to NaN) or lose
+ *   bits.  An output row depends on the same row of a alone and an output column on
+ *   the same row of b.
+ *   The logits of such a head are materialised ones for the other calls: their
+ *   LM-head forms (hidden_dim > 0) take bf16 weights.  The three
  *   products of a linear layer y = x w^T, with matrices quantised along the
  *   dimension that is summed over: y from x and w; dx from dy and w^T; dw from
  *   dy^T and x^T.

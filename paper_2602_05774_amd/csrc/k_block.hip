@@ -97,7 +97,10 @@ __global__ __launch_bounds__(kWave) void k_block_product(BlockArgs a) {
 // row take neighbouring 16-byte chunks): with the 32 x 32 instructions and 16 bytes of
 // 64 rows a load the chunks of a line were fetched by four loads.  Loads return in
 // order, so a's (from L2) are asked for before b's next block (from HBM): the other way
-// round 48 rows of 32 003 x 2048 took 36 us instead of 29.
+// round took a quarter longer (36 us against 29 for 48 rows of 32 003 x 2048, 25 since).
+// What bounds many of these rows is not arithmetic: 48 take 27.0 us to fp32 and 25.4 to
+// bf16, VALU instructions in 18 and 10 % of the cycles, matrix ones in 8 and 4 %; a
+// workgroup reads all of a (from L2: 1.5 bytes for each of b's) with one block ahead.
 // b's rows are the products' rows (registers) and a's their columns (lanes), so that
 // a's scales are one load a block and b's, of 128 rows, one for all.
 template <typename O, bool EXACT, int kGroup, int kTiles, int kWaves>

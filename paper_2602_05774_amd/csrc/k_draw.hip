@@ -330,7 +330,8 @@ __device__ __forceinline__ bool needs_sum(const DrawSettings& d) {
 constexpr int kLoads = kDrawSpan / 512;  // of 8 columns a lane
 
 // (without sums 262 MB of fp32 rows in 40 us, 6.6 TB/s; with them 4096 x 128 256 bf16 in
-// 395, which the weights' double-precision instructions take)
+// 395, which the weights' double-precision instructions take: the VALU issues in 95 % of the
+// cycles, in 19 without them)
 template <typename T>
 __global__ __launch_bounds__(256) void k_draw_sweep(DrawArgs a) {
   const int lane = threadIdx.x & 63, tasks = (a.S + a.per - 1) / a.per;
@@ -426,8 +427,8 @@ __global__ __launch_bounds__(256) void k_draw_sweep(DrawArgs a) {
 // ----------------------------------------------------------------- finish ---
 constexpr int kFinish = 256, kFinishWaves = kFinish / kWave;
 // Listed entries.  Rows of 513 to 1024 columns, whose few groups bound little, are listed
-// whole (us, 512 / 1024: 8192 rows of 1000 at T = 1.3, p = 0.99 548 / 137; 65 536 of 500
-// 698 / 835).
+// whole (us, 512 / 1024: 8192 rows of 1000 at T = 1.3, p = 0.99 548 / 137, later 101; 65 536 of 500
+// 698 / 835, later 487).
 constexpr int kCap = 512, kCapShort = 1024;
 constexpr int kGroups = kDrawSpans * 16;
 constexpr double kListScale = 4503599627370496.0;     // 2^52: a list's weights sum to at most 2^62
@@ -578,7 +579,7 @@ __device__ __forceinline__ uint32_t wave_largest(uint32_t lo, uint32_t hi, F&& r
 // One row by one wavefront (no barrier: what bounds it is how long the chain of its
 // instructions takes); kPer groups a lane.  A workgroup of four wavefronts a row, its
 // sums through LDS, took 24 us for 8 rows of 128 256 (k = 50, p = 0.9) and 119 for 4096 (p =
-// 0.95); this 19 and 72.
+// 0.95); this 19 and 73 (8 rows of 256 000: 23; 32 groups a lane take 144 bytes of scratch).
 template <typename T, int kPer, int kCap>
 __global__ __launch_bounds__(kFinish) void k_draw_finish(DrawArgs a) {
   constexpr int kDown = sizeof(T) == 2 ? 16 : 0;  // (bf16: 16 bits of order)
@@ -917,13 +918,15 @@ __global__ __launch_bounds__(kFinish) void k_draw_finish(DrawArgs a) {
 }
 
 // ------------------------------------------------------------- flat rows ---
-// A row whose kept entries do not fit a wavefront's list: two sweeps by a workgroup.  The first (top-p) sums fp32
-// weights, as integers, in 2048 bins of equal width between the largest logit and one below which
-// less than 1 - p of the mass can lie; within 1e-4 of p Z, far more than fp32 sums are
-// off, they tell the bins that hold the border.  (Top-k up to 2048: counts, and the
-// bins of the first k entries.)  The second forms the weights in 64
-// bits: of the entries above those bins per 512 columns, and the entries in them go to
-// a list, where the border is found as in k_draw_finish.
+// A row whose kept entries do not fit a wavefront's list: two sweeps by a workgroup.  The
+// first (top-p) sums fp32 weights, as integers, in 2048 bins of equal width between the
+// largest logit and one below which less than 1 - p of the mass can lie; the bins within
+// 1e-4 of p Z are taken for the border's.  Each weight is rounded to an integer, so they
+// may be off by n / 2^30 of Z (2.4e-4 at 262 144 columns, were all rounded one way): a
+// border elsewhere is noticed from the exact sums, and the row left to draw_row.  (Top-k up
+// to 2048: counts, and the bins of the first k entries.)  The second sweep forms the
+// weights in 64 bits: of the entries above those bins per 512 columns, and the entries in
+// them go to a list, where the border is found as in k_draw_finish.
 constexpr int kBins = 2048, kFlatCap = 2048, kPieces = kDrawSpans * kDrawSpan / 512;
 template <int kThreads>
 struct FlatShared {

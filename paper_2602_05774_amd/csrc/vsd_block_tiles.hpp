@@ -11,9 +11,10 @@
 // the other half of the phase's products; the scales ride through LDS, loaded two
 // stages ahead with the operands.
 // 6144 x 128 256 x 4096 to bf16: 2.95 to 3.08 ms, 2.1 to 2.2 PFLOP/s; a stage takes some 3700
-// cycles, 2048 of them matrix instructions (an earlier form's 3281 us were 2914 without
-// the joins, 2795 without loads, 2894 without stores).  32 000 x 2048 x 9001 to fp32: 1.2
-// ms, 0.99 PFLOP/s, the VALU shared by the conversions to bf16 and the other group's joins.
+// cycles, 2048 of them matrix instructions, VALU instructions in 42 % (an earlier form's
+// 3281 us were 2914 without the joins, 2795 without loads, 2894 without stores).  32 000 x 2048 x
+// 9001 to fp32: 1.2 ms, 0.99 PFLOP/s, the VALU shared by the conversions to bf16 and the
+// other group's joins (63 % of the cycles, matrix instructions in 44 %).
 //   phase  reads   refills             multiplies   waits for
 //   1      U0(t)   U1(t+1)             U0 V0
 //   2      V1(t)   V0(t+2)             U0 V1

@@ -669,7 +669,7 @@ struct DrawArgs {
   double* span_sum;            // [R, S] weights relative to the span's largest logit
   float* span_max;             // [R, S]
   int32_t* span_count;         // [R, S] entries; -1: a NaN among them
-  int32_t* todo;               // rows left to k_draw_row, ntodo[0] of them
+  int32_t* todo;               // rows left to k_draw_left, ntodo[0] of them
   int32_t* ntodo;
 };
 constexpr int kDrawSpan = 2048, kDrawGroup = 128, kDrawSpans = 128;  // (the most spans that the records are for)
@@ -761,7 +761,7 @@ inline BlockPlan block_plan(int64_t M, int64_t N, int64_t blocks, int64_t lda, i
   const int64_t mt = (M + 255) / 256, nt = (N + 255) / 256;
   // by tiles, in us: a block of a tile takes about two (fp32 results four), a run four
   // to start, a tile three to be stored; the ranges' sums are written and read at some
-  // 4 MB a us.  (Measured against it: 48 x 128 256 x 4096 126 / 138, 48 x 32 003 x 2048
+  // 4 MB a us.  (Measured / this: 48 x 128 256 x 4096 126 to 140 / 138, 48 x 32 003 x 2048
   // 32 / 34, to fp32 45 / 50.)
   double best = 0.0;
   if ((lda > ldb ? lda : ldb) <= kBlockMaxLd && mt * nt < 1 << 22) {
@@ -786,8 +786,8 @@ inline BlockPlan block_plan(int64_t M, int64_t N, int64_t blocks, int64_t lda, i
     }
   }
   // as a stream: b at 5.6 MB a us, and every 16 rows of a a quarter of that again
-  // (measured / this: 1 x 128 256 x 4096 94 / 124, 48 x 128 256 x 4096 171 / 171, 48 x 32 003
-  // x 2048 26 / 27)
+  // (measured / this: 1 x 128 256 x 4096 94 to 99 / 124, 48 x 128 256 x 4096 171 / 171, 48 x
+  // 32 003 x 2048 25 / 27; to fp32 the last two 180 and 27)
   const double stream = 6.0 + 1e-6 * (double)(N * blocks * 128) * (0.18 + 0.045 * (double)((M + 15) / 16));
   if (M <= kBlockFewRows && (!p.tiles || M <= 16 || stream < best)) {
     // a workgroup per 32 columns; its wavefronts, and where those workgroups do not

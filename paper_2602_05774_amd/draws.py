@@ -49,7 +49,8 @@ def sample_rows(Y, u, temp_target=1.0, top_k=0, top_p=1.0, min_p=0.0, workspace=
     index order, the one in which their cumulative probability passes u.
 
     temp_target (0: the largest logit), top_k (0: off), top_p (1: off) and min_p
-    (0: off) are a number for all rows or a [R] tensor (float32; top_k: int32).
+    (0: off) are a number for all rows or a [R] tensor (float32; top_k: int32).  A
+    top_k of all of a row's entries or more keeps what 0 does, more slowly.
     Equal logits: the smaller index first.  Returns RowSamples."""
     lib = _lib.load()
     if isinstance(Y, LmHead):
